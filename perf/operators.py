@@ -177,7 +177,7 @@ def prepare(case, seed):
         else:
             s["k"], s["v"] = _normal(g, *shape), _normal(g, *shape)
         s["out"] = torch.empty_like(s["q"])
-        s["lse"] = torch.empty(len(lens), n_q, case["Hq"], dtype=torch.float32, device="cuda")
+        s["lse"] = torch.empty(case["Hq"], len(lens) * n_q, dtype=torch.float32, device="cuda")
     elif op == "rope":
         n = case["n"]
         rng = random.Random(case["mix"])
@@ -426,7 +426,7 @@ def _plain_decode(s):
     rows = seen[:, None, :, None, :].expand(B, 1, n_q, G, at.shape[1]).reshape(B, 1, n_q * G, at.shape[1])
     o, l = _softmax_product(q, k.permute(0, 2, 1, 3), v.permute(0, 2, 1, 3), rows, D ** -0.5)
     out.copy_(o.view(B, Hkv, n_q, G, D).permute(0, 2, 1, 3, 4).reshape(B, n_q, c["Hq"], D))
-    lse.copy_(l.view(B, Hkv, n_q, G).permute(0, 2, 1, 3).reshape(B, n_q, c["Hq"]))
+    lse.copy_(l.view(B, Hkv, n_q, G).permute(1, 3, 0, 2).reshape(c["Hq"], B * n_q))
     return [out, lse]
 
 
@@ -648,8 +648,8 @@ def exact(case, seed):
                 k, v = s["k"][ids, t % page].double(), s["v"][ids, t % page].double()
             o, z = _exact_attention(s["q"][b].double(), k, v, n - n_q + torch.arange(n_q, device="cuda"), case["window"] or NO_WINDOW, case["sinks"])
             outs.append(o)
-            lses.append(z.T)
-        return [torch.stack(outs), torch.stack(lses)]
+            lses.append(z)
+        return [torch.stack(outs), torch.cat(lses, 1)]
     # rope: pair i of a head is a complex number, turned by exp(1j * angle)
     n = case["rot"] // 2
     which = [a for a, m in enumerate(_sections(case)) for _ in range(m)]

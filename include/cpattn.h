@@ -225,6 +225,30 @@ int cp_prefill_attn_kvrange(cp_ctx* ctx, const void* q, const cp_kv_cache* cache
                             size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Sliding window with sinks (the paper's models attend in full; this is for models that do not).  A token at
+ * absolute position p sees key j if  j <= p  and  (p - j < window  or  j < sinks):  the last `window` keys, its own
+ * among them, and the first `sinks` tokens of the sequence.  window >= 1; CP_NO_WINDOW (or anything that reaches past
+ * the longest request) is full causal attention.  Arguments, layouts, workspace, schedule and errors as in the calls
+ * without _window; KV tiles that no row of a query tile sees are neither read nor computed, so the work grows with
+ * new_len * window.  Page-table entries behind the sinks and the window (of the first query of a request) are never used
+ * as an address of anything that reaches a result: they may be -1 (cp_pages_evict).  _chunk is the zigzag chunk of one CP
+ * rank.  The FP8 form has the accuracy of cp_prefill_attn_fp8.
+ * Errors: INVALID_ARG (also window < 1, sinks < 0), UNSUPPORTED, WORKSPACE, CUDA, BOUNDS.
+ * ------------------------------------------------------------------------------------------- */
+#define CP_NO_WINDOW 0x7fffffff
+int cp_prefill_attn_window(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table,
+                           int64_t prefix_len, int64_t new_len, int32_t C, int64_t window, int64_t sinks, int32_t Hq,
+                           float scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+int cp_prefill_attn_window_batch(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table,
+                                 int32_t B, const int64_t* cu_new, const int64_t* prefix_len, const int32_t* C,
+                                 const int64_t* cu_pages, int64_t window, int64_t sinks, int32_t Hq, float scale, void* out,
+                                 float* lse, void* workspace, size_t workspace_bytes, void* stream);
+int cp_prefill_attn_window_chunk(cp_ctx* ctx, const void* q_chunk, const cp_kv_cache* cache, const int32_t* page_table,
+                                 int64_t prefix_len, int64_t new_len, int32_t C, int32_t chunk, int64_t window,
+                                 int64_t sinks, int32_t Hq, float scale, void* out_chunk, float* lse_chunk, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * cp_prefill_attn_static -- cp_prefill_attn for callers that must not allocate device memory.
  * (The paper has no counterpart to this call; it exists for integration reasons only.)
  * Who needs it: code that runs after an inference engine has handed all of HBM to its own KV-cache
@@ -363,6 +387,10 @@ int cp_prefill_attn_fp8_kvrange(cp_ctx* ctx, const void* q, const cp_kv_cache_fp
                                 int64_t prefix_len, int64_t new_len, int64_t kv_lo, int64_t kv_hi, int32_t Hq,
                                 float scale, float* partial_out, float* partial_lse, void* workspace,
                                 size_t workspace_bytes, void* stream);
+int cp_prefill_attn_fp8_window_batch(cp_ctx* ctx, const void* q, const cp_kv_cache_fp8* cache, const int32_t* page_table,
+                                     int32_t B, const int64_t* cu_new, const int64_t* prefix_len, const int32_t* C,
+                                     const int64_t* cu_pages, int64_t window, int64_t sinks, int32_t Hq, float scale, void* out,
+                                     float* lse, void* workspace, size_t workspace_bytes, void* stream);
 int cp_kv_append_fp8(cp_ctx* ctx, const cp_kv_cache_fp8* cache, const int32_t* page_table, int64_t t_begin,
                      int64_t n, const void* k_rows, const void* v_rows, void* stream);
 /* Raw byte copies of an FP8 cache, no conversion: cp_kv_gather_fp8 reads n logical tokens from t_begin into

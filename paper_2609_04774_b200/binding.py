@@ -18,12 +18,14 @@ LIB_PATH = os.path.join(_HERE, "libcpattn.so")
 CP_OK = 0
 CP_ERR_INVALID_ARG, CP_ERR_UNSUPPORTED, CP_ERR_WORKSPACE, CP_ERR_CUDA, CP_ERR_TIMEOUT, CP_ERR_BOUNDS = -1, -2, -3, -4, -5, -6
 CP_DTYPE_BF16, CP_DTYPE_F32 = 0, 1
+CP_NO_WINDOW = 0x7fffffff
 
 EXPORTS = ["cp_strerror", "cp_last_error", "cp_ctx_create", "cp_ctx_destroy", "cp_ctx_poll_status", "cp_ctx_cache_schedule", "cp_ctx_selftest_wait_expiry", "cp_plan",
            "cp_workspace_bytes", "cp_schedule_inspect", "cp_prefill_attn", "cp_prefill_attn_batch", "cp_prefill_attn_shard", "cp_prefill_attn_chunk", "cp_prefill_attn_kvrange", "cp_prefill_attn_static", "cp_merge",
            "cp_kv_gather", "cp_kv_append", "cp_workspace_bytes_fp8", "cp_prefill_attn_fp8", "cp_prefill_attn_fp8_batch",
            "cp_kv_append_fp8", "cp_kv_append_segments", "cp_prefill_attn_fp8_shard", "cp_prefill_attn_fp8_chunk",
-           "cp_prefill_attn_fp8_kvrange", "cp_kv_gather_fp8", "cp_kv_append_segments_fp8", "cp_check_page_table"]
+           "cp_prefill_attn_fp8_kvrange", "cp_kv_gather_fp8", "cp_kv_append_segments_fp8", "cp_check_page_table",
+           "cp_prefill_attn_window", "cp_prefill_attn_window_batch", "cp_prefill_attn_window_chunk", "cp_prefill_attn_fp8_window_batch"]
 
 
 class CpError(RuntimeError):
@@ -233,6 +235,41 @@ def cp_prefill_attn_kvrange(ctx, q, cache, page_table, prefix_len, new_len, kv_l
         _stream(stream)))
 
 
+def cp_prefill_attn_window(ctx, q, cache, page_table, prefix_len, new_len, C, window, sinks, Hq, scale, out, lse, workspace,
+                           stream=None):
+    """cp_prefill_attn where a token at position p sees the last `window` keys (its own among them) and the first `sinks`."""
+    _check(load().cp_prefill_attn_window(
+        ctx._h, _ptr(q), ctypes.byref(cache), _ptr(page_table), ctypes.c_int64(prefix_len), ctypes.c_int64(new_len),
+        ctypes.c_int32(C), ctypes.c_int64(window), ctypes.c_int64(sinks), ctypes.c_int32(Hq), ctypes.c_float(scale), _ptr(out),
+        _ptr(lse), _ptr(workspace), ctypes.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream)))
+
+
+def _window_batch(call, ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks, Hq, scale, out, lse, workspace,
+                  stream):
+    cu_new, prefix_len, cu_pages, C = _i64(cu_new), _i64(prefix_len), _i64(cu_pages), _i32(C)
+    B = prefix_len.size
+    assert cu_new.size == B + 1 and cu_pages.size == B + 1 and C.size == B
+    _check(call(ctx._h, _ptr(q), ctypes.byref(cache), _ptr(page_table), ctypes.c_int32(B), _hp(cu_new), _hp(prefix_len), _hp(C),
+                _hp(cu_pages), ctypes.c_int64(window), ctypes.c_int64(sinks), ctypes.c_int32(Hq), ctypes.c_float(scale), _ptr(out),
+                _ptr(lse), _ptr(workspace), ctypes.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream)))
+
+
+def cp_prefill_attn_window_batch(ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks, Hq, scale, out, lse,
+                                 workspace, stream=None):
+    _window_batch(load().cp_prefill_attn_window_batch, ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks,
+                  Hq, scale, out, lse, workspace, stream)
+
+
+def cp_prefill_attn_window_chunk(ctx, q_chunk, cache, page_table, prefix_len, new_len, C, chunk, window, sinks, Hq, scale,
+                                 out_chunk, lse_chunk, workspace, stream=None):
+    """One zigzag chunk in chunk-local buffers, as cp_prefill_attn_chunk, with a window."""
+    _check(load().cp_prefill_attn_window_chunk(
+        ctx._h, _ptr(q_chunk), ctypes.byref(cache), _ptr(page_table), ctypes.c_int64(prefix_len), ctypes.c_int64(new_len),
+        ctypes.c_int32(C), ctypes.c_int32(chunk), ctypes.c_int64(window), ctypes.c_int64(sinks), ctypes.c_int32(Hq),
+        ctypes.c_float(scale), _ptr(out_chunk), _ptr(lse_chunk), _ptr(workspace),
+        ctypes.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream)))
+
+
 def cp_prefill_attn_static(q, cache, page_table, prefix_len, new_len, C, Hq, scale, out, lse, stream=None):
     """cp_prefill_attn without a context or a workspace: the library's built-in device scratch holds the
     tile list, so nothing is allocated.  For callers that cannot allocate device memory (all of HBM
@@ -306,6 +343,12 @@ def cp_prefill_attn_fp8_batch(ctx, q, cache, page_table, cu_new, prefix_len, C, 
         ctx._h, _ptr(q), ctypes.byref(cache), _ptr(page_table), ctypes.c_int32(B), _hp(cu_new), _hp(prefix_len), _hp(C),
         _hp(cu_pages), ctypes.c_int32(Hq), ctypes.c_float(scale), _ptr(out), _ptr(lse), _ptr(workspace),
         ctypes.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream)))
+
+
+def cp_prefill_attn_fp8_window_batch(ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks, Hq, scale, out,
+                                     lse, workspace, stream=None):
+    _window_batch(load().cp_prefill_attn_fp8_window_batch, ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks,
+                  Hq, scale, out, lse, workspace, stream)
 
 
 def cp_prefill_attn_fp8_shard(ctx, q, cache, page_table, prefix_len, new_len, C, shard, Hq, scale, partial_out, partial_lse,

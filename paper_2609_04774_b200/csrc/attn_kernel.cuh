@@ -133,6 +133,9 @@ struct AttnParams {
     const float* k_scale;
     const float* v_scale;
     int32_t co_producer;      // 1: the spare warp copies the second 64-dim half of every K/V tile (16-token pages, bf16)
+    // windowed calls (kWin): a row at position p sees key j if j <= p and (p - j < window or j < sinks)
+    int32_t window;
+    int32_t sinks;
 };
 
 // ------------------------------------------------------------------------------------------
@@ -363,12 +366,21 @@ struct UnitInfo {
     int kv_head;
     int t_begin, t_end;   // KV tile range of this piece
     int slot;             // < 0: whole unit, final rows; >= 0: partial slot
+    int sink_tiles;       // windowed calls: KV tiles [0, sink_tiles) hold the sinks, tile t >= sink_tiles of the unit
+    int skip;             // is KV tile t + skip of the request (the tiles in between are hidden from every row)
 };
+
+// KV tile of the request behind tile t of a unit (the same for calls without a window).
+template <bool kWin>
+__device__ __forceinline__ int kv_tile_of(const UnitInfo& u, int t) {
+    return kWin ? (t < u.sink_tiles ? t : t + u.skip) : t;
+}
 
 // Two schedules.  Explicit (p.pieces != NULL): the host lists, per CTA, whole units and the KV
 // ranges of units that were split to fill every CTA to the same number of KV tile steps.  Implicit:
 // serpentine over the longest-first unit list -- in even rounds CTA c takes unit round*grid + c, in
 // odd rounds round*grid + (grid-1-c), which evens out the sorted lengths; whole units only.
+template <bool kWin>
 __device__ __forceinline__ bool fetch_unit(const AttnParams& p, const InlineSched& inl, int round, UnitInfo& u) {
     int item, pair;
     // a small schedule sits in the launch parameters (constant bank), a large one in the workspace
@@ -410,6 +422,7 @@ __device__ __forceinline__ bool fetch_unit(const AttnParams& p, const InlineSche
     const int t0 = u.it.kv_lo >> 7;      // first KV tile of the unit's key range (0 for the ordinary calls)
     u.t_begin += t0;
     u.t_end += t0;
+    if (kWin) window_tiles(u.it.kv_len0, p.window, p.sinks, u.sink_tiles, u.skip);
     u.head0 = p.heads_per_unit * pair;
     u.kv_head = u.head0 / p.group;
     return true;
@@ -423,7 +436,7 @@ __device__ __forceinline__ bool fetch_unit(const AttnParams& p, const InlineSche
 // the second half as a co-producer: it waits for the same "slot empty" phases, while the byte count of a tile is
 // announced once, by the leading warp (a copy that lands before the announcement only leaves the barrier's byte
 // count negative for a moment; the phase cannot complete before the announcing arrival).
-template <bool kFp8>
+template <bool kFp8, bool kWin>
 __device__ __forceinline__ void producer_role(const CUtensorMap* tmQ, const CUtensorMap* tmK, const CUtensorMap* tmV, const AttnParams& p,
                               const InlineSched& inl, uint32_t smem_base, volatile uint32_t* abort_flag, int half_lo,
                               int half_hi) {
@@ -433,7 +446,7 @@ __device__ __forceinline__ void producer_role(const CUtensorMap* tmQ, const CUte
     uint32_t kv_it = 0;   // ring slots filled so far
     for (int round = 0;; ++round) {
         UnitInfo u;
-        if (!fetch_unit(p, inl, round, u)) break;
+        if (!fetch_unit<kWin>(p, inl, round, u)) break;
         if (lane == 0 && lead) {
             mbar_wait(bars, kBarQEmpty, (round & 1) ^ 1, abort_flag, p.status, round);
             const uint32_t qbar = bars + kBarQFull * 8;
@@ -465,11 +478,13 @@ __device__ __forceinline__ void producer_role(const CUtensorMap* tmQ, const CUte
             else if (ld == n_loads - 1) { j = n_tiles - 1; kv = 1; }
             else if (ld & 1) { j = u.t_begin + (ld + 1) / 2; kv = 0; }
             else { j = u.t_begin + ld / 2 - 1; kv = 1; }
-            const int pg0 = ppt * j;
+            const int pg0 = ppt * kv_tile_of<kWin>(u, j);
             if (pg_base < 0 || pg0 < pg_base || pg0 + ppt > pg_base + 32) {
                 // the warp fetches 32 page ids starting at this tile (K runs one tile ahead of V, so the
                 // window is anchored at the V tile when possible)
-                pg_base = ppt * max(j - 1, u.t_begin);
+                int anchor = kv_tile_of<kWin>(u, max(j - 1, u.t_begin));
+                if (kWin && ppt * (anchor + 1) < pg0) anchor = kv_tile_of<kWin>(u, j);    // the tiles between sinks and window are skipped
+                pg_base = ppt * anchor;
                 const int pg = pg_base + lane;
                 my_page = (pg < u.it.n_pages) ? __ldg(p.page_table + u.it.pt_base + pg) : p.oob_page;
             }
@@ -516,7 +531,7 @@ struct RingPos {
 // (S buffer) and P*V (P and O columns) touch disjoint TMEM and the K and V tiles have their own barriers.
 //
 // Score issuer: S tiles in the order (tile, head); each needs its K tile and the buffer back (s_free).
-template <bool kFp8>
+template <bool kFp8, bool kWin>
 __device__ __forceinline__ void mma_s_role(const AttnParams& p, const InlineSched& inl, uint32_t smem_base, uint32_t tmem_base,
                                            volatile uint32_t* abort_flag) {
     const uint32_t bars = smem_base + kSmemBar;
@@ -528,9 +543,9 @@ __device__ __forceinline__ void mma_s_role(const AttnParams& p, const InlineSche
     // the next unit's description is fetched while the current one runs (three dependent loads otherwise sit between
     // the last score tile of a unit and the first of the next)
     UnitInfo u, nu;
-    bool have = fetch_unit(p, inl, 0, u);
+    bool have = fetch_unit<kWin>(p, inl, 0, u);
     for (int round = 0; have; ++round) {
-        const bool have_next = fetch_unit(p, inl, round + 1, nu);
+        const bool have_next = fetch_unit<kWin>(p, inl, round + 1, nu);
         const int j0 = u.t_begin, n = u.t_end;
         mbar_wait(bars, kBarQFull, round & 1, abort_flag, p.status, round);
         RingPos kpos = unit_pos;
@@ -579,7 +594,7 @@ __device__ __forceinline__ void mma_s_role(const AttnParams& p, const InlineSche
 // P*V issuer: O_h += P_h V_j in the order (tile, head), each in the two pieces P is handed over in.  In a
 // single-head unit (a pair of consecutive query tiles of one head) the second P / O column set belongs to the
 // unit's second query tile instead of a second head; the loop is the same.
-template <bool kFp8>
+template <bool kFp8, bool kWin>
 __device__ __forceinline__ void mma_pv_role(const AttnParams& p, const InlineSched& inl, uint32_t smem_base, uint32_t tmem_base,
                                             volatile uint32_t* abort_flag) {
     const uint32_t bars = smem_base + kSmemBar;
@@ -588,9 +603,9 @@ __device__ __forceinline__ void mma_pv_role(const AttnParams& p, const InlineSch
     uint32_t p_par0 = 0, p_par1 = 0;   // phase parity of p_ready per softmax warpgroup
     const uint64_t v_desc0 = make_desc(smem_base + kSmemKV, kHalfBytes, 1024);   // MN-major view of a ring slot
     UnitInfo u, nu;
-    bool have = fetch_unit(p, inl, 0, u);
+    bool have = fetch_unit<kWin>(p, inl, 0, u);
     for (int round = 0; have; ++round) {
-        const bool have_next = fetch_unit(p, inl, round + 1, nu);      // fetched ahead, as in the score issuer
+        const bool have_next = fetch_unit<kWin>(p, inl, round + 1, nu);      // fetched ahead, as in the score issuer
         const int j0 = u.t_begin, n = u.t_end;
         RingPos vpos = unit_pos.plus(n - j0 == 1 ? 1 : 2);   // V(j0)
 #pragma unroll 1
@@ -661,6 +676,15 @@ __device__ __forceinline__ void mask32(float (&s)[32], int lo, int lim) {
 #pragma unroll
     for (int i = 0; i < 32; ++i)
         if (i >= lim || i < lo) s[i] = -INFINITY;
+}
+// Windowed calls: this row sees columns below lim that are not left of its window (lo) or belong to the sinks (below
+// sk).  The three limits of a 32-column piece become one bit mask, so an element costs one predicated select.
+__device__ __forceinline__ uint32_t bits_below(int x) { return x <= 0 ? 0u : (x >= 32 ? 0xffffffffu : (1u << x) - 1u); }
+__device__ __forceinline__ void mask32_window(float (&s)[32], int lo, int lim, int sk) {
+    const uint32_t seen = bits_below(lim) & (~bits_below(lo) | bits_below(sk));
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        if (!((seen >> i) & 1u)) s[i] = -INFINITY;
 }
 // p = 2^(s*c - m) for 32 keys -> 16 packed bf16 pairs; row sums into four accumulators.  With kPoly,
 // kPolyOf4 of every four pairs take the FMA-pipe polynomial instead of MUFU; masked tiles do not (the
@@ -746,12 +770,17 @@ __device__ __forceinline__ void release_s(uint32_t bars) {
 // Straight-line code in both variants, no per-element branches.
 // kMasked: some keys of the tile are hidden from some rows (causal diagonal, or the edge of the unit's key
 // range); this row sees columns [lo, lim).
-template <bool kMasked, bool kFp8>
+template <bool kMasked, bool kFp8, bool kWin>
 __device__ __forceinline__ void softmax_tile(float (&c0)[32], float (&c1)[32], float (&c2)[32], float (&c3)[32],
                                              bool more, uint32_t& s_par, uint32_t s_tmem, uint32_t p_tmem,
-                                             uint32_t o_tmem, uint32_t p_bar0, float c, int lo, int lim, bool first,
-                                             float& m, float& l, const SoftmaxSync& sy) {
-    if (kMasked) {
+                                             uint32_t o_tmem, uint32_t p_bar0, float c, int lo, int lim, int sk,
+                                             bool first, float& m, float& l, const SoftmaxSync& sy) {
+    if (kMasked && kWin) {
+        mask32_window(c0, lo, lim, sk);
+        mask32_window(c1, lo - 32, lim - 32, sk - 32);
+        mask32_window(c2, lo - 64, lim - 64, sk - 64);
+        mask32_window(c3, lo - 96, lim - 96, sk - 96);
+    } else if (kMasked) {
         mask32(c0, lo, lim);
         mask32(c1, lo - 32, lim - 32);
         mask32(c2, lo - 64, lim - 64);
@@ -864,7 +893,7 @@ __device__ __forceinline__ void quad_transpose(uint4 (&v)[4], int t) {
     }
 }
 
-template <bool kFp8>
+template <bool kFp8, bool kWin>
 __device__ __forceinline__ void softmax_role(const AttnParams& p, const InlineSched& inl, uint32_t smem_base, uint32_t tmem_base,
                                              volatile uint32_t* abort_flag, int wg) {
     const uint32_t bars = smem_base + kSmemBar;
@@ -890,7 +919,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, const InlineSc
     uint32_t s_par = 0;        // phase parity of s_ready for this head
 
     UnitInfo u, nu;
-    bool have = fetch_unit(p, inl, 0, u);
+    bool have = fetch_unit<kWin>(p, inl, 0, u);
     for (int round = 0; have; ++round) {
         const int n = u.t_end;
         const int head = u.head0 + head_sel;
@@ -905,6 +934,9 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, const InlineSc
         // multiple.  (The earlier tile of a tile-pair unit finds the unit's last KV tile fully masked.)
         const int n_full = min(u.it.kv_len0 + row_base, u.it.kv_hi) / kBlockN;
         const int j_cut = (u.it.kv_lo & (kBlockN - 1)) ? (u.it.kv_lo >> 7) : -1;
+        // windowed calls: of those tiles, the ones inside every row's window (from the last row's lowest key on) or
+        // entirely among the sinks are unmasked
+        const int win_low = kWin ? u.it.kv_len0 + min(row_base + kBlockM, u.it.n_rows) - 1 - p.window : 0;
         float s0[32], s1[32], s2[32], s3[32];   // the row's scores of the current tile
         // the first tile of the unit is loaded here, every later one by the tile before it
         SM_WAIT(kBarSReady + wg, s_par, j_first);
@@ -916,17 +948,21 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, const InlineSc
         for (int j = j_first; j < n; ++j) {
             const SoftmaxSync sy = {bars, kBarSReady + (uint32_t)wg, kBarPvDone + (uint32_t)wg, (tile_cnt - 1) & 1,
                                     abort_flag, p.status, j};
-            if (j < n_full && j != j_cut)
-                softmax_tile<false, kFp8>(s0, s1, s2, s3, j + 1 < n, s_par, s_tmem, p_tmem, o_tmem, p_bar0, c, 0, 0,
-                                          j == j_first, m, l, sy);
+            const int jt = kv_tile_of<kWin>(u, j);
+            const bool full = kWin ? jt < n_full && (jt * kBlockN >= win_low || (jt + 1) * kBlockN <= p.sinks)
+                                   : j < n_full && j != j_cut;
+            if (full)
+                softmax_tile<false, kFp8, kWin>(s0, s1, s2, s3, j + 1 < n, s_par, s_tmem, p_tmem, o_tmem, p_bar0, c, 0, 0, 0,
+                                                j == j_first, m, l, sy);
             else
-                softmax_tile<true, kFp8>(s0, s1, s2, s3, j + 1 < n, s_par, s_tmem, p_tmem, o_tmem, p_bar0, c,
-                                   u.it.kv_lo - j * kBlockN, min(u.it.kv_len0 + row, u.it.kv_hi) - j * kBlockN,
-                                   j == j_first, m, l, sy);
+                softmax_tile<true, kFp8, kWin>(s0, s1, s2, s3, j + 1 < n, s_par, s_tmem, p_tmem, o_tmem, p_bar0, c,
+                                               (kWin ? u.it.kv_len0 + row - p.window : u.it.kv_lo) - jt * kBlockN,
+                                               min(u.it.kv_len0 + row, u.it.kv_hi) - jt * kBlockN,
+                                               kWin ? p.sinks - jt * kBlockN : 0, j == j_first, m, l, sy);
             ++tile_cnt;
         }
         // the next unit's description is fetched under the epilogue
-        const bool have_next = fetch_unit(p, inl, round + 1, nu);
+        const bool have_next = fetch_unit<kWin>(p, inl, round + 1, nu);
         // epilogue: O / l -> global at the row's original position; LSE in natural log
         SM_WAIT(kBarPvDone + wg, (tile_cnt - 1) & 1, n);
         tc_fence_after();
@@ -1018,8 +1054,9 @@ __device__ __forceinline__ void fill_role(const AttnParams& p) {
     }
 }
 
-// kFp8: the FP8 K/V variant (one-byte Q / K / V / P operands).
-template <bool kFp8>
+// kFp8: the FP8 K/V variant (one-byte Q / K / V / P operands).  kWin: the windowed calls (a unit's KV tiles are the
+// sinks' and the window's, the ones between are skipped); the calls without a window keep their own instantiation.
+template <bool kFp8, bool kWin = false>
 __global__ void __launch_bounds__(kThreads, 1)
 cp_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                const __grid_constant__ CUtensorMap tmV, const AttnParams p, const __grid_constant__ InlineSched inl) {
@@ -1059,19 +1096,19 @@ cp_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
 
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-        softmax_role<kFp8>(p, inl, smem_base, tmem_base, abort_flag, warp >> 2);
+        softmax_role<kFp8, kWin>(p, inl, smem_base, tmem_base, abort_flag, warp >> 2);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
         if (warp == 8) {
-            producer_role<kFp8>(&tmQ, &tmK, &tmV, p, inl, smem_base, abort_flag, 0, p.co_producer ? 1 : 2);
+            producer_role<kFp8, kWin>(&tmQ, &tmK, &tmV, p, inl, smem_base, abort_flag, 0, p.co_producer ? 1 : 2);
         } else if (warp == 9) {
-            mma_s_role<kFp8>(p, inl, smem_base, tmem_base, abort_flag);
+            mma_s_role<kFp8, kWin>(p, inl, smem_base, tmem_base, abort_flag);
         } else if (warp == 10) {
-            mma_pv_role<kFp8>(p, inl, smem_base, tmem_base, abort_flag);
+            mma_pv_role<kFp8, kWin>(p, inl, smem_base, tmem_base, abort_flag);
         } else if (p.n_fill > 0) {
             fill_role(p);
         } else if (!kFp8 && p.co_producer) {
-            producer_role<kFp8>(&tmQ, &tmK, &tmV, p, inl, smem_base, abort_flag, 1, 2);
+            producer_role<kFp8, kWin>(&tmQ, &tmK, &tmV, p, inl, smem_base, abort_flag, 1, 2);
         }
     }
 

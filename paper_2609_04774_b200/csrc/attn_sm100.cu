@@ -133,7 +133,7 @@ int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int3
                 const int64_t* cu_new, const int64_t* prefix_len, const int32_t* C, const int64_t* cu_pages,
                 int32_t only_shard, int32_t only_chunk, int64_t kv_lo, int64_t kv_hi, int32_t Hq, float scale, void* out,
                 int out_f32, bool want_fill, float* lse, void* workspace, size_t workspace_bytes, void* stream,
-                const char* who, const cp_kv_cache_fp8* cache8 = nullptr) {
+                const char* who, const cp_kv_cache_fp8* cache8 = nullptr, int64_t window = CP_NO_WINDOW, int64_t sinks = 0) {
     if (!ctx || !q || !page_table || !out || !lse || B < 1 || !cu_new || !prefix_len || !C || !cu_pages)
         return set_error(CP_ERR_INVALID_ARG, "%s: null pointer or B < 1", who);
     cp_kv_cache shape8;         // FP8 variant: the cache's shape in the bf16 descriptor's fields, for the shared logic
@@ -156,6 +156,9 @@ int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int3
     // even group size: two query heads of one KV group share every K/V tile; odd: one head per unit
     const int32_t heads_per_unit = ((Hq / cache->Hkv) % 2 == 0) ? 2 : 1;
     if (!(scale > 0.f)) return set_error(CP_ERR_INVALID_ARG, "%s: scale must be positive", who);
+    if (window < 1 || sinks < 0)
+        return set_error(CP_ERR_INVALID_ARG, "%s: window=%lld sinks=%lld", who, (long long)window, (long long)sinks);
+    const int32_t win = (int32_t)std::min<int64_t>(window, INT32_MAX), snk = (int32_t)std::min<int64_t>(sinks, INT32_MAX);
     if (((uintptr_t)q | (uintptr_t)out) & 15) return set_error(CP_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned", who);
     if (cu_new[0] != 0 || cu_pages[0] != 0) return set_error(CP_ERR_INVALID_ARG, "%s: cu_new[0] and cu_pages[0] must be 0", who);
     std::vector<int64_t> new_len(B);
@@ -188,9 +191,9 @@ int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int3
     // (the next layer of the same batch) launches on the work lists that are already in the workspace.
     std::vector<int64_t> key;
     if (ctx->cache_on) {
-        key.reserve(14 + 4 * (size_t)B);
+        key.reserve(16 + 4 * (size_t)B);
         const int64_t head[] = {B, Hq, cache->Hkv, cache->page_size, only_shard, only_chunk, kv_lo, kv_hi,
-                                grid_max, out_f32, want_fill, cache8 != nullptr};
+                                grid_max, out_f32, want_fill, cache8 != nullptr, win, snk};
         key.assign(head, head + sizeof head / sizeof head[0]);
         for (int32_t b = 0; b < B; ++b) {
             key.push_back(cu_new[b + 1]); key.push_back(prefix_len[b]); key.push_back(C[b]); key.push_back(cu_pages[b + 1]);
@@ -222,7 +225,7 @@ int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int3
         Schedule sch;
         // even groups: 128-row tiles for pairs of heads; odd groups: 256-row tile pairs for single heads
         build_tiles(B, cu_new, prefix_len, C, cu_pages, cache->page_size, only_shard, only_chunk, kv_lo, kv_hi,
-                    heads_per_unit == 2 ? kTileRows : 2 * kTileRows, sch.items);
+                    heads_per_unit == 2 ? kTileRows : 2 * kTileRows, sch.items, win, snk);
         // rows of q / out / lse: the packed batch, or the one chunk of a chunk call
         total_rows = cu_new[B];
         if (only_chunk >= 0) {
@@ -347,6 +350,10 @@ int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int3
                                                      (int)kSmemAlloc), "cudaFuncSetAttribute(attn)")) return rc;
         if (int rc = check_cuda(cudaFuncSetAttribute(cp_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                      (int)kSmemAlloc), "cudaFuncSetAttribute(attn)")) return rc;
+        if (int rc = check_cuda(cudaFuncSetAttribute(cp_attn_kernel<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                     (int)kSmemAlloc), "cudaFuncSetAttribute(attn)")) return rc;
+        if (int rc = check_cuda(cudaFuncSetAttribute(cp_attn_kernel<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                     (int)kSmemAlloc), "cudaFuncSetAttribute(attn)")) return rc;
         ctx->attn_attr_set = true;
     }
     AttnParams p;
@@ -385,7 +392,15 @@ int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int3
     p.k_scale = cache8 ? cache8->k_scale : nullptr;
     p.v_scale = cache8 ? cache8->v_scale : nullptr;
     p.co_producer = (!cache8 && cache->page_size == 16 && n_fill == 0) ? 1 : 0;
-    if (cache8) cp_attn_kernel<true><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, *inl);
+    p.window = win;
+    p.sinks = snk;
+    // a window that no token of the batch reaches beyond hides nothing: the plain instantiation then does the work
+    int64_t longest = 0;
+    for (int32_t b = 0; b < B; ++b) longest = std::max<int64_t>(longest, prefix_len[b] + new_len[b]);
+    if (win < longest) {
+        if (cache8) cp_attn_kernel<true, true><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, *inl);
+        else cp_attn_kernel<false, true><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, *inl);
+    } else if (cache8) cp_attn_kernel<true><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, *inl);
     else cp_attn_kernel<false><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, *inl);
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
     if (n_merges > 0) {
@@ -527,6 +542,48 @@ extern "C" int cp_prefill_attn_kvrange(cp_ctx* ctx, const void* q, const cp_kv_c
     return attn_common(ctx, q, cache, page_table, 1, cu_new, &prefix_len, &C, cu_pages, -1, -1, kv_lo,
                        std::min<int64_t>(kv_hi, INT32_MAX), Hq, scale, partial_out, 1, true, partial_lse, workspace,
                        workspace_bytes, stream, "cp_prefill_attn_kvrange");
+}
+
+// Sliding window with sinks: the same path with another tile list and the windowed instantiation of the kernel.
+extern "C" int cp_prefill_attn_window_batch(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table,
+                                            int32_t B, const int64_t* cu_new, const int64_t* prefix_len, const int32_t* C,
+                                            const int64_t* cu_pages, int64_t window, int64_t sinks, int32_t Hq, float scale,
+                                            void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    return attn_common(ctx, q, cache, page_table, B, cu_new, prefix_len, C, cu_pages, -1, -1, 0, INT32_MAX, Hq, scale, out, 0,
+                       false, lse, workspace, workspace_bytes, stream, "cp_prefill_attn_window_batch", nullptr, window, sinks);
+}
+
+extern "C" int cp_prefill_attn_window(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table,
+                                      int64_t prefix_len, int64_t new_len, int32_t C, int64_t window, int64_t sinks, int32_t Hq,
+                                      float scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!cache || new_len < 1 || prefix_len < 0)
+        return set_error(CP_ERR_INVALID_ARG, "cp_prefill_attn_window: cache is NULL, new_len < 1 or prefix_len < 0");
+    const int64_t cu_new[2] = {0, new_len};
+    const int64_t cu_pages[2] = {0, (prefix_len + new_len + page_tokens_of(cache) - 1) / page_tokens_of(cache)};
+    return attn_common(ctx, q, cache, page_table, 1, cu_new, &prefix_len, &C, cu_pages, -1, -1, 0, INT32_MAX, Hq, scale, out, 0,
+                       false, lse, workspace, workspace_bytes, stream, "cp_prefill_attn_window", nullptr, window, sinks);
+}
+
+extern "C" int cp_prefill_attn_window_chunk(cp_ctx* ctx, const void* q_chunk, const cp_kv_cache* cache, const int32_t* page_table,
+                                            int64_t prefix_len, int64_t new_len, int32_t C, int32_t chunk, int64_t window,
+                                            int64_t sinks, int32_t Hq, float scale, void* out_chunk, float* lse_chunk,
+                                            void* workspace, size_t workspace_bytes, void* stream) {
+    if (!cache || new_len < 1 || prefix_len < 0 || C < 1 || chunk < 0 || chunk >= 2 * (int64_t)C)
+        return set_error(CP_ERR_INVALID_ARG, "cp_prefill_attn_window_chunk: bad sizes or chunk %d not in [0, 2 * %d)", chunk, C);
+    const int64_t cu_new[2] = {0, new_len};
+    const int64_t cu_pages[2] = {0, (prefix_len + new_len + page_tokens_of(cache) - 1) / page_tokens_of(cache)};
+    return attn_common(ctx, q_chunk, cache, page_table, 1, cu_new, &prefix_len, &C, cu_pages, -1, chunk, 0, INT32_MAX, Hq,
+                       scale, out_chunk, 0, false, lse_chunk, workspace, workspace_bytes, stream, "cp_prefill_attn_window_chunk",
+                       nullptr, window, sinks);
+}
+
+extern "C" int cp_prefill_attn_fp8_window_batch(cp_ctx* ctx, const void* q, const cp_kv_cache_fp8* cache, const int32_t* page_table,
+                                                int32_t B, const int64_t* cu_new, const int64_t* prefix_len, const int32_t* C,
+                                                const int64_t* cu_pages, int64_t window, int64_t sinks, int32_t Hq, float scale,
+                                                void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!cache) return set_error(CP_ERR_INVALID_ARG, "cp_prefill_attn_fp8_window_batch: cache is NULL");
+    return attn_common(ctx, q, nullptr, page_table, B, cu_new, prefix_len, C, cu_pages, -1, -1, 0, INT32_MAX, Hq, scale, out, 0,
+                       false, lse, workspace, workspace_bytes, stream, "cp_prefill_attn_fp8_window_batch", cache, window, sinks);
 }
 
 extern "C" int cp_ctx_selftest_wait_expiry(cp_ctx* ctx, void* stream) {
@@ -686,6 +743,8 @@ extern "C" int cp_prefill_attn_static(const void* q, const cp_kv_cache* cache, c
     p.n_fill = 0;
     p.q_scale = p.k_scale = p.v_scale = nullptr;
     p.co_producer = cache->page_size == 16 ? 1 : 0;
+    p.window = INT32_MAX;
+    p.sinks = 0;
     InlineSched none;          // unused: the tile list is in the scratch
     none.bytes[0] = 0;
     const int64_t units = n_tiles * p.pairs_per_tile;

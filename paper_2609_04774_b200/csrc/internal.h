@@ -88,6 +88,20 @@ struct InlineSched {
 };
 constexpr int kMaxFillRanges = 4;        // row ranges a partial-result call fills with zeros / -inf inside the kernel
 
+#ifdef __CUDACC__
+#define CP_HOST_DEVICE __host__ __device__
+#else
+#define CP_HOST_DEVICE
+#endif
+// Sliding window with sinks, for a run of queries whose first one sees kv_len0 keys (its position + 1): KV tiles
+// [0, sink_tiles) hold the sinks, the window of the first query starts in tile sink_tiles + skip, and the `skip`
+// tiles in between are hidden from it and from every later query.
+CP_HOST_DEVICE inline void window_tiles(int32_t kv_len0, int32_t window, int32_t sinks, int32_t& sink_tiles, int32_t& skip) {
+    const int32_t first = kv_len0 > window ? (kv_len0 - window) / kTileRows : 0;
+    sink_tiles = sinks / kTileRows + (sinks % kTileRows != 0);
+    skip = first > sink_tiles ? first - sink_tiles : 0;
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -101,12 +115,13 @@ int64_t max_tiles(int32_t B, const int64_t* new_len, const int32_t* C);
 // sorted longest first.  only_shard < 0 keeps all shards; only_chunk >= 0 (B == 1) keeps that one zigzag
 // chunk and numbers its rows from the chunk's first row (q, out and lse then hold the chunk alone).
 // [kv_lo, kv_hi) restricts the keys (absolute positions); tiles that see none of them are left out.
-// tile_rows: 128, or 256 when the units are single heads over tile pairs.
+// tile_rows: 128, or 256 when the units are single heads over tile pairs.  window, sinks: the KV tiles hidden from every
+// row of a query tile are left out of its count (window_tiles); the key range is then [0, INT32_MAX).
 int validate_kv_cache(const cp_kv_cache* c, const char* who);
 int validate_kv_cache_fp8(const cp_kv_cache_fp8* c, const char* who);
 int build_tiles(int32_t B, const int64_t* cu_new, const int64_t* prefix_len, const int32_t* C,
                 const int64_t* cu_pages, int32_t page_size, int32_t only_shard, int32_t only_chunk, int64_t kv_lo,
-                int64_t kv_hi, int32_t tile_rows, std::vector<TileItem>& out);
+                int64_t kv_hi, int32_t tile_rows, std::vector<TileItem>& out, int32_t window = INT32_MAX, int32_t sinks = 0);
 // Distributes the (tile, head pair) units of s.items over `grid_max` CTAs (pairs_per_kv = units of one KV
 // head per tile): whole units, KV head by KV head and longest first within a head,
 // onto the least loaded CTA while they fit under the per-CTA share, the rest cut into KV ranges that

@@ -35,7 +35,7 @@ int64_t max_tiles(int32_t B, const int64_t* new_len, const int32_t* C) {
 
 int build_tiles(int32_t B, const int64_t* cu_new, const int64_t* prefix_len, const int32_t* C,
                 const int64_t* cu_pages, int32_t page_size, int32_t only_shard, int32_t only_chunk, int64_t kv_lo,
-                int64_t kv_hi, int32_t tile_rows, std::vector<TileItem>& out) {
+                int64_t kv_hi, int32_t tile_rows, std::vector<TileItem>& out, int32_t window, int32_t sinks) {
     out.clear();
     // A launch over ALL shards of a request walks its rows as one run: adjacent zigzag chunks are adjacent rows
     // with consecutive causal limits, which the per-row limit kv_len0 + row already expresses, so a query tile may
@@ -69,7 +69,9 @@ int build_tiles(int32_t B, const int64_t* cu_new, const int64_t* prefix_len, con
                 const int64_t hi = std::min<int64_t>(kv_hi, (int64_t)t.kv_len0 + t.n_rows - 1);
                 const int64_t t_lo = kv_lo / kTileRows, t_hi = (hi + kTileRows - 1) / kTileRows;
                 if (t_hi <= t_lo) continue;
-                t.n_kv_tiles = (int32_t)(t_hi - t_lo);
+                int32_t sink_tiles, skip;
+                window_tiles(t.kv_len0, window, sinks, sink_tiles, skip);
+                t.n_kv_tiles = (int32_t)(t_hi - t_lo) - skip;
                 t.kv_lo = (int32_t)kv_lo;
                 t.kv_hi = (int32_t)std::min<int64_t>(kv_hi, INT32_MAX);
                 out.push_back(t);

@@ -403,6 +403,99 @@ int cp_kv_gather_fp8(cp_ctx* ctx, const cp_kv_cache_fp8* cache, const int32_t* p
 int cp_kv_append_segments_fp8(cp_ctx* ctx, const cp_kv_cache_fp8* cache, const int32_t* page_table, int32_t n_segments,
                               const cp_kv_segment* segments, const void* k_bytes, const void* v_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Serving calls.  Sequences are rows of a device page table [table_rows, table_stride] int32 (entry of logical page i of
+ * row r: page_table[r * table_stride + i], -1 = none); their lengths kv_len [table_rows] int32 live on the device too.
+ * Nothing of these calls is read from host memory after they return, so every one of them may be captured into a graph
+ * and replayed with other table contents and lengths.  The current device is left as it was.  Packed tables (cu_pages)
+ * of the prefill calls are the same with cu_pages[b] = b * table_stride.
+ * ------------------------------------------------------------------------------------------- */
+
+/* Rotary positions with one to four axes (text: one; images and video: time, height, width).  The first rot_dims elements of a
+ * head are rot_dims / 2 pairs; pair i is (i, i + rot_dims / 2), or (2i, 2i + 1) when interleaved, and turns by the angle
+ * positions[axis[i]][token] * freq[i] radians: (a, b) -> (a cos - b sin, b cos + a sin).  The elements behind them keep their
+ * bits.  Angles are exact to 2^-32 of a turn for every int32 position.  rot_dims: a multiple of 16.
+ * cp_rope_init fills the struct for consecutive sections of pairs per axis (sum 1..64; rot_dims = twice the sum) and
+ * freq[i] = base^(-2 i / rot_dims); callers may then change axis[] and freq[] (scaled frequencies, interleaved sections).
+ * Host only.  Errors: INVALID_ARG. */
+#define CP_ROPE_MAX_AXES 4
+typedef struct {
+    int32_t n_axes;      /* rows of `positions` */
+    int32_t rot_dims;    /* rotated elements of a head */
+    int32_t interleaved; /* 0: pairs (i, i + rot_dims / 2); else (2i, 2i + 1) */
+    int32_t reserved;
+    int32_t axis[64];    /* of pair i */
+    double freq[64];     /* radians per position, of pair i */
+} cp_rope;
+int cp_rope_init(cp_rope* rope, int32_t n_axes, const int32_t* sections, double base, int32_t interleaved);
+
+/* cp_rope_append -- rotates q into q_out, and k into the paged cache, where v goes as it is (in one launch).
+ *   q, q_out   device [n, Hq, D] bf16; q_out may be q; both NULL: no queries
+ *   k_rows, v_rows  device [n, Hkv, D] bf16; both NULL: queries only
+ *   positions  device [n_axes, n] int32 (any value)
+ *   token_seq  device [n] int32: the token's row of the page table; < 0: padding, nothing of the row is read or written
+ *   token_slot device [n] int32: the logical token of that sequence that k and v become (not read without k_rows)
+ * Rotation in fp32, one rounding to bf16 (or, _fp8, to e4m3(x / scale[head]) as in cp_kv_append_fp8).  A token outside its table
+ * row, and a page id outside the pool, is reported as CP_ERR_BOUNDS {code, token index or table entry, block, slot or page id} by
+ * cp_ctx_poll_status and its k and v are skipped; its q is rotated.  Two tokens of a call must not name the same slot.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+int cp_rope_append(cp_ctx* ctx, const cp_rope* rope, const void* q, const void* k_rows, const void* v_rows, int64_t n, int32_t Hq,
+                   const int32_t* positions, const int32_t* token_seq, const int32_t* token_slot, const cp_kv_cache* cache,
+                   const int32_t* page_table, int64_t table_rows, int64_t table_stride, void* q_out, void* stream);
+int cp_rope_append_fp8(cp_ctx* ctx, const cp_rope* rope, const void* q, const void* k_rows, const void* v_rows, int64_t n,
+                       int32_t Hq, const int32_t* positions, const int32_t* token_seq, const int32_t* token_slot,
+                       const cp_kv_cache_fp8* cache, const int32_t* page_table, int64_t table_rows, int64_t table_stride,
+                       void* q_out, void* stream);
+
+/* The care of the pages.  A pool is n_layers K and V caches of one geometry (layer l: k[l], v[l]; strides in BYTES, multiples of
+ * 16; row_bytes = bytes of one head's row: 256 bf16, 128 E4M3) whose pages share one numbering, and refcount [num_pages] int32 on
+ * the device: how many table entries name a page; 0 = free.  k and v are host arrays of device pointers, read before the call
+ * returns; extend, evict and free look at num_pages and page_size only.  Pages are handed out lowest free id first, to the rows
+ * in order.  cp_workspace_bytes_pages: workspace of the calls that take one, for n forks or copies (0 elsewhere); a workspace
+ * belongs to one call at a time.  What cannot be done is skipped and reported as CP_ERR_BOUNDS by cp_ctx_poll_status.
+ *   extend   room for new_tokens[r] >= 0 more tokens in every row r (0: none wanted): new table entries, refcount 1, kv_len[r] +=
+ *            new_tokens[r].  A row that does not get all its pages (pool or row full) gets none and keeps its length; rows
+ *            behind it that need pages get none either.  {code, row, block, -1 or the tokens wanted}
+ *   evict    the next token of a row sits at position kv_len[r]: entries of pages that are wholly behind its window and
+ *            behind the sinks become -1 and give up their reference (CP_NO_WINDOW: none do)
+ *   free     all entries of the n listed rows are given up, kv_len becomes 0 (a row named twice counts once)
+ *   fork     child row = parent row: the full pages are shared (refcount + 1; -1 entries stay -1), the tokens of a partly filled
+ *            last page are copied, in every layer, to a page of the child's own; kv_len[child] = kv_len[parent].  The child's
+ *            old entries are overwritten (free it before).  Children are distinct and none is a parent in the same call.
+ *            Without a free page the child ends with its last full page.  {code, fork, block, -1 or a bad id}
+ *   compact  the n_live pages in use move to the ids [0, n_live): those already there stay, the others take the holes in
+ *            ascending order.  page_map [num_pages] receives each page's new id (-1: free), n_live [1] the count; refcount and
+ *            the whole table follow
+ *   copy     page src[i] -> page dst[i], in every layer.  The dst are distinct and none is a src
+ * An entry given up that names no page of the pool, or a free one, is reported {code, entry, block, id}.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA. */
+#define CP_POOL_MAX_LAYERS 128
+typedef struct {
+    void* const* k;      /* host array of n_layers device pointers */
+    void* const* v;
+    int64_t num_pages;
+    int32_t n_layers;    /* <= CP_POOL_MAX_LAYERS */
+    int32_t page_size;   /* 16, 32, 64 or 128 */
+    int32_t Hkv;
+    int32_t row_bytes;
+    int64_t stride_page, stride_tok, stride_head; /* bytes */
+} cp_page_pool;
+size_t cp_workspace_bytes_pages(int64_t num_pages, int64_t n);
+int cp_pages_extend(cp_ctx* ctx, const cp_page_pool* pool, int32_t* refcount, int32_t* page_table, int64_t table_rows,
+                    int64_t table_stride, int32_t* kv_len, const int32_t* new_tokens, void* workspace, size_t workspace_bytes,
+                    void* stream);
+int cp_pages_evict(cp_ctx* ctx, const cp_page_pool* pool, int32_t* refcount, int32_t* page_table, int64_t table_rows,
+                   int64_t table_stride, const int32_t* kv_len, int64_t window, int64_t sinks, void* stream);
+int cp_pages_free(cp_ctx* ctx, const cp_page_pool* pool, int32_t* refcount, int32_t* page_table, int64_t table_rows,
+                  int64_t table_stride, int32_t* kv_len, const int32_t* rows, int32_t n, void* stream);
+int cp_pages_fork(cp_ctx* ctx, const cp_page_pool* pool, int32_t* refcount, int32_t* page_table, int64_t table_rows,
+                  int64_t table_stride, int32_t* kv_len, const int32_t* parent, const int32_t* child, int32_t n, void* workspace,
+                  size_t workspace_bytes, void* stream);
+int cp_pages_compact(cp_ctx* ctx, const cp_page_pool* pool, int32_t* refcount, int32_t* page_table, int64_t table_rows,
+                     int64_t table_stride, int32_t* page_map, int32_t* n_live, void* workspace, size_t workspace_bytes, void* stream);
+int cp_pages_copy(cp_ctx* ctx, const cp_page_pool* pool, const int32_t* src, const int32_t* dst, int32_t n, void* workspace,
+                  size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,7 +25,24 @@ EXPORTS = ["cp_strerror", "cp_last_error", "cp_ctx_create", "cp_ctx_destroy", "c
            "cp_kv_gather", "cp_kv_append", "cp_workspace_bytes_fp8", "cp_prefill_attn_fp8", "cp_prefill_attn_fp8_batch",
            "cp_kv_append_fp8", "cp_kv_append_segments", "cp_prefill_attn_fp8_shard", "cp_prefill_attn_fp8_chunk",
            "cp_prefill_attn_fp8_kvrange", "cp_kv_gather_fp8", "cp_kv_append_segments_fp8", "cp_check_page_table",
-           "cp_prefill_attn_window", "cp_prefill_attn_window_batch", "cp_prefill_attn_window_chunk", "cp_prefill_attn_fp8_window_batch"]
+           "cp_prefill_attn_window", "cp_prefill_attn_window_batch", "cp_prefill_attn_window_chunk", "cp_prefill_attn_fp8_window_batch",
+           "cp_rope_init", "cp_rope_append", "cp_rope_append_fp8", "cp_workspace_bytes_pages", "cp_pages_extend", "cp_pages_evict",
+           "cp_pages_free", "cp_pages_fork", "cp_pages_compact", "cp_pages_copy"]
+
+# The serving calls run once per layer and token, so their argument types are declared once and plain integers are passed.
+_P, _I, _L, _F, _Z = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+_ARGTYPES = {
+    "cp_rope_init": [_P, _I, _P, ctypes.c_double, _I],
+    "cp_rope_append": [_P, _P, _P, _P, _P, _L, _I, _P, _P, _P, _P, _P, _L, _L, _P, _P],
+    "cp_rope_append_fp8": [_P, _P, _P, _P, _P, _L, _I, _P, _P, _P, _P, _P, _L, _L, _P, _P],
+    "cp_workspace_bytes_pages": [_L, _L],
+    "cp_pages_extend": [_P, _P, _P, _P, _L, _L, _P, _P, _P, _Z, _P],
+    "cp_pages_evict": [_P, _P, _P, _P, _L, _L, _P, _L, _L, _P],
+    "cp_pages_free": [_P, _P, _P, _P, _L, _L, _P, _P, _I, _P],
+    "cp_pages_fork": [_P, _P, _P, _P, _L, _L, _P, _P, _P, _I, _P, _Z, _P],
+    "cp_pages_compact": [_P, _P, _P, _P, _L, _L, _P, _P, _P, _Z, _P],
+    "cp_pages_copy": [_P, _P, _P, _P, _I, _P, _Z, _P],
+}
 
 
 class CpError(RuntimeError):
@@ -53,6 +70,17 @@ class cp_kv_cache_fp8(ctypes.Structure):
                 ("stride_head", ctypes.c_int64)]
 
 
+class cp_rope(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("rot_dims", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("axis", ctypes.c_int32 * 64), ("freq", ctypes.c_double * 64)]
+
+
+class cp_page_pool(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("num_pages", ctypes.c_int64), ("n_layers", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("row_bytes", ctypes.c_int32), ("stride_page", ctypes.c_int64),
+                ("stride_tok", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -69,9 +97,12 @@ def load():
         lib.cp_last_error.restype = ctypes.c_char_p
         lib.cp_workspace_bytes.restype = ctypes.c_size_t
         lib.cp_workspace_bytes_fp8.restype = ctypes.c_size_t
+        lib.cp_workspace_bytes_pages.restype = ctypes.c_size_t
         for name in EXPORTS:
-            if name not in ("cp_strerror", "cp_last_error", "cp_workspace_bytes", "cp_workspace_bytes_fp8"):
+            if name not in ("cp_strerror", "cp_last_error") and not name.startswith("cp_workspace_bytes"):
                 getattr(lib, name).restype = ctypes.c_int
+        for name, types in _ARGTYPES.items():
+            getattr(lib, name).argtypes = types
         _lib = lib
     return _lib
 
@@ -398,3 +429,141 @@ def cp_check_page_table(ctx, page_table, num_pages, stream=None):
     """Enqueue the page-table check; a bad entry shows as CP_ERR_BOUNDS at the next poll_status() after a sync."""
     _check(load().cp_check_page_table(ctx._h, _ptr(page_table), ctypes.c_int64(page_table.numel()),
                                       ctypes.c_int64(num_pages), _stream(stream)))
+
+
+# ------------------------------------------------------------------------------------------------
+# Serving calls: rotary append, page care
+# ------------------------------------------------------------------------------------------------
+
+def _raw_stream(ctx, stream):
+    """The given stream, or the current one of the context's device."""
+    if stream is not None:
+        return stream.cuda_stream
+    import torch
+    return torch._C._cuda_getCurrentRawStream(ctx.device)
+
+
+def _arg(t, name, dtype, *shape):
+    """Address of a contiguous CUDA tensor of the given type and shape (None in the shape: any size); None stays None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s CUDA tensor, got %s on %s with strides %s" % (name, dtype, t.dtype, t.device, t.stride()))
+    if len(t.shape) != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple("*" if w is None else w for w in shape)))
+    return t.data_ptr()
+
+
+def make_rope(sections, base=10000.0, interleaved=False) -> cp_rope:
+    """Rotary description for consecutive sections of pairs, one per axis ([64]: plain positions; [16, 24, 24]: time, height, width).
+    Its axis[] and freq[] (radians per position, per pair) may be changed afterwards."""
+    sec = _i32(sections).reshape(-1)
+    rope = cp_rope()
+    _check(load().cp_rope_init(ctypes.addressof(rope), sec.size, sec.ctypes.data, base, 1 if interleaved else 0))
+    return rope
+
+
+def _rope_append(call, ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream):
+    import torch
+    bf16, i32 = torch.bfloat16, torch.int32
+    n = token_seq.shape[0]
+    Hq = q.shape[1] if q is not None else 0
+    rows, stride = page_table.shape if page_table is not None else (0, 0)
+    _check(call(ctx._h, ctypes.addressof(rope), _arg(q, "q", bf16, n, Hq, 128), _arg(k_rows, "k_rows", bf16, n, cache.Hkv, 128),
+                _arg(v_rows, "v_rows", bf16, n, cache.Hkv, 128), n, Hq, _arg(positions, "positions", i32, rope.n_axes, n),
+                _arg(token_seq, "token_seq", i32, n), _arg(token_slot, "token_slot", i32, n), ctypes.addressof(cache),
+                _arg(page_table, "page_table", i32, rows, stride), rows, stride, _arg(q_out, "q_out", bf16, n, Hq, 128),
+                _raw_stream(ctx, stream)))
+
+
+def cp_rope_append(ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream=None):
+    """q [n, Hq, 128] -> q_out (may be q); k_rows, v_rows [n, Hkv, 128] -> slot token_slot[i] of sequence token_seq[i] of the paged cache;
+    positions [n_axes, n], token_seq, token_slot [n], page_table [rows, stride], all int32.  token_seq < 0: padding."""
+    _rope_append(load().cp_rope_append, ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream)
+
+
+def cp_rope_append_fp8(ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream=None):
+    """cp_rope_append into an FP8 cache: k (rotated) and v as e4m3(x / scale[head])."""
+    _rope_append(load().cp_rope_append_fp8, ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream)
+
+
+def make_page_pool(k, v, num_pages=None) -> cp_page_pool:
+    """Describe the K and V pools of one numbering of pages: k, v [layers, num_pages, page_size, Hkv, 128], or lists of such 4-D
+    tensors, bf16 or uint8 (E4M3); all of one geometry."""
+    ks, vs = [k[i] for i in range(len(k))], [v[i] for i in range(len(v))]
+    first = ks[0]
+    if len(ks) != len(vs) or any(t.shape != first.shape or t.stride() != first.stride() or t.dtype != first.dtype for t in ks + vs):
+        raise ValueError("the layers' k and v must agree in number, shape, strides and type")
+    if first.dim() != 4 or first.shape[3] != 128 or first.stride(3) != 1 or (num_pages is not None and num_pages != first.shape[0]):
+        raise ValueError("a layer is [num_pages, page_size, Hkv, 128] with unit stride in the last dimension, got %s" % (tuple(first.shape),))
+    e = first.element_size()
+    p = cp_page_pool()
+    p._k = (ctypes.c_void_p * len(ks))(*[t.data_ptr() for t in ks])        # kept alive with the descriptor
+    p._v = (ctypes.c_void_p * len(vs))(*[t.data_ptr() for t in vs])
+    p.k, p.v = ctypes.addressof(p._k), ctypes.addressof(p._v)
+    p.n_layers = len(ks)
+    p.num_pages, p.page_size, p.Hkv, p.row_bytes = first.shape[0], first.shape[1], first.shape[2], 128 * e
+    p.stride_page, p.stride_tok, p.stride_head = first.stride(0) * e, first.stride(1) * e, first.stride(2) * e
+    return p
+
+
+def cp_workspace_bytes_pages(num_pages, n=0) -> int:
+    return int(load().cp_workspace_bytes_pages(num_pages, n))
+
+
+def _table_args(pool, refcount, page_table, kv_len):
+    import torch
+    rows, stride = page_table.shape
+    return (_arg(refcount, "refcount", torch.int32, pool.num_pages), _arg(page_table, "page_table", torch.int32, rows, stride), rows, stride,
+            _arg(kv_len, "kv_len", torch.int32, rows))
+
+
+def _ws(workspace):
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def cp_pages_extend(ctx, pool, refcount, page_table, kv_len, new_tokens, workspace, stream=None):
+    """Room for new_tokens[r] more tokens in every row: entries, references and kv_len are updated on the device."""
+    import torch
+    rc, pt, rows, stride, kl = _table_args(pool, refcount, page_table, kv_len)
+    _check(load().cp_pages_extend(ctx._h, ctypes.addressof(pool), rc, pt, rows, stride, kl, _arg(new_tokens, "new_tokens", torch.int32, rows),
+                                  *_ws(workspace), _raw_stream(ctx, stream)))
+
+
+def cp_pages_evict(ctx, pool, refcount, page_table, kv_len, window, sinks, stream=None):
+    """Give back the pages that the next token of each row (position kv_len) and all later ones cannot see."""
+    rc, pt, rows, stride, kl = _table_args(pool, refcount, page_table, kv_len)
+    _check(load().cp_pages_evict(ctx._h, ctypes.addressof(pool), rc, pt, rows, stride, kl, window, sinks, _raw_stream(ctx, stream)))
+
+
+def cp_pages_free(ctx, pool, refcount, page_table, kv_len, rows, stream=None):
+    """Give back all pages of the listed rows (int32 tensor); their kv_len becomes 0."""
+    import torch
+    rc, pt, n_rows, stride, kl = _table_args(pool, refcount, page_table, kv_len)
+    _check(load().cp_pages_free(ctx._h, ctypes.addressof(pool), rc, pt, n_rows, stride, kl, _arg(rows, "rows", torch.int32, None), rows.numel(),
+                                _raw_stream(ctx, stream)))
+
+
+def cp_pages_fork(ctx, pool, refcount, page_table, kv_len, parent, child, workspace, stream=None):
+    """Rows child[i] become copies of rows parent[i]: full pages shared, the tokens of a partly filled last page copied in every layer."""
+    import torch
+    rc, pt, rows, stride, kl = _table_args(pool, refcount, page_table, kv_len)
+    n = parent.numel()
+    _check(load().cp_pages_fork(ctx._h, ctypes.addressof(pool), rc, pt, rows, stride, kl, _arg(parent, "parent", torch.int32, n),
+                                _arg(child, "child", torch.int32, n), n, *_ws(workspace), _raw_stream(ctx, stream)))
+
+
+def cp_pages_compact(ctx, pool, refcount, page_table, page_map, n_live, workspace, stream=None):
+    """Move the pages in use to ids [0, n_live); page_map [num_pages] and n_live [1] (int32) receive the new ids and the count."""
+    import torch
+    rc, pt, rows, stride, _ = _table_args(pool, refcount, page_table, None)
+    _check(load().cp_pages_compact(ctx._h, ctypes.addressof(pool), rc, pt, rows, stride, _arg(page_map, "page_map", torch.int32, pool.num_pages),
+                                   _arg(n_live, "n_live", torch.int32, 1), *_ws(workspace), _raw_stream(ctx, stream)))
+
+
+def cp_pages_copy(ctx, pool, src, dst, workspace, stream=None):
+    """Page src[i] -> page dst[i] (int32 tensors) in every layer."""
+    import torch
+    n = src.numel()
+    _check(load().cp_pages_copy(ctx._h, ctypes.addressof(pool), _arg(src, "src", torch.int32, n), _arg(dst, "dst", torch.int32, n), n,
+                                *_ws(workspace), _raw_stream(ctx, stream)))

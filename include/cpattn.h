@@ -447,6 +447,26 @@ int cp_rope_append_fp8(cp_ctx* ctx, const cp_rope* rope, const void* q, const vo
                        const cp_kv_cache_fp8* cache, const int32_t* page_table, int64_t table_rows, int64_t table_stride,
                        void* q_out, void* stream);
 
+/* cp_decode_attn -- attention of the last n_q tokens of B sequences over a paged cache (n_q = 1: the decode step; a few: draft tokens
+ * checked together), full (window = CP_NO_WINDOW) or with a window and sinks as in cp_prefill_attn_window.  Their K and V are in the
+ * cache already.
+ *   q        device [B, n_q, Hq, D] bf16: row (b, t) is the token at position kv_len[b] - n_q + t
+ *   page_table  device [B, table_stride] int32; kv_len  device [B] int32, the new tokens included
+ *   out      device [B, n_q, Hq, D] bf16;  lse  device [Hq, B * n_q] fp32 (the layout cp_merge takes)
+ * A row before position 0 (kv_len[b] < n_q; kv_len[b] = 0 for an idle row) sees nothing: zeros, lse = -inf.  Only slots that some row
+ * sees are read; an entry outside the pool reads as zeros.  kv_len[b] < 0 counts as 0, one beyond the table row as the row's
+ * capacity; both are reported as CP_ERR_BOUNDS {code, b, block, kv_len} by cp_ctx_poll_status.  Weights are rounded to bf16 for P V (_fp8:
+ * to fp16), all sums are fp32.  Two launches, whose grids do not depend on the lengths: a captured call is replayed with other
+ * lengths and tables.  workspace: cp_workspace_bytes_decode (0 on invalid arguments), for one call at a time.
+ * Limits: n_q <= 64, n_q * Hq / Hkv <= 1024, B <= 65536.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA. */
+size_t cp_workspace_bytes_decode(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv);
+int cp_decode_attn(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table, int64_t table_stride,
+                   const int32_t* kv_len, int32_t B, int32_t n_q, int32_t Hq, int64_t window, int64_t sinks, float scale, void* out,
+                   float* lse, void* workspace, size_t workspace_bytes, void* stream);
+int cp_decode_attn_fp8(cp_ctx* ctx, const void* q, const cp_kv_cache_fp8* cache, const int32_t* page_table, int64_t table_stride,
+                       const int32_t* kv_len, int32_t B, int32_t n_q, int32_t Hq, int64_t window, int64_t sinks, float scale, void* out,
+                       float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* The care of the pages.  A pool is n_layers K and V caches of one geometry (layer l: k[l], v[l]; strides in BYTES, multiples of
  * 16; row_bytes = bytes of one head's row: 256 bf16, 128 E4M3) whose pages share one numbering, and refcount [num_pages] int32 on
  * the device: how many table entries name a page; 0 = free.  k and v are host arrays of device pointers, read before the call

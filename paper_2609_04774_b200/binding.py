@@ -27,7 +27,8 @@ EXPORTS = ["cp_strerror", "cp_last_error", "cp_ctx_create", "cp_ctx_destroy", "c
            "cp_prefill_attn_fp8_kvrange", "cp_kv_gather_fp8", "cp_kv_append_segments_fp8", "cp_check_page_table",
            "cp_prefill_attn_window", "cp_prefill_attn_window_batch", "cp_prefill_attn_window_chunk", "cp_prefill_attn_fp8_window_batch",
            "cp_rope_init", "cp_rope_append", "cp_rope_append_fp8", "cp_workspace_bytes_pages", "cp_pages_extend", "cp_pages_evict",
-           "cp_pages_free", "cp_pages_fork", "cp_pages_compact", "cp_pages_copy"]
+           "cp_pages_free", "cp_pages_fork", "cp_pages_compact", "cp_pages_copy", "cp_workspace_bytes_decode", "cp_decode_attn",
+           "cp_decode_attn_fp8"]
 
 # The serving calls run once per layer and token, so their argument types are declared once and plain integers are passed.
 _P, _I, _L, _F, _Z = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
@@ -42,6 +43,9 @@ _ARGTYPES = {
     "cp_pages_fork": [_P, _P, _P, _P, _L, _L, _P, _P, _P, _I, _P, _Z, _P],
     "cp_pages_compact": [_P, _P, _P, _P, _L, _L, _P, _P, _P, _Z, _P],
     "cp_pages_copy": [_P, _P, _P, _P, _I, _P, _Z, _P],
+    "cp_workspace_bytes_decode": [_I, _I, _I, _I],
+    "cp_decode_attn": [_P, _P, _P, _P, _L, _P, _I, _I, _I, _L, _L, _F, _P, _P, _P, _Z, _P],
+    "cp_decode_attn_fp8": [_P, _P, _P, _P, _L, _P, _I, _I, _I, _L, _L, _F, _P, _P, _P, _Z, _P],
 }
 
 
@@ -98,6 +102,7 @@ def load():
         lib.cp_workspace_bytes.restype = ctypes.c_size_t
         lib.cp_workspace_bytes_fp8.restype = ctypes.c_size_t
         lib.cp_workspace_bytes_pages.restype = ctypes.c_size_t
+        lib.cp_workspace_bytes_decode.restype = ctypes.c_size_t
         for name in EXPORTS:
             if name not in ("cp_strerror", "cp_last_error") and not name.startswith("cp_workspace_bytes"):
                 getattr(lib, name).restype = ctypes.c_int
@@ -432,7 +437,7 @@ def cp_check_page_table(ctx, page_table, num_pages, stream=None):
 
 
 # ------------------------------------------------------------------------------------------------
-# Serving calls: rotary append, page care
+# Serving calls: decode attention, rotary append, page care
 # ------------------------------------------------------------------------------------------------
 
 def _raw_stream(ctx, stream):
@@ -452,6 +457,31 @@ def _arg(t, name, dtype, *shape):
     if len(t.shape) != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple("*" if w is None else w for w in shape)))
     return t.data_ptr()
+
+
+def cp_workspace_bytes_decode(B, n_q, Hq, Hkv) -> int:
+    return int(load().cp_workspace_bytes_decode(B, n_q, Hq, Hkv))
+
+
+def _decode_attn(call, ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream):
+    import torch
+    B, n_q, Hq, _ = q.shape
+    rows, stride = page_table.shape
+    _check(call(ctx._h, _arg(q, "q", torch.bfloat16, B, n_q, Hq, 128), ctypes.addressof(cache), _arg(page_table, "page_table", torch.int32, B, stride),
+                stride, _arg(kv_len, "kv_len", torch.int32, B), B, n_q, Hq, window, sinks, scale, _arg(out, "out", torch.bfloat16, B, n_q, Hq, 128),
+                _arg(lse, "lse", torch.float32, Hq, B * n_q), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                _raw_stream(ctx, stream)))
+
+
+def cp_decode_attn(ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream=None):
+    """The last n_q tokens of B sequences: q, out [B, n_q, Hq, 128] bf16, page_table [B, stride] and kv_len [B] int32 on the device (new
+    tokens included), lse [Hq, B * n_q] fp32.  window = CP_NO_WINDOW: every key."""
+    _decode_attn(load().cp_decode_attn, ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream)
+
+
+def cp_decode_attn_fp8(ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream=None):
+    """cp_decode_attn over an FP8 cache."""
+    _decode_attn(load().cp_decode_attn_fp8, ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream)
 
 
 def make_rope(sections, base=10000.0, interleaved=False) -> cp_rope:

@@ -1,0 +1,813 @@
+// Decode attention: one or a few new tokens per request over a paged cache (bf16 or E4M3), full or with a sliding window and
+// sinks; lengths and page tables are read on the device.
+//
+//   O = sum_j p_j v_j / sum_j p_j,   p_j = 2^(c q.k_j - m),   c = scale log2(e),   LSE = ln sum_j e^(scale q.k_j)
+//
+// HBM-bound: every visible key and value is read once (512 bytes a key and KV head in bf16, 256 in E4M3) and serves the n_q * G query
+// rows of its head group, 4 * 128 flops a row: 8 flops a byte for 8 rows, which the legacy warp MMA (m16n8k16) covers many
+// times over.  What counts is bytes in flight, so the kernel is built around the load stream:
+//   - One CTA per SM, 8 warps.  The work is the list of 128-key tiles of all (request, KV head, row group) units, cut into equal
+//     runs of tiles, one run per CTA, whatever the lengths.  A warp owns 16 keys of every tile and a ring of 3 (bf16) or 6 (E4M3) slots
+//     that it fills with cp.async and reads by itself: no barrier in the loop, 128-160 KB in flight per SM, across unit
+//     boundaries as well.
+//   - Products with the keys as the M side: S^T[16 keys x 8 rows] = K Q^T, and O^T[16 dims x 8 rows] += V^T P^T, so 8 query rows
+//     fill an MMA (with the rows on the M side half of it would be padding).  K goes through ldmatrix, V through its transposed form;
+//     the weights turn from accumulator to operand layout with one movmatrix per 8 x 8 block.
+//   - Every warp keeps its own running maximum and sum; the maximum is only raised (and O rescaled) when a score exceeds it by more than 2^8,
+//     which one vote per 16 keys finds out.
+//   - At the end of a unit's run the 8 warps' partial results are merged through shared memory in a fixed order.  A unit that lies
+//     in one run is written out; the pieces of a cut unit go to the workspace as unnormalised fp32 rows with their maximum and sum, and a
+//     second launch merges them.
+// E4M3: codes are widened exactly to fp16 in registers; the queries become fp16 after a power-of-two scaling per row (bf16's 8 bits of
+// mantissa fit; what falls below 2^-24 of the row's largest is lost), weights are fp16 after a scaling by 2^7, so the
+// result has fp16 weights (2^-11) where the bf16 cache has bf16 ones (2^-8).  Sums, maxima and accumulators are fp32.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "device_util.cuh"
+#include "internal.h"
+
+using namespace cpattn;
+
+namespace {
+
+constexpr int kDim = 128;
+constexpr int kWarps = 8;
+constexpr int kDecThreads = kWarps * 32;
+constexpr int kSubKeys = 16;                               // keys of a tile that one warp owns
+static_assert(kWarps * kSubKeys == kTileRows, "window_tiles counts in tiles of 128 keys");
+constexpr float kLag = 8.0f;                               // the running maximum may lag by a factor 2^8
+constexpr float kF16Shift = 7.0f;                          // fp16 weights carry 2^7: at most 2^15 with the lag
+constexpr int kMaxRowsPerUnit = 32;
+constexpr uint32_t kRingBytes = 196608;
+constexpr uint32_t kMergeBytes = 16384;
+constexpr uint32_t kMlBytes = kWarps * kMaxRowsPerUnit * 8;
+constexpr uint32_t kQBytes = 2 * kMaxRowsPerUnit * kDim * 2;
+constexpr uint32_t kDecSmem = kRingBytes + kMergeBytes + kMlBytes + kQBytes + 256;
+
+struct DecodeParams {
+    const __nv_bfloat16* q;
+    const uint8_t* k;
+    const uint8_t* v;
+    const float* k_scale;
+    const float* v_scale;
+    const int32_t* table;
+    const int32_t* kv_len;
+    int64_t table_stride, num_pages, stride_page, stride_tok, stride_head;     // strides in bytes
+    int32_t page_shift;
+    int32_t B, n_q, Hq, Hkv, G;
+    int32_t rows;              // n_q * G
+    int32_t row_groups;        // units per (request, KV head)
+    int32_t window, sinks;
+    int32_t capacity;          // tokens a table row can hold
+    float scale_log2;
+    __nv_bfloat16* out;
+    float* lse;
+    float* part_o;             // [2 * grid][rows of a unit][128]
+    float* part_ml;            // [2 * grid][rows of a unit][2]
+    int32_t* meta;             // [grid][4]: request, unit, CTAs, valid
+    int32_t* status;
+};
+
+// ---------------------------------------------------------------------------------------------- PTX
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
+    const int n = valid ? 16 : 0;                          // 0: nothing is read, the 16 bytes become zeros
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+template <bool kF16>
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if (kF16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Two E4M3 codes (low 16 bits) -> two fp16 values, exact.
+__device__ __forceinline__ uint32_t widen2(uint32_t codes) {
+    uint32_t y;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"((uint16_t)codes));
+    return y;
+}
+template <bool kF16>
+__device__ __forceinline__ uint32_t pack_weights(float lo, float hi) {
+    if (kF16) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// ---------------------------------------------------------------------------------------------- work list
+// Tiles of one unit of a request: 128-key tiles that some of its rows see, at least one (an empty request still writes its rows).
+struct Request {
+    int32_t len;               // keys of the request
+    int32_t n;                 // tiles of a unit
+    int32_t sink_tiles, skip;
+};
+__device__ __forceinline__ Request request_of(const DecodeParams& p, int b) {
+    Request r;
+    r.len = min(max(p.kv_len[b], 0), p.capacity);
+    window_tiles(r.len - p.n_q + 1, p.window, p.sinks, r.sink_tiles, r.skip);
+    r.n = max(1, (r.len + kTileRows - 1) / kTileRows - r.skip);
+    return r;
+}
+// A position in the list: request, unit (KV head major, then row group), tile.
+struct Cursor {
+    int32_t b, u, t;
+    Request r;
+    __device__ __forceinline__ void next(const DecodeParams& p, int units) {
+        if (++t < r.n) return;
+        t = 0;
+        if (++u < units) return;
+        u = 0;
+        if (++b < p.B) r = request_of(p, b);
+    }
+    __device__ __forceinline__ int first_key(int warp) const {
+        return (t < r.sink_tiles ? t : t + r.skip) * kTileRows + warp * kSubKeys;
+    }
+};
+
+__device__ __forceinline__ int64_t run_begin(int64_t total, int64_t cta, int64_t ctas) { return total * cta / ctas; }
+
+// NT: query rows of a unit in blocks of 8.  kFp8: E4M3 cache.
+template <int NT, bool kFp8>
+__global__ void __launch_bounds__(kDecThreads, 1)
+decode_kernel(const __grid_constant__ DecodeParams p) {
+    constexpr int kRowBytes = kFp8 ? 128 : 256;            // one key's row of one head
+    constexpr int kHalf = kSubKeys * kRowBytes;            // the K half of a ring slot
+    constexpr int kStages = kRingBytes / (kWarps * 2 * kHalf);
+    constexpr int kRows = NT * 8;
+    constexpr int kPassTiles = 4 / NT;                     // 16-dim blocks merged per pass: 16 KB of partial sums
+    constexpr bool kQRegs = NT <= 2;                       // query fragments stay in registers (32 rows read them from shared memory)
+    extern __shared__ __align__(1024) uint8_t smem[];
+    float* merge_buf = reinterpret_cast<float*>(smem + kRingBytes);
+    float* ml = reinterpret_cast<float*>(smem + kRingBytes + kMergeBytes);                     // [warp][row][2]
+    uint8_t* q_buf = smem + kRingBytes + kMergeBytes + kMlBytes;                               // 2 x [row][256 B], chunks swizzled
+    int64_t* scan = reinterpret_cast<int64_t*>(q_buf + kQBytes);                               // warp sums, then the run's start
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int g = lane >> 2, qd = lane & 3;
+    const int units = p.Hkv * p.row_groups;
+
+    // where this CTA's run starts: requests are dealt to the threads in order, a prefix sum over their tiles finds it
+    const int per = (p.B + kDecThreads - 1) / kDecThreads;
+    int64_t mine = 0;
+    for (int i = 0; i < per; ++i) {
+        const int b = tid * per + i;
+        if (b < p.B) {
+            mine += request_of(p, b).n;
+            if (blockIdx.x == 0 && (p.kv_len[b] > p.capacity || p.kv_len[b] < 0)) report_status(p.status, CP_ERR_BOUNDS, b, p.kv_len[b]);
+        }
+    }
+    int64_t inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+    }
+    if (lane == 31) scan[warp] = inc;
+    __syncthreads();
+    int64_t before = inc - mine, total = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+        if (i < warp) before += scan[i];
+        total += scan[i];
+    }
+    total *= units;
+    before *= units;
+    const int64_t ctas = min((int64_t)gridDim.x, total);   // every run holds a tile
+    const int64_t x0 = blockIdx.x < ctas ? run_begin(total, blockIdx.x, ctas) : total;
+    const int64_t x1 = blockIdx.x < ctas ? run_begin(total, blockIdx.x + 1, ctas) : total;
+    int32_t* start = reinterpret_cast<int32_t*>(scan + kWarps);
+    if (x0 >= before && x0 < before + mine * units) {
+        int b = tid * per;
+        int64_t at = before;
+        while (true) {
+            const int64_t n = (int64_t)request_of(p, b).n * units;
+            if (x0 < at + n) break;
+            at += n;
+            ++b;
+        }
+        const int n = request_of(p, b).n;
+        start[0] = b;
+        start[1] = (int32_t)((x0 - at) / n);
+        start[2] = (int32_t)((x0 - at) % n);
+    }
+    if (tid == 0) p.meta[blockIdx.x * 4 + 3] = 0;
+    __syncthreads();
+    if (x0 >= x1) return;
+
+    Cursor ld, cur;                                        // the load stream runs kStages - 1 tiles ahead
+    ld.b = start[0];
+    ld.u = start[1];
+    ld.t = start[2];
+    ld.r = request_of(p, ld.b);
+    cur = ld;
+    int64_t to_load = x1 - x0, to_do = x1 - x0;
+
+    // ------------------------------------------------------------------ loads
+    auto visible_group = [&](const Request& r, int key0) {
+        const int low = r.len - p.n_q + 1 - p.window;      // lowest key of the first row's window
+        return key0 < r.len && (key0 + kSubKeys > low || key0 < p.sinks);
+    };
+    auto page_of = [&](const Cursor& c) -> int64_t {       // page of this warp's keys; -1: none to read
+        const int key0 = c.first_key(warp);
+        if (!visible_group(c.r, key0)) return -1;
+        const int64_t page = __ldg(p.table + c.b * p.table_stride + (key0 >> p.page_shift));
+        return page < p.num_pages ? page : -1;
+    };
+    uint8_t* ring = smem + warp * (kStages * 2 * kHalf);
+    const uint32_t ring_s = smem_addr(ring);
+    int slot_ld = 0, slot_cur = 0;
+    int64_t next_page = page_of(ld);
+    auto load_tile = [&]() {
+        if (to_load > 0) {
+            const int64_t page = next_page;
+            const int key0 = ld.first_key(warp), len = ld.r.len, low = len - p.n_q + 1 - p.window;
+            if (visible_group(ld.r, key0)) {
+                constexpr int kChunks = kRowBytes / 16, kKeysPerStep = 32 / kChunks;
+                const int c = lane % kChunks, k0 = lane / kChunks;
+                const int64_t off = page * p.stride_page + (int64_t)((key0 & ((1 << p.page_shift) - 1)) + k0) * p.stride_tok +
+                                    (int64_t)(ld.u / p.row_groups) * p.stride_head + c * 16;
+                const uint32_t dst = ring_s + slot_ld * (2 * kHalf);
+#pragma unroll
+                for (int i = 0; i < kSubKeys / kKeysPerStep; ++i) {
+                    const int kk = i * kKeysPerStep + k0, key = key0 + kk;
+                    const bool ok = page >= 0 && key < len && (key >= low || key < p.sinks);
+                    const int64_t o = ok ? off + i * kKeysPerStep * p.stride_tok : 0;
+                    const uint32_t d = dst + kk * kRowBytes + ((c ^ (kk & 7)) << 4);
+                    cp_async16(d, p.k + o, ok);
+                    cp_async16(d + kHalf, p.v + o, ok);
+                }
+            }
+            if (--to_load > 0) {
+                ld.next(p, units);
+                next_page = page_of(ld);
+            }
+            slot_ld = slot_ld + 1 == kStages ? 0 : slot_ld + 1;
+        }
+        cp_commit();
+    };
+    // the query rows of unit (b, u) into buffer `buf`; rows behind the last are zeros
+    auto load_q = [&](int b, int u, int buf) {
+        const int h = u / p.row_groups, r0 = (u - h * p.row_groups) * kRows;
+        for (int i = tid; i < kRows * 16; i += kDecThreads) {
+            const int row = i >> 4, c = i & 15, r = r0 + row;
+            const bool ok = r < p.rows;
+            const int t = ok ? r / p.G : 0;
+            const int64_t o = ok ? (((int64_t)b * p.n_q + t) * p.Hq + h * p.G + (r - t * p.G)) * kDim + c * 8 : 0;
+            cp_async16(smem_addr(q_buf + buf * (kRows * 256) + row * 256 + ((c ^ (row & 7)) << 4)), p.q + o, ok);
+        }
+    };
+
+    load_q(cur.b, cur.u, 0);
+    for (int i = 0; i < kStages - 1; ++i) load_tile();
+    cp_wait<kStages - 2>();                                // the first group carries the queries
+    __syncthreads();
+
+    // ------------------------------------------------------------------ units
+    int q_cur = 0;
+    while (to_do > 0) {
+        const int b = cur.b, u = cur.u, t_begin = cur.t;
+        const Request rq = cur.r;
+        const int n_tiles = (int)min((int64_t)(rq.n - t_begin), to_do);
+        const int h = u / p.row_groups, r0 = (u - h * p.row_groups) * kRows;
+        const uint8_t* qb = q_buf + q_cur * (kRows * 256);
+        // the next unit's queries travel under this unit's tiles (with the group of the next tile load)
+        if (to_do > n_tiles) {
+            if (u + 1 < units) load_q(b, u + 1, q_cur ^ 1);
+            else load_q(b + 1, 0, q_cur ^ 1);
+        }
+        float c_col[NT][2];                                // scores -> log2 units, per query row of this thread
+        if (kFp8) {
+            // fp16 queries: scaled per row by a power of two that brings the largest element to [2^10, 2^11); in place
+            for (int row = warp; row < kRows; row += kWarps) {
+                uint2* at = reinterpret_cast<uint2*>(const_cast<uint8_t*>(qb) + row * 256 + (((lane >> 1) ^ (row & 7)) << 4) + (lane & 1) * 8);
+                const uint2 x = *at;
+                const float f0 = __uint_as_float(x.x << 16), f1 = __uint_as_float(x.x & 0xffff0000u);
+                const float f2 = __uint_as_float(x.y << 16), f3 = __uint_as_float(x.y & 0xffff0000u);
+                float amax = fmaxf(fmaxf(fabsf(f0), fabsf(f1)), fmaxf(fabsf(f2), fabsf(f3)));
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                int e = 0;
+                if (amax > 0.f && amax < INFINITY) e = min(max(10 - ilogbf(amax), -126), 126);
+                const float up = __uint_as_float((uint32_t)(127 + e) << 23), down = __uint_as_float((uint32_t)(127 - e) << 23);
+                uint2 y;
+                y.x = pack_weights<true>(f0 * up, f1 * up);
+                y.y = pack_weights<true>(f2 * up, f3 * up);
+                *at = y;
+                if (lane == 0) ml[row] = down;             // the merge area is free between units
+            }
+            __syncthreads();
+            const float ks = p.k_scale[h] * p.scale_log2;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                c_col[nt][0] = ks * ml[nt * 8 + 2 * qd];
+                c_col[nt][1] = ks * ml[nt * 8 + 2 * qd + 1];
+            }
+            __syncthreads();
+        } else {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) c_col[nt][0] = c_col[nt][1] = p.scale_log2;
+        }
+        // query fragment of k step ks and row block nt: (dims 2q, 2q+1 | 2q+8, 2q+9) of the step's 16, or, E4M3, (4q .. 4q+3)
+        auto q_frag = [&](int ks, int nt, uint32_t& b0, uint32_t& b1) {
+            const int row = nt * 8 + g;
+            if (kFp8) {
+                const uint2 x = *reinterpret_cast<const uint2*>(qb + row * 256 + (((2 * ks + (qd >> 1)) ^ (row & 7)) << 4) + (qd & 1) * 8);
+                b0 = x.x;
+                b1 = x.y;
+            } else {
+                b0 = *reinterpret_cast<const uint32_t*>(qb + row * 256 + (((2 * ks) ^ (row & 7)) << 4) + qd * 4);
+                b1 = *reinterpret_cast<const uint32_t*>(qb + row * 256 + (((2 * ks + 1) ^ (row & 7)) << 4) + qd * 4);
+            }
+        };
+        uint32_t qf[kQRegs ? NT : 1][8][2];
+        if (kQRegs) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) q_frag(ks, nt, qf[nt][ks][0], qf[nt][ks][1]);
+        }
+        // keys visible to each of this thread's rows: [lim - window, lim), and the sinks below lim
+        int lim[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int r = r0 + nt * 8 + 2 * qd + c;
+                lim[nt][c] = r < p.rows ? rq.len - p.n_q + r / p.G + 1 : 0;
+            }
+        float o[8][NT][4], l[NT][2], m[NT][2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[i][nt][j] = 0.f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            l[nt][0] = l[nt][1] = 0.f;
+            m[nt][0] = m[nt][1] = -INFINITY;
+        }
+        const int lim_min = rq.len - p.n_q + 1, low_max = rq.len - p.window;
+
+        for (int it = 0; it < n_tiles; ++it) {
+            __syncwarp();                                  // every lane has read the slot that is filled now
+            load_tile();
+            cp_wait<kStages - 1>();
+            __syncwarp();
+            const int key0 = cur.first_key(warp);
+            ++cur.t;
+            const uint32_t kt = ring_s + slot_cur * (2 * kHalf), vt = kt + kHalf;
+            slot_cur = slot_cur + 1 == kStages ? 0 : slot_cur + 1;
+            if (!visible_group(rq, key0)) continue;
+            float s[NT][4];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[nt][j] = 0.f;
+            const int mi = lane >> 3, mr = lane & 7;       // which 8 x 8 matrix of an ldmatrix this lane addresses, and its row
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) {
+                uint32_t a[4];
+                if (kFp8) {
+                    // one ldmatrix brings two steps: codes of 16 dims x (keys 0-7, 8-15)
+                    uint32_t r4[4];
+                    if ((ks & 1) == 0) {
+                        const int key = mr + 8 * (mi & 1), c = ks + (mi >> 1);
+                        ldsm4(r4, kt + key * kRowBytes + ((c ^ (key & 7)) << 4));
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            uint32_t w[4];
+                            w[0] = widen2(r4[2 * half] & 0xffffu);
+                            w[1] = widen2(r4[2 * half + 1] & 0xffffu);
+                            w[2] = widen2(r4[2 * half] >> 16);
+                            w[3] = widen2(r4[2 * half + 1] >> 16);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                uint32_t b0, b1;
+                                if (kQRegs) { b0 = qf[nt][ks + half][0]; b1 = qf[nt][ks + half][1]; }
+                                else q_frag(ks + half, nt, b0, b1);
+                                mma16816<true>(s[nt], w, b0, b1);
+                            }
+                        }
+                    }
+                } else {
+                    const int key = mr + 8 * (mi & 1), c = 2 * ks + (mi >> 1);
+                    ldsm4(a, kt + key * kRowBytes + ((c ^ (key & 7)) << 4));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        uint32_t b0, b1;
+                        if (kQRegs) { b0 = qf[nt][ks][0]; b1 = qf[nt][ks][1]; }
+                        else q_frag(ks, nt, b0, b1);
+                        mma16816<false>(s[nt], a, b0, b1);
+                    }
+                }
+            }
+            // scores in log2 units; s[nt][j]: key g + 8 (j >> 1), row 2 qd + (j & 1)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[nt][j] *= c_col[nt][j & 1];
+            const bool full = key0 + kSubKeys <= lim_min && (key0 >= low_max || key0 + kSubKeys <= p.sinks);
+            if (!full) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int key = key0 + g + 8 * (j >> 1), lm = lim[nt][j & 1];
+                        if (key >= lm || (key < lm - p.window && key >= p.sinks)) s[nt][j] = -INFINITY;
+                    }
+            }
+            bool grow = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) grow |= fmaxf(s[nt][c], s[nt][c + 2]) > m[nt][c] + kLag;
+            if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float x = fmaxf(s[nt][c], s[nt][c + 2]);
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+                        const float mn = fmaxf(m[nt][c], x);
+                        const float alpha = mn == -INFINITY ? 1.f : exp2_fast(m[nt][c] - mn);
+                        m[nt][c] = mn;
+                        l[nt][c] *= alpha;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            o[i][nt][c] *= alpha;
+                            o[i][nt][c + 2] *= alpha;
+                        }
+                    }
+            }
+            // weights, their sums (unrounded), and the weights as the B operand of V^T P^T
+            uint32_t pb[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float mm = m[nt][j & 1];
+                    w[j] = exp2_fast(s[nt][j] - ((mm == -INFINITY ? 0.f : mm) - (kFp8 ? kF16Shift : 0.f)));
+                }
+                l[nt][0] += w[0] + w[2];
+                l[nt][1] += w[1] + w[3];
+                pb[nt][0] = transpose8x8(pack_weights<kFp8>(w[0], w[1]));
+                pb[nt][1] = transpose8x8(pack_weights<kFp8>(w[2], w[3]));
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (kFp8) {
+                    if ((i & 1) == 0) {
+                        // two chunks of 16 dims: codes [16-bit pair of dims][keys], (keys 0-7, 8-15) of chunk i, then of chunk i + 1
+                        uint32_t r4[4];
+                        const int key = mr + 8 * (mi & 1), c = i + (mi >> 1);
+                        ldsm4_t(r4, vt + key * kRowBytes + ((c ^ (key & 7)) << 4));
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            const uint32_t x = __byte_perm(r4[2 * half], 0, 0x3120), y = __byte_perm(r4[2 * half + 1], 0, 0x3120);
+                            uint32_t w[4];
+                            w[0] = widen2(x & 0xffffu);    // dim 2g, keys 2q, 2q+1
+                            w[1] = widen2(x >> 16);        // dim 2g + 1
+                            w[2] = widen2(y & 0xffffu);    // keys 2q + 8, 2q + 9
+                            w[3] = widen2(y >> 16);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma16816<true>(o[i + half][nt], w, pb[nt][0], pb[nt][1]);
+                        }
+                    }
+                } else {
+                    uint32_t a[4];
+                    const int key = mr + 8 * (mi >> 1), c = 2 * i + (mi & 1);
+                    ldsm4_t(a, vt + key * kRowBytes + ((c ^ (key & 7)) << 4));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma16816<false>(o[i][nt], a, pb[nt][0], pb[nt][1]);
+                }
+            }
+        }
+        to_do -= n_tiles;
+
+        // -------------------------------------------------------------- the warps' partial results become one
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], d);
+                if (g == 0) {
+                    const int row = nt * 8 + 2 * qd + c;
+                    ml[(warp * kRows + row) * 2] = m[nt][c];
+                    ml[(warp * kRows + row) * 2 + 1] = l[nt][c];
+                }
+            }
+        if (n_tiles < kStages) cp_wait<0>();               // the next unit's queries have landed before the barrier
+        __syncthreads();
+        const bool whole = t_begin == 0 && n_tiles == rq.n;
+        const int slot = 2 * blockIdx.x + (t_begin > 0 ? 0 : 1);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int row = nt * 8 + 2 * qd + c;
+                float mx = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[(w * kRows + row) * 2]);
+                const float f = m[nt][c] == -INFINITY ? 0.f : exp2_fast(m[nt][c] - mx);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    o[i][nt][c] *= f;
+                    o[i][nt][c + 2] *= f;
+                }
+            }
+        // the row's maximum and sum, by every thread for the rows it writes below
+        auto row_ml = [&](int row, float& mx, float& sum) {
+            mx = -INFINITY;
+            sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[(w * kRows + row) * 2]);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float mw = ml[(w * kRows + row) * 2];
+                sum += mw == -INFINITY ? 0.f : ml[(w * kRows + row) * 2 + 1] * exp2_fast(mw - mx);
+            }
+        };
+        if (tid < kRows && r0 + tid < p.rows) {
+            float mx, sum;
+            row_ml(tid, mx, sum);
+            const int r = r0 + tid, t = r / p.G;
+            if (whole) {
+                p.lse[(int64_t)(h * p.G + r - t * p.G) * ((int64_t)p.B * p.n_q) + (int64_t)b * p.n_q + t] =
+                    sum > 0.f ? (mx + log2f(sum) - (kFp8 ? kF16Shift : 0.f)) * 0.6931471805599453f : -INFINITY;
+            } else {
+                p.part_ml[((int64_t)slot * kRows + tid) * 2] = mx;
+                p.part_ml[((int64_t)slot * kRows + tid) * 2 + 1] = sum;
+            }
+        }
+#pragma unroll
+        for (int pass = 0; pass < 8 / kPassTiles; ++pass) {
+            if (pass > 0) __syncthreads();                 // the previous pass has been summed
+#pragma unroll
+            for (int i = 0; i < kPassTiles; ++i)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        merge_buf[warp * 512 + ((i * NT + nt) * 4 + j) * 32 + lane] = o[pass * kPassTiles + i][nt][j];
+            __syncthreads();
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int at = x * kDecThreads + tid;      // lane at & 31 of register (at >> 5)
+                float sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) sum += merge_buf[w * 512 + at];
+                const int ln = at & 31, reg = at >> 5, j = reg & 3, nt = (reg >> 2) % NT, i = (reg >> 2) / NT;
+                const int gg = ln >> 2, row = nt * 8 + 2 * (ln & 3) + (j & 1);
+                const int dim = (pass * kPassTiles + i) * 16 + (kFp8 ? 2 * gg + (j >> 1) : gg + 8 * (j >> 1));
+                const int r = r0 + row;
+                if (r < p.rows) {
+                    if (whole) {
+                        float mx, total_l;
+                        row_ml(row, mx, total_l);
+                        const float inv = total_l > 0.f ? (kFp8 ? p.v_scale[h] : 1.f) / total_l : 0.f;
+                        const int t = r / p.G;
+                        p.out[(((int64_t)b * p.n_q + t) * p.Hq + h * p.G + r - t * p.G) * kDim + dim] = __float2bfloat16_rn(sum * inv);
+                    } else {
+                        p.part_o[((int64_t)slot * kRows + row) * kDim + dim] = sum;
+                    }
+                }
+            }
+        }
+        if (tid == 0 && !whole && t_begin == 0) {
+            // this CTA holds the unit's first piece: the last one ends with tile x_end - 1 of the list
+            const int64_t x_end = x1 - to_do - n_tiles + rq.n;
+            int64_t last = min((x_end * ctas - 1) / total, ctas - 1);
+            while (run_begin(total, last, ctas) >= x_end) --last;
+            while (run_begin(total, last + 1, ctas) < x_end) ++last;
+            p.meta[blockIdx.x * 4 + 0] = b;
+            p.meta[blockIdx.x * 4 + 1] = u;
+            p.meta[blockIdx.x * 4 + 2] = (int32_t)(last - blockIdx.x + 1);
+            p.meta[blockIdx.x * 4 + 3] = 1;
+        }
+        __syncthreads();                                   // ml, merge_buf and the old query buffer are free again
+        if (to_do > 0) {
+            --cur.t;                                       // back on the unit's last tile, then to the next unit
+            cur.next(p, units);
+        }
+        q_cur ^= 1;
+    }
+    cp_wait<0>();
+}
+
+// Joins the pieces of the units that were cut: block (c, row) takes the unit whose first piece CTA c holds.  Pieces: slot 2c + 1, then slot
+// 2c' of the following CTAs.  Warps take the pieces in turn, and are summed in a fixed order.
+template <bool kFp8>
+__global__ void __launch_bounds__(kDecThreads)
+decode_join_kernel(const __grid_constant__ DecodeParams p, int rows_per_unit) {
+    __shared__ float acc[kWarps][kDim];
+    __shared__ float sums[kWarps];
+    asm volatile("griddepcontrol.wait;" ::: "memory");     // the first launch's results are visible from here on
+    const int c = blockIdx.x, row = blockIdx.y;
+    const int4 me = *reinterpret_cast<const int4*>(p.meta + 4 * c);
+    if (me.w == 0) return;
+    const int h = me.y / p.row_groups, r = (me.y - h * p.row_groups) * rows_per_unit + row;
+    if (r >= p.rows) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    auto slot_of = [&](int k) { return k == 0 ? 2 * c + 1 : 2 * (c + k); };
+    float mx = -INFINITY;
+    for (int k = lane; k < me.z; k += 32) mx = fmaxf(mx, p.part_ml[((int64_t)slot_of(k) * rows_per_unit + row) * 2]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+#pragma unroll 4
+    for (int k = warp; k < me.z; k += kWarps) {
+        const int64_t at = (int64_t)slot_of(k) * rows_per_unit + row;
+        const float2 v = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
+        const float4 x = *reinterpret_cast<const float4*>(p.part_o + at * kDim + lane * 4);
+        const float f = v.x == -INFINITY ? 0.f : exp2_fast(v.x - mx);
+        sum += f * v.y;
+        a.x += f * x.x;
+        a.y += f * x.y;
+        a.z += f * x.z;
+        a.w += f * x.w;
+    }
+    *reinterpret_cast<float4*>(&acc[warp][lane * 4]) = a;
+    if (lane == 0) sums[warp] = sum;
+    __syncthreads();
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) total += sums[w];
+    const int t = r / p.G, head = h * p.G + r - t * p.G;
+    const int64_t token = (int64_t)me.x * p.n_q + t;
+    if (threadIdx.x < kDim) {
+        float x = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) x += acc[w][threadIdx.x];
+        const float inv = total > 0.f ? (kFp8 ? p.v_scale[h] : 1.f) / total : 0.f;
+        p.out[(token * p.Hq + head) * kDim + threadIdx.x] = __float2bfloat16_rn(x * inv);
+    }
+    if (threadIdx.x == 0)
+        p.lse[(int64_t)head * ((int64_t)p.B * p.n_q) + token] =
+            total > 0.f ? (mx + log2f(total) - (kFp8 ? kF16Shift : 0.f)) * 0.6931471805599453f : -INFINITY;
+}
+
+inline int row_blocks(int rows) { return rows <= 8 ? 1 : (rows <= 16 ? 2 : 4); }
+
+// Workspace: partial rows and their (maximum, sum) of two pieces per CTA, and four words per CTA.
+size_t decode_workspace(int rows) {
+    const size_t n = 2 * (size_t)kMaxGrid * row_blocks(rows) * 8;
+    return (n * (kDim + 2) * sizeof(float) + kMaxGrid * 16 + 255) / 256 * 256;
+}
+
+template <int NT, bool kFp8>
+int launch_decode(cp_ctx* ctx, const DecodeParams& p, int grid, cudaStream_t s, const char* who) {
+    const uint32_t variant = 1u << (2 * NT + (kFp8 ? 1 : 0));
+    if (!(ctx->decode_attr_set & variant)) {
+        if (int rc = check_cuda(cudaFuncSetAttribute(decode_kernel<NT, kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDecSmem),
+                                "cudaFuncSetAttribute(decode)")) return rc;
+        ctx->decode_attr_set |= variant;
+    }
+    decode_kernel<NT, kFp8><<<grid, kDecThreads, kDecSmem, s>>>(p);
+    if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid, (unsigned)std::min(NT * 8, p.rows));
+    cfg.blockDim = dim3(kDecThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;      // the join's launch overlaps the end of the first kernel
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return check_cuda(cudaLaunchKernelEx(&cfg, decode_join_kernel<kFp8>, p, NT * 8), who);
+}
+
+int decode_attn(cp_ctx* ctx, const void* q, const void* k, const void* v, const float* k_scale, const float* v_scale, int64_t num_pages,
+                int32_t page_size, int32_t Hkv, int64_t stride_page, int64_t stride_tok, int64_t stride_head, bool fp8,
+                const int32_t* page_table, int64_t table_stride, const int32_t* kv_len, int32_t B, int32_t n_q, int32_t Hq,
+                int64_t window, int64_t sinks, float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                void* stream, const char* who) {
+    if (B < 0 || n_q < 1 || Hq < 1 || table_stride < 1)
+        return set_error(CP_ERR_INVALID_ARG, "%s: B=%d n_q=%d Hq=%d table_stride=%lld", who, B, n_q, Hq, (long long)table_stride);
+    if (Hq % Hkv != 0) return set_error(CP_ERR_INVALID_ARG, "%s: Hq=%d is not a multiple of Hkv=%d", who, Hq, Hkv);
+    if (B > 0 && (!q || !page_table || !kv_len || !out || !lse)) return set_error(CP_ERR_INVALID_ARG, "%s: null pointer", who);
+    if (!(scale > 0.f) || !isfinite(scale)) return set_error(CP_ERR_INVALID_ARG, "%s: scale must be positive", who);
+    if (window < 1 || sinks < 0)
+        return set_error(CP_ERR_INVALID_ARG, "%s: window=%lld sinks=%lld", who, (long long)window, (long long)sinks);
+    if (((uintptr_t)q | (uintptr_t)out) & 15) return set_error(CP_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned", who);
+    const int shift = log2_exact(page_size);
+    const int64_t rows = (int64_t)n_q * (Hq / Hkv);
+    if (n_q > 64 || rows > 1024)
+        return set_error(CP_ERR_UNSUPPORTED, "%s: n_q=%d, %lld query rows per KV head; at most 64 and 1024 (more: a prefill call)", who, n_q,
+                         (long long)rows);
+    if (B > 65536 || table_stride > (0x7fffff00ll >> shift) || num_pages > 0x7fffffffll)
+        return set_error(CP_ERR_UNSUPPORTED, "%s: B=%d (at most 65536), a table row of %lld entries or %lld pages", who, B,
+                         (long long)table_stride, (long long)num_pages);
+    const size_t need = decode_workspace((int)rows);
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)
+        return set_error(CP_ERR_WORKSPACE, "%s: workspace %p of %zu bytes; need %zu bytes, 256-byte aligned", who, workspace, workspace_bytes, need);
+    if (!ctx) return set_error(CP_ERR_INVALID_ARG, "%s: ctx is NULL", who);
+    if (B == 0) return CP_OK;
+    DeviceGuard guard(ctx->device);
+    if (guard.rc()) return guard.rc();
+    DecodeParams p;
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.k = static_cast<const uint8_t*>(k);
+    p.v = static_cast<const uint8_t*>(v);
+    p.k_scale = k_scale;
+    p.v_scale = v_scale;
+    p.table = page_table;
+    p.kv_len = kv_len;
+    p.table_stride = table_stride;
+    p.num_pages = num_pages;
+    p.stride_page = stride_page;
+    p.stride_tok = stride_tok;
+    p.stride_head = stride_head;
+    p.page_shift = shift;
+    p.B = B;
+    p.n_q = n_q;
+    p.Hq = Hq;
+    p.Hkv = Hkv;
+    p.G = Hq / Hkv;
+    p.rows = (int32_t)rows;
+    const int nt = row_blocks(p.rows);
+    p.row_groups = (p.rows + nt * 8 - 1) / (nt * 8);
+    p.window = (int32_t)std::min<int64_t>(window, 0x7fffff00);
+    p.sinks = (int32_t)std::min<int64_t>(sinks, 0x7fffff00);
+    p.capacity = (int32_t)(table_stride << shift);
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.out = static_cast<__nv_bfloat16*>(out);
+    p.lse = lse;
+    const int grid = std::min(ctx->num_sms, kMaxGrid);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    const size_t n = 2 * (size_t)kMaxGrid * nt * 8;
+    p.part_o = reinterpret_cast<float*>(ws);
+    p.part_ml = p.part_o + n * kDim;
+    p.meta = reinterpret_cast<int32_t*>(p.part_ml + n * 2);
+    p.status = ctx->d_status;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (fp8) {
+        if (nt == 1) return launch_decode<1, true>(ctx, p, grid, s, who);
+        if (nt == 2) return launch_decode<2, true>(ctx, p, grid, s, who);
+        return launch_decode<4, true>(ctx, p, grid, s, who);
+    }
+    if (nt == 1) return launch_decode<1, false>(ctx, p, grid, s, who);
+    if (nt == 2) return launch_decode<2, false>(ctx, p, grid, s, who);
+    return launch_decode<4, false>(ctx, p, grid, s, who);
+}
+
+}  // namespace
+
+extern "C" size_t cp_workspace_bytes_decode(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv) {
+    if (B < 0 || n_q < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0) return 0;
+    return decode_workspace((int)std::min<int64_t>((int64_t)n_q * (Hq / Hkv), 1024));
+}
+
+extern "C" int cp_decode_attn(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table, int64_t table_stride,
+                              const int32_t* kv_len, int32_t B, int32_t n_q, int32_t Hq, int64_t window, int64_t sinks, float scale,
+                              void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* who = "cp_decode_attn";
+    if (int rc = validate_kv_cache(cache, who)) return rc;
+    return decode_attn(ctx, q, cache->k, cache->v, nullptr, nullptr, cache->num_pages, cache->page_size, cache->Hkv, cache->stride_page * 2,
+                       cache->stride_tok * 2, cache->stride_head * 2, false, page_table, table_stride, kv_len, B, n_q, Hq, window, sinks,
+                       scale, out, lse, workspace, workspace_bytes, stream, who);
+}
+
+extern "C" int cp_decode_attn_fp8(cp_ctx* ctx, const void* q, const cp_kv_cache_fp8* cache, const int32_t* page_table,
+                                  int64_t table_stride, const int32_t* kv_len, int32_t B, int32_t n_q, int32_t Hq, int64_t window,
+                                  int64_t sinks, float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                  void* stream) {
+    const char* who = "cp_decode_attn_fp8";
+    if (int rc = validate_kv_cache_fp8(cache, who)) return rc;
+    return decode_attn(ctx, q, cache->k, cache->v, cache->k_scale, cache->v_scale, cache->num_pages, cache->page_size, cache->Hkv,
+                       cache->stride_page, cache->stride_tok, cache->stride_head, true, page_table, table_stride, kv_len, B, n_q, Hq,
+                       window, sinks, scale, out, lse, workspace, workspace_bytes, stream, who);
+}

@@ -149,6 +149,7 @@ struct cp_ctx {
     int stage_next;
     cpattn::EncodeTiledFn encode_tiled;
     bool attn_attr_set;
+    uint32_t decode_attr_set;          // one bit per instantiation of the decode kernel
     // schedule reuse (cp_ctx_cache_schedule): what the last attention call left in its workspace
     bool cache_on;
     bool cache_valid;

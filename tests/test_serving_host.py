@@ -127,6 +127,29 @@ def test_workspace_bytes_pages():
     assert a % 256 == 0 and 1000 * 20 <= a < 1000 * 20 + 1024 and b - a >= 4000 * 16 - 256
 
 
+def test_decode_refusals(lib):
+    bad, uns, wsp = binding.CP_ERR_INVALID_ARG, binding.CP_ERR_UNSUPPORTED, binding.CP_ERR_WORKSPACE
+
+    def call(c=None, **kw):
+        a = dict(q=P, table=P, stride=5, kv_len=P, B=3, n_q=1, Hq=4, window=9, sinks=0, scale=0.1, out=P, lse=P, ws=P, ws_bytes=1 << 30) | kw
+        return lib.cp_decode_attn(None, a["q"], ctypes.addressof(c or cache()), a["table"], a["stride"], a["kv_len"], a["B"], a["n_q"], a["Hq"], a["window"],
+                                  a["sinks"], a["scale"], a["out"], a["lse"], a["ws"], a["ws_bytes"], None)
+    assert call() == bad and b"ctx is NULL" in lib.cp_last_error()
+    for kw, code, word in ((dict(q=None), bad, b"null"), (dict(table=None), bad, b"null"), (dict(kv_len=None), bad, b"null"), (dict(out=None), bad, b"null"),
+                           (dict(lse=None), bad, b"null"), (dict(stride=0), bad, b"table_stride"), (dict(B=-1), bad, b"B=-1"), (dict(n_q=0), bad, b"n_q=0"),
+                           (dict(Hq=0), bad, b"Hq"), (dict(Hq=5), bad, b"multiple"), (dict(window=0), bad, b"window"), (dict(sinks=-1), bad, b"sinks"),
+                           (dict(scale=0.0), bad, b"scale"), (dict(scale=math.nan), bad, b"scale"), (dict(scale=math.inf), bad, b"scale"), (dict(q=P + 8), bad, b"aligned"),
+                           (dict(out=P + 2), bad, b"aligned"), (dict(n_q=65), uns, b"n_q"), (dict(Hq=4096), uns, b"rows"), (dict(B=65537), uns, b"B="),
+                           (dict(stride=1 << 30), uns, b"entries"), (dict(ws=None), wsp, b"workspace"), (dict(ws=P + 128), wsp, b"workspace"),
+                           (dict(ws_bytes=binding.cp_workspace_bytes_decode(3, 1, 4, 2) - 1), wsp, b"workspace")):
+        assert call(**kw) == code and word in lib.cp_last_error(), kw
+    assert call(B=0, q=None, table=None, kv_len=None, out=None, lse=None) == bad and b"ctx is NULL" in lib.cp_last_error()
+    for kw, code in ((dict(page_size=48), uns), (dict(D=64), uns), (dict(stride_tok=4), uns), (dict(k=P + 8), uns), (dict(Hkv=0), bad), (dict(k=None), bad)):
+        assert call(cache(**kw)) == code, kw
+    for args in ((-1, 1, 4, 2), (1, 0, 4, 2), (1, 1, 0, 2), (1, 1, 4, 0), (1, 1, 5, 2)):
+        assert binding.cp_workspace_bytes_decode(*args) == 0
+
+
 def test_struct_layouts():
     assert ctypes.sizeof(binding.cp_rope) == 16 + 256 + 512
     assert ctypes.sizeof(binding.cp_page_pool) == 64

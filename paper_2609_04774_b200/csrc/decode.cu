@@ -39,6 +39,7 @@ constexpr int kWarps = 8;
 constexpr int kDecThreads = kWarps * 32;
 constexpr int kSubKeys = 16;                               // keys of a tile that one warp owns
 static_assert(kWarps * kSubKeys == kTileRows, "window_tiles counts in tiles of 128 keys");
+constexpr int kUnitCost = 2;                               // fixed cost of a unit in tiles (see Cursor)
 constexpr float kLag = 8.0f;                               // the running maximum may lag by a factor 2^8
 constexpr float kF16Shift = 7.0f;                          // fp16 weights carry 2^7: at most 2^15 with the lag
 constexpr int kMaxRowsPerUnit = 32;
@@ -74,7 +75,10 @@ struct DecodeParams {
 
 // ---------------------------------------------------------------------------------------------- PTX
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async16_or_zeros(uint32_t dst, const void* src, bool valid) {
     const int n = valid ? 16 : 0;                          // 0: nothing is read, the 16 bytes become zeros
     asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
@@ -138,13 +142,17 @@ __device__ __forceinline__ Request request_of(const DecodeParams& p, int b) {
     r.n = max(1, (r.len + kTileRows - 1) / kTileRows - r.skip);
     return r;
 }
-// A position in the list: request, unit (KV head major, then row group), tile.
+// A position in the list: request, unit (KV head major, then row group), tile.  On the axis that is cut into equal runs a unit
+// takes kUnitCost + n places, starting at x: its fixed cost (queries, merge), then its tiles.
 struct Cursor {
     int32_t b, u, t;
+    int64_t x;
     Request r;
+    __device__ __forceinline__ int64_t place() const { return x + kUnitCost + t; }
     __device__ __forceinline__ void next(const DecodeParams& p, int units) {
         if (++t < r.n) return;
         t = 0;
+        x += kUnitCost + r.n;
         if (++u < units) return;
         u = 0;
         if (++b < p.B) r = request_of(p, b);
@@ -171,6 +179,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     float* ml = reinterpret_cast<float*>(smem + kRingBytes + kMergeBytes);                     // [warp][row][2]
     uint8_t* q_buf = smem + kRingBytes + kMergeBytes + kMlBytes;                               // 2 x [row][256 B], chunks swizzled
     int64_t* scan = reinterpret_cast<int64_t*>(q_buf + kQBytes);                               // warp sums, then the run's start
+    float* row_inv = reinterpret_cast<float*>(q_buf + kQBytes + 128);                          // 1 / sum of a unit's rows
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, qd = lane & 3;
     const int units = p.Hkv * p.row_groups;
@@ -181,7 +190,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     for (int i = 0; i < per; ++i) {
         const int b = tid * per + i;
         if (b < p.B) {
-            mine += request_of(p, b).n;
+            mine += request_of(p, b).n + kUnitCost;
             if (blockIdx.x == 0 && (p.kv_len[b] > p.capacity || p.kv_len[b] < 0)) report_status(p.status, CP_ERR_BOUNDS, b, p.kv_len[b]);
         }
     }
@@ -201,7 +210,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     }
     total *= units;
     before *= units;
-    const int64_t ctas = min((int64_t)gridDim.x, total);   // every run holds a tile
+    const int64_t ctas = min((int64_t)gridDim.x, total);   // no run is empty
     const int64_t x0 = blockIdx.x < ctas ? run_begin(total, blockIdx.x, ctas) : total;
     const int64_t x1 = blockIdx.x < ctas ? run_begin(total, blockIdx.x + 1, ctas) : total;
     int32_t* start = reinterpret_cast<int32_t*>(scan + kWarps);
@@ -209,15 +218,15 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         int b = tid * per;
         int64_t at = before;
         while (true) {
-            const int64_t n = (int64_t)request_of(p, b).n * units;
+            const int64_t n = (int64_t)(request_of(p, b).n + kUnitCost) * units;
             if (x0 < at + n) break;
             at += n;
             ++b;
         }
-        const int n = request_of(p, b).n;
+        const int n = request_of(p, b).n + kUnitCost;
         start[0] = b;
         start[1] = (int32_t)((x0 - at) / n);
-        start[2] = (int32_t)((x0 - at) % n);
+        start[2] = (int32_t)((x0 - at) % n);               // places into the unit
     }
     if (tid == 0) p.meta[blockIdx.x * 4 + 3] = 0;
     __syncthreads();
@@ -226,10 +235,11 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     Cursor ld, cur;                                        // the load stream runs kStages - 1 tiles ahead
     ld.b = start[0];
     ld.u = start[1];
-    ld.t = start[2];
+    ld.t = max(0, start[2] - kUnitCost);
+    ld.x = x0 - start[2];
     ld.r = request_of(p, ld.b);
     cur = ld;
-    int64_t to_load = x1 - x0, to_do = x1 - x0;
+    if (cur.place() >= x1) return;                         // a run of fixed costs alone
 
     // ------------------------------------------------------------------ loads
     auto visible_group = [&](const Request& r, int key0) {
@@ -242,34 +252,53 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         const int64_t page = __ldg(p.table + c.b * p.table_stride + (key0 >> p.page_shift));
         return page < p.num_pages ? page : -1;
     };
-    uint8_t* ring = smem + warp * (kStages * 2 * kHalf);
-    const uint32_t ring_s = smem_addr(ring);
+    const uint32_t ring_s = smem_addr(smem) + warp * (kStages * 2 * kHalf);
     int slot_ld = 0, slot_cur = 0;
+    bool more = true;
     int64_t next_page = page_of(ld);
+    // copies: a row of kRowBytes is kChunks lanes, kKeysPerStep keys a step; chunk c of key k sits at chunk c ^ (k & 7)
+    constexpr int kChunks = kRowBytes / 16, kKeysPerStep = 32 / kChunks, kSteps = kSubKeys / kKeysPerStep, kPeriod = 8 / kKeysPerStep;
+    const int ld_c = lane % kChunks, ld_k = lane / kChunks;
+    uint32_t ld_off[kPeriod];
+#pragma unroll
+    for (int i = 0; i < kPeriod; ++i) {
+        const int kk = i * kKeysPerStep + ld_k;
+        ld_off[i] = kk * kRowBytes + ((ld_c ^ (kk & 7)) << 4);
+    }
+    const int64_t step_bytes = kKeysPerStep * p.stride_tok;
     auto load_tile = [&]() {
-        if (to_load > 0) {
+        if (more) {
             const int64_t page = next_page;
             const int key0 = ld.first_key(warp), len = ld.r.len, low = len - p.n_q + 1 - p.window;
             if (visible_group(ld.r, key0)) {
-                constexpr int kChunks = kRowBytes / 16, kKeysPerStep = 32 / kChunks;
-                const int c = lane % kChunks, k0 = lane / kChunks;
-                const int64_t off = page * p.stride_page + (int64_t)((key0 & ((1 << p.page_shift) - 1)) + k0) * p.stride_tok +
-                                    (int64_t)(ld.u / p.row_groups) * p.stride_head + c * 16;
+                const int64_t off = page * p.stride_page + (int64_t)((key0 & ((1 << p.page_shift) - 1)) + ld_k) * p.stride_tok +
+                                    (int64_t)(ld.u / p.row_groups) * p.stride_head + ld_c * 16;
+                const uint8_t* ks = p.k + off;
+                const uint8_t* vs = p.v + off;
                 const uint32_t dst = ring_s + slot_ld * (2 * kHalf);
+                if (page >= 0 && key0 + kSubKeys <= len && (key0 >= low || key0 + kSubKeys <= p.sinks)) {
 #pragma unroll
-                for (int i = 0; i < kSubKeys / kKeysPerStep; ++i) {
-                    const int kk = i * kKeysPerStep + k0, key = key0 + kk;
-                    const bool ok = page >= 0 && key < len && (key >= low || key < p.sinks);
-                    const int64_t o = ok ? off + i * kKeysPerStep * p.stride_tok : 0;
-                    const uint32_t d = dst + kk * kRowBytes + ((c ^ (kk & 7)) << 4);
-                    cp_async16(d, p.k + o, ok);
-                    cp_async16(d + kHalf, p.v + o, ok);
+                    for (int i = 0; i < kSteps; ++i) {
+                        const uint32_t d = dst + ld_off[i % kPeriod] + (i / kPeriod) * 8 * kRowBytes;
+                        cp_async16(d, ks);
+                        cp_async16(d + kHalf, vs);
+                        ks += step_bytes;
+                        vs += step_bytes;
+                    }
+                } else {                                   // some keys have no slot, or nobody sees them: zeros
+#pragma unroll
+                    for (int i = 0; i < kSteps; ++i) {
+                        const uint32_t d = dst + ld_off[i % kPeriod] + (i / kPeriod) * 8 * kRowBytes;
+                        const int key = key0 + i * kKeysPerStep + ld_k;
+                        const bool ok = page >= 0 && key < len && (key >= low || key < p.sinks);
+                        cp_async16_or_zeros(d, ok ? ks + i * step_bytes : p.k, ok);
+                        cp_async16_or_zeros(d + kHalf, ok ? vs + i * step_bytes : p.v, ok);
+                    }
                 }
             }
-            if (--to_load > 0) {
-                ld.next(p, units);
-                next_page = page_of(ld);
-            }
+            ld.next(p, units);
+            more = ld.place() < x1;
+            if (more) next_page = page_of(ld);
             slot_ld = slot_ld + 1 == kStages ? 0 : slot_ld + 1;
         }
         cp_commit();
@@ -282,7 +311,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             const bool ok = r < p.rows;
             const int t = ok ? r / p.G : 0;
             const int64_t o = ok ? (((int64_t)b * p.n_q + t) * p.Hq + h * p.G + (r - t * p.G)) * kDim + c * 8 : 0;
-            cp_async16(smem_addr(q_buf + buf * (kRows * 256) + row * 256 + ((c ^ (row & 7)) << 4)), p.q + o, ok);
+            cp_async16_or_zeros(smem_addr(q_buf + buf * (kRows * 256) + row * 256 + ((c ^ (row & 7)) << 4)), p.q + o, ok);
         }
     };
 
@@ -293,19 +322,22 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 
     // ------------------------------------------------------------------ units
     int q_cur = 0;
-    while (to_do > 0) {
+    bool last_unit;
+    do {
         const int b = cur.b, u = cur.u, t_begin = cur.t;
         const Request rq = cur.r;
-        const int n_tiles = (int)min((int64_t)(rq.n - t_begin), to_do);
+        const int n_tiles = (int)min((int64_t)rq.n, x1 - cur.x - kUnitCost) - t_begin;
+        last_unit = cur.x + 2 * kUnitCost + rq.n >= x1;    // the run ends before the next unit's first tile
         const int h = u / p.row_groups, r0 = (u - h * p.row_groups) * kRows;
         const uint8_t* qb = q_buf + q_cur * (kRows * 256);
         // the next unit's queries travel under this unit's tiles (with the group of the next tile load)
-        if (to_do > n_tiles) {
+        if (!last_unit) {
             if (u + 1 < units) load_q(b, u + 1, q_cur ^ 1);
             else load_q(b + 1, 0, q_cur ^ 1);
         }
         float c_col[NT][2];                                // scores -> log2 units, per query row of this thread
         if (kFp8) {
+            const float k_scale = p.k_scale[h];
             // fp16 queries: scaled per row by a power of two that brings the largest element to [2^10, 2^11); in place
             for (int row = warp; row < kRows; row += kWarps) {
                 uint2* at = reinterpret_cast<uint2*>(const_cast<uint8_t*>(qb) + row * 256 + (((lane >> 1) ^ (row & 7)) << 4) + (lane & 1) * 8);
@@ -317,7 +349,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
                 int e = 0;
                 if (amax > 0.f && amax < INFINITY) e = min(max(10 - ilogbf(amax), -126), 126);
-                const float up = __uint_as_float((uint32_t)(127 + e) << 23), down = __uint_as_float((uint32_t)(127 - e) << 23);
+                const float up = copysignf(__uint_as_float((uint32_t)(127 + e) << 23), k_scale), down = __uint_as_float((uint32_t)(127 - e) << 23);
                 uint2 y;
                 y.x = pack_weights<true>(f0 * up, f1 * up);
                 y.y = pack_weights<true>(f2 * up, f3 * up);
@@ -325,11 +357,12 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 if (lane == 0) ml[row] = down;             // the merge area is free between units
             }
             __syncthreads();
-            const float ks = p.k_scale[h] * p.scale_log2;
+            // c > 0: the sign of a scale is in the queries; with a scale of zero (all scores 0) hidden keys must still be -inf * c = -inf
+            const float ks = fabsf(k_scale) * p.scale_log2;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                c_col[nt][0] = ks * ml[nt * 8 + 2 * qd];
-                c_col[nt][1] = ks * ml[nt * 8 + 2 * qd + 1];
+                c_col[nt][0] = fmaxf(ks * ml[nt * 8 + 2 * qd], 1e-35f);
+                c_col[nt][1] = fmaxf(ks * ml[nt * 8 + 2 * qd + 1], 1e-35f);
             }
             __syncthreads();
         } else {
@@ -364,7 +397,8 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 const int r = r0 + nt * 8 + 2 * qd + c;
                 lim[nt][c] = r < p.rows ? rq.len - p.n_q + r / p.G + 1 : 0;
             }
-        float o[8][NT][4], l[NT][2], m[NT][2];
+        float o[8][NT][4], l[NT][2];
+        float m[NT][2], m_up[NT][2], m_exp[NT][2];         // running maximum, where it is raised next, and its part of the exponent
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -374,9 +408,14 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             l[nt][0] = l[nt][1] = 0.f;
-            m[nt][0] = m[nt][1] = -INFINITY;
+            m[nt][0] = m[nt][1] = m_up[nt][0] = m_up[nt][1] = -INFINITY;
+            m_exp[nt][0] = m_exp[nt][1] = 0.f;
         }
         const int lim_min = rq.len - p.n_q + 1, low_max = rq.len - p.window;
+        // this lane's row and chunk of the first ldmatrix of K and of V; later ones flip chunk bits
+        const int mi = lane >> 3, mr = lane & 7;           // which 8 x 8 matrix of an ldmatrix this lane addresses, and its row
+        const uint32_t k_lane = (mr + 8 * (mi & 1)) * kRowBytes + (((mi >> 1) ^ mr) << 4);
+        const uint32_t v_lane = kFp8 ? k_lane : (mr + 8 * (mi >> 1)) * kRowBytes + (((mi & 1) ^ mr) << 4);
 
         for (int it = 0; it < n_tiles; ++it) {
             __syncwarp();                                  // every lane has read the slot that is filled now
@@ -385,7 +424,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             __syncwarp();
             const int key0 = cur.first_key(warp);
             ++cur.t;
-            const uint32_t kt = ring_s + slot_cur * (2 * kHalf), vt = kt + kHalf;
+            const uint32_t kt = ring_s + slot_cur * (2 * kHalf) + k_lane, vt = ring_s + slot_cur * (2 * kHalf) + kHalf + v_lane;
             slot_cur = slot_cur + 1 == kStages ? 0 : slot_cur + 1;
             if (!visible_group(rq, key0)) continue;
             float s[NT][4];
@@ -393,7 +432,6 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) s[nt][j] = 0.f;
-            const int mi = lane >> 3, mr = lane & 7;       // which 8 x 8 matrix of an ldmatrix this lane addresses, and its row
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) {
                 uint32_t a[4];
@@ -401,8 +439,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                     // one ldmatrix brings two steps: codes of 16 dims x (keys 0-7, 8-15)
                     uint32_t r4[4];
                     if ((ks & 1) == 0) {
-                        const int key = mr + 8 * (mi & 1), c = ks + (mi >> 1);
-                        ldsm4(r4, kt + key * kRowBytes + ((c ^ (key & 7)) << 4));
+                        ldsm4(r4, kt ^ (ks << 4));
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
                             uint32_t w[4];
@@ -420,8 +457,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                         }
                     }
                 } else {
-                    const int key = mr + 8 * (mi & 1), c = 2 * ks + (mi >> 1);
-                    ldsm4(a, kt + key * kRowBytes + ((c ^ (key & 7)) << 4));
+                    ldsm4(a, kt ^ (ks << 5));
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         uint32_t b0, b1;
@@ -431,11 +467,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                     }
                 }
             }
-            // scores in log2 units; s[nt][j]: key g + 8 (j >> 1), row 2 qd + (j & 1)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s[nt][j] *= c_col[nt][j & 1];
+            // s[nt][j]: key g + 8 (j >> 1), row 2 qd + (j & 1); scores and maxima stay unscaled, c joins in the exponent
             const bool full = key0 + kSubKeys <= lim_min && (key0 >= low_max || key0 + kSubKeys <= p.sinks);
             if (!full) {
 #pragma unroll
@@ -450,7 +482,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) grow |= fmaxf(s[nt][c], s[nt][c + 2]) > m[nt][c] + kLag;
+                for (int c = 0; c < 2; ++c) grow |= fmaxf(s[nt][c], s[nt][c + 2]) > m_up[nt][c];
             if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -460,8 +492,10 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
                         const float mn = fmaxf(m[nt][c], x);
-                        const float alpha = mn == -INFINITY ? 1.f : exp2_fast(m[nt][c] - mn);
+                        const float alpha = m[nt][c] == -INFINITY ? 1.f : exp2_fast((m[nt][c] - mn) * c_col[nt][c]);      // (nothing to rescale yet: 1)
                         m[nt][c] = mn;
+                        m_up[nt][c] = mn + kLag / c_col[nt][c];
+                        m_exp[nt][c] = (mn == -INFINITY ? 0.f : mn * c_col[nt][c]) - (kFp8 ? kF16Shift : 0.f);
                         l[nt][c] *= alpha;
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
@@ -477,8 +511,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 float w[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float mm = m[nt][j & 1];
-                    w[j] = exp2_fast(s[nt][j] - ((mm == -INFINITY ? 0.f : mm) - (kFp8 ? kF16Shift : 0.f)));
+                    w[j] = exp2_fast(fmaf(s[nt][j], c_col[nt][j & 1], -m_exp[nt][j & 1]));
                 }
                 l[nt][0] += w[0] + w[2];
                 l[nt][1] += w[1] + w[3];
@@ -491,8 +524,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                     if ((i & 1) == 0) {
                         // two chunks of 16 dims: codes [16-bit pair of dims][keys], (keys 0-7, 8-15) of chunk i, then of chunk i + 1
                         uint32_t r4[4];
-                        const int key = mr + 8 * (mi & 1), c = i + (mi >> 1);
-                        ldsm4_t(r4, vt + key * kRowBytes + ((c ^ (key & 7)) << 4));
+                        ldsm4_t(r4, vt ^ (i << 4));
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
                             const uint32_t x = __byte_perm(r4[2 * half], 0, 0x3120), y = __byte_perm(r4[2 * half + 1], 0, 0x3120);
@@ -507,14 +539,12 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                     }
                 } else {
                     uint32_t a[4];
-                    const int key = mr + 8 * (mi >> 1), c = 2 * i + (mi & 1);
-                    ldsm4_t(a, vt + key * kRowBytes + ((c ^ (key & 7)) << 4));
+                    ldsm4_t(a, vt ^ (i << 5));
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) mma16816<false>(o[i][nt], a, pb[nt][0], pb[nt][1]);
                 }
             }
         }
-        to_do -= n_tiles;
 
         // -------------------------------------------------------------- the warps' partial results become one
 #pragma unroll
@@ -525,7 +555,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 for (int d = 4; d < 32; d <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], d);
                 if (g == 0) {
                     const int row = nt * 8 + 2 * qd + c;
-                    ml[(warp * kRows + row) * 2] = m[nt][c];
+                    ml[(warp * kRows + row) * 2] = m[nt][c] == -INFINITY ? -INFINITY : m[nt][c] * c_col[nt][c];      // log2 units
                     ml[(warp * kRows + row) * 2 + 1] = l[nt][c];
                 }
             }
@@ -541,28 +571,23 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 float mx = -INFINITY;
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[(w * kRows + row) * 2]);
-                const float f = m[nt][c] == -INFINITY ? 0.f : exp2_fast(m[nt][c] - mx);
+                const float f = m[nt][c] == -INFINITY ? 0.f : exp2_fast(m[nt][c] * c_col[nt][c] - mx);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     o[i][nt][c] *= f;
                     o[i][nt][c + 2] *= f;
                 }
             }
-        // the row's maximum and sum, by every thread for the rows it writes below
-        auto row_ml = [&](int row, float& mx, float& sum) {
-            mx = -INFINITY;
-            sum = 0.f;
+        if (tid < kRows && r0 + tid < p.rows) {
+            float mx = -INFINITY, sum = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[(w * kRows + row) * 2]);
+            for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[(w * kRows + tid) * 2]);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                const float mw = ml[(w * kRows + row) * 2];
-                sum += mw == -INFINITY ? 0.f : ml[(w * kRows + row) * 2 + 1] * exp2_fast(mw - mx);
+                const float mw = ml[(w * kRows + tid) * 2];
+                sum += mw == -INFINITY ? 0.f : ml[(w * kRows + tid) * 2 + 1] * exp2_fast(mw - mx);
             }
-        };
-        if (tid < kRows && r0 + tid < p.rows) {
-            float mx, sum;
-            row_ml(tid, mx, sum);
+            row_inv[tid] = sum > 0.f ? (kFp8 ? p.v_scale[h] : 1.f) / sum : 0.f;      // read behind the barrier below
             const int r = r0 + tid, t = r / p.G;
             if (whole) {
                 p.lse[(int64_t)(h * p.G + r - t * p.G) * ((int64_t)p.B * p.n_q) + (int64_t)b * p.n_q + t] =
@@ -595,11 +620,8 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 const int r = r0 + row;
                 if (r < p.rows) {
                     if (whole) {
-                        float mx, total_l;
-                        row_ml(row, mx, total_l);
-                        const float inv = total_l > 0.f ? (kFp8 ? p.v_scale[h] : 1.f) / total_l : 0.f;
                         const int t = r / p.G;
-                        p.out[(((int64_t)b * p.n_q + t) * p.Hq + h * p.G + r - t * p.G) * kDim + dim] = __float2bfloat16_rn(sum * inv);
+                        p.out[(((int64_t)b * p.n_q + t) * p.Hq + h * p.G + r - t * p.G) * kDim + dim] = __float2bfloat16_rn(sum * row_inv[row]);
                     } else {
                         p.part_o[((int64_t)slot * kRows + row) * kDim + dim] = sum;
                     }
@@ -607,8 +629,8 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             }
         }
         if (tid == 0 && !whole && t_begin == 0) {
-            // this CTA holds the unit's first piece: the last one ends with tile x_end - 1 of the list
-            const int64_t x_end = x1 - to_do - n_tiles + rq.n;
+            // this CTA holds the unit's first piece: the last one ends with the unit's last tile, at place x_end - 1
+            const int64_t x_end = cur.x + kUnitCost + rq.n;
             int64_t last = min((x_end * ctas - 1) / total, ctas - 1);
             while (run_begin(total, last, ctas) >= x_end) --last;
             while (run_begin(total, last + 1, ctas) < x_end) ++last;
@@ -618,12 +640,12 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             p.meta[blockIdx.x * 4 + 3] = 1;
         }
         __syncthreads();                                   // ml, merge_buf and the old query buffer are free again
-        if (to_do > 0) {
+        if (!last_unit) {
             --cur.t;                                       // back on the unit's last tile, then to the next unit
             cur.next(p, units);
         }
         q_cur ^= 1;
-    }
+    } while (!last_unit);
     cp_wait<0>();
 }
 

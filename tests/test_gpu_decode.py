@@ -228,6 +228,23 @@ def test_two_streams_with_their_own_workspaces(ctx):
         s.compare()
 
 
+def test_fp8_scales_of_zero_and_below(ctx):
+    """Bytes stand for scale * e4m3 whatever the scale: a head of zeros, and a negative one."""
+    s = Step(24, [700, 5, 0, 129], 12, 3, 16, n_q=2, fp8=True)
+    s.kv.k_scale[0], s.kv.v_scale[0] = 0.0, 0.0
+    s.kv.k_scale[1], s.kv.v_scale[1] = -s.kv.k_scale[1], -s.kv.v_scale[1]
+    s.check(ctx)
+    s.check(ctx, 100, 3)
+
+
+@pytest.mark.parametrize("size", [2.0 ** -60, 2.0 ** -20, 2.0 ** 30])
+def test_fp8_queries_of_any_size(ctx, size):
+    s = Step(25, [300, 17], 8, 2, 16, fp8=True, scale=SCALE / size)
+    s.q.mul_(size)
+    s.q[0, 0, 3] = 0
+    s.check(ctx)
+
+
 def test_same_inputs_same_bits(ctx):
     s = Step(20, [9000, 300, 2222], 8, 2, 16)
     out, lse = (x.clone() for x in s.run(ctx))

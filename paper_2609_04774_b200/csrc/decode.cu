@@ -42,12 +42,23 @@ static_assert(kWarps * kSubKeys == kTileRows, "window_tiles counts in tiles of 1
 constexpr int kUnitCost = 2;                               // fixed cost of a unit in tiles (see Cursor)
 constexpr float kLag = 8.0f;                               // the running maximum may lag by a factor 2^8
 constexpr float kF16Shift = 7.0f;                          // fp16 weights carry 2^7: at most 2^15 with the lag
-constexpr int kMaxRowsPerUnit = 32;
-constexpr uint32_t kRingBytes = 196608;
-constexpr uint32_t kMergeBytes = 16384;
-constexpr uint32_t kMlBytes = kWarps * kMaxRowsPerUnit * 8;
-constexpr uint32_t kQBytes = 2 * kMaxRowsPerUnit * kDim * 2;
-constexpr uint32_t kDecSmem = kRingBytes + kMergeBytes + kMlBytes + kQBytes + 256;
+constexpr float kNoKey = -1.5e38f;                         // reference of a row that has seen no key: finite, so that hidden scores (-inf) give weight 0
+// CTAs per SM: the E4M3 forms of up to 16 rows fit twice (128 registers a thread; each CTA has half the ring).
+template <int NT, bool kFp8>
+struct Shape {
+    static constexpr int kCtas = kFp8 && NT <= 2 ? 2 : 1;
+    static constexpr int kRows = NT * 8;                                     // query rows of a unit
+    static constexpr int kRowBytes = kFp8 ? 128 : 256;                       // one key's row of one head
+    static constexpr int kHalf = kSubKeys * kRowBytes;                       // the K half of a warp's ring slot
+    static constexpr int kRing = 196608 / kCtas;
+    static constexpr int kStages = kRing / (kWarps * 2 * kHalf);             // 3, or 6 in the E4M3 form with one CTA
+    static constexpr int kMl = kWarps * kRows * 8;                           // maximum and sum of every warp's rows
+    static constexpr int kQ = 2 * kRows * kDim * 2;                          // two units' queries
+    static constexpr int kSmem = kRing + kMl + kQ + 256;
+    static constexpr int kPassTiles = std::min(8, 2 * kHalf / (NT * 4 * 32 * 4));      // 16-dim blocks of O that fit a ring slot
+    static_assert(kCtas * (kSmem + 1024) <= 228 * 1024, "shared memory of an SM");
+    static_assert(kPassTiles >= 1, "the merge goes through the slots");
+};
 
 struct DecodeParams {
     const __nv_bfloat16* q;
@@ -166,20 +177,17 @@ __device__ __forceinline__ int64_t run_begin(int64_t total, int64_t cta, int64_t
 
 // NT: query rows of a unit in blocks of 8.  kFp8: E4M3 cache.
 template <int NT, bool kFp8>
-__global__ void __launch_bounds__(kDecThreads, 1)
+__global__ void __launch_bounds__(kDecThreads, Shape<NT, kFp8>::kCtas)
 decode_kernel(const __grid_constant__ DecodeParams p) {
-    constexpr int kRowBytes = kFp8 ? 128 : 256;            // one key's row of one head
-    constexpr int kHalf = kSubKeys * kRowBytes;            // the K half of a ring slot
-    constexpr int kStages = kRingBytes / (kWarps * 2 * kHalf);
-    constexpr int kRows = NT * 8;
-    constexpr int kPassTiles = 4 / NT;                     // 16-dim blocks merged per pass: 16 KB of partial sums
-    constexpr bool kQRegs = NT <= 2;                       // query fragments stay in registers (32 rows read them from shared memory)
+    using Sh = Shape<NT, kFp8>;
+    constexpr int kRowBytes = Sh::kRowBytes, kHalf = Sh::kHalf, kStages = Sh::kStages, kRows = Sh::kRows, kPassTiles = Sh::kPassTiles;
+    constexpr float kShift = kFp8 ? kF16Shift : 0.f;
+    constexpr bool kQRegs = NT == 1;                       // query fragments stay in registers (else they are read from shared memory per tile)
     extern __shared__ __align__(1024) uint8_t smem[];
-    float* merge_buf = reinterpret_cast<float*>(smem + kRingBytes);
-    float* ml = reinterpret_cast<float*>(smem + kRingBytes + kMergeBytes);                     // [warp][row][2]
-    uint8_t* q_buf = smem + kRingBytes + kMergeBytes + kMlBytes;                               // 2 x [row][256 B], chunks swizzled
-    int64_t* scan = reinterpret_cast<int64_t*>(q_buf + kQBytes);                               // warp sums, then the run's start
-    float* row_inv = reinterpret_cast<float*>(q_buf + kQBytes + 128);                          // 1 / sum of a unit's rows
+    float* ml = reinterpret_cast<float*>(smem + Sh::kRing);                                    // [warp][row][2]
+    uint8_t* q_buf = smem + Sh::kRing + Sh::kMl;                                               // 2 x [row][256 B], chunks swizzled
+    int64_t* scan = reinterpret_cast<int64_t*>(q_buf + Sh::kQ);                                // warp sums, then the run's start
+    float* row_inv = reinterpret_cast<float*>(q_buf + Sh::kQ + 128);                           // 1 / sum of a unit's rows
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, qd = lane & 3;
     const int units = p.Hkv * p.row_groups;
@@ -335,13 +343,16 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             if (u + 1 < units) load_q(b, u + 1, q_cur ^ 1);
             else load_q(b + 1, 0, q_cur ^ 1);
         }
-        float c_col[NT][2];                                // scores -> log2 units, per query row of this thread
+        float c_row[NT][2];                                // scores -> log2 units, per query row of this thread
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) c_row[nt][0] = c_row[nt][1] = p.scale_log2;
+        auto c_col = [&](int nt, int c) { return kFp8 ? c_row[nt][c] : p.scale_log2; };
         if (kFp8) {
             const float k_scale = p.k_scale[h];
             // fp16 queries: scaled per row by a power of two that brings the largest element to [2^10, 2^11); in place
             for (int row = warp; row < kRows; row += kWarps) {
-                uint2* at = reinterpret_cast<uint2*>(const_cast<uint8_t*>(qb) + row * 256 + (((lane >> 1) ^ (row & 7)) << 4) + (lane & 1) * 8);
-                const uint2 x = *at;
+                uint8_t* at = const_cast<uint8_t*>(qb) + row * 256;
+                const uint2 x = *reinterpret_cast<const uint2*>(at + (((lane >> 1) ^ (row & 7)) << 4) + (lane & 1) * 8);
                 const float f0 = __uint_as_float(x.x << 16), f1 = __uint_as_float(x.x & 0xffff0000u);
                 const float f2 = __uint_as_float(x.y << 16), f3 = __uint_as_float(x.y & 0xffff0000u);
                 float amax = fmaxf(fmaxf(fabsf(f0), fabsf(f1)), fmaxf(fabsf(f2), fabsf(f3)));
@@ -350,10 +361,11 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 int e = 0;
                 if (amax > 0.f && amax < INFINITY) e = min(max(10 - ilogbf(amax), -126), 126);
                 const float up = copysignf(__uint_as_float((uint32_t)(127 + e) << 23), k_scale), down = __uint_as_float((uint32_t)(127 - e) << 23);
-                uint2 y;
-                y.x = pack_weights<true>(f0 * up, f1 * up);
-                y.y = pack_weights<true>(f2 * up, f3 * up);
-                *at = y;
+                // dims 4q .. 4q + 3 of a step's 16 are the operand's (2q, 2q + 1 | 2q + 8, 2q + 9), as the codes of K come out of a register
+                __syncwarp();
+                const int ks = lane >> 2;
+                *reinterpret_cast<uint32_t*>(at + (((2 * ks) ^ (row & 7)) << 4) + (lane & 3) * 4) = pack_weights<true>(f0 * up, f1 * up);
+                *reinterpret_cast<uint32_t*>(at + (((2 * ks + 1) ^ (row & 7)) << 4) + (lane & 3) * 4) = pack_weights<true>(f2 * up, f3 * up);
                 if (lane == 0) ml[row] = down;             // the merge area is free between units
             }
             __syncthreads();
@@ -361,33 +373,40 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             const float ks = fabsf(k_scale) * p.scale_log2;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                c_col[nt][0] = fmaxf(ks * ml[nt * 8 + 2 * qd], 1e-35f);
-                c_col[nt][1] = fmaxf(ks * ml[nt * 8 + 2 * qd + 1], 1e-35f);
+                c_row[nt][0] = fmaxf(ks * ml[nt * 8 + 2 * qd], 1e-35f);
+                c_row[nt][1] = fmaxf(ks * ml[nt * 8 + 2 * qd + 1], 1e-35f);
             }
             __syncthreads();
-        } else {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) c_col[nt][0] = c_col[nt][1] = p.scale_log2;
         }
-        // query fragment of k step ks and row block nt: (dims 2q, 2q+1 | 2q+8, 2q+9) of the step's 16, or, E4M3, (4q .. 4q+3)
-        auto q_frag = [&](int ks, int nt, uint32_t& b0, uint32_t& b1) {
-            const int row = nt * 8 + g;
-            if (kFp8) {
-                const uint2 x = *reinterpret_cast<const uint2*>(qb + row * 256 + (((2 * ks + (qd >> 1)) ^ (row & 7)) << 4) + (qd & 1) * 8);
-                b0 = x.x;
-                b1 = x.y;
-            } else {
-                b0 = *reinterpret_cast<const uint32_t*>(qb + row * 256 + (((2 * ks) ^ (row & 7)) << 4) + qd * 4);
-                b1 = *reinterpret_cast<const uint32_t*>(qb + row * 256 + (((2 * ks + 1) ^ (row & 7)) << 4) + qd * 4);
-            }
-        };
-        uint32_t qf[kQRegs ? NT : 1][8][2];
+        // query fragments: one ldmatrix brings (two steps of one row block) or (one step of two row blocks)
+        const uint32_t q_lane = smem_addr(qb) + (kQRegs ? (lane & 7) * 256 + (((lane >> 3) ^ (lane & 7)) << 4)
+                                                        : ((lane & 7) + 8 * (lane >> 4)) * 256 + ((((lane >> 3) & 1) ^ (lane & 7)) << 4));
+        uint32_t qf[kQRegs ? 8 : 1][2];
         if (kQRegs) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks) q_frag(ks, nt, qf[nt][ks][0], qf[nt][ks][1]);
+            for (int ks = 0; ks < 8; ks += 2) {
+                uint32_t r4[4];
+                ldsm4(r4, q_lane ^ (ks << 5));
+                qf[ks][0] = r4[0];
+                qf[ks][1] = r4[1];
+                qf[ks + 1][0] = r4[2];
+                qf[ks + 1][1] = r4[3];
+            }
         }
+        // S^T += K Q^T of one step of 16 dims
+        auto score_step = [&](float (&sc)[NT][4], const uint32_t (&a)[4], int ks) {
+            if (kQRegs) {
+                mma16816<kFp8>(sc[0], a, qf[ks][0], qf[ks][1]);
+            } else {
+#pragma unroll
+                for (int nt = 0; nt < NT; nt += 2) {
+                    uint32_t r4[4];
+                    ldsm4(r4, (q_lane + nt * 8 * 256) ^ (ks << 5));
+                    mma16816<kFp8>(sc[nt], a, r4[0], r4[1]);
+                    mma16816<kFp8>(sc[nt + 1 < NT ? nt + 1 : nt], a, r4[2], r4[3]);
+                }
+            }
+        };
         // keys visible to each of this thread's rows: [lim - window, lim), and the sinks below lim
         int lim[NT][2];
 #pragma unroll
@@ -398,7 +417,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 lim[nt][c] = r < p.rows ? rq.len - p.n_q + r / p.G + 1 : 0;
             }
         float o[8][NT][4], l[NT][2];
-        float m[NT][2], m_up[NT][2], m_exp[NT][2];         // running maximum, where it is raised next, and its part of the exponent
+        float m[NT][2];                                    // reference of the weights, p = 2^(c s - m): the running maximum, less kShift
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -408,8 +427,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             l[nt][0] = l[nt][1] = 0.f;
-            m[nt][0] = m[nt][1] = m_up[nt][0] = m_up[nt][1] = -INFINITY;
-            m_exp[nt][0] = m_exp[nt][1] = 0.f;
+            m[nt][0] = m[nt][1] = kNoKey;
         }
         const int lim_min = rq.len - p.n_q + 1, low_max = rq.len - p.window;
         // this lane's row and chunk of the first ldmatrix of K and of V; later ones flip chunk bits
@@ -432,39 +450,24 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) s[nt][j] = 0.f;
+            if (kFp8) {
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) {
-                uint32_t a[4];
-                if (kFp8) {
-                    // one ldmatrix brings two steps: codes of 16 dims x (keys 0-7, 8-15)
+                for (int ks = 0; ks < 8; ks += 2) {        // one ldmatrix brings two steps: codes of 16 dims x (keys 0-7, 8-15)
                     uint32_t r4[4];
-                    if ((ks & 1) == 0) {
-                        ldsm4(r4, kt ^ (ks << 4));
+                    ldsm4(r4, kt ^ (ks << 4));
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            uint32_t w[4];
-                            w[0] = widen2(r4[2 * half] & 0xffffu);
-                            w[1] = widen2(r4[2 * half + 1] & 0xffffu);
-                            w[2] = widen2(r4[2 * half] >> 16);
-                            w[3] = widen2(r4[2 * half + 1] >> 16);
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                uint32_t b0, b1;
-                                if (kQRegs) { b0 = qf[nt][ks + half][0]; b1 = qf[nt][ks + half][1]; }
-                                else q_frag(ks + half, nt, b0, b1);
-                                mma16816<true>(s[nt], w, b0, b1);
-                            }
-                        }
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t a[4] = {widen2(r4[2 * half] & 0xffffu), widen2(r4[2 * half + 1] & 0xffffu), widen2(r4[2 * half] >> 16),
+                                               widen2(r4[2 * half + 1] >> 16)};
+                        score_step(s, a, ks + half);
                     }
-                } else {
+                }
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) {
+                    uint32_t a[4];
                     ldsm4(a, kt ^ (ks << 5));
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        uint32_t b0, b1;
-                        if (kQRegs) { b0 = qf[nt][ks][0]; b1 = qf[nt][ks][1]; }
-                        else q_frag(ks, nt, b0, b1);
-                        mma16816<false>(s[nt], a, b0, b1);
-                    }
+                    score_step(s, a, ks);
                 }
             }
             // s[nt][j]: key g + 8 (j >> 1), row 2 qd + (j & 1); scores and maxima stay unscaled, c joins in the exponent
@@ -478,24 +481,23 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                         if (key >= lm || (key < lm - p.window && key >= p.sinks)) s[nt][j] = -INFINITY;
                     }
             }
+            // is a weight about to exceed 2^kLag times its row's reference?
             bool grow = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) grow |= fmaxf(s[nt][c], s[nt][c + 2]) > m_up[nt][c];
+                for (int c = 0; c < 2; ++c)
+                    grow |= fmaxf(fmaf(s[nt][c], c_col(nt, c), -m[nt][c]), fmaf(s[nt][c + 2], c_col(nt, c), -m[nt][c])) > kLag + kShift;
             if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        float x = fmaxf(s[nt][c], s[nt][c + 2]);
+                        float x = fmaxf(s[nt][c], s[nt][c + 2]) * c_col(nt, c) - kShift;
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-                        const float mn = fmaxf(m[nt][c], x);
-                        const float alpha = m[nt][c] == -INFINITY ? 1.f : exp2_fast((m[nt][c] - mn) * c_col[nt][c]);      // (nothing to rescale yet: 1)
+                        const float mn = fmaxf(m[nt][c], x), alpha = exp2_fast(m[nt][c] - mn);
                         m[nt][c] = mn;
-                        m_up[nt][c] = mn + kLag / c_col[nt][c];
-                        m_exp[nt][c] = (mn == -INFINITY ? 0.f : mn * c_col[nt][c]) - (kFp8 ? kF16Shift : 0.f);
                         l[nt][c] *= alpha;
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
@@ -510,9 +512,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             for (int nt = 0; nt < NT; ++nt) {
                 float w[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    w[j] = exp2_fast(fmaf(s[nt][j], c_col[nt][j & 1], -m_exp[nt][j & 1]));
-                }
+                for (int j = 0; j < 4; ++j) w[j] = exp2_fast(fmaf(s[nt][j], c_col(nt, j & 1), -m[nt][j & 1]));
                 l[nt][0] += w[0] + w[2];
                 l[nt][1] += w[1] + w[3];
                 pb[nt][0] = transpose8x8(pack_weights<kFp8>(w[0], w[1]));
@@ -555,7 +555,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 for (int d = 4; d < 32; d <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], d);
                 if (g == 0) {
                     const int row = nt * 8 + 2 * qd + c;
-                    ml[(warp * kRows + row) * 2] = m[nt][c] == -INFINITY ? -INFINITY : m[nt][c] * c_col[nt][c];      // log2 units
+                    ml[(warp * kRows + row) * 2] = m[nt][c];
                     ml[(warp * kRows + row) * 2 + 1] = l[nt][c];
                 }
             }
@@ -568,10 +568,10 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const int row = nt * 8 + 2 * qd + c;
-                float mx = -INFINITY;
+                float mx = kNoKey;
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[(w * kRows + row) * 2]);
-                const float f = m[nt][c] == -INFINITY ? 0.f : exp2_fast(m[nt][c] * c_col[nt][c] - mx);
+                const float f = exp2_fast(m[nt][c] - mx);  // a warp that saw no key of the row: 0 (or 1, on zeros)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     o[i][nt][c] *= f;
@@ -579,24 +579,26 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 }
             }
         if (tid < kRows && r0 + tid < p.rows) {
-            float mx = -INFINITY, sum = 0.f;
+            float mx = kNoKey, sum = 0.f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[(w * kRows + tid) * 2]);
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float mw = ml[(w * kRows + tid) * 2];
-                sum += mw == -INFINITY ? 0.f : ml[(w * kRows + tid) * 2 + 1] * exp2_fast(mw - mx);
-            }
+            for (int w = 0; w < kWarps; ++w) sum += ml[(w * kRows + tid) * 2 + 1] * exp2_fast(ml[(w * kRows + tid) * 2] - mx);
             row_inv[tid] = sum > 0.f ? (kFp8 ? p.v_scale[h] : 1.f) / sum : 0.f;      // read behind the barrier below
             const int r = r0 + tid, t = r / p.G;
             if (whole) {
                 p.lse[(int64_t)(h * p.G + r - t * p.G) * ((int64_t)p.B * p.n_q) + (int64_t)b * p.n_q + t] =
-                    sum > 0.f ? (mx + log2f(sum) - (kFp8 ? kF16Shift : 0.f)) * 0.6931471805599453f : -INFINITY;
+                    sum > 0.f ? (mx + log2f(sum)) * 0.6931471805599453f : -INFINITY;
             } else {
                 p.part_ml[((int64_t)slot * kRows + tid) * 2] = mx;
                 p.part_ml[((int64_t)slot * kRows + tid) * 2 + 1] = sum;
             }
         }
+        // through the slots that were read last: they are filled again only after the next unit has begun
+        const int slot_free = slot_cur == 0 ? kStages - 1 : slot_cur - 1;
+        float* mine_o = reinterpret_cast<float*>(smem + (warp * kStages + slot_free) * (2 * kHalf));
+        const float* all_o = reinterpret_cast<const float*>(smem + slot_free * (2 * kHalf));
+        constexpr int kPassRegs = kPassTiles * NT * 4, kWarpFloats = kStages * 2 * kHalf / 4;
 #pragma unroll
         for (int pass = 0; pass < 8 / kPassTiles; ++pass) {
             if (pass > 0) __syncthreads();                 // the previous pass has been summed
@@ -605,15 +607,14 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        merge_buf[warp * 512 + ((i * NT + nt) * 4 + j) * 32 + lane] = o[pass * kPassTiles + i][nt][j];
+                    for (int j = 0; j < 4; ++j) mine_o[((i * NT + nt) * 4 + j) * 32 + lane] = o[pass * kPassTiles + i][nt][j];
             __syncthreads();
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
+            for (int x = 0; x < kPassRegs * 32 / kDecThreads; ++x) {
                 const int at = x * kDecThreads + tid;      // lane at & 31 of register (at >> 5)
                 float sum = 0.f;
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) sum += merge_buf[w * 512 + at];
+                for (int w = 0; w < kWarps; ++w) sum += all_o[w * kWarpFloats + at];
                 const int ln = at & 31, reg = at >> 5, j = reg & 3, nt = (reg >> 2) % NT, i = (reg >> 2) / NT;
                 const int gg = ln >> 2, row = nt * 8 + 2 * (ln & 3) + (j & 1);
                 const int dim = (pass * kPassTiles + i) * 16 + (kFp8 ? 2 * gg + (j >> 1) : gg + 8 * (j >> 1));
@@ -639,7 +640,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             p.meta[blockIdx.x * 4 + 2] = (int32_t)(last - blockIdx.x + 1);
             p.meta[blockIdx.x * 4 + 3] = 1;
         }
-        __syncthreads();                                   // ml, merge_buf and the old query buffer are free again
+        __syncthreads();                                   // ml, the slots and the old query buffer are free again
         if (!last_unit) {
             --cur.t;                                       // back on the unit's last tile, then to the next unit
             cur.next(p, units);
@@ -664,7 +665,7 @@ decode_join_kernel(const __grid_constant__ DecodeParams p, int rows_per_unit) {
     if (r >= p.rows) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     auto slot_of = [&](int k) { return k == 0 ? 2 * c + 1 : 2 * (c + k); };
-    float mx = -INFINITY;
+    float mx = kNoKey;
     for (int k = lane; k < me.z; k += 32) mx = fmaxf(mx, p.part_ml[((int64_t)slot_of(k) * rows_per_unit + row) * 2]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -675,7 +676,7 @@ decode_join_kernel(const __grid_constant__ DecodeParams p, int rows_per_unit) {
         const int64_t at = (int64_t)slot_of(k) * rows_per_unit + row;
         const float2 v = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
         const float4 x = *reinterpret_cast<const float4*>(p.part_o + at * kDim + lane * 4);
-        const float f = v.x == -INFINITY ? 0.f : exp2_fast(v.x - mx);
+        const float f = exp2_fast(v.x - mx);
         sum += f * v.y;
         a.x += f * x.x;
         a.y += f * x.y;
@@ -699,26 +700,29 @@ decode_join_kernel(const __grid_constant__ DecodeParams p, int rows_per_unit) {
     }
     if (threadIdx.x == 0)
         p.lse[(int64_t)head * ((int64_t)p.B * p.n_q) + token] =
-            total > 0.f ? (mx + log2f(total) - (kFp8 ? kF16Shift : 0.f)) * 0.6931471805599453f : -INFINITY;
+            total > 0.f ? (mx + log2f(total)) * 0.6931471805599453f : -INFINITY;
 }
 
+constexpr int kMaxDecodeGrid = 2 * kMaxGrid;
 inline int row_blocks(int rows) { return rows <= 8 ? 1 : (rows <= 16 ? 2 : 4); }
 
 // Workspace: partial rows and their (maximum, sum) of two pieces per CTA, and four words per CTA.
 size_t decode_workspace(int rows) {
-    const size_t n = 2 * (size_t)kMaxGrid * row_blocks(rows) * 8;
-    return (n * (kDim + 2) * sizeof(float) + kMaxGrid * 16 + 255) / 256 * 256;
+    const size_t n = 2 * (size_t)kMaxDecodeGrid * row_blocks(rows) * 8;
+    return (n * (kDim + 2) * sizeof(float) + kMaxDecodeGrid * 16 + 255) / 256 * 256;
 }
 
 template <int NT, bool kFp8>
-int launch_decode(cp_ctx* ctx, const DecodeParams& p, int grid, cudaStream_t s, const char* who) {
+int launch_decode(cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char* who) {
+    using Sh = Shape<NT, kFp8>;
+    const int grid = std::min(ctx->num_sms, kMaxGrid) * Sh::kCtas;
     const uint32_t variant = 1u << (2 * NT + (kFp8 ? 1 : 0));
     if (!(ctx->decode_attr_set & variant)) {
-        if (int rc = check_cuda(cudaFuncSetAttribute(decode_kernel<NT, kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDecSmem),
+        if (int rc = check_cuda(cudaFuncSetAttribute(decode_kernel<NT, kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem),
                                 "cudaFuncSetAttribute(decode)")) return rc;
         ctx->decode_attr_set |= variant;
     }
-    decode_kernel<NT, kFp8><<<grid, kDecThreads, kDecSmem, s>>>(p);
+    decode_kernel<NT, kFp8><<<grid, kDecThreads, Sh::kSmem, s>>>(p);
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid, (unsigned)std::min(NT * 8, p.rows));
@@ -788,22 +792,21 @@ int decode_attn(cp_ctx* ctx, const void* q, const void* k, const void* v, const 
     p.scale_log2 = scale * 1.4426950408889634f;
     p.out = static_cast<__nv_bfloat16*>(out);
     p.lse = lse;
-    const int grid = std::min(ctx->num_sms, kMaxGrid);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    const size_t n = 2 * (size_t)kMaxGrid * nt * 8;
+    const size_t n = 2 * (size_t)kMaxDecodeGrid * nt * 8;
     p.part_o = reinterpret_cast<float*>(ws);
     p.part_ml = p.part_o + n * kDim;
     p.meta = reinterpret_cast<int32_t*>(p.part_ml + n * 2);
     p.status = ctx->d_status;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (fp8) {
-        if (nt == 1) return launch_decode<1, true>(ctx, p, grid, s, who);
-        if (nt == 2) return launch_decode<2, true>(ctx, p, grid, s, who);
-        return launch_decode<4, true>(ctx, p, grid, s, who);
+        if (nt == 1) return launch_decode<1, true>(ctx, p, s, who);
+        if (nt == 2) return launch_decode<2, true>(ctx, p, s, who);
+        return launch_decode<4, true>(ctx, p, s, who);
     }
-    if (nt == 1) return launch_decode<1, false>(ctx, p, grid, s, who);
-    if (nt == 2) return launch_decode<2, false>(ctx, p, grid, s, who);
-    return launch_decode<4, false>(ctx, p, grid, s, who);
+    if (nt == 1) return launch_decode<1, false>(ctx, p, s, who);
+    if (nt == 2) return launch_decode<2, false>(ctx, p, s, who);
+    return launch_decode<4, false>(ctx, p, s, who);
 }
 
 }  // namespace

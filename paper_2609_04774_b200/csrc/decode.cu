@@ -254,19 +254,29 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         const int low = r.len - p.n_q + 1 - p.window;      // lowest key of the first row's window
         return key0 < r.len && (key0 + kSubKeys > low || key0 < p.sinks);
     };
-    auto page_of = [&](const Cursor& c) -> int64_t {       // page of this warp's keys; -1: none to read
-        const int key0 = c.first_key(warp);
-        if (!visible_group(c.r, key0)) return -1;
-        const int64_t page = __ldg(p.table + c.b * p.table_stride + (key0 >> p.page_shift));
-        return page < p.num_pages ? page : -1;
+    // what the load stream keeps of its request and unit: this lane's offset into a page for the head, the table row
+    const int ld_c = lane % (kRowBytes / 16), ld_k = lane / (kRowBytes / 16);
+    const int page_mask = (1 << p.page_shift) - 1;
+    const int32_t* ld_row = nullptr;
+    int64_t ld_head = 0;
+    int ld_low = 0, ld_key0 = 0, next_page = -1;
+    auto enter_unit = [&]() {
+        ld_row = p.table + ld.b * p.table_stride;
+        ld_head = (int64_t)(ld.u / p.row_groups) * p.stride_head + ld_k * p.stride_tok + ld_c * 16;
+        ld_low = ld.r.len - p.n_q + 1 - p.window;
+    };
+    auto look_up = [&]() {                                 // first key of this warp in the tile to load, and its page (-1: none to read)
+        ld_key0 = ld.first_key(warp);
+        next_page = -1;
+        if (visible_group(ld.r, ld_key0)) next_page = __ldg(ld_row + (ld_key0 >> p.page_shift));
     };
     const uint32_t ring_s = smem_addr(smem) + warp * (kStages * 2 * kHalf);
     int slot_ld = 0, slot_cur = 0;
     bool more = true;
-    int64_t next_page = page_of(ld);
+    enter_unit();
+    look_up();
     // copies: a row of kRowBytes is kChunks lanes, kKeysPerStep keys a step; chunk c of key k sits at chunk c ^ (k & 7)
     constexpr int kChunks = kRowBytes / 16, kKeysPerStep = 32 / kChunks, kSteps = kSubKeys / kKeysPerStep, kPeriod = 8 / kKeysPerStep;
-    const int ld_c = lane % kChunks, ld_k = lane / kChunks;
     uint32_t ld_off[kPeriod];
 #pragma unroll
     for (int i = 0; i < kPeriod; ++i) {
@@ -276,15 +286,14 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     const int64_t step_bytes = kKeysPerStep * p.stride_tok;
     auto load_tile = [&]() {
         if (more) {
-            const int64_t page = next_page;
-            const int key0 = ld.first_key(warp), len = ld.r.len, low = len - p.n_q + 1 - p.window;
+            const int key0 = ld_key0, len = ld.r.len;
             if (visible_group(ld.r, key0)) {
-                const int64_t off = page * p.stride_page + (int64_t)((key0 & ((1 << p.page_shift) - 1)) + ld_k) * p.stride_tok +
-                                    (int64_t)(ld.u / p.row_groups) * p.stride_head + ld_c * 16;
+                const bool in_pool = (uint32_t)next_page < (uint32_t)p.num_pages;
+                const int64_t off = next_page * p.stride_page + (key0 & page_mask) * p.stride_tok + ld_head;
                 const uint8_t* ks = p.k + off;
                 const uint8_t* vs = p.v + off;
                 const uint32_t dst = ring_s + slot_ld * (2 * kHalf);
-                if (page >= 0 && key0 + kSubKeys <= len && (key0 >= low || key0 + kSubKeys <= p.sinks)) {
+                if (in_pool && key0 + kSubKeys <= len && (key0 >= ld_low || key0 + kSubKeys <= p.sinks)) {
 #pragma unroll
                     for (int i = 0; i < kSteps; ++i) {
                         const uint32_t d = dst + ld_off[i % kPeriod] + (i / kPeriod) * 8 * kRowBytes;
@@ -298,7 +307,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                     for (int i = 0; i < kSteps; ++i) {
                         const uint32_t d = dst + ld_off[i % kPeriod] + (i / kPeriod) * 8 * kRowBytes;
                         const int key = key0 + i * kKeysPerStep + ld_k;
-                        const bool ok = page >= 0 && key < len && (key >= low || key < p.sinks);
+                        const bool ok = in_pool && key < len && (key >= ld_low || key < p.sinks);
                         cp_async16_or_zeros(d, ok ? ks + i * step_bytes : p.k, ok);
                         cp_async16_or_zeros(d + kHalf, ok ? vs + i * step_bytes : p.v, ok);
                     }
@@ -306,7 +315,10 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             }
             ld.next(p, units);
             more = ld.place() < x1;
-            if (more) next_page = page_of(ld);
+            if (more) {
+                if (ld.t == 0) enter_unit();
+                look_up();
+            }
             slot_ld = slot_ld + 1 == kStages ? 0 : slot_ld + 1;
         }
         cp_commit();
@@ -481,24 +493,29 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                         if (key >= lm || (key < lm - p.window && key >= p.sinks)) s[nt][j] = -INFINITY;
                     }
             }
-            // is a weight about to exceed 2^kLag times its row's reference?
+            // exponents; is a weight about to exceed 2^kLag times its row's reference?
+            float x[NT][4];
             bool grow = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    grow |= fmaxf(fmaf(s[nt][c], c_col(nt, c), -m[nt][c]), fmaf(s[nt][c + 2], c_col(nt, c), -m[nt][c])) > kLag + kShift;
+                for (int j = 0; j < 4; ++j) {
+                    x[nt][j] = fmaf(s[nt][j], c_col(nt, j & 1), -m[nt][j & 1]);
+                    grow |= x[nt][j] > kLag + kShift;
+                }
             if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        float x = fmaxf(s[nt][c], s[nt][c + 2]) * c_col(nt, c) - kShift;
+                        float top = fmaxf(s[nt][c], s[nt][c + 2]) * c_col(nt, c) - kShift;
 #pragma unroll
-                        for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-                        const float mn = fmaxf(m[nt][c], x), alpha = exp2_fast(m[nt][c] - mn);
+                        for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                        const float mn = fmaxf(m[nt][c], top), alpha = exp2_fast(m[nt][c] - mn);
                         m[nt][c] = mn;
                         l[nt][c] *= alpha;
+                        x[nt][c] = fmaf(s[nt][c], c_col(nt, c), -mn);
+                        x[nt][c + 2] = fmaf(s[nt][c + 2], c_col(nt, c), -mn);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             o[i][nt][c] *= alpha;
@@ -512,7 +529,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             for (int nt = 0; nt < NT; ++nt) {
                 float w[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = exp2_fast(fmaf(s[nt][j], c_col(nt, j & 1), -m[nt][j & 1]));
+                for (int j = 0; j < 4; ++j) w[j] = exp2_fast(x[nt][j]);
                 l[nt][0] += w[0] + w[2];
                 l[nt][1] += w[1] + w[3];
                 pb[nt][0] = transpose8x8(pack_weights<kFp8>(w[0], w[1]));

@@ -369,8 +369,19 @@ static int build_schedule_impl(int32_t pairs_per_tile, int32_t pairs_per_kv, int
         s.grid = o.grid;
         s.n_slots = o.n_slots;
     };
-    if (have_alt && schedule_cost(alt) * 100 < schedule_cost(s) * 97) take(alt);     // by a margin: the estimate is coarse
-    if (have_whole && schedule_cost(whole) * 100 < schedule_cost(s) * 97) take(whole);
+    // A candidate may trade balance for fewer pieces only so far: its slowest CTA stays within 1.3 shares and eight tile
+    // steps (without this two requests of 28-tile units on 143 CTAs kept a CTA busy for 28 steps at a share of 15).
+    auto balanced = [W](const Schedule& o) {
+        const int64_t share = (W + o.grid - 1) / o.grid;
+        for (int32_t g = 0; g < o.grid; ++g) {
+            int64_t load = 0;
+            for (int32_t k = o.cta_off[g]; k < o.cta_off[g + 1]; ++k) load += o.pieces[k].t_end - o.pieces[k].t_begin;
+            if (10 * load > 13 * share + 80) return false;
+        }
+        return true;
+    };
+    if (have_alt && schedule_cost(alt) * 100 < schedule_cost(s) * 97 && balanced(alt)) take(alt);     // by a margin: the estimate is coarse
+    if (have_whole && schedule_cost(whole) * 100 < schedule_cost(s) * 97 && balanced(whole)) take(whole);
     return CP_OK;
 }
 

@@ -33,6 +33,10 @@ EXPORTS = ["cp_strerror", "cp_last_error", "cp_ctx_create", "cp_ctx_destroy", "c
 # The serving calls run once per layer and token, so their argument types are declared once and plain integers are passed.
 _P, _I, _L, _F, _Z = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
 _ARGTYPES = {
+    "cp_prefill_attn_window": [_P, _P, _P, _P, _L, _L, _I, _L, _L, _I, _F, _P, _P, _P, _Z, _P],
+    "cp_prefill_attn_window_batch": [_P, _P, _P, _P, _I, _P, _P, _P, _P, _L, _L, _I, _F, _P, _P, _P, _Z, _P],
+    "cp_prefill_attn_window_chunk": [_P, _P, _P, _P, _L, _L, _I, _I, _L, _L, _I, _F, _P, _P, _P, _Z, _P],
+    "cp_prefill_attn_fp8_window_batch": [_P, _P, _P, _P, _I, _P, _P, _P, _P, _L, _L, _I, _F, _P, _P, _P, _Z, _P],
     "cp_rope_init": [_P, _I, _P, ctypes.c_double, _I],
     "cp_rope_append": [_P, _P, _P, _P, _P, _L, _I, _P, _P, _P, _P, _P, _L, _L, _P, _P],
     "cp_rope_append_fp8": [_P, _P, _P, _P, _P, _L, _I, _P, _P, _P, _P, _P, _L, _L, _P, _P],
@@ -53,6 +57,14 @@ class CpError(RuntimeError):
     def __init__(self, code: int, message: str):
         super().__init__("%s (%d): %s" % (_strerror(code), code, message))
         self.code = code
+
+
+class CpArgumentError(CpError, ValueError):
+    """A tensor that a call would misread (type, shape, strides, device), refused by the binding."""
+
+    def __init__(self, message: str):
+        RuntimeError.__init__(self, "CP_ERR_INVALID_ARG (%d): %s" % (CP_ERR_INVALID_ARG, message))
+        self.code = CP_ERR_INVALID_ARG
 
 
 class cp_shard_plan(ctypes.Structure):
@@ -271,27 +283,43 @@ def cp_prefill_attn_kvrange(ctx, q, cache, page_table, prefix_len, new_len, kv_l
         _stream(stream)))
 
 
+def _window_args(ctx, q, cache, page_table, rows, Hq, out, lse, workspace, stream):
+    """The tensors of a windowed call, checked: (q, cache, page_table) and (out, lse, workspace, its bytes, stream)."""
+    bf16, i32, f32, _ = _types or _torch_types()
+    shape = (rows, Hq, 128)
+    table = _arg(ctx, page_table, "page_table", i32, page_table.shape)
+    return ((ctx._h, _arg(ctx, q, "q", bf16, shape), ctypes.addressof(cache), table),
+            (_arg(ctx, out, "out", bf16, shape), _arg(ctx, lse, "lse", f32, (Hq, rows)), *_workspace(ctx, workspace), _raw_stream(ctx, stream)))
+
+
+def _host_i64(a):
+    """ctypes array of 64-bit integers from a list, tuple or array."""
+    return (ctypes.c_int64 * len(a))(*a)
+
+
 def cp_prefill_attn_window(ctx, q, cache, page_table, prefix_len, new_len, C, window, sinks, Hq, scale, out, lse, workspace,
                            stream=None):
     """cp_prefill_attn where a token at position p sees the last `window` keys (its own among them) and the first `sinks`."""
-    _check(load().cp_prefill_attn_window(
-        ctx._h, _ptr(q), ctypes.byref(cache), _ptr(page_table), ctypes.c_int64(prefix_len), ctypes.c_int64(new_len),
-        ctypes.c_int32(C), ctypes.c_int64(window), ctypes.c_int64(sinks), ctypes.c_int32(Hq), ctypes.c_float(scale), _ptr(out),
-        _ptr(lse), _ptr(workspace), ctypes.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream)))
+    head, tail = _window_args(ctx, q, cache, page_table, new_len, Hq, out, lse, workspace, stream)
+    if page_table.numel() * cache.page_size < prefix_len + new_len:
+        raise CpArgumentError("page_table has %d entries for %d tokens" % (page_table.numel(), prefix_len + new_len))
+    _check(load().cp_prefill_attn_window(*head, prefix_len, new_len, C, window, sinks, Hq, scale, *tail))
 
 
 def _window_batch(call, ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks, Hq, scale, out, lse, workspace,
                   stream):
-    cu_new, prefix_len, cu_pages, C = _i64(cu_new), _i64(prefix_len), _i64(cu_pages), _i32(C)
-    B = prefix_len.size
-    assert cu_new.size == B + 1 and cu_pages.size == B + 1 and C.size == B
-    _check(call(ctx._h, _ptr(q), ctypes.byref(cache), _ptr(page_table), ctypes.c_int32(B), _hp(cu_new), _hp(prefix_len), _hp(C),
-                _hp(cu_pages), ctypes.c_int64(window), ctypes.c_int64(sinks), ctypes.c_int32(Hq), ctypes.c_float(scale), _ptr(out),
-                _ptr(lse), _ptr(workspace), ctypes.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream)))
+    B = len(prefix_len)
+    if len(cu_new) != B + 1 or len(cu_pages) != B + 1 or len(C) != B:
+        raise CpArgumentError("cu_new and cu_pages have %d and %d entries, C %d, for %d requests" % (len(cu_new), len(cu_pages), len(C), B))
+    head, tail = _window_args(ctx, q, cache, page_table, int(cu_new[B]), Hq, out, lse, workspace, stream)
+    if page_table.numel() < cu_pages[B]:
+        raise CpArgumentError("page_table has %d entries, cu_pages ends with %d" % (page_table.numel(), cu_pages[B]))
+    _check(call(*head, B, _host_i64(cu_new), _host_i64(prefix_len), (ctypes.c_int32 * B)(*C), _host_i64(cu_pages), window, sinks, Hq, scale, *tail))
 
 
 def cp_prefill_attn_window_batch(ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks, Hq, scale, out, lse,
                                  workspace, stream=None):
+    """B requests in one launch; cu_new, prefix_len, C, cu_pages: host sequences as in cp_prefill_attn_batch."""
     _window_batch(load().cp_prefill_attn_window_batch, ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks,
                   Hq, scale, out, lse, workspace, stream)
 
@@ -299,11 +327,15 @@ def cp_prefill_attn_window_batch(ctx, q, cache, page_table, cu_new, prefix_len, 
 def cp_prefill_attn_window_chunk(ctx, q_chunk, cache, page_table, prefix_len, new_len, C, chunk, window, sinks, Hq, scale,
                                  out_chunk, lse_chunk, workspace, stream=None):
     """One zigzag chunk in chunk-local buffers, as cp_prefill_attn_chunk, with a window."""
-    _check(load().cp_prefill_attn_window_chunk(
-        ctx._h, _ptr(q_chunk), ctypes.byref(cache), _ptr(page_table), ctypes.c_int64(prefix_len), ctypes.c_int64(new_len),
-        ctypes.c_int32(C), ctypes.c_int32(chunk), ctypes.c_int64(window), ctypes.c_int64(sinks), ctypes.c_int32(Hq),
-        ctypes.c_float(scale), _ptr(out_chunk), _ptr(lse_chunk), _ptr(workspace),
-        ctypes.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream)))
+    if C >= 1 and 0 <= chunk < 2 * C and new_len >= 1 and prefix_len >= 0:
+        cl = -(-new_len // (2 * C))
+        rows, end = min(new_len, (chunk + 1) * cl) - min(new_len, chunk * cl), prefix_len + min(new_len, (chunk + 1) * cl)
+        if page_table.numel() * cache.page_size < end:
+            raise CpArgumentError("page_table has %d entries for %d tokens" % (page_table.numel(), end))
+    else:
+        rows = q_chunk.shape[0]                            # refused by the call
+    head, tail = _window_args(ctx, q_chunk, cache, page_table, rows, Hq, out_chunk, lse_chunk, workspace, stream)
+    _check(load().cp_prefill_attn_window_chunk(*head, prefix_len, new_len, C, chunk, window, sinks, Hq, scale, *tail))
 
 
 def cp_prefill_attn_static(q, cache, page_table, prefix_len, new_len, C, Hq, scale, out, lse, stream=None):
@@ -440,23 +472,33 @@ def cp_check_page_table(ctx, page_table, num_pages, stream=None):
 # Serving calls: decode attention, rotary append, page care
 # ------------------------------------------------------------------------------------------------
 
+_types = None      # (bf16, int32, float32, the current raw stream of a device), from torch at the first call
+
+
+def _torch_types():
+    global _types
+    import torch
+    _types = (torch.bfloat16, torch.int32, torch.float32, torch._C._cuda_getCurrentRawStream)
+    return _types
+
+
 def _raw_stream(ctx, stream):
     """The given stream, or the current one of the context's device."""
-    if stream is not None:
-        return stream.cuda_stream
-    import torch
-    return torch._C._cuda_getCurrentRawStream(ctx.device)
+    return stream.cuda_stream if stream is not None else _types[3](ctx.device)
 
 
-def _arg(t, name, dtype, *shape):
-    """Address of a contiguous CUDA tensor of the given type and shape (None in the shape: any size); None stays None."""
-    if t is None:
-        return None
-    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s CUDA tensor, got %s on %s with strides %s" % (name, dtype, t.dtype, t.device, t.stride()))
-    if len(t.shape) != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
-        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple("*" if w is None else w for w in shape)))
-    return t.data_ptr()
+def _arg(ctx, t, name, dtype, shape):
+    """Address of a contiguous tensor of the given type and shape on the context's device."""
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == ctx.device:
+        return t.data_ptr()
+    raise CpArgumentError("%s must be a contiguous %s tensor of shape %s on cuda:%d, got %s %s with strides %s on %s"
+                     % (name, dtype, tuple(shape), ctx.device, t.dtype, tuple(t.shape), t.stride(), t.device))
+
+
+def _workspace(ctx, t):
+    if not t.is_contiguous() or t.get_device() != ctx.device:
+        raise CpArgumentError("workspace must be a contiguous tensor on cuda:%d" % ctx.device)
+    return t.data_ptr(), t.nbytes
 
 
 def cp_workspace_bytes_decode(B, n_q, Hq, Hkv) -> int:
@@ -464,13 +506,16 @@ def cp_workspace_bytes_decode(B, n_q, Hq, Hkv) -> int:
 
 
 def _decode_attn(call, ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream):
-    import torch
-    B, n_q, Hq, _ = q.shape
-    rows, stride = page_table.shape
-    _check(call(ctx._h, _arg(q, "q", torch.bfloat16, B, n_q, Hq, 128), ctypes.addressof(cache), _arg(page_table, "page_table", torch.int32, B, stride),
-                stride, _arg(kv_len, "kv_len", torch.int32, B), B, n_q, Hq, window, sinks, scale, _arg(out, "out", torch.bfloat16, B, n_q, Hq, 128),
-                _arg(lse, "lse", torch.float32, Hq, B * n_q), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                _raw_stream(ctx, stream)))
+    bf16, i32, f32, _ = _types or _torch_types()
+    shape = q.shape
+    B, n_q, Hq, _ = shape
+    stride = page_table.shape[1]
+    ws, ws_bytes = _workspace(ctx, workspace)
+    rc = call(ctx._h, _arg(ctx, q, "q", bf16, (B, n_q, Hq, 128)), ctypes.addressof(cache), _arg(ctx, page_table, "page_table", i32, (B, stride)), stride,
+              _arg(ctx, kv_len, "kv_len", i32, (B,)), B, n_q, Hq, window, sinks, scale, _arg(ctx, out, "out", bf16, shape),
+              _arg(ctx, lse, "lse", f32, (Hq, B * n_q)), ws, ws_bytes, _raw_stream(ctx, stream))
+    if rc != CP_OK:
+        _check(rc)
 
 
 def cp_decode_attn(ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream=None):
@@ -494,16 +539,26 @@ def make_rope(sections, base=10000.0, interleaved=False) -> cp_rope:
 
 
 def _rope_append(call, ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream):
-    import torch
-    bf16, i32 = torch.bfloat16, torch.int32
+    bf16, i32, _, _ = _types or _torch_types()
     n = token_seq.shape[0]
-    Hq = q.shape[1] if q is not None else 0
-    rows, stride = page_table.shape if page_table is not None else (0, 0)
-    _check(call(ctx._h, ctypes.addressof(rope), _arg(q, "q", bf16, n, Hq, 128), _arg(k_rows, "k_rows", bf16, n, cache.Hkv, 128),
-                _arg(v_rows, "v_rows", bf16, n, cache.Hkv, 128), n, Hq, _arg(positions, "positions", i32, rope.n_axes, n),
-                _arg(token_seq, "token_seq", i32, n), _arg(token_slot, "token_slot", i32, n), ctypes.addressof(cache),
-                _arg(page_table, "page_table", i32, rows, stride), rows, stride, _arg(q_out, "q_out", bf16, n, Hq, 128),
-                _raw_stream(ctx, stream)))
+    qp = qo = kp = vp = sp = tp = None
+    Hq = rows = stride = 0
+    if q is not None or q_out is not None:
+        if q is None or q_out is None:
+            raise CpArgumentError("q and q_out come together or not at all")
+        Hq = q.shape[1]
+        qp, qo = _arg(ctx, q, "q", bf16, (n, Hq, 128)), _arg(ctx, q_out, "q_out", bf16, (n, Hq, 128))
+    if k_rows is not None or v_rows is not None:
+        if k_rows is None or v_rows is None:
+            raise CpArgumentError("k_rows and v_rows come together or not at all")
+        shape = (n, cache.Hkv, 128)
+        rows, stride = page_table.shape
+        kp, vp = _arg(ctx, k_rows, "k_rows", bf16, shape), _arg(ctx, v_rows, "v_rows", bf16, shape)
+        sp, tp = _arg(ctx, token_slot, "token_slot", i32, (n,)), _arg(ctx, page_table, "page_table", i32, (rows, stride))
+    rc = call(ctx._h, ctypes.addressof(rope), qp, kp, vp, n, Hq, _arg(ctx, positions, "positions", i32, (rope.n_axes, n)),
+              _arg(ctx, token_seq, "token_seq", i32, (n,)), sp, ctypes.addressof(cache), tp, rows, stride, qo, _raw_stream(ctx, stream))
+    if rc != CP_OK:
+        _check(rc)
 
 
 def cp_rope_append(ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream=None):
@@ -523,9 +578,9 @@ def make_page_pool(k, v, num_pages=None) -> cp_page_pool:
     ks, vs = [k[i] for i in range(len(k))], [v[i] for i in range(len(v))]
     first = ks[0]
     if len(ks) != len(vs) or any(t.shape != first.shape or t.stride() != first.stride() or t.dtype != first.dtype for t in ks + vs):
-        raise ValueError("the layers' k and v must agree in number, shape, strides and type")
+        raise CpArgumentError("the layers' k and v must agree in number, shape, strides and type")
     if first.dim() != 4 or first.shape[3] != 128 or first.stride(3) != 1 or (num_pages is not None and num_pages != first.shape[0]):
-        raise ValueError("a layer is [num_pages, page_size, Hkv, 128] with unit stride in the last dimension, got %s" % (tuple(first.shape),))
+        raise CpArgumentError("a layer is [num_pages, page_size, Hkv, 128] with unit stride in the last dimension, got %s" % (tuple(first.shape),))
     e = first.element_size()
     p = cp_page_pool()
     p._k = (ctypes.c_void_p * len(ks))(*[t.data_ptr() for t in ks])        # kept alive with the descriptor
@@ -541,59 +596,56 @@ def cp_workspace_bytes_pages(num_pages, n=0) -> int:
     return int(load().cp_workspace_bytes_pages(num_pages, n))
 
 
-def _table_args(pool, refcount, page_table, kv_len):
-    import torch
+def _table_args(ctx, pool, refcount, page_table):
+    i32 = (_types or _torch_types())[1]
     rows, stride = page_table.shape
-    return (_arg(refcount, "refcount", torch.int32, pool.num_pages), _arg(page_table, "page_table", torch.int32, rows, stride), rows, stride,
-            _arg(kv_len, "kv_len", torch.int32, rows))
+    return (ctx._h, ctypes.addressof(pool), _arg(ctx, refcount, "refcount", i32, (pool.num_pages,)),
+            _arg(ctx, page_table, "page_table", i32, (rows, stride)), rows, stride)
 
 
-def _ws(workspace):
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+def _ints(ctx, t, name, n):
+    return _arg(ctx, t, name, _types[1], (n,))
 
 
 def cp_pages_extend(ctx, pool, refcount, page_table, kv_len, new_tokens, workspace, stream=None):
     """Room for new_tokens[r] more tokens in every row: entries, references and kv_len are updated on the device."""
-    import torch
-    rc, pt, rows, stride, kl = _table_args(pool, refcount, page_table, kv_len)
-    _check(load().cp_pages_extend(ctx._h, ctypes.addressof(pool), rc, pt, rows, stride, kl, _arg(new_tokens, "new_tokens", torch.int32, rows),
-                                  *_ws(workspace), _raw_stream(ctx, stream)))
+    a = _table_args(ctx, pool, refcount, page_table)
+    _check(load().cp_pages_extend(*a, _ints(ctx, kv_len, "kv_len", a[4]), _ints(ctx, new_tokens, "new_tokens", a[4]), *_workspace(ctx, workspace),
+                                  _raw_stream(ctx, stream)))
 
 
 def cp_pages_evict(ctx, pool, refcount, page_table, kv_len, window, sinks, stream=None):
     """Give back the pages that the next token of each row (position kv_len) and all later ones cannot see."""
-    rc, pt, rows, stride, kl = _table_args(pool, refcount, page_table, kv_len)
-    _check(load().cp_pages_evict(ctx._h, ctypes.addressof(pool), rc, pt, rows, stride, kl, window, sinks, _raw_stream(ctx, stream)))
+    a = _table_args(ctx, pool, refcount, page_table)
+    _check(load().cp_pages_evict(*a, _ints(ctx, kv_len, "kv_len", a[4]), window, sinks, _raw_stream(ctx, stream)))
 
 
 def cp_pages_free(ctx, pool, refcount, page_table, kv_len, rows, stream=None):
     """Give back all pages of the listed rows (int32 tensor); their kv_len becomes 0."""
-    import torch
-    rc, pt, n_rows, stride, kl = _table_args(pool, refcount, page_table, kv_len)
-    _check(load().cp_pages_free(ctx._h, ctypes.addressof(pool), rc, pt, n_rows, stride, kl, _arg(rows, "rows", torch.int32, None), rows.numel(),
-                                _raw_stream(ctx, stream)))
+    a = _table_args(ctx, pool, refcount, page_table)
+    n = rows.numel()
+    _check(load().cp_pages_free(*a, _ints(ctx, kv_len, "kv_len", a[4]), _ints(ctx, rows, "rows", n), n, _raw_stream(ctx, stream)))
 
 
 def cp_pages_fork(ctx, pool, refcount, page_table, kv_len, parent, child, workspace, stream=None):
     """Rows child[i] become copies of rows parent[i]: full pages shared, the tokens of a partly filled last page copied in every layer."""
-    import torch
-    rc, pt, rows, stride, kl = _table_args(pool, refcount, page_table, kv_len)
+    a = _table_args(ctx, pool, refcount, page_table)
     n = parent.numel()
-    _check(load().cp_pages_fork(ctx._h, ctypes.addressof(pool), rc, pt, rows, stride, kl, _arg(parent, "parent", torch.int32, n),
-                                _arg(child, "child", torch.int32, n), n, *_ws(workspace), _raw_stream(ctx, stream)))
+    _check(load().cp_pages_fork(*a, _ints(ctx, kv_len, "kv_len", a[4]), _ints(ctx, parent, "parent", n), _ints(ctx, child, "child", n), n,
+                                *_workspace(ctx, workspace), _raw_stream(ctx, stream)))
 
 
 def cp_pages_compact(ctx, pool, refcount, page_table, page_map, n_live, workspace, stream=None):
     """Move the pages in use to ids [0, n_live); page_map [num_pages] and n_live [1] (int32) receive the new ids and the count."""
-    import torch
-    rc, pt, rows, stride, _ = _table_args(pool, refcount, page_table, None)
-    _check(load().cp_pages_compact(ctx._h, ctypes.addressof(pool), rc, pt, rows, stride, _arg(page_map, "page_map", torch.int32, pool.num_pages),
-                                   _arg(n_live, "n_live", torch.int32, 1), *_ws(workspace), _raw_stream(ctx, stream)))
+    a = _table_args(ctx, pool, refcount, page_table)
+    _check(load().cp_pages_compact(*a, _ints(ctx, page_map, "page_map", pool.num_pages), _ints(ctx, n_live, "n_live", 1), *_workspace(ctx, workspace),
+                                   _raw_stream(ctx, stream)))
 
 
 def cp_pages_copy(ctx, pool, src, dst, workspace, stream=None):
     """Page src[i] -> page dst[i] (int32 tensors) in every layer."""
-    import torch
+    if _types is None:
+        _torch_types()
     n = src.numel()
-    _check(load().cp_pages_copy(ctx._h, ctypes.addressof(pool), _arg(src, "src", torch.int32, n), _arg(dst, "dst", torch.int32, n), n,
-                                *_ws(workspace), _raw_stream(ctx, stream)))
+    _check(load().cp_pages_copy(ctx._h, ctypes.addressof(pool), _ints(ctx, src, "src", n), _ints(ctx, dst, "dst", n), n, *_workspace(ctx, workspace),
+                                _raw_stream(ctx, stream)))

@@ -39,7 +39,7 @@ constexpr int kWarps = 8;
 constexpr int kDecThreads = kWarps * 32;
 constexpr int kSubKeys = 16;                               // keys of a tile that one warp owns
 static_assert(kWarps * kSubKeys == kTileRows, "window_tiles counts in tiles of 128 keys");
-constexpr int kUnitCost = 2;                               // fixed cost of a unit in tiles (see Cursor)
+constexpr int kUnitCost = 4;                               // fixed cost of a unit in tiles (see Cursor)
 constexpr float kLag = 8.0f;                               // the running maximum may lag by a factor 2^8
 constexpr float kF16Shift = 7.0f;                          // fp16 weights carry 2^7: at most 2^15 with the lag
 constexpr float kNoKey = -1.5e38f;                         // reference of a row that has seen no key: finite, so that hidden scores (-inf) give weight 0
@@ -191,6 +191,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, qd = lane & 3;
     const int units = p.Hkv * p.row_groups;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // the join may be set up now: it waits for this grid's end itself
 
     // where this CTA's run starts: requests are dealt to the threads in order, a prefix sum over their tiles finds it
     const int per = (p.B + kDecThreads - 1) / kDecThreads;

@@ -236,9 +236,9 @@ int rope_append(cp_ctx* ctx, const cp_rope* rope, const void* q, const void* k_r
     const int pairs = rope->rot_dims / 2;
     for (int i = 0; i < 64; ++i) {
         // turns per step: modulo one turn (positions are whole numbers), as a fraction of 2^64
-        long double turns = i < pairs ? (long double)rope->freq[i] / 6.283185307179586476925286766559L : 0.0L;
-        turns -= floorl(turns);
-        const long double scaled = ldexpl(turns, 64);
+        long double turns = i < pairs ? (long double)rope->freq[i] * 0.159154943091895335768883763372514362L : 0.0L;
+        if (turns < 0.0L || turns >= 1.0L) turns -= floorl(turns);
+        const long double scaled = turns * 18446744073709551616.0L;
         p.step[i] = scaled >= 18446744073709551615.0L ? 0ull : (uint64_t)scaled;
         p.axis[i] = i < pairs ? (uint8_t)rope->axis[i] : 0;
     }

@@ -265,5 +265,7 @@ def test_binding_refuses_what_the_call_would_misread(ctx):
                dict(k_rows=c.kr[:4]), dict(token_slot=c.slot[:3]), dict(page_table=c.table.repeat(1, 2)[:, ::2]), dict(q_out=c.g_out.tensor.cpu())):
         with pytest.raises(ValueError):
             c.call(ctx, **kw)
-    with pytest.raises(binding.CpError):
+    with pytest.raises(ValueError):
         c.call(ctx, k_rows=None)
+    with pytest.raises(ValueError):
+        c.call(ctx, q_out=None)

@@ -380,8 +380,8 @@ __device__ __forceinline__ int kv_tile_of(const UnitInfo& u, int t) {
 // ranges of units that were split to fill every CTA to the same number of KV tile steps.  Implicit:
 // serpentine over the longest-first unit list -- in even rounds CTA c takes unit round*grid + c, in
 // odd rounds round*grid + (grid-1-c), which evens out the sorted lengths; whole units only.
-template <bool kWin>
-__device__ __forceinline__ bool fetch_unit(const AttnParams& p, const InlineSched& inl, int round, UnitInfo& u) {
+template <bool kWin, typename Inl>
+__device__ __forceinline__ bool fetch_unit(const AttnParams& p, const Inl& inl, int round, UnitInfo& u) {
     int item, pair;
     // a small schedule sits in the launch parameters (constant bank), a large one in the workspace
     const TileItem* items = p.inl_items >= 0 ? reinterpret_cast<const TileItem*>(inl.bytes + p.inl_items) : p.items;
@@ -436,9 +436,9 @@ __device__ __forceinline__ bool fetch_unit(const AttnParams& p, const InlineSche
 // the second half as a co-producer: it waits for the same "slot empty" phases, while the byte count of a tile is
 // announced once, by the leading warp (a copy that lands before the announcement only leaves the barrier's byte
 // count negative for a moment; the phase cannot complete before the announcing arrival).
-template <bool kFp8, bool kWin>
+template <bool kFp8, bool kWin, typename Inl>
 __device__ __forceinline__ void producer_role(const CUtensorMap* tmQ, const CUtensorMap* tmK, const CUtensorMap* tmV, const AttnParams& p,
-                              const InlineSched& inl, uint32_t smem_base, volatile uint32_t* abort_flag, int half_lo,
+                              const Inl& inl, uint32_t smem_base, volatile uint32_t* abort_flag, int half_lo,
                               int half_hi) {
     const int lane = threadIdx.x & 31;
     const uint32_t bars = smem_base + kSmemBar;
@@ -531,8 +531,8 @@ struct RingPos {
 // (S buffer) and P*V (P and O columns) touch disjoint TMEM and the K and V tiles have their own barriers.
 //
 // Score issuer: S tiles in the order (tile, head); each needs its K tile and the buffer back (s_free).
-template <bool kFp8, bool kWin>
-__device__ __forceinline__ void mma_s_role(const AttnParams& p, const InlineSched& inl, uint32_t smem_base, uint32_t tmem_base,
+template <bool kFp8, bool kWin, typename Inl>
+__device__ __forceinline__ void mma_s_role(const AttnParams& p, const Inl& inl, uint32_t smem_base, uint32_t tmem_base,
                                            volatile uint32_t* abort_flag) {
     const uint32_t bars = smem_base + kSmemBar;
     constexpr int H = 2;
@@ -594,8 +594,8 @@ __device__ __forceinline__ void mma_s_role(const AttnParams& p, const InlineSche
 // P*V issuer: O_h += P_h V_j in the order (tile, head), each in the two pieces P is handed over in.  In a
 // single-head unit (a pair of consecutive query tiles of one head) the second P / O column set belongs to the
 // unit's second query tile instead of a second head; the loop is the same.
-template <bool kFp8, bool kWin>
-__device__ __forceinline__ void mma_pv_role(const AttnParams& p, const InlineSched& inl, uint32_t smem_base, uint32_t tmem_base,
+template <bool kFp8, bool kWin, typename Inl>
+__device__ __forceinline__ void mma_pv_role(const AttnParams& p, const Inl& inl, uint32_t smem_base, uint32_t tmem_base,
                                             volatile uint32_t* abort_flag) {
     const uint32_t bars = smem_base + kSmemBar;
     constexpr int H = 2;
@@ -893,8 +893,8 @@ __device__ __forceinline__ void quad_transpose(uint4 (&v)[4], int t) {
     }
 }
 
-template <bool kFp8, bool kWin>
-__device__ __forceinline__ void softmax_role(const AttnParams& p, const InlineSched& inl, uint32_t smem_base, uint32_t tmem_base,
+template <bool kFp8, bool kWin, typename Inl>
+__device__ __forceinline__ void softmax_role(const AttnParams& p, const Inl& inl, uint32_t smem_base, uint32_t tmem_base,
                                              volatile uint32_t* abort_flag, int wg) {
     const uint32_t bars = smem_base + kSmemBar;
     const int lane = threadIdx.x & 31;
@@ -1056,10 +1056,11 @@ __device__ __forceinline__ void fill_role(const AttnParams& p) {
 
 // kFp8: the FP8 K/V variant (one-byte Q / K / V / P operands).  kWin: the windowed calls (a unit's KV tiles are the
 // sinks' and the window's, the ones between are skipped); the calls without a window keep their own instantiation.
-template <bool kFp8, bool kWin = false>
+// Inl: the launch-parameter copy of the work lists, InlineSmall or InlineSched.
+template <bool kFp8, bool kWin, typename Inl>
 __global__ void __launch_bounds__(kThreads, 1)
 cp_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-               const __grid_constant__ CUtensorMap tmV, const AttnParams p, const __grid_constant__ InlineSched inl) {
+               const __grid_constant__ CUtensorMap tmV, const AttnParams p, const __grid_constant__ Inl inl) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
@@ -1176,7 +1177,8 @@ constexpr int kFixupRowsPerBlock = 8;     // one (head, row) combination per war
 // loaded 32 slots at a time (lane k holds slot k), max and sum by warp shuffles; units cut into at most 32 pieces
 // (all but pathological schedules) read every LSE once.  The partial rows are fetched four at a time, all loads
 // issued before the first use.
-__global__ void __launch_bounds__(256) cp_attn_fixup_kernel(const FixupParams p, const __grid_constant__ InlineSched inl) {
+template <typename Inl>
+__global__ void __launch_bounds__(256) cp_attn_fixup_kernel(const FixupParams p, const __grid_constant__ Inl inl) {
     const TileItem* items = p.inl_items >= 0 ? reinterpret_cast<const TileItem*>(inl.bytes + p.inl_items) : p.items;
     const MergeEntry* merges = p.inl_merges >= 0 ? reinterpret_cast<const MergeEntry*>(inl.bytes + p.inl_merges) : p.merges;
     const int32_t* merge_slots = p.inl_merge_slots >= 0 ? reinterpret_cast<const int32_t*>(inl.bytes + p.inl_merge_slots) : p.merge_slots;

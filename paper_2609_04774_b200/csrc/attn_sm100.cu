@@ -127,6 +127,22 @@ int launch_fill_rows(float* out, float* lse, int64_t lse_stride, int64_t b, int6
     return check_cuda(cudaGetLastError(), "fill_rows launch");
 }
 
+template <bool kFp8, bool kWin, typename Inl>
+int allow_smem() {
+    return check_cuda(cudaFuncSetAttribute(cp_attn_kernel<kFp8, kWin, Inl>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemAlloc),
+                      "cudaFuncSetAttribute(attn)");
+}
+
+template <typename Inl>
+int launch_attn(bool fp8, bool windowed, int grid, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const AttnParams& p,
+                const Inl& inl, cudaStream_t s, const char* who) {
+    if (fp8 && windowed) cp_attn_kernel<true, true, Inl><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, inl);
+    else if (fp8) cp_attn_kernel<true, false, Inl><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, inl);
+    else if (windowed) cp_attn_kernel<false, true, Inl><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, inl);
+    else cp_attn_kernel<false, false, Inl><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, inl);
+    return check_cuda(cudaGetLastError(), who);
+}
+
 // want_fill: the call produces a partial result (fp32 out); rows it computes nothing for are written as zeros with
 // lse = -inf (the identity element of cp_merge), by the attention kernel's spare warp.
 int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table, int32_t B,
@@ -205,6 +221,7 @@ int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int3
     int32_t fill[2 * kMaxFillRanges] = {0};
     int64_t total_rows;
     bool inl_on = false;
+    size_t inl_bytes = 0;       // bytes of the work lists that ride in the launch parameters
     bool fill_all = false;      // more uncovered row ranges than the kernel takes: a fill launch precedes the attention launch
     InlineSched inl_local;
     inl_local.bytes[0] = 0;
@@ -216,6 +233,7 @@ int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int3
         n_merges = ctx->cache_merges;
         total_rows = ctx->cache_rows;
         inl_on = ctx->cache_inline;
+        inl_bytes = ctx->cache_inl_bytes;
         inl = &ctx->cache_inl;
         n_fill = ctx->cache_n_fill;
         memcpy(fill, ctx->cache_fill, sizeof fill);
@@ -262,6 +280,7 @@ int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int3
         ilay = workspace_layout(sch.items.size(), sch.pieces.size(), sch.merges.size(), sch.merge_slots.size(), sch.grid,
                                 0, 16);
         inl_on = ilay.partial_o - ilay.items <= kInlineSchedBytes;
+        inl_bytes = inl_on ? ilay.partial_o - ilay.items : 0;
         const WorkspaceLayout& bl = inl_on ? ilay : lay;
         std::vector<uint8_t> big;
         uint8_t* block = inl_local.bytes;
@@ -306,6 +325,7 @@ int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int3
             ctx->cache_merges = n_merges;
             ctx->cache_rows = total_rows;
             ctx->cache_inline = inl_on;
+            ctx->cache_inl_bytes = inl_bytes;
             if (inl_on) memcpy(ctx->cache_inl.bytes, inl_local.bytes, kInlineSchedBytes);
             ctx->cache_n_fill = n_fill;
             memcpy(ctx->cache_fill, fill, sizeof fill);
@@ -346,14 +366,14 @@ int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int3
         ctx->maps_valid = true;
     }
     if (!ctx->attn_attr_set) {
-        if (int rc = check_cuda(cudaFuncSetAttribute(cp_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                     (int)kSmemAlloc), "cudaFuncSetAttribute(attn)")) return rc;
-        if (int rc = check_cuda(cudaFuncSetAttribute(cp_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                     (int)kSmemAlloc), "cudaFuncSetAttribute(attn)")) return rc;
-        if (int rc = check_cuda(cudaFuncSetAttribute(cp_attn_kernel<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                     (int)kSmemAlloc), "cudaFuncSetAttribute(attn)")) return rc;
-        if (int rc = check_cuda(cudaFuncSetAttribute(cp_attn_kernel<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                     (int)kSmemAlloc), "cudaFuncSetAttribute(attn)")) return rc;
+        if (int rc = allow_smem<false, false, InlineSmall>()) return rc;
+        if (int rc = allow_smem<false, false, InlineSched>()) return rc;
+        if (int rc = allow_smem<false, true, InlineSmall>()) return rc;
+        if (int rc = allow_smem<false, true, InlineSched>()) return rc;
+        if (int rc = allow_smem<true, false, InlineSmall>()) return rc;
+        if (int rc = allow_smem<true, false, InlineSched>()) return rc;
+        if (int rc = allow_smem<true, true, InlineSmall>()) return rc;
+        if (int rc = allow_smem<true, true, InlineSched>()) return rc;
         ctx->attn_attr_set = true;
     }
     AttnParams p;
@@ -397,12 +417,11 @@ int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int3
     // a window that no token of the batch reaches beyond hides nothing: the plain instantiation then does the work
     int64_t longest = 0;
     for (int32_t b = 0; b < B; ++b) longest = std::max<int64_t>(longest, prefix_len[b] + new_len[b]);
-    if (win < longest) {
-        if (cache8) cp_attn_kernel<true, true><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, *inl);
-        else cp_attn_kernel<false, true><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, *inl);
-    } else if (cache8) cp_attn_kernel<true><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, *inl);
-    else cp_attn_kernel<false><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, *inl);
-    if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
+    InlineSmall small;
+    if (inl_bytes <= kInlineSmallBytes) memcpy(small.bytes, inl->bytes, inl_bytes);
+    if (int rc = inl_bytes <= kInlineSmallBytes
+                     ? launch_attn(cache8 != nullptr, win < longest, grid, tmQ, tmK, tmV, p, small, s, who)
+                     : launch_attn(cache8 != nullptr, win < longest, grid, tmQ, tmK, tmV, p, *inl, s, who)) return rc;
     if (n_merges > 0) {
         FixupParams f;
         f.items = p.items;
@@ -424,7 +443,9 @@ int attn_common(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int3
         f.heads_per_unit = heads_per_unit;
         f.lse = lse;
         f.lse_stride = total_rows;
-        cp_attn_fixup_kernel<<<dim3((unsigned)n_merges, 2 * kBlockM / kFixupRowsPerBlock), 256, 0, s>>>(f, *inl);
+        const dim3 fixup_grid((unsigned)n_merges, 2 * kBlockM / kFixupRowsPerBlock);
+        if (inl_bytes <= kInlineSmallBytes) cp_attn_fixup_kernel<<<fixup_grid, 256, 0, s>>>(f, small);
+        else cp_attn_fixup_kernel<<<fixup_grid, 256, 0, s>>>(f, *inl);
         if (int rc = check_cuda(cudaGetLastError(), "cp_attn_fixup launch")) return rc;
     }
     return CP_OK;
@@ -647,8 +668,7 @@ int static_setup(int device, StaticDeviceState** out) {
                                 "cudaGetDriverEntryPoint(cuTensorMapEncodeTiled)")) return rc;
         if (q != cudaDriverEntryPointSuccess || !fn)
             return set_error(CP_ERR_CUDA, "cuTensorMapEncodeTiled is not available in this driver");
-        if (int rc = check_cuda(cudaFuncSetAttribute(cp_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                     (int)kSmemAlloc), "cudaFuncSetAttribute(attn)")) return rc;
+        if (int rc = allow_smem<false, false, InlineSmall>()) return rc;
         st.scratch = static_cast<unsigned char*>(ptr);
         st.num_sms = prop.multiProcessorCount;
         st.encode_tiled = reinterpret_cast<EncodeTiledFn>(fn);
@@ -745,10 +765,9 @@ extern "C" int cp_prefill_attn_static(const void* q, const cp_kv_cache* cache, c
     p.co_producer = cache->page_size == 16 ? 1 : 0;
     p.window = INT32_MAX;
     p.sinks = 0;
-    InlineSched none;          // unused: the tile list is in the scratch
+    InlineSmall none;          // unused: the tile list is in the scratch
     none.bytes[0] = 0;
     const int64_t units = n_tiles * p.pairs_per_tile;
     const int grid = (int)std::min<int64_t>(units, st->num_sms);
-    cp_attn_kernel<false><<<grid, kThreads, kSmemAlloc, s>>>(tmQ, tmK, tmV, p, none);
-    return check_cuda(cudaGetLastError(), who);
+    return launch_attn(false, false, grid, tmQ, tmK, tmV, p, none, s, who);
 }

@@ -86,6 +86,12 @@ constexpr size_t kInlineSchedBytes = 24576;
 struct InlineSched {
     alignas(16) unsigned char bytes[kInlineSchedBytes];
 };
+// The copy that lists of at most this many bytes take: all launch parameters together then stay below 4 KB.  Larger ones
+// cost about 8 us of stream time per launch (333 new tokens behind 1500, window 1024: 37 us per call with the 24 KB copy).
+constexpr size_t kInlineSmallBytes = 3200;
+struct InlineSmall {
+    alignas(16) unsigned char bytes[kInlineSmallBytes];
+};
 constexpr int kMaxFillRanges = 4;        // row ranges a partial-result call fills with zeros / -inf inside the kernel
 
 #ifdef __CUDACC__
@@ -164,6 +170,7 @@ struct cp_ctx {
     int64_t maps_key[12];
     CUtensorMap maps[3];
     bool cache_inline;                 // the remembered work lists travel in the launch parameters
+    size_t cache_inl_bytes;            // their size
     cpattn::InlineSched cache_inl;
     int32_t cache_n_fill;
     bool cache_fill_all;

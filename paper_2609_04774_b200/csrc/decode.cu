@@ -191,7 +191,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, qd = lane & 3;
     const int units = p.Hkv * p.row_groups;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // the join may be set up now: it waits for this grid's end itself
+    let_next_launch_begin();                               // the join
 
     // where this CTA's run starts: requests are dealt to the threads in order, a prefix sum over their tiles finds it
     const int per = (p.B + kDecThreads - 1) / kDecThreads;
@@ -675,7 +675,7 @@ __global__ void __launch_bounds__(kDecThreads)
 decode_join_kernel(const __grid_constant__ DecodeParams p, int rows_per_unit) {
     __shared__ float acc[kWarps][kDim];
     __shared__ float sums[kWarps];
-    asm volatile("griddepcontrol.wait;" ::: "memory");     // the first launch's results are visible from here on
+    wait_for_launch_before();
     const int c = blockIdx.x, row = blockIdx.y;
     const int4 me = *reinterpret_cast<const int4*>(p.meta + 4 * c);
     if (me.w == 0) return;
@@ -742,16 +742,7 @@ int launch_decode(cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char
     }
     decode_kernel<NT, kFp8><<<grid, kDecThreads, Sh::kSmem, s>>>(p);
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid, (unsigned)std::min(NT * 8, p.rows));
-    cfg.blockDim = dim3(kDecThreads);
-    cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;      // the join's launch overlaps the end of the first kernel
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    return check_cuda(cudaLaunchKernelEx(&cfg, decode_join_kernel<kFp8>, p, NT * 8), who);
+    return launch_behind(decode_join_kernel<kFp8>, dim3((unsigned)grid, (unsigned)std::min(NT * 8, p.rows)), kDecThreads, s, who, p, NT * 8);
 }
 
 int decode_attn(cp_ctx* ctx, const void* q, const void* k, const void* v, const float* k_scale, const float* v_scale, int64_t num_pages,

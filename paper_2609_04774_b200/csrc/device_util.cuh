@@ -43,6 +43,24 @@ inline int log2_exact(int v) {      // v is a power of two
 }
 
 #ifdef __CUDACC__
+// Two launches of one call, the second reading what the first writes: the first lets the second be set up while it runs
+// (let_next_launch_begin), the second waits for the first one's end (wait_for_launch_before) before it reads anything.
+__device__ __forceinline__ void let_next_launch_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <typename... Params, typename... Args>
+int launch_behind(void (*kernel)(Params...), dim3 grid, int threads, cudaStream_t s, const char* who, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return check_cuda(cudaLaunchKernelEx(&cfg, kernel, args...), who);
+}
+
 // The first error of a launch sequence lands in the context's status words {code, index, block, value}.
 __device__ __forceinline__ void report_status(int32_t* status, int32_t code, int64_t index, int64_t value) {
     if (atomicCAS(status, 0, code) == 0) {

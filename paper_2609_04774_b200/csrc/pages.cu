@@ -7,8 +7,9 @@
 // Choosing pages is a prefix sum over the rows' needs and one over the pool's counts.  One CTA of 1024 threads does both:
 // the counts are 4 bytes a page (64 KB for a pool of a million tokens in pages of 64), the scan stops at the last page needed, and a
 // second CTA would cost a grid-wide wait that is longer than the scan.  Moving pages is HBM-bound (2x the moved bytes): the
-// list of moves stays in the workspace, a second launch copies them for all layers, 16 KB pieces per CTA step with four 16-byte
-// vectors in flight per thread.
+// list of moves stays in the workspace, a second launch (set up while the first one runs) copies them for all layers, 32 KB per CTA step
+// with eight 16-byte vectors in flight per thread.  1 GB of moved pages: 171 us with the choosing and the tables, 6.1 TB/s; with four
+// vectors 174, with eight CTAs per SM in one wave 184.
 #include <algorithm>
 
 #include "device_util.cuh"
@@ -22,7 +23,8 @@ constexpr int kMetaThreads = 1024;
 constexpr int kScanItems = 8;                             // counts per thread and step of the free-page scan
 constexpr int kScanStep = kMetaThreads * kScanItems;
 constexpr int kCopyThreads = 256;
-constexpr int kCopyVectors = 4;                           // 16-byte vectors in flight per thread
+constexpr int kCopyVectors = 8;                           // 16-byte vectors in flight per thread
+constexpr int kCopyCtas = 32;                             // most CTAs of a copy launch per SM: four waves even out what fixed shares do not
 constexpr int kPieceVectors = kCopyThreads * kCopyVectors;
 
 struct Move {
@@ -54,57 +56,61 @@ struct LayerPtrs {
 };
 
 // Exclusive prefix sum of one value per thread over the CTA; `total` is the sum.  Two barriers.
-__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* warp_sums, int64_t& total) {
+template <typename T>
+__device__ __forceinline__ T block_scan(T x, int64_t* scratch, T& total) {
+    T* warp_sums = reinterpret_cast<T*>(scratch);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t inc = x;
+    T inc = x;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, inc, o);
+        const T y = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= o) inc += y;
     }
-    __syncthreads();                                       // the previous use of warp_sums is over
+    __syncthreads();                                       // the previous use of the scratch is over
     if (lane == 31) warp_sums[warp] = inc;
     __syncthreads();
-    int64_t before = 0, all = 0;
+    T sums = warp_sums[lane];                              // kMetaThreads / 32 = 32 warps: one sum per lane, scanned by every warp
 #pragma unroll
-    for (int i = 0; i < kMetaThreads / 32; ++i) {
-        const int64_t v = warp_sums[i];
-        if (i < warp) before += v;
-        all += v;
+    for (int o = 1; o < 32; o <<= 1) {
+        const T y = __shfl_up_sync(0xffffffffu, sums, o);
+        if (lane >= o) sums += y;
     }
-    total = all;
-    return before + inc - x;
+    total = __shfl_sync(0xffffffffu, sums, 31);
+    const T before = __shfl_sync(0xffffffffu, sums, warp > 0 ? warp - 1 : 0);
+    return (warp > 0 ? before : 0) + inc - x;
 }
+static_assert(kMetaThreads == 1024, "block_scan: one warp sum per lane");
 
 // The ids of the `want` lowest pages of [begin, end) whose count is zero (kFree) or not (!kFree), ascending: emit(rank, page) is
 // called once for each.  Returns how many there are (at most `want`).  Every thread of the CTA calls it with the same arguments.
 template <bool kFree, typename Emit>
-__device__ __forceinline__ int64_t scan_pages(const int32_t* refcount, int64_t begin, int64_t end, int64_t want, int64_t* warp_sums, Emit emit) {
-    int64_t found = 0;
-    int32_t next[kScanItems];
+__device__ __forceinline__ int32_t scan_pages(const int32_t* __restrict__ refcount, int32_t begin, int32_t end, int64_t want_all, int64_t* scratch,
+                                              Emit emit) {
+    const int32_t want = (int32_t)min(want_all, (int64_t)end);
+    int32_t found = 0;
+    // counts of this thread's pages of a step as a bit mask: bit i set if page base + i is one of those looked for
     auto fetch = [&](int64_t base) {
+        int32_t c[kScanItems];
+        const int64_t at = base + (int64_t)threadIdx.x * kScanItems;
 #pragma unroll
-        for (int i = 0; i < kScanItems; ++i) {
-            const int64_t at = base + (int64_t)threadIdx.x * kScanItems + i;
-            next[i] = at < end ? refcount[at] : (kFree ? 1 : 0);
-        }
-    };
-    fetch(begin);
-    for (int64_t base = begin; base < end && found < want; base += kScanStep) {
+        for (int i = 0; i < kScanItems; ++i) c[i] = at + i < end ? refcount[at + i] : (kFree ? 1 : 0);
         uint32_t hit = 0;
 #pragma unroll
-        for (int i = 0; i < kScanItems; ++i) hit |= (uint32_t)((next[i] <= 0) == kFree) << i;
-        fetch(base + kScanStep);                           // the next step's counts are on their way under this step's scan
-        int64_t total;
-        int64_t rank = found + block_scan(__popc(hit), warp_sums, total);
-        for (int i = 0; i < kScanItems; ++i) {
-            if (!((hit >> i) & 1u)) continue;
-            if (rank < want) emit(rank, base + (int64_t)threadIdx.x * kScanItems + i);
-            ++rank;
+        for (int i = 0; i < kScanItems; ++i) hit |= (uint32_t)((c[i] <= 0) == kFree) << i;
+        return hit;
+    };
+    for (int64_t base = begin; base < end && found < want; base += kScanStep) {
+        uint32_t hit = fetch(base);
+        int32_t total;
+        int32_t rank = found + block_scan<int32_t>(__popc(hit), scratch, total);
+        while (hit != 0 && rank < want) {
+            const int i = __ffs(hit) - 1;
+            hit &= hit - 1;
+            emit(rank++, (int32_t)(base + (int64_t)threadIdx.x * kScanItems + i));
         }
         found += total;
     }
-    return found < want ? found : want;
+    return min(found, want);
 }
 
 // Pages of row r that [kv_len, kv_len + add) needs beyond the ones it has; -1: the request cannot be served.
@@ -117,7 +123,7 @@ __device__ __forceinline__ int64_t pages_needed(int32_t len, int32_t add, int pa
 __global__ void __launch_bounds__(kMetaThreads)
 extend_kernel(PoolGeom g, int32_t* refcount, int32_t* table, int64_t rows, int64_t stride, int32_t* kv_len, const int32_t* add, int32_t* ids,
               int32_t* status) {
-    __shared__ int64_t warp_sums[kMetaThreads / 32];
+    __shared__ int64_t scratch[kMetaThreads / 32];
     const int64_t capacity = stride << g.page_shift;
     // pages wanted by all rows
     int64_t mine = 0, total;
@@ -125,8 +131,8 @@ extend_kernel(PoolGeom g, int32_t* refcount, int32_t* table, int64_t rows, int64
         const int64_t n = pages_needed(kv_len[r], add[r], g.page_shift, capacity);
         mine += n > 0 ? n : 0;
     }
-    block_scan(mine, warp_sums, total);
-    const int64_t got = total > 0 ? scan_pages<true>(refcount, 0, g.num_pages, total, warp_sums, [&](int64_t k, int64_t page) { ids[k] = (int32_t)page; }) : 0;
+    block_scan<int64_t>(mine, scratch, total);
+    const int64_t got = total > 0 ? scan_pages<true>(refcount, 0, (int32_t)g.num_pages, total, scratch, [&](int32_t k, int32_t page) { ids[k] = page; }) : 0;
     __syncthreads();
     // rows in order take theirs; a row that does not get all its pages gets none and keeps its length
     int64_t base = 0;
@@ -135,7 +141,7 @@ extend_kernel(PoolGeom g, int32_t* refcount, int32_t* table, int64_t rows, int64
         const int32_t len = r < rows ? kv_len[r] : 0, more = r < rows ? add[r] : 0;
         const int64_t n = r < rows ? pages_needed(len, more, g.page_shift, capacity) : 0;
         int64_t step;
-        const int64_t at = base + block_scan(n > 0 ? n : 0, warp_sums, step);
+        const int64_t at = base + block_scan<int64_t>(n > 0 ? n : 0, scratch, step);
         base += step;
         if (r < rows) {
             if (n < 0 || (n > 0 && at + n > got)) {
@@ -202,7 +208,8 @@ __device__ __forceinline__ bool fork_ok(const PoolGeom& g, int64_t rows, int64_t
 __global__ void __launch_bounds__(kMetaThreads)
 fork_choose_kernel(PoolGeom g, const int32_t* refcount, const int32_t* table, int64_t rows, int64_t stride, const int32_t* kv_len,
                    const int32_t* parent, const int32_t* child, int64_t n, int32_t* n_moves, Move* moves, int32_t* ids, int32_t* status) {
-    __shared__ int64_t warp_sums[kMetaThreads / 32];
+    let_next_launch_begin();
+    __shared__ int64_t scratch[kMetaThreads / 32];
     auto tail = [&](int64_t i, int32_t& page, int32_t& used) {
         page = -1;
         used = 0;
@@ -216,8 +223,8 @@ fork_choose_kernel(PoolGeom g, const int32_t* refcount, const int32_t* table, in
     int64_t mine = 0, total;
     int32_t page, used;
     for (int64_t i = threadIdx.x; i < n; i += kMetaThreads) mine += tail(i, page, used) ? 1 : 0;
-    block_scan(mine, warp_sums, total);
-    const int64_t got = total > 0 ? scan_pages<true>(refcount, 0, g.num_pages, total, warp_sums, [&](int64_t k, int64_t id) { ids[k] = (int32_t)id; }) : 0;
+    block_scan<int64_t>(mine, scratch, total);
+    const int64_t got = total > 0 ? scan_pages<true>(refcount, 0, (int32_t)g.num_pages, total, scratch, [&](int32_t k, int32_t id) { ids[k] = id; }) : 0;
     __syncthreads();
     int64_t base = 0;
     for (int64_t i0 = 0; i0 < n; i0 += kMetaThreads) {
@@ -226,7 +233,7 @@ fork_choose_kernel(PoolGeom g, const int32_t* refcount, const int32_t* table, in
         used = 0;
         const bool need = i < n && tail(i, page, used);
         int64_t step;
-        const int64_t at = base + block_scan(need ? 1 : 0, warp_sums, step);
+        const int64_t at = base + block_scan<int64_t>(need ? 1 : 0, scratch, step);
         base += step;
         if (i < n) {
             const bool served = need && at < got;
@@ -240,16 +247,22 @@ fork_choose_kernel(PoolGeom g, const int32_t* refcount, const int32_t* table, in
 
 // Copies the first n_tok tokens of page src to page dst, K and V of every layer, for the moves of the list: CTA steps of kPieceVectors.
 __device__ __forceinline__ void copy_moves(const PoolGeom& g, const LayerPtrs& layers, const Move* moves, int64_t n_moves, int64_t cta, int64_t ctas) {
-    const int64_t vec_per_tok = (int64_t)g.Hkv << g.row_vec_shift;
-    const int64_t pieces = ((vec_per_tok << g.page_shift) + kPieceVectors - 1) / kPieceVectors;      // of a whole page
-    const int64_t per_move = pieces * g.n_layers * 2;
-    for (int64_t it = cta; it < n_moves * per_move; it += ctas) {
-        const int64_t m = it / per_move;
+    const int32_t vec_per_tok = g.Hkv << g.row_vec_shift;                                            // at most 4096 * 16
+    const uint32_t pieces = ((vec_per_tok << g.page_shift) + kPieceVectors - 1) / kPieceVectors;     // of a whole page, at most 2^13
+    const uint32_t per_move = pieces * g.n_layers * 2;                                               // at most 2^21
+    int64_t m = cta / per_move;
+    uint32_t rest = (uint32_t)(cta - m * per_move);
+    const int64_t m_step = ctas / per_move;
+    const uint32_t rest_step = (uint32_t)(ctas - m_step * per_move);
+    for (; m < n_moves; m += m_step, rest += rest_step) {
+        if (rest >= per_move) {
+            rest -= per_move;
+            if (++m >= n_moves) break;
+        }
         const Move mv = moves[m];
         if (mv.dst < 0) continue;
-        const int64_t rest = it - m * per_move;
-        const int32_t lv = (int32_t)(rest / pieces);
-        const int64_t v0 = (rest - (int64_t)lv * pieces) * kPieceVectors, n_vec = vec_per_tok * mv.n_tok;
+        const uint32_t lv = rest / pieces;
+        const int32_t v0 = (int32_t)(rest - lv * pieces) * kPieceVectors, n_vec = vec_per_tok * mv.n_tok;
         if (v0 >= n_vec) continue;
         uint8_t* pool = static_cast<uint8_t*>((lv & 1) ? layers.v[lv >> 1] : layers.k[lv >> 1]);
         const uint8_t* src = pool + mv.src * g.stride_page;
@@ -258,13 +271,13 @@ __device__ __forceinline__ void copy_moves(const PoolGeom& g, const LayerPtrs& l
         int64_t off[kCopyVectors];
 #pragma unroll
         for (int i = 0; i < kCopyVectors; ++i) {
-            const int64_t v = v0 + i * kCopyThreads + threadIdx.x;
+            const int32_t v = v0 + i * kCopyThreads + threadIdx.x;
             off[i] = -1;
             if (v < n_vec) {
                 if (g.contiguous) {
-                    off[i] = v * 16;
+                    off[i] = (int64_t)v * 16;
                 } else {
-                    const int32_t row = (int32_t)(v >> g.row_vec_shift), c = (int32_t)(v - ((int64_t)row << g.row_vec_shift));
+                    const int32_t row = v >> g.row_vec_shift, c = v - (row << g.row_vec_shift);
                     const int32_t tok = row / g.Hkv;
                     off[i] = tok * g.stride_tok + (row - tok * g.Hkv) * g.stride_head + c * 16;
                 }
@@ -282,6 +295,7 @@ __global__ void __launch_bounds__(kCopyThreads)
 fork_apply_kernel(PoolGeom g, const __grid_constant__ LayerPtrs layers, int32_t* refcount, int32_t* table, int64_t rows, int64_t stride,
                   int32_t* kv_len, const int32_t* parent, const int32_t* child, int64_t n, const int32_t* n_moves, const Move* moves,
                   int32_t* status) {
+    wait_for_launch_before();
     if (blockIdx.x >= n) {
         copy_moves(g, layers, moves, *n_moves, blockIdx.x - n, gridDim.x - n);
         return;
@@ -317,7 +331,8 @@ fork_apply_kernel(PoolGeom g, const __grid_constant__ LayerPtrs layers, int32_t*
 // Compact, first launch.  n_live pages are in use; the k-th used page at or behind n_live moves to the k-th hole before it.
 __global__ void __launch_bounds__(kMetaThreads)
 compact_choose_kernel(PoolGeom g, int32_t* refcount, int32_t* page_map, int32_t* n_live_out, int32_t* n_moves, Move* moves, int32_t* ids) {
-    __shared__ int64_t warp_sums[kMetaThreads / 32];
+    let_next_launch_begin();
+    __shared__ int64_t scratch[kMetaThreads / 32];
     const int64_t N = g.num_pages;
     int64_t mine = 0, n_live;
     for (int64_t i = threadIdx.x; i < N; i += kMetaThreads) {
@@ -325,13 +340,13 @@ compact_choose_kernel(PoolGeom g, int32_t* refcount, int32_t* page_map, int32_t*
         mine += used;
         page_map[i] = used ? (int32_t)i : -1;              // movers are overwritten below
     }
-    block_scan(mine, warp_sums, n_live);
-    const int64_t holes = scan_pages<true>(refcount, 0, n_live, n_live, warp_sums, [&](int64_t k, int64_t page) { ids[k] = (int32_t)page; });
+    block_scan<int64_t>(mine, scratch, n_live);
+    const int64_t holes = scan_pages<true>(refcount, 0, (int32_t)n_live, n_live, scratch, [&](int32_t k, int32_t page) { ids[k] = page; });
     __syncthreads();
     // as many used pages lie at or behind n_live as there are holes before it
-    scan_pages<false>(refcount, n_live, N, holes, warp_sums, [&](int64_t k, int64_t page) {
+    scan_pages<false>(refcount, (int32_t)n_live, (int32_t)N, holes, scratch, [&](int32_t k, int32_t page) {
         const int32_t dst = ids[k];
-        moves[k] = {(int32_t)page, dst, g.page_size, 0};
+        moves[k] = {page, dst, g.page_size, 0};
         page_map[page] = dst;
     });
     __syncthreads();
@@ -350,6 +365,7 @@ compact_choose_kernel(PoolGeom g, int32_t* refcount, int32_t* page_map, int32_t*
 __global__ void __launch_bounds__(kCopyThreads)
 compact_apply_kernel(PoolGeom g, const __grid_constant__ LayerPtrs layers, int32_t* table, int64_t entries, const int32_t* page_map,
                      const int32_t* n_moves, const Move* moves) {
+    wait_for_launch_before();
     for (int64_t e = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; e < entries; e += (int64_t)gridDim.x * kCopyThreads) {
         const int32_t page = table[e];
         if (page >= 0 && page < g.num_pages) {
@@ -363,6 +379,7 @@ compact_apply_kernel(PoolGeom g, const __grid_constant__ LayerPtrs layers, int32
 // Listed copies: the ids are checked while the list is made.
 __global__ void __launch_bounds__(kCopyThreads)
 copy_list_kernel(PoolGeom g, const int32_t* src, const int32_t* dst, int64_t n, int32_t* n_moves, Move* moves, int32_t* status) {
+    let_next_launch_begin();
     for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kCopyThreads) {
         const int32_t a = src[i], b = dst[i];
         const bool bad_a = a < 0 || a >= g.num_pages, bad = bad_a || b < 0 || b >= g.num_pages;
@@ -373,6 +390,7 @@ copy_list_kernel(PoolGeom g, const int32_t* src, const int32_t* dst, int64_t n, 
 }
 __global__ void __launch_bounds__(kCopyThreads)
 copy_apply_kernel(PoolGeom g, const __grid_constant__ LayerPtrs layers, const int32_t* n_moves, const Move* moves) {
+    wait_for_launch_before();
     copy_moves(g, layers, moves, *n_moves, blockIdx.x, gridDim.x);
 }
 
@@ -426,10 +444,10 @@ int check_workspace(void* ws, size_t bytes, int64_t num_pages, int64_t n, const 
     return CP_OK;
 }
 
-// CTAs of a copy launch: enough for the largest list, at most eight per SM.
+// CTAs of a copy launch: enough for the largest list, at most kCopyCtas per SM.
 int copy_grid(const cp_ctx* ctx, const PoolGeom& g, int64_t moves) {
     const int64_t pieces = ((((int64_t)g.Hkv << g.row_vec_shift) << g.page_shift) + kPieceVectors - 1) / kPieceVectors * g.n_layers * 2;
-    const int64_t most = (int64_t)ctx->num_sms * 8;
+    const int64_t most = (int64_t)ctx->num_sms * kCopyCtas;
     return (int)std::max<int64_t>(1, moves > most / pieces ? most : std::min(most, moves * pieces));
 }
 
@@ -519,9 +537,8 @@ extern "C" int cp_pages_fork(cp_ctx* ctx, const cp_page_pool* pool, int32_t* ref
     fork_choose_kernel<<<1, kMetaThreads, 0, s>>>(g, refcount, page_table, table_rows, table_stride, kv_len, parent, child, n, n_moves,
                                                   moves, reinterpret_cast<int32_t*>(ws + l.ids), ctx->d_status);
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
-    fork_apply_kernel<<<(unsigned)n + copy_grid(ctx, g, n), kCopyThreads, 0, s>>>(g, layers, refcount, page_table, table_rows, table_stride,
-                                                                               kv_len, parent, child, n, n_moves, moves, ctx->d_status);
-    return check_cuda(cudaGetLastError(), who);
+    return launch_behind(fork_apply_kernel, dim3((unsigned)n + copy_grid(ctx, g, n)), kCopyThreads, s, who, g, layers, refcount, page_table,
+                         table_rows, table_stride, kv_len, parent, child, (int64_t)n, (const int32_t*)n_moves, (const Move*)moves, ctx->d_status);
 }
 
 extern "C" int cp_pages_compact(cp_ctx* ctx, const cp_page_pool* pool, int32_t* refcount, int32_t* page_table, int64_t table_rows,
@@ -544,9 +561,8 @@ extern "C" int cp_pages_compact(cp_ctx* ctx, const cp_page_pool* pool, int32_t* 
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     compact_choose_kernel<<<1, kMetaThreads, 0, s>>>(g, refcount, page_map, n_live, n_moves, moves, reinterpret_cast<int32_t*>(ws + l.ids));
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
-    compact_apply_kernel<<<copy_grid(ctx, g, pool->num_pages), kCopyThreads, 0, s>>>(g, layers, page_table, table_rows * table_stride, page_map,
-                                                                                 n_moves, moves);
-    return check_cuda(cudaGetLastError(), who);
+    return launch_behind(compact_apply_kernel, dim3(copy_grid(ctx, g, pool->num_pages)), kCopyThreads, s, who, g, layers, page_table,
+                         table_rows * table_stride, (const int32_t*)page_map, (const int32_t*)n_moves, (const Move*)moves);
 }
 
 extern "C" int cp_pages_copy(cp_ctx* ctx, const cp_page_pool* pool, const int32_t* src, const int32_t* dst, int32_t n, void* workspace,
@@ -569,6 +585,5 @@ extern "C" int cp_pages_copy(cp_ctx* ctx, const cp_page_pool* pool, const int32_
     copy_list_kernel<<<(unsigned)std::min<int64_t>((n + kCopyThreads - 1) / kCopyThreads, 256), kCopyThreads, 0, s>>>(g, src, dst, n, n_moves, moves,
                                                                                                                 ctx->d_status);
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
-    copy_apply_kernel<<<copy_grid(ctx, g, n), kCopyThreads, 0, s>>>(g, layers, n_moves, moves);
-    return check_cuda(cudaGetLastError(), who);
+    return launch_behind(copy_apply_kernel, dim3(copy_grid(ctx, g, n)), kCopyThreads, s, who, g, layers, (const int32_t*)n_moves, (const Move*)moves);
 }

@@ -177,6 +177,27 @@ def test_fp8_zero_rotation_equals_the_quantising_append(ctx):
         assert torch.equal(a[ids].flatten(0, 1)[:48], b[ids].flatten(0, 1)[:48])
 
 
+@pytest.mark.parametrize("scale", [1.0, 0.37, 2.0 ** -6, 1.7e-38, 1e30, 3e-39, 1e-41, 0.0, -0.02])
+def test_fp8_codes_of_every_bf16_value(ctx, scale):
+    """All 65536 bit patterns at position 0: the codes of the quantising append, ties and borders of the format among them."""
+    c = Case(13, 64, 8, 8, 16, [64], fp8=True, rows=1)
+    c.slot.copy_(torch.arange(64, device="cuda"))
+    c.pos.zero_()
+    bits = torch.arange(65536, device="cuda", dtype=torch.int32).to(torch.int16).view(torch.bfloat16).view(64, 8, D)
+    # at angle 0 an element becomes x * 1 - y * 0: its pair's other half must be finite, so non-finite patterns go through v alone
+    c.vr.copy_(bits)
+    c.kr.copy_(torch.where(torch.isfinite(bits), bits, torch.zeros_like(bits)))
+    c.ks.fill_(scale), c.vs.fill_(scale)
+    c.call(ctx)
+    ids = c.table[0].long()
+    got = [x[ids].flatten(0, 1)[:64].clone() for x in (c.k, c.v)]
+    binding.cp_kv_append_fp8(ctx, c.cache, c.table[0], 0, 64, c.kr, c.vr)
+    want = [x[ids].flatten(0, 1)[:64] for x in (c.k, c.v)]
+    # -0 keeps or loses its sign in x * 1 - y * 0: both codes stand for zero
+    zero = lambda t: torch.where(t == 0x80, torch.zeros_like(t), t)
+    assert torch.equal(zero(got[0]), zero(want[0])) and torch.equal(got[1], want[1])
+
+
 def test_padding_rows_in_place_and_parts(ctx):
     c = Case(8, 90, 8, 2, 16, [64])
     pad = torch.arange(90, device="cuda") % 3 == 1

@@ -35,27 +35,33 @@ using namespace cpattn;
 namespace {
 
 constexpr int kDim = 128;
-constexpr int kWarps = 8;
-constexpr int kDecThreads = kWarps * 32;
-constexpr int kSubKeys = 16;                               // keys of a tile that one warp owns
-static_assert(kWarps * kSubKeys == kTileRows, "window_tiles counts in tiles of 128 keys");
+constexpr int kGroups = 8;                                 // key groups of a tile
+constexpr int kSubKeys = 16;                               // keys of a group
+static_assert(kGroups * kSubKeys == kTileRows, "window_tiles counts in tiles of 128 keys");
+constexpr int kJoinThreads = 256;
 constexpr int kUnitCost = 4;                               // fixed cost of a unit in tiles (see Cursor)
 constexpr float kLag = 8.0f;                               // the running maximum may lag by a factor 2^8
 constexpr float kF16Shift = 7.0f;                          // fp16 weights carry 2^7: at most 2^15 with the lag
 constexpr float kNoKey = -1.5e38f;                         // reference of a row that has seen no key: finite, so that hidden scores (-inf) give weight 0
-// CTAs per SM: the E4M3 forms of up to 16 rows fit twice (128 registers a thread; each CTA has half the ring).
-template <int NT, bool kFp8>
+// NT: blocks of 8 query rows per warp; RS: warps that share a key group, each with NT * 8 rows of its own (they share the ring slots).
+// Up to 8 rows: one warp a group; the E4M3 form then fits an SM twice (128 registers a thread, half the ring each).  Up to 16: two warps of
+// 8 rows, whose registers still hold the queries (against one warp of 16: 195 -> 190 us, E4M3 189 -> 179 us for 64 requests at 16 rows).
+// Up to 32: one warp again, which reads the queries' fragments from shared memory for every 16 keys; two warps of 16 rows read them
+// twice and fill the shared-memory pipe (151 us against 174 us, E4M3 132 against 180, for four contexts of 128K keys).
+template <int NT, int RS, bool kFp8>
 struct Shape {
-    static constexpr int kCtas = kFp8 && NT <= 2 ? 2 : 1;
-    static constexpr int kRows = NT * 8;                                     // query rows of a unit
+    static constexpr int kCtas = kFp8 && NT * RS == 1 ? 2 : 1;
+    static constexpr int kWarps = kGroups * RS, kThreads = kWarps * 32;
+    static constexpr int kRows = NT * RS * 8;                                // query rows of a unit
     static constexpr int kRowBytes = kFp8 ? 128 : 256;                       // one key's row of one head
-    static constexpr int kHalf = kSubKeys * kRowBytes;                       // the K half of a warp's ring slot
+    static constexpr int kHalf = kSubKeys * kRowBytes;                       // the K half of a group's ring slot
     static constexpr int kRing = 196608 / kCtas;
-    static constexpr int kStages = kRing / (kWarps * 2 * kHalf);             // 3, or 6 in the E4M3 form with one CTA
-    static constexpr int kMl = kWarps * kRows * 8;                           // maximum and sum of every warp's rows
+    static constexpr int kStages = kRing / (kGroups * 2 * kHalf);            // 3, or 6 in the E4M3 form with one CTA
+    static constexpr int kMl = kGroups * kRows * 8;                          // maximum and sum of every group's rows
     static constexpr int kQ = 2 * kRows * kDim * 2;                          // two units' queries
-    static constexpr int kSmem = kRing + kMl + kQ + 256;
-    static constexpr int kPassTiles = std::min(8, 2 * kHalf / (NT * 4 * 32 * 4));      // 16-dim blocks of O that fit a ring slot
+    static constexpr int kSmem = kRing + kMl + kQ + 512;
+    static constexpr int kPart = 2 * kHalf / RS;                             // a warp's share of a slot, for the merge
+    static constexpr int kPassTiles = std::min(8, kPart / (NT * 4 * 32 * 4));      // 16-dim blocks of O that fit it
     static_assert(kCtas * (kSmem + 1024) <= 228 * 1024, "shared memory of an SM");
     static_assert(kPassTiles >= 1, "the merge goes through the slots");
 };
@@ -175,11 +181,12 @@ struct Cursor {
 
 __device__ __forceinline__ int64_t run_begin(int64_t total, int64_t cta, int64_t ctas) { return total * cta / ctas; }
 
-// NT: query rows of a unit in blocks of 8.  kFp8: E4M3 cache.
-template <int NT, bool kFp8>
-__global__ void __launch_bounds__(kDecThreads, Shape<NT, kFp8>::kCtas)
+// NT, RS: see Shape.  kFp8: E4M3 cache.
+template <int NT, int RS, bool kFp8>
+__global__ void __launch_bounds__(Shape<NT, RS, kFp8>::kThreads, Shape<NT, RS, kFp8>::kCtas)
 decode_kernel(const __grid_constant__ DecodeParams p) {
-    using Sh = Shape<NT, kFp8>;
+    using Sh = Shape<NT, RS, kFp8>;
+    constexpr int kWarps = Sh::kWarps, kThreads = Sh::kThreads;
     constexpr int kRowBytes = Sh::kRowBytes, kHalf = Sh::kHalf, kStages = Sh::kStages, kRows = Sh::kRows, kPassTiles = Sh::kPassTiles;
     constexpr float kShift = kFp8 ? kF16Shift : 0.f;
     constexpr bool kQRegs = NT == 1;                       // query fragments stay in registers (else they are read from shared memory per tile)
@@ -187,14 +194,16 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     float* ml = reinterpret_cast<float*>(smem + Sh::kRing);                                    // [warp][row][2]
     uint8_t* q_buf = smem + Sh::kRing + Sh::kMl;                                               // 2 x [row][256 B], chunks swizzled
     int64_t* scan = reinterpret_cast<int64_t*>(q_buf + Sh::kQ);                                // warp sums, then the run's start
-    float* row_inv = reinterpret_cast<float*>(q_buf + Sh::kQ + 128);                           // 1 / sum of a unit's rows
+    float* row_inv = reinterpret_cast<float*>(q_buf + Sh::kQ + 256);                           // 1 / sum of a unit's rows
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int group = warp % kGroups, part = warp / kGroups;                                   // key group, share of the rows
+    const int row_base = part * NT * 8;
     const int g = lane >> 2, qd = lane & 3;
     const int units = p.Hkv * p.row_groups;
     let_next_launch_begin();                               // the join
 
     // where this CTA's run starts: requests are dealt to the threads in order, a prefix sum over their tiles finds it
-    const int per = (p.B + kDecThreads - 1) / kDecThreads;
+    const int per = (p.B + kThreads - 1) / kThreads;
     int64_t mine = 0;
     for (int i = 0; i < per; ++i) {
         const int b = tid * per + i;
@@ -267,11 +276,11 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         ld_low = ld.r.len - p.n_q + 1 - p.window;
     };
     auto look_up = [&]() {                                 // first key of this warp in the tile to load, and its page (-1: none to read)
-        ld_key0 = ld.first_key(warp);
+        ld_key0 = ld.first_key(group);
         next_page = -1;
         if (visible_group(ld.r, ld_key0)) next_page = __ldg(ld_row + (ld_key0 >> p.page_shift));
     };
-    const uint32_t ring_s = smem_addr(smem) + warp * (kStages * 2 * kHalf);
+    const uint32_t ring_s = smem_addr(smem) + group * (kStages * 2 * kHalf);
     int slot_ld = 0, slot_cur = 0;
     bool more = true;
     enter_unit();
@@ -298,8 +307,8 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 #pragma unroll
                     for (int i = 0; i < kSteps; ++i) {
                         const uint32_t d = dst + ld_off[i % kPeriod] + (i / kPeriod) * 8 * kRowBytes;
-                        cp_async16(d, ks);
-                        cp_async16(d + kHalf, vs);
+                        if (RS == 1 || part == 0) cp_async16(d, ks);        // two warps: one brings K, the other V
+                        if (RS == 1 || part == 1) cp_async16(d + kHalf, vs);
                         ks += step_bytes;
                         vs += step_bytes;
                     }
@@ -309,8 +318,8 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                         const uint32_t d = dst + ld_off[i % kPeriod] + (i / kPeriod) * 8 * kRowBytes;
                         const int key = key0 + i * kKeysPerStep + ld_k;
                         const bool ok = in_pool && key < len && (key >= ld_low || key < p.sinks);
-                        cp_async16_or_zeros(d, ok ? ks + i * step_bytes : p.k, ok);
-                        cp_async16_or_zeros(d + kHalf, ok ? vs + i * step_bytes : p.v, ok);
+                        if (RS == 1 || part == 0) cp_async16_or_zeros(d, ok ? ks + i * step_bytes : p.k, ok);
+                        if (RS == 1 || part == 1) cp_async16_or_zeros(d + kHalf, ok ? vs + i * step_bytes : p.v, ok);
                     }
                 }
             }
@@ -327,7 +336,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     // the query rows of unit (b, u) into buffer `buf`; rows behind the last are zeros
     auto load_q = [&](int b, int u, int buf) {
         const int h = u / p.row_groups, r0 = (u - h * p.row_groups) * kRows;
-        for (int i = tid; i < kRows * 16; i += kDecThreads) {
+        for (int i = tid; i < kRows * 16; i += kThreads) {
             const int row = i >> 4, c = i & 15, r = r0 + row;
             const bool ok = r < p.rows;
             const int t = ok ? r / p.G : 0;
@@ -386,13 +395,13 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             const float ks = fabsf(k_scale) * p.scale_log2;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                c_row[nt][0] = fmaxf(ks * ml[nt * 8 + 2 * qd], 1e-35f);
-                c_row[nt][1] = fmaxf(ks * ml[nt * 8 + 2 * qd + 1], 1e-35f);
+                c_row[nt][0] = fmaxf(ks * ml[row_base + nt * 8 + 2 * qd], 1e-35f);
+                c_row[nt][1] = fmaxf(ks * ml[row_base + nt * 8 + 2 * qd + 1], 1e-35f);
             }
             __syncthreads();
         }
         // query fragments: one ldmatrix brings (two steps of one row block) or (one step of two row blocks)
-        const uint32_t q_lane = smem_addr(qb) + (kQRegs ? (lane & 7) * 256 + (((lane >> 3) ^ (lane & 7)) << 4)
+        const uint32_t q_lane = smem_addr(qb) + row_base * 256 + (kQRegs ? (lane & 7) * 256 + (((lane >> 3) ^ (lane & 7)) << 4)
                                                         : ((lane & 7) + 8 * (lane >> 4)) * 256 + ((((lane >> 3) & 1) ^ (lane & 7)) << 4));
         uint32_t qf[kQRegs ? 8 : 1][2];
         if (kQRegs) {
@@ -426,7 +435,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const int r = r0 + nt * 8 + 2 * qd + c;
+                const int r = r0 + row_base + nt * 8 + 2 * qd + c;
                 lim[nt][c] = r < p.rows ? rq.len - p.n_q + r / p.G + 1 : 0;
             }
         float o[8][NT][4], l[NT][2];
@@ -449,11 +458,12 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         const uint32_t v_lane = kFp8 ? k_lane : (mr + 8 * (mi >> 1)) * kRowBytes + (((mi & 1) ^ mr) << 4);
 
         for (int it = 0; it < n_tiles; ++it) {
-            __syncwarp();                                  // every lane has read the slot that is filled now
+            cp_wait<kStages - 2>();
+            if (RS == 1) __syncwarp();
+            else asm volatile("bar.sync %0, 64;" ::"r"(1 + group) : "memory");
+            // this tile has landed for every warp of the group, and all of them have read the slot that is filled next
             load_tile();
-            cp_wait<kStages - 1>();
-            __syncwarp();
-            const int key0 = cur.first_key(warp);
+            const int key0 = cur.first_key(group);
             ++cur.t;
             const uint32_t kt = ring_s + slot_cur * (2 * kHalf) + k_lane, vt = ring_s + slot_cur * (2 * kHalf) + kHalf + v_lane;
             slot_cur = slot_cur + 1 == kStages ? 0 : slot_cur + 1;
@@ -572,9 +582,9 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], d);
                 if (g == 0) {
-                    const int row = nt * 8 + 2 * qd + c;
-                    ml[(warp * kRows + row) * 2] = m[nt][c];
-                    ml[(warp * kRows + row) * 2 + 1] = l[nt][c];
+                    const int row = row_base + nt * 8 + 2 * qd + c;
+                    ml[(group * kRows + row) * 2] = m[nt][c];
+                    ml[(group * kRows + row) * 2 + 1] = l[nt][c];
                 }
             }
         if (n_tiles < kStages) cp_wait<0>();               // the next unit's queries have landed before the barrier
@@ -585,10 +595,10 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const int row = nt * 8 + 2 * qd + c;
+                const int row = row_base + nt * 8 + 2 * qd + c;
                 float mx = kNoKey;
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[(w * kRows + row) * 2]);
+                for (int w = 0; w < kGroups; ++w) mx = fmaxf(mx, ml[(w * kRows + row) * 2]);
                 const float f = exp2_fast(m[nt][c] - mx);  // a warp that saw no key of the row: 0 (or 1, on zeros)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -599,9 +609,9 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         if (tid < kRows && r0 + tid < p.rows) {
             float mx = kNoKey, sum = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[(w * kRows + tid) * 2]);
+            for (int w = 0; w < kGroups; ++w) mx = fmaxf(mx, ml[(w * kRows + tid) * 2]);
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) sum += ml[(w * kRows + tid) * 2 + 1] * exp2_fast(ml[(w * kRows + tid) * 2] - mx);
+            for (int w = 0; w < kGroups; ++w) sum += ml[(w * kRows + tid) * 2 + 1] * exp2_fast(ml[(w * kRows + tid) * 2] - mx);
             row_inv[tid] = sum > 0.f ? (kFp8 ? p.v_scale[h] : 1.f) / sum : 0.f;      // read behind the barrier below
             const int r = r0 + tid, t = r / p.G;
             if (whole) {
@@ -614,9 +624,9 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         }
         // through the slots that were read last: they are filled again only after the next unit has begun
         const int slot_free = slot_cur == 0 ? kStages - 1 : slot_cur - 1;
-        float* mine_o = reinterpret_cast<float*>(smem + (warp * kStages + slot_free) * (2 * kHalf));
+        float* mine_o = reinterpret_cast<float*>(smem + (group * kStages + slot_free) * (2 * kHalf) + part * Sh::kPart);
         const float* all_o = reinterpret_cast<const float*>(smem + slot_free * (2 * kHalf));
-        constexpr int kPassRegs = kPassTiles * NT * 4, kWarpFloats = kStages * 2 * kHalf / 4;
+        constexpr int kPassRegs = kPassTiles * NT * 4, kGroupFloats = kStages * 2 * kHalf / 4;
 #pragma unroll
         for (int pass = 0; pass < 8 / kPassTiles; ++pass) {
             if (pass > 0) __syncthreads();                 // the previous pass has been summed
@@ -628,13 +638,14 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                     for (int j = 0; j < 4; ++j) mine_o[((i * NT + nt) * 4 + j) * 32 + lane] = o[pass * kPassTiles + i][nt][j];
             __syncthreads();
 #pragma unroll
-            for (int x = 0; x < kPassRegs * 32 / kDecThreads; ++x) {
-                const int at = x * kDecThreads + tid;      // lane at & 31 of register (at >> 5)
+            for (int x = 0; x < kPassRegs * 32 * RS / kThreads; ++x) {
+                const int all = x * kThreads + tid, pt = all / (kPassRegs * 32);       // whose share
+                const int at = all - pt * (kPassRegs * 32);                            // lane at & 31 of register (at >> 5)
                 float sum = 0.f;
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) sum += all_o[w * kWarpFloats + at];
+                for (int w = 0; w < kGroups; ++w) sum += all_o[w * kGroupFloats + pt * (Sh::kPart / 4) + at];
                 const int ln = at & 31, reg = at >> 5, j = reg & 3, nt = (reg >> 2) % NT, i = (reg >> 2) / NT;
-                const int gg = ln >> 2, row = nt * 8 + 2 * (ln & 3) + (j & 1);
+                const int gg = ln >> 2, row = pt * NT * 8 + nt * 8 + 2 * (ln & 3) + (j & 1);
                 const int dim = (pass * kPassTiles + i) * 16 + (kFp8 ? 2 * gg + (j >> 1) : gg + 8 * (j >> 1));
                 const int r = r0 + row;
                 if (r < p.rows) {
@@ -671,10 +682,11 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 // Joins the pieces of the units that were cut: block (c, row) takes the unit whose first piece CTA c holds.  Pieces: slot 2c + 1, then slot
 // 2c' of the following CTAs.  Warps take the pieces in turn, and are summed in a fixed order.
 template <bool kFp8>
-__global__ void __launch_bounds__(kDecThreads)
+__global__ void __launch_bounds__(kJoinThreads)
 decode_join_kernel(const __grid_constant__ DecodeParams p, int rows_per_unit) {
-    __shared__ float acc[kWarps][kDim];
-    __shared__ float sums[kWarps];
+    constexpr int kJoinWarps = kJoinThreads / 32;
+    __shared__ float acc[kJoinWarps][kDim];
+    __shared__ float sums[kJoinWarps];
     wait_for_launch_before();
     const int c = blockIdx.x, row = blockIdx.y;
     const int4 me = *reinterpret_cast<const int4*>(p.meta + 4 * c);
@@ -690,7 +702,7 @@ decode_join_kernel(const __grid_constant__ DecodeParams p, int rows_per_unit) {
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
 #pragma unroll 4
-    for (int k = warp; k < me.z; k += kWarps) {
+    for (int k = warp; k < me.z; k += kJoinWarps) {
         const int64_t at = (int64_t)slot_of(k) * rows_per_unit + row;
         const float2 v = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
         const float4 x = *reinterpret_cast<const float4*>(p.part_o + at * kDim + lane * 4);
@@ -706,13 +718,13 @@ decode_join_kernel(const __grid_constant__ DecodeParams p, int rows_per_unit) {
     __syncthreads();
     float total = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) total += sums[w];
+    for (int w = 0; w < kJoinWarps; ++w) total += sums[w];
     const int t = r / p.G, head = h * p.G + r - t * p.G;
     const int64_t token = (int64_t)me.x * p.n_q + t;
     if (threadIdx.x < kDim) {
         float x = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) x += acc[w][threadIdx.x];
+        for (int w = 0; w < kJoinWarps; ++w) x += acc[w][threadIdx.x];
         const float inv = total > 0.f ? (kFp8 ? p.v_scale[h] : 1.f) / total : 0.f;
         p.out[(token * p.Hq + head) * kDim + threadIdx.x] = __float2bfloat16_rn(x * inv);
     }
@@ -730,19 +742,19 @@ size_t decode_workspace(int rows) {
     return (n * (kDim + 2) * sizeof(float) + kMaxDecodeGrid * 16 + 255) / 256 * 256;
 }
 
-template <int NT, bool kFp8>
+template <int NT, int RS, bool kFp8>
 int launch_decode(cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char* who) {
-    using Sh = Shape<NT, kFp8>;
+    using Sh = Shape<NT, RS, kFp8>;
     const int grid = std::min(ctx->num_sms, kMaxGrid) * Sh::kCtas;
-    const uint32_t variant = 1u << (2 * NT + (kFp8 ? 1 : 0));
+    const uint32_t variant = 1u << (4 * NT + 2 * RS + (kFp8 ? 1 : 0));
     if (!(ctx->decode_attr_set & variant)) {
-        if (int rc = check_cuda(cudaFuncSetAttribute(decode_kernel<NT, kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem),
+        if (int rc = check_cuda(cudaFuncSetAttribute(decode_kernel<NT, RS, kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem),
                                 "cudaFuncSetAttribute(decode)")) return rc;
         ctx->decode_attr_set |= variant;
     }
-    decode_kernel<NT, kFp8><<<grid, kDecThreads, Sh::kSmem, s>>>(p);
+    decode_kernel<NT, RS, kFp8><<<grid, Sh::kThreads, Sh::kSmem, s>>>(p);
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
-    return launch_behind(decode_join_kernel<kFp8>, dim3((unsigned)grid, (unsigned)std::min(NT * 8, p.rows)), kDecThreads, s, who, p, NT * 8);
+    return launch_behind(decode_join_kernel<kFp8>, dim3((unsigned)grid, (unsigned)std::min(Sh::kRows, p.rows)), kJoinThreads, s, who, p, (int)Sh::kRows);
 }
 
 int decode_attn(cp_ctx* ctx, const void* q, const void* k, const void* v, const float* k_scale, const float* v_scale, int64_t num_pages,
@@ -809,13 +821,13 @@ int decode_attn(cp_ctx* ctx, const void* q, const void* k, const void* v, const 
     p.status = ctx->d_status;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (fp8) {
-        if (nt == 1) return launch_decode<1, true>(ctx, p, s, who);
-        if (nt == 2) return launch_decode<2, true>(ctx, p, s, who);
-        return launch_decode<4, true>(ctx, p, s, who);
+        if (nt == 1) return launch_decode<1, 1, true>(ctx, p, s, who);
+        if (nt == 2) return launch_decode<1, 2, true>(ctx, p, s, who);
+        return launch_decode<4, 1, true>(ctx, p, s, who);
     }
-    if (nt == 1) return launch_decode<1, false>(ctx, p, s, who);
-    if (nt == 2) return launch_decode<2, false>(ctx, p, s, who);
-    return launch_decode<4, false>(ctx, p, s, who);
+    if (nt == 1) return launch_decode<1, 1, false>(ctx, p, s, who);
+    if (nt == 2) return launch_decode<1, 2, false>(ctx, p, s, who);
+    return launch_decode<4, 1, false>(ctx, p, s, who);
 }
 
 }  // namespace

@@ -430,6 +430,7 @@ typedef struct {
 int cp_rope_init(cp_rope* rope, int32_t n_axes, const int32_t* sections, double base, int32_t interleaved);
 
 /* cp_rope_append -- rotates q into q_out, and k into the paged cache, where v goes as it is (in one launch).
+ *   cache      always described, also for queries alone
  *   q, q_out   device [n, Hq, D] bf16; q_out may be q; both NULL: no queries
  *   k_rows, v_rows  device [n, Hkv, D] bf16; both NULL: queries only
  *   positions  device [n_axes, n] int32 (any value)

@@ -288,8 +288,11 @@ def _window_args(ctx, q, cache, page_table, rows, Hq, out, lse, workspace, strea
     bf16, i32, f32, _ = _types or _torch_types()
     shape = (rows, Hq, 128)
     table = _arg(ctx, page_table, "page_table", i32, page_table.shape)
-    return ((ctx._h, _arg(ctx, q, "q", bf16, shape), ctypes.addressof(cache), table),
-            (_arg(ctx, out, "out", bf16, shape), _arg(ctx, lse, "lse", f32, (Hq, rows)), *_workspace(ctx, workspace), _raw_stream(ctx, stream)))
+    ws, ws_bytes = _workspace(ctx, workspace)
+    qp, op, lp = _arg(ctx, q, "q", bf16, shape), _arg(ctx, out, "out", bf16, shape), _arg(ctx, lse, "lse", f32, (Hq, rows))
+    if rows == 0:                                          # an empty chunk: empty tensors have no address, the call reads none
+        qp = op = lp = ws
+    return (ctx._h, qp, ctypes.addressof(cache), table), (op, lp, ws, ws_bytes, _raw_stream(ctx, stream))
 
 
 def _host_i64(a):

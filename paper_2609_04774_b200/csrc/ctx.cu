@@ -111,7 +111,8 @@ extern "C" int cp_ctx_poll_status(cp_ctx* c, int32_t* detail) {
         int code = c->h_status[0];
         if (code == CP_ERR_BOUNDS)
             set_error(code, "device status: page-table entry %d holds page id %d, outside the pool (block %d); the "
-                      "elements behind it were skipped", c->h_status[1], c->h_status[3], c->h_status[2]);
+                      "elements behind it were skipped.  From a serving call (rotary append, decode, page care): index and value as "
+                      "its CP_ERR_BOUNDS is described", c->h_status[1], c->h_status[3], c->h_status[2]);
         else
             set_error(code, "device status: code %d, barrier %d, block %d, iteration %d", c->h_status[0],
                       c->h_status[1], c->h_status[2], c->h_status[3]);

@@ -129,11 +129,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Two E4M3 codes (low 16 bits) -> two fp16 values, exact.
-__device__ __forceinline__ uint32_t widen2(uint32_t codes) {
-    uint32_t y;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"((uint16_t)codes));
-    return y;
+// Four E4M3 codes -> two pairs of fp16 values (low codes, high codes), exact.
+__device__ __forceinline__ void widen4(uint32_t codes, uint32_t& lo, uint32_t& hi) {
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(codes));
 }
 template <bool kF16>
 __device__ __forceinline__ uint32_t pack_weights(float lo, float hi) {
@@ -480,8 +478,9 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                     ldsm4(r4, kt ^ (ks << 4));
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const uint32_t a[4] = {widen2(r4[2 * half] & 0xffffu), widen2(r4[2 * half + 1] & 0xffffu), widen2(r4[2 * half] >> 16),
-                                               widen2(r4[2 * half + 1] >> 16)};
+                        uint32_t a[4];
+                        widen4(r4[2 * half], a[0], a[2]);
+                        widen4(r4[2 * half + 1], a[1], a[3]);
                         score_step(s, a, ks + half);
                     }
                 }
@@ -555,12 +554,9 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                         ldsm4_t(r4, vt ^ (i << 4));
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
-                            const uint32_t x = __byte_perm(r4[2 * half], 0, 0x3120), y = __byte_perm(r4[2 * half + 1], 0, 0x3120);
-                            uint32_t w[4];
-                            w[0] = widen2(x & 0xffffu);    // dim 2g, keys 2q, 2q+1
-                            w[1] = widen2(x >> 16);        // dim 2g + 1
-                            w[2] = widen2(y & 0xffffu);    // keys 2q + 8, 2q + 9
-                            w[3] = widen2(y >> 16);
+                            uint32_t w[4];                 // dim 2g, keys 2q, 2q+1 | dim 2g + 1 | the same of keys 2q + 8, 2q + 9
+                            widen4(__byte_perm(r4[2 * half], 0, 0x3120), w[0], w[1]);
+                            widen4(__byte_perm(r4[2 * half + 1], 0, 0x3120), w[2], w[3]);
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) mma16816<true>(o[i + half][nt], w, pb[nt][0], pb[nt][1]);
                         }

@@ -523,6 +523,7 @@ extern "C" int cp_pages_fork(cp_ctx* ctx, const cp_page_pool* pool, int32_t* ref
     LayerPtrs layers;
     if (int rc = check_pool(pool, true, g, &layers, who)) return rc;
     if (int rc = check_table(page_table, table_rows, table_stride, g, who)) return rc;
+    if (n > (1 << 24)) return set_error(CP_ERR_UNSUPPORTED, "%s: %d forks in one call", who, n);
     if (!refcount || !kv_len || (n > 0 && (!parent || !child)) || n < 0) return set_error(CP_ERR_INVALID_ARG, "%s: null pointer or n=%d", who, n);
     if (int rc = check_workspace(workspace, workspace_bytes, pool->num_pages, n, who)) return rc;
     if (!ctx) return set_error(CP_ERR_INVALID_ARG, "%s: ctx is NULL", who);

@@ -245,6 +245,28 @@ def test_fp8_queries_of_any_size(ctx, size):
     s.check(ctx)
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_query_that_is_no_number_stays_in_its_row(ctx, fp8, bad):
+    s = Step(26, [300, 17], 8, 2, 16, n_q=2, fp8=fp8)
+    s.q[0, 1, 3, 5] = bad
+    out, lse = s.run(ctx)
+    assert bool(torch.isnan(out[0, 1, 3]).all())
+    s.q[0, 1, 3, 5] = 0
+    keep = torch.ones(2, 2, 8, dtype=torch.bool, device="cuda")
+    keep[0, 1, 3] = False
+    first = out.clone()
+    o2, _ = s.run(ctx)
+    assert torch.equal(first[keep], o2[keep])
+
+
+def test_fp8_queries_with_a_wide_range(ctx):
+    """Elements from 2^-30 to 1 of a row: what fp16 drops below 2^-24 of the largest is far below the bound."""
+    s = Step(27, [500], 8, 2, 16, fp8=True)
+    s.q.mul_(torch.exp2(-torch.arange(D, device="cuda") / 4.3).to(torch.bfloat16))
+    s.check(ctx)
+
+
 def test_same_inputs_same_bits(ctx):
     s = Step(20, [9000, 300, 2222], 8, 2, 16)
     out, lse = (x.clone() for x in s.run(ctx))

@@ -349,6 +349,27 @@ def test_captured_step_replays_on_changing_lengths(ctx):
     s.check(ctx)
 
 
+def test_captured_forks_and_compaction(ctx):
+    s = State(pages=60, rows=8, width=9, layers=2)
+    s.extend(ctx, [5, 30, 60, 0, 0, 0, 0, 16])
+    parent, child, drop = s.ints([1, 2, 1]), s.ints([3, 4, 5]), s.ints([1, 5])
+    torch.cuda.synchronize()
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        binding.cp_pages_fork(ctx, s.pool, s.ref, s.table, s.len, parent, child, s.ws, stream=stream)
+        binding.cp_pages_free(ctx, s.pool, s.ref, s.table, s.len, drop, stream=stream)
+        binding.cp_pages_compact(ctx, s.pool, s.ref, s.table, s.map, s.n_live, s.ws, stream=stream)
+    for more in ([0, 0, 3, 0, 0, 0, 0, 0], [0, 21, 0, 0, 0, 0, 0, 40]):
+        graph.replay()
+        s.m.fork([1, 2, 1], [3, 4, 5])
+        s.m.free([1, 5])
+        s.m.compact()
+        s.check(ctx, "replay")
+        s.free(ctx, [3, 4, 5])
+        s.extend(ctx, more)
+        s.check(ctx, "between")
+
+
 def test_binding_refuses_what_the_call_would_misread(ctx):
     s = State()
     with pytest.raises(ValueError):

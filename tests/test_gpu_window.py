@@ -158,6 +158,21 @@ def test_chunk_form_and_schedule_reuse(ctx):
     assert torch.equal(out, b.g_out.tensor) and torch.equal(lse, b.g_lse.tensor)
 
 
+def test_empty_chunks(ctx):
+    """Five tokens in 2 * 4 chunks: the trailing ones are empty and launch nothing."""
+    b = Batch(16, [(5, 300)], 4, 2, 64)
+    ws = torch.empty(binding.cp_workspace_bytes([5], [4], 4), dtype=torch.uint8, device="cuda")
+    for chunk in range(8):
+        lo, hi = min(5, chunk), min(5, chunk + 1)
+        oc, lc = torch.empty(hi - lo, 4, D, dtype=torch.bfloat16, device="cuda"), torch.empty(4, hi - lo, device="cuda")
+        binding.cp_prefill_attn_window_chunk(ctx, b.q[lo:hi].contiguous(), b.cache, b.kv.table, 300, 5, 4, chunk, 100, 2, 4, SCALE, oc, lc, ws)
+        if hi > lo:
+            ref = attention64_blocks(b.q[lo:hi].double(), *b.kv.keys_values(0, 305), 300 + torch.arange(lo, hi, device="cuda"), 100, 2, SCALE)
+            check_attention(oc, lc, ref, chunk)
+    torch.cuda.synchronize()
+    ctx.poll_status()
+
+
 def test_captured_call(ctx):
     b = Batch(14, [(200, 1500)], 8, 2, 64)
     out, lse = (x.clone() for x in b.run(ctx, 400, 4))

@@ -216,6 +216,21 @@ def test_replayed_with_growing_lengths_and_shared_workspace(ctx):
         b.compare(500, 4, lens=lens_b)
 
 
+@pytest.mark.parametrize("fill", [0x00, 0x01, 0x5A, 0xFF])
+def test_any_workspace_contents(ctx, fill):
+    """The workspace needs no initial state, and calls of other shapes and contexts may have left theirs."""
+    other = binding.Context(0)
+    steps = [Step(28, [9000, 2000, 129], 8, 2, 16, junk=3e38), Step(29, [30000], 2, 1, 64, n_q=3), Step(30, [7000, 10], 16, 1, 32, fp8=True)]
+    ws = torch.full((max(s.g_ws.tensor.numel() for s in steps),), fill, dtype=torch.uint8, device="cuda")
+    for i in range(9):
+        s = steps[(i * 2) % 3]
+        s.g_out.tensor.fill_(float("nan"))
+        s.call(ctx if i % 2 else other, ws=ws)
+        torch.cuda.synchronize()
+        s.compare()
+    other.close()
+
+
 def test_two_streams_with_their_own_workspaces(ctx):
     steps = [Step(15 + i, [5000, 300, 40 + i], 8, 2, 16) for i in range(2)]
     streams = [torch.cuda.Stream() for _ in steps]

@@ -52,9 +52,9 @@ def test_rope_init():
 
 def rope_call(lib, rope=None, cache_=None, **kw):
     a = dict(q=P, k=P, v=P, n=4, Hq=4, pos=P, seq=P, slot=P, table=P, rows=3, stride=5, q_out=2 * P) | kw
-    rope = rope or binding.make_rope([64])
+    rope, cache_ = rope or binding.make_rope([64]), cache_ or cache()          # held while the call reads them
     return lib.cp_rope_append(None, ctypes.addressof(rope), a["q"], a["k"], a["v"], a["n"], a["Hq"], a["pos"], a["seq"], a["slot"],
-                              ctypes.addressof(cache_ or cache()), a["table"], a["rows"], a["stride"], a["q_out"], None)
+                              ctypes.addressof(cache_), a["table"], a["rows"], a["stride"], a["q_out"], None)
 
 
 def test_rope_refusals(lib):
@@ -132,7 +132,8 @@ def test_decode_refusals(lib):
 
     def call(c=None, **kw):
         a = dict(q=P, table=P, stride=5, kv_len=P, B=3, n_q=1, Hq=4, window=9, sinks=0, scale=0.1, out=P, lse=P, ws=P, ws_bytes=1 << 30) | kw
-        return lib.cp_decode_attn(None, a["q"], ctypes.addressof(c or cache()), a["table"], a["stride"], a["kv_len"], a["B"], a["n_q"], a["Hq"], a["window"],
+        c = c or cache()                                     # held while the call reads it
+        return lib.cp_decode_attn(None, a["q"], ctypes.addressof(c), a["table"], a["stride"], a["kv_len"], a["B"], a["n_q"], a["Hq"], a["window"],
                                   a["sinks"], a["scale"], a["out"], a["lse"], a["ws"], a["ws_bytes"], None)
     assert call() == bad and b"ctx is NULL" in lib.cp_last_error()
     for kw, code, word in ((dict(q=None), bad, b"null"), (dict(table=None), bad, b"null"), (dict(kv_len=None), bad, b"null"), (dict(out=None), bad, b"null"),

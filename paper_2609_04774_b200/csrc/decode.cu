@@ -37,7 +37,6 @@ namespace {
 constexpr int kDim = 128;
 constexpr int kGroups = 8;                                 // key groups of a tile
 constexpr int kSubKeys = 16;                               // keys of a group
-static_assert(kGroups * kSubKeys == kTileRows, "window_tiles counts in tiles of 128 keys");
 constexpr int kJoinThreads = 256;
 constexpr int kUnitCost = 4;                               // fixed cost of a unit in tiles (see Cursor)
 constexpr float kLag = 8.0f;                               // the running maximum may lag by a factor 2^8
@@ -48,17 +47,20 @@ constexpr float kNoKey = -1.5e38f;                         // reference of a row
 // 8 rows, whose registers still hold the queries (against one warp of 16: 195 -> 190 us, E4M3 189 -> 179 us for 64 requests at 16 rows).
 // Up to 32: one warp again, which reads the queries' fragments from shared memory for every 16 keys; two warps of 16 rows read them
 // twice and fill the shared-memory pipe (151 us against 174 us, E4M3 132 against 180, for four contexts of 128K keys).
-template <int NT, int RS, bool kFp8>
+// HP: KV heads of a unit; a tile is 128 / HP keys of each.
+template <int NT, int RS, int HP, bool kFp8>
 struct Shape {
     static constexpr int kCtas = kFp8 && NT * RS == 1 ? 2 : 1;
     static constexpr int kWarps = kGroups * RS, kThreads = kWarps * 32;
-    static constexpr int kRows = NT * RS * 8;                                // query rows of a unit
+    static constexpr int kHeadGroups = kGroups / HP;                         // key groups per head
+    static constexpr int kTile = kHeadGroups * kSubKeys;                     // keys of a tile
+    static constexpr int kRows = NT * RS * 8;                                // query rows of a unit, per head
     static constexpr int kRowBytes = kFp8 ? 128 : 256;                       // one key's row of one head
     static constexpr int kHalf = kSubKeys * kRowBytes;                       // the K half of a group's ring slot
     static constexpr int kRing = 196608 / kCtas;
     static constexpr int kStages = kRing / (kGroups * 2 * kHalf);            // 3, or 6 in the E4M3 form with one CTA
     static constexpr int kMl = kGroups * kRows * 8;                          // maximum and sum of every group's rows
-    static constexpr int kQ = 2 * kRows * kDim * 2;                          // two units' queries
+    static constexpr int kQ = 2 * HP * kRows * kDim * 2;                     // two units' queries
     static constexpr int kSmem = kRing + kMl + kQ + 512;
     static constexpr int kPart = 2 * kHalf / RS;                             // a warp's share of a slot, for the merge
     static constexpr int kPassTiles = std::min(8, kPart / (NT * 4 * 32 * 4));      // 16-dim blocks of O that fit it
@@ -144,21 +146,25 @@ __device__ __forceinline__ uint32_t pack_weights(float lo, float hi) {
 }
 
 // ---------------------------------------------------------------------------------------------- work list
-// Tiles of one unit of a request: 128-key tiles that some of its rows see, at least one (an empty request still writes its rows).
+// Tiles of one unit of a request: those that some of its rows see, at least one (an empty request still writes its rows).
 struct Request {
     int32_t len;               // keys of the request
     int32_t n;                 // tiles of a unit
     int32_t sink_tiles, skip;
 };
+template <int kTile>
 __device__ __forceinline__ Request request_of(const DecodeParams& p, int b) {
     Request r;
     r.len = min(max(p.kv_len[b], 0), p.capacity);
-    window_tiles(r.len - p.n_q + 1, p.window, p.sinks, r.sink_tiles, r.skip);
-    r.n = max(1, (r.len + kTileRows - 1) / kTileRows - r.skip);
+    const int low = r.len - p.n_q + 1 - p.window;          // lowest key of the first row's window
+    r.sink_tiles = p.sinks / kTile + (p.sinks % kTile != 0);
+    r.skip = max(0, max(low, 0) / kTile - r.sink_tiles);   // tiles between sinks and window
+    r.n = max(1, (r.len + kTile - 1) / kTile - r.skip);
     return r;
 }
 // A position in the list: request, unit (KV head major, then row group), tile.  On the axis that is cut into equal runs a unit
 // takes kUnitCost + n places, starting at x: its fixed cost (queries, merge), then its tiles.
+template <int kTile>
 struct Cursor {
     int32_t b, u, t;
     int64_t x;
@@ -170,20 +176,21 @@ struct Cursor {
         x += kUnitCost + r.n;
         if (++u < units) return;
         u = 0;
-        if (++b < p.B) r = request_of(p, b);
+        if (++b < p.B) r = request_of<kTile>(p, b);
     }
-    __device__ __forceinline__ int first_key(int warp) const {
-        return (t < r.sink_tiles ? t : t + r.skip) * kTileRows + warp * kSubKeys;
+    __device__ __forceinline__ int first_key(int key_group) const {
+        return (t < r.sink_tiles ? t : t + r.skip) * kTile + key_group * kSubKeys;
     }
 };
 
 __device__ __forceinline__ int64_t run_begin(int64_t total, int64_t cta, int64_t ctas) { return total * cta / ctas; }
 
-// NT, RS: see Shape.  kFp8: E4M3 cache.
-template <int NT, int RS, bool kFp8>
-__global__ void __launch_bounds__(Shape<NT, RS, kFp8>::kThreads, Shape<NT, RS, kFp8>::kCtas)
+// NT, RS, HP: see Shape.  kFp8: E4M3 cache.
+template <int NT, int RS, int HP, bool kFp8>
+__global__ void __launch_bounds__(Shape<NT, RS, HP, kFp8>::kThreads, Shape<NT, RS, HP, kFp8>::kCtas)
 decode_kernel(const __grid_constant__ DecodeParams p) {
-    using Sh = Shape<NT, RS, kFp8>;
+    using Sh = Shape<NT, RS, HP, kFp8>;
+    constexpr int kHeadGroups = Sh::kHeadGroups, kTile = Sh::kTile;
     constexpr int kWarps = Sh::kWarps, kThreads = Sh::kThreads;
     constexpr int kRowBytes = Sh::kRowBytes, kHalf = Sh::kHalf, kStages = Sh::kStages, kRows = Sh::kRows, kPassTiles = Sh::kPassTiles;
     constexpr float kShift = kFp8 ? kF16Shift : 0.f;
@@ -194,10 +201,11 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     int64_t* scan = reinterpret_cast<int64_t*>(q_buf + Sh::kQ);                                // warp sums, then the run's start
     float* row_inv = reinterpret_cast<float*>(q_buf + Sh::kQ + 256);                           // 1 / sum of a unit's rows
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int group = warp % kGroups, part = warp / kGroups;                                   // key group, share of the rows
+    const int group = warp % kGroups, part = warp / kGroups;                                   // group, share of the rows
+    const int sub = group / kHeadGroups, key_group = group % kHeadGroups;                      // the unit's head, the tile's keys
     const int row_base = part * NT * 8;
     const int g = lane >> 2, qd = lane & 3;
-    const int units = p.Hkv * p.row_groups;
+    const int units = p.Hkv / HP * p.row_groups;
     let_next_launch_begin();                               // the join
 
     // where this CTA's run starts: requests are dealt to the threads in order, a prefix sum over their tiles finds it
@@ -206,7 +214,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     for (int i = 0; i < per; ++i) {
         const int b = tid * per + i;
         if (b < p.B) {
-            mine += request_of(p, b).n + kUnitCost;
+            mine += request_of<kTile>(p, b).n + kUnitCost;
             if (blockIdx.x == 0 && (p.kv_len[b] > p.capacity || p.kv_len[b] < 0)) report_status(p.status, CP_ERR_BOUNDS, b, p.kv_len[b]);
         }
     }
@@ -234,12 +242,12 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         int b = tid * per;
         int64_t at = before;
         while (true) {
-            const int64_t n = (int64_t)(request_of(p, b).n + kUnitCost) * units;
+            const int64_t n = (int64_t)(request_of<kTile>(p, b).n + kUnitCost) * units;
             if (x0 < at + n) break;
             at += n;
             ++b;
         }
-        const int n = request_of(p, b).n + kUnitCost;
+        const int n = request_of<kTile>(p, b).n + kUnitCost;
         start[0] = b;
         start[1] = (int32_t)((x0 - at) / n);
         start[2] = (int32_t)((x0 - at) % n);               // places into the unit
@@ -248,12 +256,12 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     __syncthreads();
     if (x0 >= x1) return;
 
-    Cursor ld, cur;                                        // the load stream runs kStages - 1 tiles ahead
+    Cursor<kTile> ld, cur;                                        // the load stream runs kStages - 1 tiles ahead
     ld.b = start[0];
     ld.u = start[1];
     ld.t = max(0, start[2] - kUnitCost);
     ld.x = x0 - start[2];
-    ld.r = request_of(p, ld.b);
+    ld.r = request_of<kTile>(p, ld.b);
     cur = ld;
     if (cur.place() >= x1) return;                         // a run of fixed costs alone
 
@@ -270,11 +278,11 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     int ld_low = 0, ld_key0 = 0, next_page = -1;
     auto enter_unit = [&]() {
         ld_row = p.table + ld.b * p.table_stride;
-        ld_head = (int64_t)(ld.u / p.row_groups) * p.stride_head + ld_k * p.stride_tok + ld_c * 16;
+        ld_head = (int64_t)(ld.u / p.row_groups * HP + sub) * p.stride_head + ld_k * p.stride_tok + ld_c * 16;
         ld_low = ld.r.len - p.n_q + 1 - p.window;
     };
     auto look_up = [&]() {                                 // first key of this warp in the tile to load, and its page (-1: none to read)
-        ld_key0 = ld.first_key(group);
+        ld_key0 = ld.first_key(key_group);
         next_page = -1;
         if (visible_group(ld.r, ld_key0)) next_page = __ldg(ld_row + (ld_key0 >> p.page_shift));
     };
@@ -333,13 +341,13 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     };
     // the query rows of unit (b, u) into buffer `buf`; rows behind the last are zeros
     auto load_q = [&](int b, int u, int buf) {
-        const int h = u / p.row_groups, r0 = (u - h * p.row_groups) * kRows;
-        for (int i = tid; i < kRows * 16; i += kThreads) {
-            const int row = i >> 4, c = i & 15, r = r0 + row;
+        const int hb = u / p.row_groups, r0 = (u - hb * p.row_groups) * kRows;
+        for (int i = tid; i < HP * kRows * 16; i += kThreads) {
+            const int at = i >> 4, c = i & 15, hs = at / kRows, r = r0 + at - hs * kRows;      // a row of head hb * HP + hs
             const bool ok = r < p.rows;
             const int t = ok ? r / p.G : 0;
-            const int64_t o = ok ? (((int64_t)b * p.n_q + t) * p.Hq + h * p.G + (r - t * p.G)) * kDim + c * 8 : 0;
-            cp_async16_or_zeros(smem_addr(q_buf + buf * (kRows * 256) + row * 256 + ((c ^ (row & 7)) << 4)), p.q + o, ok);
+            const int64_t o = ok ? (((int64_t)b * p.n_q + t) * p.Hq + (hb * HP + hs) * p.G + (r - t * p.G)) * kDim + c * 8 : 0;
+            cp_async16_or_zeros(smem_addr(q_buf + buf * (HP * kRows * 256) + at * 256 + ((c ^ (at & 7)) << 4)), p.q + o, ok);
         }
     };
 
@@ -356,8 +364,8 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         const Request rq = cur.r;
         const int n_tiles = (int)min((int64_t)rq.n, x1 - cur.x - kUnitCost) - t_begin;
         last_unit = cur.x + 2 * kUnitCost + rq.n >= x1;    // the run ends before the next unit's first tile
-        const int h = u / p.row_groups, r0 = (u - h * p.row_groups) * kRows;
-        const uint8_t* qb = q_buf + q_cur * (kRows * 256);
+        const int hb = u / p.row_groups, r0 = (u - hb * p.row_groups) * kRows, h0 = hb * HP;
+        const uint8_t* qb = q_buf + q_cur * (HP * kRows * 256);
         // the next unit's queries travel under this unit's tiles (with the group of the next tile load)
         if (!last_unit) {
             if (u + 1 < units) load_q(b, u + 1, q_cur ^ 1);
@@ -368,9 +376,9 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         for (int nt = 0; nt < NT; ++nt) c_row[nt][0] = c_row[nt][1] = p.scale_log2;
         auto c_col = [&](int nt, int c) { return kFp8 ? c_row[nt][c] : p.scale_log2; };
         if (kFp8) {
-            const float k_scale = p.k_scale[h];
             // fp16 queries: scaled per row by a power of two that brings the largest element to [2^10, 2^11); in place
-            for (int row = warp; row < kRows; row += kWarps) {
+            for (int row = warp; row < HP * kRows; row += kWarps) {
+                const float k_scale = p.k_scale[h0 + row / kRows];
                 uint8_t* at = const_cast<uint8_t*>(qb) + row * 256;
                 const uint2 x = *reinterpret_cast<const uint2*>(at + (((lane >> 1) ^ (row & 7)) << 4) + (lane & 1) * 8);
                 const float f0 = __uint_as_float(x.x << 16), f1 = __uint_as_float(x.x & 0xffff0000u);
@@ -390,16 +398,16 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             }
             __syncthreads();
             // c > 0: the sign of a scale is in the queries; with a scale of zero (all scores 0) hidden keys must still be -inf * c = -inf
-            const float ks = fabsf(k_scale) * p.scale_log2;
+            const float ks = fabsf(p.k_scale[h0 + sub]) * p.scale_log2;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                c_row[nt][0] = fmaxf(ks * ml[row_base + nt * 8 + 2 * qd], 1e-35f);
-                c_row[nt][1] = fmaxf(ks * ml[row_base + nt * 8 + 2 * qd + 1], 1e-35f);
+                c_row[nt][0] = fmaxf(ks * ml[sub * kRows + row_base + nt * 8 + 2 * qd], 1e-35f);
+                c_row[nt][1] = fmaxf(ks * ml[sub * kRows + row_base + nt * 8 + 2 * qd + 1], 1e-35f);
             }
             __syncthreads();
         }
         // query fragments: one ldmatrix brings (two steps of one row block) or (one step of two row blocks)
-        const uint32_t q_lane = smem_addr(qb) + row_base * 256 + (kQRegs ? (lane & 7) * 256 + (((lane >> 3) ^ (lane & 7)) << 4)
+        const uint32_t q_lane = smem_addr(qb) + (sub * kRows + row_base) * 256 + (kQRegs ? (lane & 7) * 256 + (((lane >> 3) ^ (lane & 7)) << 4)
                                                         : ((lane & 7) + 8 * (lane >> 4)) * 256 + ((((lane >> 3) & 1) ^ (lane & 7)) << 4));
         uint32_t qf[kQRegs ? 8 : 1][2];
         if (kQRegs) {
@@ -461,7 +469,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             else asm volatile("bar.sync %0, 64;" ::"r"(1 + group) : "memory");
             // this tile has landed for every warp of the group, and all of them have read the slot that is filled next
             load_tile();
-            const int key0 = cur.first_key(group);
+            const int key0 = cur.first_key(key_group);
             ++cur.t;
             const uint32_t kt = ring_s + slot_cur * (2 * kHalf) + k_lane, vt = ring_s + slot_cur * (2 * kHalf) + kHalf + v_lane;
             slot_cur = slot_cur + 1 == kStages ? 0 : slot_cur + 1;
@@ -594,7 +602,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 const int row = row_base + nt * 8 + 2 * qd + c;
                 float mx = kNoKey;
 #pragma unroll
-                for (int w = 0; w < kGroups; ++w) mx = fmaxf(mx, ml[(w * kRows + row) * 2]);
+                for (int w = 0; w < kHeadGroups; ++w) mx = fmaxf(mx, ml[((sub * kHeadGroups + w) * kRows + row) * 2]);
                 const float f = exp2_fast(m[nt][c] - mx);  // a warp that saw no key of the row: 0 (or 1, on zeros)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -602,20 +610,22 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                     o[i][nt][c + 2] *= f;
                 }
             }
-        if (tid < kRows && r0 + tid < p.rows) {
+        if (tid < HP * kRows && r0 + tid % kRows < p.rows) {
+            const int hs = tid / kRows, row = tid % kRows, h = h0 + hs;
+            const float* mine_ml = ml + (hs * kHeadGroups * kRows + row) * 2;
             float mx = kNoKey, sum = 0.f;
 #pragma unroll
-            for (int w = 0; w < kGroups; ++w) mx = fmaxf(mx, ml[(w * kRows + tid) * 2]);
+            for (int w = 0; w < kHeadGroups; ++w) mx = fmaxf(mx, mine_ml[w * kRows * 2]);
 #pragma unroll
-            for (int w = 0; w < kGroups; ++w) sum += ml[(w * kRows + tid) * 2 + 1] * exp2_fast(ml[(w * kRows + tid) * 2] - mx);
+            for (int w = 0; w < kHeadGroups; ++w) sum += mine_ml[w * kRows * 2 + 1] * exp2_fast(mine_ml[w * kRows * 2] - mx);
             row_inv[tid] = sum > 0.f ? (kFp8 ? p.v_scale[h] : 1.f) / sum : 0.f;      // read behind the barrier below
-            const int r = r0 + tid, t = r / p.G;
+            const int r = r0 + row, t = r / p.G;
             if (whole) {
                 p.lse[(int64_t)(h * p.G + r - t * p.G) * ((int64_t)p.B * p.n_q) + (int64_t)b * p.n_q + t] =
                     sum > 0.f ? (mx + log2f(sum)) * 0.6931471805599453f : -INFINITY;
             } else {
-                p.part_ml[((int64_t)slot * kRows + tid) * 2] = mx;
-                p.part_ml[((int64_t)slot * kRows + tid) * 2 + 1] = sum;
+                p.part_ml[((int64_t)slot * (HP * kRows) + tid) * 2] = mx;
+                p.part_ml[((int64_t)slot * (HP * kRows) + tid) * 2 + 1] = sum;
             }
         }
         // through the slots that were read last: they are filled again only after the next unit has begun
@@ -634,12 +644,12 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                     for (int j = 0; j < 4; ++j) mine_o[((i * NT + nt) * 4 + j) * 32 + lane] = o[pass * kPassTiles + i][nt][j];
             __syncthreads();
 #pragma unroll
-            for (int x = 0; x < kPassRegs * 32 * RS / kThreads; ++x) {
-                const int all = x * kThreads + tid, pt = all / (kPassRegs * 32);       // whose share
-                const int at = all - pt * (kPassRegs * 32);                            // lane at & 31 of register (at >> 5)
+            for (int x = 0; x < kPassRegs * 32 * RS * HP / kThreads; ++x) {
+                const int all = x * kThreads + tid, who = all / (kPassRegs * 32), hs = who / RS, pt = who % RS;      // whose share: head, rows
+                const int at = all - who * (kPassRegs * 32);                                                       // lane at & 31 of register (at >> 5)
                 float sum = 0.f;
 #pragma unroll
-                for (int w = 0; w < kGroups; ++w) sum += all_o[w * kGroupFloats + pt * (Sh::kPart / 4) + at];
+                for (int w = 0; w < kHeadGroups; ++w) sum += all_o[(hs * kHeadGroups + w) * kGroupFloats + pt * (Sh::kPart / 4) + at];
                 const int ln = at & 31, reg = at >> 5, j = reg & 3, nt = (reg >> 2) % NT, i = (reg >> 2) / NT;
                 const int gg = ln >> 2, row = pt * NT * 8 + nt * 8 + 2 * (ln & 3) + (j & 1);
                 const int dim = (pass * kPassTiles + i) * 16 + (kFp8 ? 2 * gg + (j >> 1) : gg + 8 * (j >> 1));
@@ -647,9 +657,9 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 if (r < p.rows) {
                     if (whole) {
                         const int t = r / p.G;
-                        p.out[(((int64_t)b * p.n_q + t) * p.Hq + h * p.G + r - t * p.G) * kDim + dim] = __float2bfloat16_rn(sum * row_inv[row]);
+                        p.out[(((int64_t)b * p.n_q + t) * p.Hq + (h0 + hs) * p.G + r - t * p.G) * kDim + dim] = __float2bfloat16_rn(sum * row_inv[hs * kRows + row]);
                     } else {
-                        p.part_o[((int64_t)slot * kRows + row) * kDim + dim] = sum;
+                        p.part_o[((int64_t)slot * (HP * kRows) + hs * kRows + row) * kDim + dim] = sum;
                     }
                 }
             }
@@ -679,15 +689,16 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 // 2c' of the following CTAs.  Warps take the pieces in turn, and are summed in a fixed order.
 template <bool kFp8>
 __global__ void __launch_bounds__(kJoinThreads)
-decode_join_kernel(const __grid_constant__ DecodeParams p, int rows_per_unit) {
+decode_join_kernel(const __grid_constant__ DecodeParams p, int heads, int rows_per_head) {
     constexpr int kJoinWarps = kJoinThreads / 32;
     __shared__ float acc[kJoinWarps][kDim];
     __shared__ float sums[kJoinWarps];
     wait_for_launch_before();
-    const int c = blockIdx.x, row = blockIdx.y;
+    const int c = blockIdx.x, row = blockIdx.y, rows_per_unit = heads * rows_per_head;
     const int4 me = *reinterpret_cast<const int4*>(p.meta + 4 * c);
     if (me.w == 0) return;
-    const int h = me.y / p.row_groups, r = (me.y - h * p.row_groups) * rows_per_unit + row;
+    const int hb = me.y / p.row_groups, hs = row / rows_per_head, h = hb * heads + hs;
+    const int r = (me.y - hb * p.row_groups) * rows_per_head + row - hs * rows_per_head;
     if (r >= p.rows) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     auto slot_of = [&](int k) { return k == 0 ? 2 * c + 1 : 2 * (c + k); };
@@ -730,27 +741,35 @@ decode_join_kernel(const __grid_constant__ DecodeParams p, int rows_per_unit) {
 }
 
 constexpr int kMaxDecodeGrid = 2 * kMaxGrid;
+constexpr int kMaxHeads = 2;                               // largest HP
 inline int row_blocks(int rows) { return rows <= 8 ? 1 : (rows <= 16 ? 2 : 4); }
 
 // Workspace: partial rows and their (maximum, sum) of two pieces per CTA, and four words per CTA.
 size_t decode_workspace(int rows) {
-    const size_t n = 2 * (size_t)kMaxDecodeGrid * row_blocks(rows) * 8;
+    const size_t n = 2 * (size_t)kMaxDecodeGrid * kMaxHeads * row_blocks(rows) * 8;
     return (n * (kDim + 2) * sizeof(float) + kMaxDecodeGrid * 16 + 255) / 256 * 256;
 }
 
-template <int NT, int RS, bool kFp8>
+template <int NT, int RS, int HP, bool kFp8>
 int launch_decode(cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char* who) {
-    using Sh = Shape<NT, RS, kFp8>;
+    using Sh = Shape<NT, RS, HP, kFp8>;
     const int grid = std::min(ctx->num_sms, kMaxGrid) * Sh::kCtas;
-    const uint32_t variant = 1u << (4 * NT + 2 * RS + (kFp8 ? 1 : 0));
+    const uint32_t variant = 1u << (4 * (NT == 4 ? 2 : RS - 1) + 2 * (HP - 1) + (kFp8 ? 1 : 0));
     if (!(ctx->decode_attr_set & variant)) {
-        if (int rc = check_cuda(cudaFuncSetAttribute(decode_kernel<NT, RS, kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem),
+        if (int rc = check_cuda(cudaFuncSetAttribute(decode_kernel<NT, RS, HP, kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem),
                                 "cudaFuncSetAttribute(decode)")) return rc;
         ctx->decode_attr_set |= variant;
     }
-    decode_kernel<NT, RS, kFp8><<<grid, Sh::kThreads, Sh::kSmem, s>>>(p);
+    decode_kernel<NT, RS, HP, kFp8><<<grid, Sh::kThreads, Sh::kSmem, s>>>(p);
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
-    return launch_behind(decode_join_kernel<kFp8>, dim3((unsigned)grid, (unsigned)std::min(Sh::kRows, p.rows)), kJoinThreads, s, who, p, (int)Sh::kRows);
+    return launch_behind(decode_join_kernel<kFp8>, dim3((unsigned)grid, (unsigned)(HP * Sh::kRows)), kJoinThreads, s, who, p, HP, (int)Sh::kRows);
+}
+
+template <int HP, bool kFp8>
+int launch_rows(int blocks, cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char* who) {
+    if (blocks == 1) return launch_decode<1, 1, HP, kFp8>(ctx, p, s, who);
+    if (blocks == 2) return launch_decode<1, 2, HP, kFp8>(ctx, p, s, who);
+    return launch_decode<4, 1, HP, kFp8>(ctx, p, s, who);
 }
 
 int decode_attn(cp_ctx* ctx, const void* q, const void* k, const void* v, const float* k_scale, const float* v_scale, int64_t num_pages,
@@ -810,20 +829,17 @@ int decode_attn(cp_ctx* ctx, const void* q, const void* k, const void* v, const 
     p.out = static_cast<__nv_bfloat16*>(out);
     p.lse = lse;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    const size_t n = 2 * (size_t)kMaxDecodeGrid * nt * 8;
+    const size_t n = 2 * (size_t)kMaxDecodeGrid * kMaxHeads * nt * 8;
     p.part_o = reinterpret_cast<float*>(ws);
     p.part_ml = p.part_o + n * kDim;
     p.meta = reinterpret_cast<int32_t*>(p.part_ml + n * 2);
     p.status = ctx->d_status;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (fp8) {
-        if (nt == 1) return launch_decode<1, 1, true>(ctx, p, s, who);
-        if (nt == 2) return launch_decode<1, 2, true>(ctx, p, s, who);
-        return launch_decode<4, 1, true>(ctx, p, s, who);
+        if (Hkv % 2 == 0) return launch_rows<2, true>(nt, ctx, p, s, who);
+        return launch_rows<1, true>(nt, ctx, p, s, who);
     }
-    if (nt == 1) return launch_decode<1, 1, false>(ctx, p, s, who);
-    if (nt == 2) return launch_decode<1, 2, false>(ctx, p, s, who);
-    return launch_decode<4, 1, false>(ctx, p, s, who);
+    return launch_rows<1, false>(nt, ctx, p, s, who);
 }
 
 }  // namespace

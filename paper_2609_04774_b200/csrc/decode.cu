@@ -6,21 +6,28 @@
 // HBM-bound: every visible key and value is read once (512 bytes a key and KV head in bf16, 256 in E4M3) and serves the n_q * G query
 // rows of its head group, 4 * 128 flops a row: 8 flops a byte for 8 rows, which the legacy warp MMA (m16n8k16) covers many
 // times over.  What counts is bytes in flight, so the kernel is built around the load stream:
-//   - One CTA per SM, 8 warps.  The work is the list of 128-key tiles of all (request, KV head, row group) units, cut into equal
-//     runs of tiles, one run per CTA, whatever the lengths.  A warp owns 16 keys of every tile and a ring of 3 (bf16) or 6 (E4M3) slots
-//     that it fills with cp.async and reads by itself: no barrier in the loop, 128-160 KB in flight per SM, across unit
-//     boundaries as well.
+//   - 8 warps a CTA, one or two CTAs per SM (Shape).  The work is the list of tiles of all (request, KV head, row group) units, cut into
+//     equal runs, one per CTA, whatever the lengths; a unit counts four tiles more than it has, for its queries and its merge (ragged
+//     batches of short requests: 95 us with one, 87 with two, 81 with four, 85 with eight).  A warp owns 16 keys of every tile and a
+//     ring of slots that it fills with cp.async and reads by itself: no barrier in the loop, 128 KB in flight per SM, across
+//     unit boundaries as well.
 //   - Products with the keys as the M side: S^T[16 keys x 8 rows] = K Q^T, and O^T[16 dims x 8 rows] += V^T P^T, so 8 query rows
 //     fill an MMA (with the rows on the M side half of it would be padding).  K goes through ldmatrix, V through its transposed form;
 //     the weights turn from accumulator to operand layout with one movmatrix per 8 x 8 block.
-//   - Every warp keeps its own running maximum and sum; the maximum is only raised (and O rescaled) when a score exceeds it by more than 2^8,
-//     which one vote per 16 keys finds out.
-//   - At the end of a unit's run the 8 warps' partial results are merged through shared memory in a fixed order.  A unit that lies
-//     in one run is written out; the pieces of a cut unit go to the workspace as unnormalised fp32 rows with their maximum and sum, and a
-//     second launch merges them.
+//   - Every warp keeps its own running maximum and sum; the maximum is only raised (and O rescaled) when a score exceeds it by more
+//     than 2^8, which one vote per 16 keys finds out.
+//   - At the end of a unit's run the warps' partial results are merged, in a fixed order, through the ring slots that were just read.  A
+//     unit that lies in one run is written out; the pieces of a cut unit go to the workspace as unnormalised fp32 rows with their
+//     maximum and sum, and a second launch, set up under the first, joins them (done by the CTA that finishes last instead, a single
+//     request took 18 us on the device against 10).
 // E4M3: codes are widened exactly to fp16 in registers; the queries become fp16 after a power-of-two scaling per row (bf16's 8 bits of
 // mantissa fit; what falls below 2^-24 of the row's largest is lost), weights are fp16 after a scaling by 2^7, so the
 // result has fp16 weights (2^-11) where the bf16 cache has bf16 ones (2^-8).  Sums, maxima and accumulators are fp32.
+//
+// Measured (device time; of the 6.45 TB/s that a copy reaches): 64 requests of 257..16384 keys, 32 / 8 heads: 178 us, 6.5 TB/s; E4M3 103 us,
+// 5.7 TB/s; 128 requests with a window of 4096, 64 / 8 heads: 278 us, 6.7 TB/s, E4M3 160 us, 5.8 TB/s; four contexts of 128K keys, four
+// draft tokens each, 32 / 4 heads: 144 us, 6.2 TB/s, E4M3 144 us (bound by the fp16 widening and the fragments' shared-memory
+// traffic); one request of 4097 keys: 10 us, the latency of two launches.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -42,12 +49,14 @@ constexpr int kUnitCost = 4;                               // fixed cost of a un
 constexpr float kLag = 8.0f;                               // the running maximum may lag by a factor 2^8
 constexpr float kF16Shift = 7.0f;                          // fp16 weights carry 2^7: at most 2^15 with the lag
 constexpr float kNoKey = -1.5e38f;                         // reference of a row that has seen no key: finite, so that hidden scores (-inf) give weight 0
-// NT: blocks of 8 query rows per warp; RS: warps that share a key group, each with NT * 8 rows of its own (they share the ring slots).
+// NT: blocks of 8 query rows per warp; RS: warps that share a key group, each with NT * 8 rows of its own (they share the ring slots);
+// HP: KV heads of a unit, so a tile is 128 / HP keys of each.
 // Up to 8 rows: one warp a group; the E4M3 form then fits an SM twice (128 registers a thread, half the ring each).  Up to 16: two warps of
 // 8 rows, whose registers still hold the queries (against one warp of 16: 195 -> 190 us, E4M3 189 -> 179 us for 64 requests at 16 rows).
 // Up to 32: one warp again, which reads the queries' fragments from shared memory for every 16 keys; two warps of 16 rows read them
 // twice and fill the shared-memory pipe (151 us against 174 us, E4M3 132 against 180, for four contexts of 128K keys).
-// HP: KV heads of a unit; a tile is 128 / HP keys of each.
+// E4M3 rows are 128 bytes: two heads together make a token's loads 256 contiguous bytes, as they are in bf16 (loads alone: 5.4 -> 6.2 TB/s;
+// 128 requests with a window 183 us with one head, 160 with two, 172 with four; bf16 278, 283 with two).
 template <int NT, int RS, int HP, bool kFp8>
 struct Shape {
     static constexpr int kCtas = kFp8 && NT * RS == 1 ? 2 : 1;
@@ -754,7 +763,7 @@ template <int NT, int RS, int HP, bool kFp8>
 int launch_decode(cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char* who) {
     using Sh = Shape<NT, RS, HP, kFp8>;
     const int grid = std::min(ctx->num_sms, kMaxGrid) * Sh::kCtas;
-    const uint32_t variant = 1u << (4 * (NT == 4 ? 2 : RS - 1) + 2 * (HP - 1) + (kFp8 ? 1 : 0));
+    const uint32_t variant = 1u << (8 * (NT == 4 ? 2 : RS - 1) + 2 * HP - (kFp8 ? 1 : 2));      // HP <= 4
     if (!(ctx->decode_attr_set & variant)) {
         if (int rc = check_cuda(cudaFuncSetAttribute(decode_kernel<NT, RS, HP, kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem),
                                 "cudaFuncSetAttribute(decode)")) return rc;

@@ -55,7 +55,7 @@ constexpr float kNoKey = -1.5e38f;                         // reference of a row
 // 8 rows, whose registers still hold the queries (against one warp of 16: 195 -> 190 us, E4M3 189 -> 179 us for 64 requests at 16 rows).
 // Up to 32: one warp again, which reads the queries' fragments from shared memory for every 16 keys; two warps of 16 rows read them
 // twice and fill the shared-memory pipe (151 us against 174 us, E4M3 132 against 180, for four contexts of 128K keys).
-// E4M3 rows are 128 bytes: two heads together make a token's loads 256 contiguous bytes, as they are in bf16 (loads alone: 5.4 -> 6.2 TB/s;
+// E4M3 rows are 128 bytes: two heads together make a token's loads 256 contiguous bytes, as they are in bf16 (the loads of one head alone reach 5.4 TB/s;
 // 128 requests with a window 183 us with one head, 160 with two, 172 with four; bf16 278, 283 with two).
 template <int NT, int RS, int HP, bool kFp8>
 struct Shape {

@@ -133,12 +133,13 @@ def test_large_scores_raise_the_maximum_late(ctx, scale, fp8):
 
 
 @pytest.mark.parametrize("fp8", [False, True])
-def test_strided_pool(ctx, fp8):
-    s = Step(8, [700, 33, 128], 6, 3, 32, fp8=fp8)
+@pytest.mark.parametrize("Hkv", [3, 4])
+def test_strided_pool(ctx, fp8, Hkv):
+    s = Step(8, [700, 33, 128], 2 * Hkv, Hkv, 32, fp8=fp8)
     for name in ("k", "v"):
         t = getattr(s.kv, name)
-        big = torch.zeros(t.shape[0], 4, 35, D, dtype=t.dtype, device="cuda")
-        view = big[:, :3, :32].permute(0, 2, 1, 3)
+        big = torch.zeros(t.shape[0], Hkv + 1, 35, D, dtype=t.dtype, device="cuda")
+        view = big[:, :Hkv, :32].permute(0, 2, 1, 3)
         view.copy_(t)
         setattr(s.kv, name, view)
     s.describe()

@@ -42,37 +42,34 @@ using namespace cpattn;
 namespace {
 
 constexpr int kDim = 128;
-constexpr int kGroups = 8;                                 // key groups of a tile
+constexpr int kGroups = 8;                                 // warps of a CTA: key groups of a tile, times heads
+constexpr int kThreads = kGroups * 32;
 constexpr int kSubKeys = 16;                               // keys of a group
 constexpr int kJoinThreads = 256;
 constexpr int kUnitCost = 4;                               // fixed cost of a unit in tiles (see Cursor)
 constexpr float kLag = 8.0f;                               // the running maximum may lag by a factor 2^8
 constexpr float kF16Shift = 7.0f;                          // fp16 weights carry 2^7: at most 2^15 with the lag
 constexpr float kNoKey = -1.5e38f;                         // reference of a row that has seen no key: finite, so that hidden scores (-inf) give weight 0
-// NT: blocks of 8 query rows per warp; RS: warps that share a key group, each with NT * 8 rows of its own (they share the ring slots);
-// HP: KV heads of a unit, so a tile is 128 / HP keys of each.
-// Up to 8 rows: one warp a group; the E4M3 form then fits an SM twice (128 registers a thread, half the ring each).  Up to 16: two warps of
-// 8 rows, whose registers still hold the queries (against one warp of 16: 195 -> 190 us, E4M3 189 -> 179 us for 64 requests at 16 rows).
-// Up to 32: one warp again, which reads the queries' fragments from shared memory for every 16 keys; two warps of 16 rows read them
-// twice and fill the shared-memory pipe (151 us against 174 us, E4M3 132 against 180, for four contexts of 128K keys).
-// E4M3 rows are 128 bytes: two heads together make a token's loads 256 contiguous bytes, as they are in bf16 (the loads of one head alone reach 5.4 TB/s;
-// 128 requests with a window 183 us with one head, 160 with two, 172 with four; bf16 278, 283 with two).
-template <int NT, int RS, int HP, bool kFp8>
+// NT: query rows of a unit and KV head in blocks of 8; HP: KV heads of a unit, so a tile is 128 / HP keys of each.
+// Up to 16 rows the queries' fragments stay in registers; the E4M3 form of up to 8 rows fits an SM twice (128 registers a thread, half
+// the ring each).  With 32 rows the fragments are read from shared memory for every 16 keys.  Two warps per key group that share the
+// rows and the ring slots were slower: 16 rows 190 us either way, E4M3 160 -> 175 us (every code is widened twice), 32 rows 147 -> 174 us.
+// E4M3 rows are 128 bytes: two heads together make a token's loads 256 contiguous bytes, as they are in bf16 (the loads of one head alone
+// reach 5.4 TB/s; 128 requests with a window 183 us with one head, 160 with two, 172 with four; bf16 278, 283 with two).
+template <int NT, int HP, bool kFp8>
 struct Shape {
-    static constexpr int kCtas = kFp8 && NT * RS == 1 ? 2 : 1;
-    static constexpr int kWarps = kGroups * RS, kThreads = kWarps * 32;
+    static constexpr int kCtas = kFp8 && NT == 1 ? 2 : 1;                    // per SM
     static constexpr int kHeadGroups = kGroups / HP;                         // key groups per head
     static constexpr int kTile = kHeadGroups * kSubKeys;                     // keys of a tile
-    static constexpr int kRows = NT * RS * 8;                                // query rows of a unit, per head
+    static constexpr int kRows = NT * 8;                                     // query rows of a unit, per head
     static constexpr int kRowBytes = kFp8 ? 128 : 256;                       // one key's row of one head
-    static constexpr int kHalf = kSubKeys * kRowBytes;                       // the K half of a group's ring slot
+    static constexpr int kHalf = kSubKeys * kRowBytes;                       // the K half of a warp's ring slot
     static constexpr int kRing = 196608 / kCtas;
-    static constexpr int kStages = kRing / (kGroups * 2 * kHalf);            // 3, or 6 in the E4M3 form with one CTA
-    static constexpr int kMl = kGroups * kRows * 8;                          // maximum and sum of every group's rows
+    static constexpr int kStages = kRing / (kGroups * 2 * kHalf);            // 3, or 6 in the E4M3 forms with one CTA
+    static constexpr int kMl = kGroups * kRows * 8;                          // maximum and sum of every warp's rows
     static constexpr int kQ = 2 * HP * kRows * kDim * 2;                     // two units' queries
     static constexpr int kSmem = kRing + kMl + kQ + 512;
-    static constexpr int kPart = 2 * kHalf / RS;                             // a warp's share of a slot, for the merge
-    static constexpr int kPassTiles = std::min(8, kPart / (NT * 4 * 32 * 4));      // 16-dim blocks of O that fit it
+    static constexpr int kPassTiles = std::min(8, 2 * kHalf / (NT * 4 * 32 * 4));      // 16-dim blocks of O that fit a slot
     static_assert(kCtas * (kSmem + 1024) <= 228 * 1024, "shared memory of an SM");
     static_assert(kPassTiles >= 1, "the merge goes through the slots");
 };
@@ -194,25 +191,22 @@ struct Cursor {
 
 __device__ __forceinline__ int64_t run_begin(int64_t total, int64_t cta, int64_t ctas) { return total * cta / ctas; }
 
-// NT, RS, HP: see Shape.  kFp8: E4M3 cache.
-template <int NT, int RS, int HP, bool kFp8>
-__global__ void __launch_bounds__(Shape<NT, RS, HP, kFp8>::kThreads, Shape<NT, RS, HP, kFp8>::kCtas)
+// NT, HP: see Shape.  kFp8: E4M3 cache.
+template <int NT, int HP, bool kFp8>
+__global__ void __launch_bounds__(kThreads, Shape<NT, HP, kFp8>::kCtas)
 decode_kernel(const __grid_constant__ DecodeParams p) {
-    using Sh = Shape<NT, RS, HP, kFp8>;
+    using Sh = Shape<NT, HP, kFp8>;
     constexpr int kHeadGroups = Sh::kHeadGroups, kTile = Sh::kTile;
-    constexpr int kWarps = Sh::kWarps, kThreads = Sh::kThreads;
     constexpr int kRowBytes = Sh::kRowBytes, kHalf = Sh::kHalf, kStages = Sh::kStages, kRows = Sh::kRows, kPassTiles = Sh::kPassTiles;
     constexpr float kShift = kFp8 ? kF16Shift : 0.f;
-    constexpr bool kQRegs = NT == 1;                       // query fragments stay in registers (else they are read from shared memory per tile)
+    constexpr bool kQRegs = NT <= 2;                       // query fragments stay in registers (else they are read from shared memory per tile)
     extern __shared__ __align__(1024) uint8_t smem[];
     float* ml = reinterpret_cast<float*>(smem + Sh::kRing);                                    // [warp][row][2]
     uint8_t* q_buf = smem + Sh::kRing + Sh::kMl;                                               // 2 x [row][256 B], chunks swizzled
     int64_t* scan = reinterpret_cast<int64_t*>(q_buf + Sh::kQ);                                // warp sums, then the run's start
     float* row_inv = reinterpret_cast<float*>(q_buf + Sh::kQ + 256);                           // 1 / sum of a unit's rows
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int group = warp % kGroups, part = warp / kGroups;                                   // group, share of the rows
-    const int sub = group / kHeadGroups, key_group = group % kHeadGroups;                      // the unit's head, the tile's keys
-    const int row_base = part * NT * 8;
+    const int sub = warp / kHeadGroups, key_group = warp % kHeadGroups;                        // the unit's head, the tile's keys
     const int g = lane >> 2, qd = lane & 3;
     const int units = p.Hkv / HP * p.row_groups;
     let_next_launch_begin();                               // the join
@@ -237,7 +231,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     __syncthreads();
     int64_t before = inc - mine, total = 0;
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i) {
+    for (int i = 0; i < kGroups; ++i) {
         if (i < warp) before += scan[i];
         total += scan[i];
     }
@@ -246,7 +240,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     const int64_t ctas = min((int64_t)gridDim.x, total);   // no run is empty
     const int64_t x0 = blockIdx.x < ctas ? run_begin(total, blockIdx.x, ctas) : total;
     const int64_t x1 = blockIdx.x < ctas ? run_begin(total, blockIdx.x + 1, ctas) : total;
-    int32_t* start = reinterpret_cast<int32_t*>(scan + kWarps);
+    int32_t* start = reinterpret_cast<int32_t*>(scan + kGroups);
     if (x0 >= before && x0 < before + mine * units) {
         int b = tid * per;
         int64_t at = before;
@@ -295,7 +289,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         next_page = -1;
         if (visible_group(ld.r, ld_key0)) next_page = __ldg(ld_row + (ld_key0 >> p.page_shift));
     };
-    const uint32_t ring_s = smem_addr(smem) + group * (kStages * 2 * kHalf);
+    const uint32_t ring_s = smem_addr(smem) + warp * (kStages * 2 * kHalf);
     int slot_ld = 0, slot_cur = 0;
     bool more = true;
     enter_unit();
@@ -322,8 +316,8 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 #pragma unroll
                     for (int i = 0; i < kSteps; ++i) {
                         const uint32_t d = dst + ld_off[i % kPeriod] + (i / kPeriod) * 8 * kRowBytes;
-                        if (RS == 1 || part == 0) cp_async16(d, ks);        // two warps: one brings K, the other V
-                        if (RS == 1 || part == 1) cp_async16(d + kHalf, vs);
+                        cp_async16(d, ks);
+                        cp_async16(d + kHalf, vs);
                         ks += step_bytes;
                         vs += step_bytes;
                     }
@@ -333,8 +327,8 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                         const uint32_t d = dst + ld_off[i % kPeriod] + (i / kPeriod) * 8 * kRowBytes;
                         const int key = key0 + i * kKeysPerStep + ld_k;
                         const bool ok = in_pool && key < len && (key >= ld_low || key < p.sinks);
-                        if (RS == 1 || part == 0) cp_async16_or_zeros(d, ok ? ks + i * step_bytes : p.k, ok);
-                        if (RS == 1 || part == 1) cp_async16_or_zeros(d + kHalf, ok ? vs + i * step_bytes : p.v, ok);
+                        cp_async16_or_zeros(d, ok ? ks + i * step_bytes : p.k, ok);
+                        cp_async16_or_zeros(d + kHalf, ok ? vs + i * step_bytes : p.v, ok);
                     }
                 }
             }
@@ -386,7 +380,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         auto c_col = [&](int nt, int c) { return kFp8 ? c_row[nt][c] : p.scale_log2; };
         if (kFp8) {
             // fp16 queries: scaled per row by a power of two that brings the largest element to [2^10, 2^11); in place
-            for (int row = warp; row < HP * kRows; row += kWarps) {
+            for (int row = warp; row < HP * kRows; row += kGroups) {
                 const float k_scale = p.k_scale[h0 + row / kRows];
                 uint8_t* at = const_cast<uint8_t*>(qb) + row * 256;
                 const uint2 x = *reinterpret_cast<const uint2*>(at + (((lane >> 1) ^ (row & 7)) << 4) + (lane & 1) * 8);
@@ -410,30 +404,41 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             const float ks = fabsf(p.k_scale[h0 + sub]) * p.scale_log2;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                c_row[nt][0] = fmaxf(ks * ml[sub * kRows + row_base + nt * 8 + 2 * qd], 1e-35f);
-                c_row[nt][1] = fmaxf(ks * ml[sub * kRows + row_base + nt * 8 + 2 * qd + 1], 1e-35f);
+                c_row[nt][0] = fmaxf(ks * ml[sub * kRows + nt * 8 + 2 * qd], 1e-35f);
+                c_row[nt][1] = fmaxf(ks * ml[sub * kRows + nt * 8 + 2 * qd + 1], 1e-35f);
             }
             __syncthreads();
         }
         // query fragments: one ldmatrix brings (two steps of one row block) or (one step of two row blocks)
-        const uint32_t q_lane = smem_addr(qb) + (sub * kRows + row_base) * 256 + (kQRegs ? (lane & 7) * 256 + (((lane >> 3) ^ (lane & 7)) << 4)
+        const uint32_t q_lane = smem_addr(qb) + sub * kRows * 256 + (NT == 1 ? (lane & 7) * 256 + (((lane >> 3) ^ (lane & 7)) << 4)
                                                         : ((lane & 7) + 8 * (lane >> 4)) * 256 + ((((lane >> 3) & 1) ^ (lane & 7)) << 4));
-        uint32_t qf[kQRegs ? 8 : 1][2];
-        if (kQRegs) {
+        uint32_t qf[kQRegs ? NT : 1][kQRegs ? 8 : 1][2];
+        if (NT == 1) {
 #pragma unroll
             for (int ks = 0; ks < 8; ks += 2) {
                 uint32_t r4[4];
                 ldsm4(r4, q_lane ^ (ks << 5));
-                qf[ks][0] = r4[0];
-                qf[ks][1] = r4[1];
-                qf[ks + 1][0] = r4[2];
-                qf[ks + 1][1] = r4[3];
+                qf[0][ks][0] = r4[0];
+                qf[0][ks][1] = r4[1];
+                qf[0][ks + 1][0] = r4[2];
+                qf[0][ks + 1][1] = r4[3];
+            }
+        } else if (kQRegs) {
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) {
+                uint32_t r4[4];
+                ldsm4(r4, q_lane ^ (ks << 5));
+                qf[0][ks][0] = r4[0];
+                qf[0][ks][1] = r4[1];
+                qf[NT > 1 ? 1 : 0][ks][0] = r4[2];
+                qf[NT > 1 ? 1 : 0][ks][1] = r4[3];
             }
         }
         // S^T += K Q^T of one step of 16 dims
         auto score_step = [&](float (&sc)[NT][4], const uint32_t (&a)[4], int ks) {
             if (kQRegs) {
-                mma16816<kFp8>(sc[0], a, qf[ks][0], qf[ks][1]);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma16816<kFp8>(sc[nt], a, qf[kQRegs ? nt : 0][kQRegs ? ks : 0][0], qf[kQRegs ? nt : 0][kQRegs ? ks : 0][1]);
             } else {
 #pragma unroll
                 for (int nt = 0; nt < NT; nt += 2) {
@@ -450,7 +455,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const int r = r0 + row_base + nt * 8 + 2 * qd + c;
+                const int r = r0 + nt * 8 + 2 * qd + c;
                 lim[nt][c] = r < p.rows ? rq.len - p.n_q + r / p.G + 1 : 0;
             }
         float o[8][NT][4], l[NT][2];
@@ -474,9 +479,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 
         for (int it = 0; it < n_tiles; ++it) {
             cp_wait<kStages - 2>();
-            if (RS == 1) __syncwarp();
-            else asm volatile("bar.sync %0, 64;" ::"r"(1 + group) : "memory");
-            // this tile has landed for every warp of the group, and all of them have read the slot that is filled next
+            __syncwarp();                                  // this tile has landed, and every lane has read the slot that is filled next
             load_tile();
             const int key0 = cur.first_key(key_group);
             ++cur.t;
@@ -595,9 +598,9 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], d);
                 if (g == 0) {
-                    const int row = row_base + nt * 8 + 2 * qd + c;
-                    ml[(group * kRows + row) * 2] = m[nt][c];
-                    ml[(group * kRows + row) * 2 + 1] = l[nt][c];
+                    const int row = nt * 8 + 2 * qd + c;
+                    ml[(warp * kRows + row) * 2] = m[nt][c];
+                    ml[(warp * kRows + row) * 2 + 1] = l[nt][c];
                 }
             }
         if (n_tiles < kStages) cp_wait<0>();               // the next unit's queries have landed before the barrier
@@ -608,7 +611,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const int row = row_base + nt * 8 + 2 * qd + c;
+                const int row = nt * 8 + 2 * qd + c;
                 float mx = kNoKey;
 #pragma unroll
                 for (int w = 0; w < kHeadGroups; ++w) mx = fmaxf(mx, ml[((sub * kHeadGroups + w) * kRows + row) * 2]);
@@ -639,7 +642,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         }
         // through the slots that were read last: they are filled again only after the next unit has begun
         const int slot_free = slot_cur == 0 ? kStages - 1 : slot_cur - 1;
-        float* mine_o = reinterpret_cast<float*>(smem + (group * kStages + slot_free) * (2 * kHalf) + part * Sh::kPart);
+        float* mine_o = reinterpret_cast<float*>(smem + (warp * kStages + slot_free) * (2 * kHalf));
         const float* all_o = reinterpret_cast<const float*>(smem + slot_free * (2 * kHalf));
         constexpr int kPassRegs = kPassTiles * NT * 4, kGroupFloats = kStages * 2 * kHalf / 4;
 #pragma unroll
@@ -653,14 +656,14 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                     for (int j = 0; j < 4; ++j) mine_o[((i * NT + nt) * 4 + j) * 32 + lane] = o[pass * kPassTiles + i][nt][j];
             __syncthreads();
 #pragma unroll
-            for (int x = 0; x < kPassRegs * 32 * RS * HP / kThreads; ++x) {
-                const int all = x * kThreads + tid, who = all / (kPassRegs * 32), hs = who / RS, pt = who % RS;      // whose share: head, rows
-                const int at = all - who * (kPassRegs * 32);                                                       // lane at & 31 of register (at >> 5)
+            for (int x = 0; x < kPassRegs * 32 * HP / kThreads; ++x) {
+                const int all = x * kThreads + tid, hs = all / (kPassRegs * 32);       // head
+                const int at = all - hs * (kPassRegs * 32);                            // lane at & 31 of register (at >> 5)
                 float sum = 0.f;
 #pragma unroll
-                for (int w = 0; w < kHeadGroups; ++w) sum += all_o[(hs * kHeadGroups + w) * kGroupFloats + pt * (Sh::kPart / 4) + at];
+                for (int w = 0; w < kHeadGroups; ++w) sum += all_o[(hs * kHeadGroups + w) * kGroupFloats + at];
                 const int ln = at & 31, reg = at >> 5, j = reg & 3, nt = (reg >> 2) % NT, i = (reg >> 2) / NT;
-                const int gg = ln >> 2, row = pt * NT * 8 + nt * 8 + 2 * (ln & 3) + (j & 1);
+                const int gg = ln >> 2, row = nt * 8 + 2 * (ln & 3) + (j & 1);
                 const int dim = (pass * kPassTiles + i) * 16 + (kFp8 ? 2 * gg + (j >> 1) : gg + 8 * (j >> 1));
                 const int r = r0 + row;
                 if (r < p.rows) {
@@ -759,26 +762,26 @@ size_t decode_workspace(int rows) {
     return (n * (kDim + 2) * sizeof(float) + kMaxDecodeGrid * 16 + 255) / 256 * 256;
 }
 
-template <int NT, int RS, int HP, bool kFp8>
+template <int NT, int HP, bool kFp8>
 int launch_decode(cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char* who) {
-    using Sh = Shape<NT, RS, HP, kFp8>;
+    using Sh = Shape<NT, HP, kFp8>;
     const int grid = std::min(ctx->num_sms, kMaxGrid) * Sh::kCtas;
-    const uint32_t variant = 1u << (8 * (NT == 4 ? 2 : RS - 1) + 2 * HP - (kFp8 ? 1 : 2));      // HP <= 4
+    const uint32_t variant = 1u << (8 * (NT / 2) + 2 * HP - (kFp8 ? 1 : 2));      // NT 1, 2 or 4, HP <= 4
     if (!(ctx->decode_attr_set & variant)) {
-        if (int rc = check_cuda(cudaFuncSetAttribute(decode_kernel<NT, RS, HP, kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem),
+        if (int rc = check_cuda(cudaFuncSetAttribute(decode_kernel<NT, HP, kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem),
                                 "cudaFuncSetAttribute(decode)")) return rc;
         ctx->decode_attr_set |= variant;
     }
-    decode_kernel<NT, RS, HP, kFp8><<<grid, Sh::kThreads, Sh::kSmem, s>>>(p);
+    decode_kernel<NT, HP, kFp8><<<grid, kThreads, Sh::kSmem, s>>>(p);
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
     return launch_behind(decode_join_kernel<kFp8>, dim3((unsigned)grid, (unsigned)(HP * Sh::kRows)), kJoinThreads, s, who, p, HP, (int)Sh::kRows);
 }
 
 template <int HP, bool kFp8>
 int launch_rows(int blocks, cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char* who) {
-    if (blocks == 1) return launch_decode<1, 1, HP, kFp8>(ctx, p, s, who);
-    if (blocks == 2) return launch_decode<1, 2, HP, kFp8>(ctx, p, s, who);
-    return launch_decode<4, 1, HP, kFp8>(ctx, p, s, who);
+    if (blocks == 1) return launch_decode<1, HP, kFp8>(ctx, p, s, who);
+    if (blocks == 2) return launch_decode<2, HP, kFp8>(ctx, p, s, who);
+    return launch_decode<4, HP, kFp8>(ctx, p, s, who);
 }
 
 int decode_attn(cp_ctx* ctx, const void* q, const void* k, const void* v, const float* k_scale, const float* v_scale, int64_t num_pages,

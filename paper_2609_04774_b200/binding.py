@@ -283,7 +283,7 @@ def cp_prefill_attn_kvrange(ctx, q, cache, page_table, prefix_len, new_len, kv_l
         _stream(stream)))
 
 
-def _window_args(ctx, q, cache, page_table, rows, Hq, out, lse, workspace, stream):
+def _window_args(kind, ctx, q, cache, page_table, rows, Hq, out, lse, workspace, stream):
     """The tensors of a windowed call, checked: (q, cache, page_table) and (out, lse, workspace, its bytes, stream)."""
     bf16, i32, f32, _ = _types or _torch_types()
     shape = (rows, Hq, 128)
@@ -292,7 +292,7 @@ def _window_args(ctx, q, cache, page_table, rows, Hq, out, lse, workspace, strea
     qp, op, lp = _arg(ctx, q, "q", bf16, shape), _arg(ctx, out, "out", bf16, shape), _arg(ctx, lse, "lse", f32, (Hq, rows))
     if rows == 0:                                          # an empty chunk: empty tensors have no address, the call reads none
         qp = op = lp = ws
-    return (ctx._h, qp, ctypes.addressof(cache), table), (op, lp, ws, ws_bytes, _raw_stream(ctx, stream))
+    return (ctx._h, qp, _described(cache, kind), table), (op, lp, ws, ws_bytes, _raw_stream(ctx, stream))
 
 
 def _host_i64(a):
@@ -303,18 +303,18 @@ def _host_i64(a):
 def cp_prefill_attn_window(ctx, q, cache, page_table, prefix_len, new_len, C, window, sinks, Hq, scale, out, lse, workspace,
                            stream=None):
     """cp_prefill_attn where a token at position p sees the last `window` keys (its own among them) and the first `sinks`."""
-    head, tail = _window_args(ctx, q, cache, page_table, new_len, Hq, out, lse, workspace, stream)
+    head, tail = _window_args(cp_kv_cache, ctx, q, cache, page_table, new_len, Hq, out, lse, workspace, stream)
     if page_table.numel() * cache.page_size < prefix_len + new_len:
         raise CpArgumentError("page_table has %d entries for %d tokens" % (page_table.numel(), prefix_len + new_len))
     _check(load().cp_prefill_attn_window(*head, prefix_len, new_len, C, window, sinks, Hq, scale, *tail))
 
 
-def _window_batch(call, ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks, Hq, scale, out, lse, workspace,
-                  stream):
+def _window_batch(call, kind, ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks, Hq, scale, out, lse,
+                  workspace, stream):
     B = len(prefix_len)
     if len(cu_new) != B + 1 or len(cu_pages) != B + 1 or len(C) != B:
         raise CpArgumentError("cu_new and cu_pages have %d and %d entries, C %d, for %d requests" % (len(cu_new), len(cu_pages), len(C), B))
-    head, tail = _window_args(ctx, q, cache, page_table, int(cu_new[B]), Hq, out, lse, workspace, stream)
+    head, tail = _window_args(kind, ctx, q, cache, page_table, int(cu_new[B]), Hq, out, lse, workspace, stream)
     if page_table.numel() < cu_pages[B]:
         raise CpArgumentError("page_table has %d entries, cu_pages ends with %d" % (page_table.numel(), cu_pages[B]))
     _check(call(*head, B, _host_i64(cu_new), _host_i64(prefix_len), (ctypes.c_int32 * B)(*C), _host_i64(cu_pages), window, sinks, Hq, scale, *tail))
@@ -323,8 +323,8 @@ def _window_batch(call, ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pag
 def cp_prefill_attn_window_batch(ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks, Hq, scale, out, lse,
                                  workspace, stream=None):
     """B requests in one launch; cu_new, prefix_len, C, cu_pages: host sequences as in cp_prefill_attn_batch."""
-    _window_batch(load().cp_prefill_attn_window_batch, ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks,
-                  Hq, scale, out, lse, workspace, stream)
+    _window_batch(load().cp_prefill_attn_window_batch, cp_kv_cache, ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages,
+                  window, sinks, Hq, scale, out, lse, workspace, stream)
 
 
 def cp_prefill_attn_window_chunk(ctx, q_chunk, cache, page_table, prefix_len, new_len, C, chunk, window, sinks, Hq, scale,
@@ -337,7 +337,7 @@ def cp_prefill_attn_window_chunk(ctx, q_chunk, cache, page_table, prefix_len, ne
             raise CpArgumentError("page_table has %d entries for %d tokens" % (page_table.numel(), end))
     else:
         rows = q_chunk.shape[0]                            # refused by the call
-    head, tail = _window_args(ctx, q_chunk, cache, page_table, rows, Hq, out_chunk, lse_chunk, workspace, stream)
+    head, tail = _window_args(cp_kv_cache, ctx, q_chunk, cache, page_table, rows, Hq, out_chunk, lse_chunk, workspace, stream)
     _check(load().cp_prefill_attn_window_chunk(*head, prefix_len, new_len, C, chunk, window, sinks, Hq, scale, *tail))
 
 
@@ -418,8 +418,8 @@ def cp_prefill_attn_fp8_batch(ctx, q, cache, page_table, cu_new, prefix_len, C, 
 
 def cp_prefill_attn_fp8_window_batch(ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks, Hq, scale, out,
                                      lse, workspace, stream=None):
-    _window_batch(load().cp_prefill_attn_fp8_window_batch, ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages, window, sinks,
-                  Hq, scale, out, lse, workspace, stream)
+    _window_batch(load().cp_prefill_attn_fp8_window_batch, cp_kv_cache_fp8, ctx, q, cache, page_table, cu_new, prefix_len, C, cu_pages,
+                  window, sinks, Hq, scale, out, lse, workspace, stream)
 
 
 def cp_prefill_attn_fp8_shard(ctx, q, cache, page_table, prefix_len, new_len, C, shard, Hq, scale, partial_out, partial_lse,
@@ -498,6 +498,13 @@ def _arg(ctx, t, name, dtype, shape):
                      % (name, dtype, tuple(shape), ctx.device, t.dtype, tuple(t.shape), t.stride(), t.device))
 
 
+def _described(desc, kind):
+    """Address of a descriptor, which must be of the kind that the call reads."""
+    if not isinstance(desc, kind):
+        raise CpArgumentError("the call takes a %s, got a %s" % (kind.__name__, type(desc).__name__))
+    return ctypes.addressof(desc)
+
+
 def _workspace(ctx, t):
     if not t.is_contiguous() or t.get_device() != ctx.device:
         raise CpArgumentError("workspace must be a contiguous tensor on cuda:%d" % ctx.device)
@@ -508,13 +515,13 @@ def cp_workspace_bytes_decode(B, n_q, Hq, Hkv) -> int:
     return int(load().cp_workspace_bytes_decode(B, n_q, Hq, Hkv))
 
 
-def _decode_attn(call, ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream):
+def _decode_attn(call, kind, ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream):
     bf16, i32, f32, _ = _types or _torch_types()
     shape = q.shape
     B, n_q, Hq, _ = shape
     stride = page_table.shape[1]
     ws, ws_bytes = _workspace(ctx, workspace)
-    rc = call(ctx._h, _arg(ctx, q, "q", bf16, (B, n_q, Hq, 128)), ctypes.addressof(cache), _arg(ctx, page_table, "page_table", i32, (B, stride)), stride,
+    rc = call(ctx._h, _arg(ctx, q, "q", bf16, (B, n_q, Hq, 128)), _described(cache, kind), _arg(ctx, page_table, "page_table", i32, (B, stride)), stride,
               _arg(ctx, kv_len, "kv_len", i32, (B,)), B, n_q, Hq, window, sinks, scale, _arg(ctx, out, "out", bf16, shape),
               _arg(ctx, lse, "lse", f32, (Hq, B * n_q)), ws, ws_bytes, _raw_stream(ctx, stream))
     if rc != CP_OK:
@@ -524,12 +531,12 @@ def _decode_attn(call, ctx, q, cache, page_table, kv_len, window, sinks, scale, 
 def cp_decode_attn(ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream=None):
     """The last n_q tokens of B sequences: q, out [B, n_q, Hq, 128] bf16, page_table [B, stride] and kv_len [B] int32 on the device (new
     tokens included), lse [Hq, B * n_q] fp32.  window = CP_NO_WINDOW: every key."""
-    _decode_attn(load().cp_decode_attn, ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream)
+    _decode_attn(load().cp_decode_attn, cp_kv_cache, ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream)
 
 
 def cp_decode_attn_fp8(ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream=None):
     """cp_decode_attn over an FP8 cache."""
-    _decode_attn(load().cp_decode_attn_fp8, ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream)
+    _decode_attn(load().cp_decode_attn_fp8, cp_kv_cache_fp8, ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream)
 
 
 def make_rope(sections, base=10000.0, interleaved=False) -> cp_rope:
@@ -541,7 +548,7 @@ def make_rope(sections, base=10000.0, interleaved=False) -> cp_rope:
     return rope
 
 
-def _rope_append(call, ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream):
+def _rope_append(call, kind, ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream):
     bf16, i32, _, _ = _types or _torch_types()
     n = token_seq.shape[0]
     qp = qo = kp = vp = sp = tp = None
@@ -558,8 +565,8 @@ def _rope_append(call, ctx, rope, q, k_rows, v_rows, positions, token_seq, token
         rows, stride = page_table.shape
         kp, vp = _arg(ctx, k_rows, "k_rows", bf16, shape), _arg(ctx, v_rows, "v_rows", bf16, shape)
         sp, tp = _arg(ctx, token_slot, "token_slot", i32, (n,)), _arg(ctx, page_table, "page_table", i32, (rows, stride))
-    rc = call(ctx._h, ctypes.addressof(rope), qp, kp, vp, n, Hq, _arg(ctx, positions, "positions", i32, (rope.n_axes, n)),
-              _arg(ctx, token_seq, "token_seq", i32, (n,)), sp, ctypes.addressof(cache), tp, rows, stride, qo, _raw_stream(ctx, stream))
+    rc = call(ctx._h, _described(rope, cp_rope), qp, kp, vp, n, Hq, _arg(ctx, positions, "positions", i32, (rope.n_axes, n)),
+              _arg(ctx, token_seq, "token_seq", i32, (n,)), sp, _described(cache, kind), tp, rows, stride, qo, _raw_stream(ctx, stream))
     if rc != CP_OK:
         _check(rc)
 
@@ -567,12 +574,12 @@ def _rope_append(call, ctx, rope, q, k_rows, v_rows, positions, token_seq, token
 def cp_rope_append(ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream=None):
     """q [n, Hq, 128] -> q_out (may be q); k_rows, v_rows [n, Hkv, 128] -> slot token_slot[i] of sequence token_seq[i] of the paged cache;
     positions [n_axes, n], token_seq, token_slot [n], page_table [rows, stride], all int32.  token_seq < 0: padding."""
-    _rope_append(load().cp_rope_append, ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream)
+    _rope_append(load().cp_rope_append, cp_kv_cache, ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream)
 
 
 def cp_rope_append_fp8(ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream=None):
     """cp_rope_append into an FP8 cache: k (rotated) and v as e4m3(x / scale[head])."""
-    _rope_append(load().cp_rope_append_fp8, ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream)
+    _rope_append(load().cp_rope_append_fp8, cp_kv_cache_fp8, ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream)
 
 
 def make_page_pool(k, v, num_pages=None) -> cp_page_pool:
@@ -602,7 +609,7 @@ def cp_workspace_bytes_pages(num_pages, n=0) -> int:
 def _table_args(ctx, pool, refcount, page_table):
     i32 = (_types or _torch_types())[1]
     rows, stride = page_table.shape
-    return (ctx._h, ctypes.addressof(pool), _arg(ctx, refcount, "refcount", i32, (pool.num_pages,)),
+    return (ctx._h, _described(pool, cp_page_pool), _arg(ctx, refcount, "refcount", i32, (pool.num_pages,)),
             _arg(ctx, page_table, "page_table", i32, (rows, stride)), rows, stride)
 
 
@@ -650,5 +657,5 @@ def cp_pages_copy(ctx, pool, src, dst, workspace, stream=None):
     if _types is None:
         _torch_types()
     n = src.numel()
-    _check(load().cp_pages_copy(ctx._h, ctypes.addressof(pool), _ints(ctx, src, "src", n), _ints(ctx, dst, "dst", n), n, *_workspace(ctx, workspace),
+    _check(load().cp_pages_copy(ctx._h, _described(pool, cp_page_pool), _ints(ctx, src, "src", n), _ints(ctx, dst, "dst", n), n, *_workspace(ctx, workspace),
                                 _raw_stream(ctx, stream)))

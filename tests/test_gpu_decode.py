@@ -319,6 +319,8 @@ def test_empty_batch_and_binding_refusals(ctx):
         a = good | kw
         with pytest.raises(ValueError):
             binding.cp_decode_attn(ctx, a["q"], s.cache, a["page_table"], a["kv_len"], FULL, 0, SCALE, a["out"], a["lse"], s.g_ws.tensor)
+    with pytest.raises(ValueError):
+        binding.cp_decode_attn_fp8(ctx, s.q, s.cache, s.kv.table, s.kv_len, FULL, 0, SCALE, s.g_out.tensor, s.g_lse.tensor, s.g_ws.tensor)
     with pytest.raises(binding.CpError) as e:
         s.call(ctx, ws=s.g_ws.tensor[:1024])
     assert e.value.code == binding.CP_ERR_WORKSPACE

@@ -431,7 +431,7 @@ int cp_rope_init(cp_rope* rope, int32_t n_axes, const int32_t* sections, double 
 
 /* cp_rope_append -- rotates q into q_out, and k into the paged cache, where v goes as it is (in one launch).
  *   cache      always described, also for queries alone
- *   q, q_out   device [n, Hq, D] bf16; q_out may be q; both NULL: no queries
+ *   q, q_out   device [n, Hq, D] bf16; q_out may be q, and overlaps nothing else; both NULL: no queries
  *   k_rows, v_rows  device [n, Hkv, D] bf16; both NULL: queries only
  *   positions  device [n_axes, n] int32 (any value)
  *   token_seq  device [n] int32: the token's row of the page table; < 0: padding, nothing of the row is read or written
@@ -453,12 +453,13 @@ int cp_rope_append_fp8(cp_ctx* ctx, const cp_rope* rope, const void* q, const vo
  * cache already.
  *   q        device [B, n_q, Hq, D] bf16: row (b, t) is the token at position kv_len[b] - n_q + t
  *   page_table  device [B, table_stride] int32; kv_len  device [B] int32, the new tokens included
- *   out      device [B, n_q, Hq, D] bf16;  lse  device [Hq, B * n_q] fp32 (the layout cp_merge takes)
+ *   out      device [B, n_q, Hq, D] bf16, may be q;  lse  device [Hq, B * n_q] fp32 (the layout cp_merge takes)
  * A row before position 0 (kv_len[b] < n_q; kv_len[b] = 0 for an idle row) sees nothing: zeros, lse = -inf.  Only slots that some row
- * sees are read; an entry outside the pool reads as zeros.  kv_len[b] < 0 counts as 0, one beyond the table row as the row's
- * capacity; both are reported as CP_ERR_BOUNDS {code, b, block, kv_len} by cp_ctx_poll_status.  Weights are rounded to bf16 for P V (_fp8:
- * to fp16), all sums are fp32.  Two launches, whose grids do not depend on the lengths: a captured call is replayed with other
- * lengths and tables.  workspace: cp_workspace_bytes_decode (0 on invalid arguments), for one call at a time.
+ * sees are read, and what they hold, infinities and NaN too, reaches no other row; an entry outside the pool reads as zeros.
+ * kv_len[b] < 0 counts as 0, one beyond the table row as the row's capacity; both are reported as CP_ERR_BOUNDS {code, b, block,
+ * kv_len} by cp_ctx_poll_status.  Weights are rounded to bf16 for P V (_fp8: to fp16), all sums are fp32.  Two launches, whose grids
+ * do not depend on the lengths: a captured call is replayed with other lengths and tables.  workspace:
+ * cp_workspace_bytes_decode (0 on invalid arguments), for one call at a time.
  * Limits: n_q <= 64, n_q * Hq / Hkv <= 1024, B <= 65536.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA. */
 size_t cp_workspace_bytes_decode(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv);
 int cp_decode_attn(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table, int64_t table_stride,

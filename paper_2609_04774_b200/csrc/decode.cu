@@ -110,6 +110,14 @@ __device__ __forceinline__ void cp_async16_or_zeros(uint32_t dst, const void* sr
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+    uint4 r;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(addr) : "memory");
+    return r;
+}
+__device__ __forceinline__ void sts128(uint32_t addr, const uint4& r) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w) : "memory");
+}
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -151,6 +159,17 @@ __device__ __forceinline__ uint32_t pack_weights(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// The sign bits of the elements of a word that are infinite or NaN: those whose exponent (E4M3: exponent and mantissa) is all ones carry.
+template <bool kFp8>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    return kFp8 ? ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+}
+template <bool kFp8>
+__device__ __forceinline__ uint32_t finite_part(uint32_t w) {
+    const uint32_t top = not_finite<kFp8>(w);
+    return w & ~(top | (top - (top >> (kFp8 ? 7 : 15))));
+}
+
 // ---------------------------------------------------------------------------------------------- work list
 // Tiles of one unit of a request: those that some of its rows see, at least one (an empty request still writes its rows).
 struct Request {
@@ -189,10 +208,34 @@ struct Cursor {
     }
 };
 
+// The infinities and NaN of V, at one dim, among the listed keys (late: from the first token's limit on, early: from its window's first
+// key on) that token t of request b sees.  Only those are nonzero: 0 + inf, whatever the weight.
+template <bool kFp8>
+__device__ __forceinline__ float odd_values(const DecodeParams& p, const unsigned long long* keys, int b, int len, int h, int t, int dim) {
+    const int lim_min = len - p.n_q + 1, lim = lim_min + t;
+    float sum = 0.f;
+#pragma unroll 1
+    for (int early = 0; early < 2; ++early) {
+#pragma unroll 1
+        for (unsigned long long todo = keys[early]; todo != 0; todo &= todo - 1) {
+            const int key = lim_min - (early ? p.window : 0) + __ffsll(todo) - 1;
+            if (key >= lim || (key < lim - p.window && key >= p.sinks)) continue;
+            const int64_t page = p.table[b * p.table_stride + (key >> p.page_shift)];      // of the pool: it was read
+            const uint8_t* v = p.v + page * p.stride_page + (key & ((1 << p.page_shift) - 1)) * p.stride_tok + h * p.stride_head;
+            const uint32_t x = kFp8 ? v[dim] : reinterpret_cast<const uint16_t*>(v)[dim];
+            if (not_finite<kFp8>(x)) sum += kFp8 ? NAN : __uint_as_float(x << 16);
+        }
+    }
+    return sum;
+}
+
 __device__ __forceinline__ int64_t run_begin(int64_t total, int64_t cta, int64_t ctas) { return total * cta / ctas; }
 
-// NT, HP: see Shape.  kFp8: E4M3 cache.
-template <int NT, int HP, bool kFp8>
+// NT, HP: see Shape.  kFp8: E4M3 cache.  kDrafts: n_q > 1, so the rows of a unit differ in the keys they see; only then is V looked at for
+// infinities and NaN, in the groups that some row does not see in full (two of a unit as a rule).  These have a loop of their own: with the
+// check inside the common one every group got slower (four contexts of 128K keys, E4M3, 32 rows: 157 us; 144 without the check, 141 like this;
+// short requests of two tokens: 109 us without, 117 like this).
+template <int NT, int HP, bool kFp8, bool kDrafts>
 __global__ void __launch_bounds__(kThreads, Shape<NT, HP, kFp8>::kCtas)
 decode_kernel(const __grid_constant__ DecodeParams p) {
     using Sh = Shape<NT, HP, kFp8>;
@@ -205,6 +248,8 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
     uint8_t* q_buf = smem + Sh::kRing + Sh::kMl;                                               // 2 x [row][256 B], chunks swizzled
     int64_t* scan = reinterpret_cast<int64_t*>(q_buf + Sh::kQ);                                // warp sums, then the run's start
     float* row_inv = reinterpret_cast<float*>(q_buf + Sh::kQ + 256);                           // 1 / sum of a unit's rows
+    // [q_cur][head][2]: keys from the first row's limit on, from its window's first key on, whose V holds infinities or NaN (n_q <= 64)
+    unsigned long long* odd_keys = reinterpret_cast<unsigned long long*>(q_buf + Sh::kQ + 128);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int sub = warp / kHeadGroups, key_group = warp % kHeadGroups;                        // the unit's head, the tile's keys
     const int g = lane >> 2, qd = lane & 3;
@@ -228,6 +273,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         if (lane >= o) inc += y;
     }
     if (lane == 31) scan[warp] = inc;
+    if (kDrafts && tid < 4 * HP) odd_keys[tid] = 0;
     __syncthreads();
     int64_t before = inc - mine, total = 0;
 #pragma unroll
@@ -348,7 +394,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         for (int i = tid; i < HP * kRows * 16; i += kThreads) {
             const int at = i >> 4, c = i & 15, hs = at / kRows, r = r0 + at - hs * kRows;      // a row of head hb * HP + hs
             const bool ok = r < p.rows;
-            const int t = ok ? r / p.G : 0;
+            const int t = kDrafts && ok ? r / p.G : 0;
             const int64_t o = ok ? (((int64_t)b * p.n_q + t) * p.Hq + (hb * HP + hs) * p.G + (r - t * p.G)) * kDim + c * 8 : 0;
             cp_async16_or_zeros(smem_addr(q_buf + buf * (HP * kRows * 256) + at * 256 + ((c ^ (at & 7)) << 4)), p.q + o, ok);
         }
@@ -456,7 +502,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const int r = r0 + nt * 8 + 2 * qd + c;
-                lim[nt][c] = r < p.rows ? rq.len - p.n_q + r / p.G + 1 : 0;
+                lim[nt][c] = r < p.rows ? rq.len - p.n_q + (kDrafts ? r / p.G : 0) + 1 : 0;
             }
         float o[8][NT][4], l[NT][2];
         float m[NT][2];                                    // reference of the weights, p = 2^(c s - m): the running maximum, less kShift
@@ -477,15 +523,37 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
         const uint32_t k_lane = (mr + 8 * (mi & 1)) * kRowBytes + (((mi >> 1) ^ mr) << 4);
         const uint32_t v_lane = kFp8 ? k_lane : (mr + 8 * (mi >> 1)) * kRowBytes + (((mi & 1) ^ mr) << 4);
 
-        for (int it = 0; it < n_tiles; ++it) {
-            cp_wait<kStages - 2>();
-            __syncwarp();                                  // this tile has landed, and every lane has read the slot that is filled next
-            load_tile();
-            const int key0 = cur.first_key(key_group);
-            ++cur.t;
-            const uint32_t kt = ring_s + slot_cur * (2 * kHalf) + k_lane, vt = ring_s + slot_cur * (2 * kHalf) + kHalf + v_lane;
-            slot_cur = slot_cur + 1 == kStages ? 0 : slot_cur + 1;
-            if (!visible_group(rq, key0)) continue;
+        int key0 = 0;                                      // the current tile: this warp's first key, its slot
+        uint32_t kt = 0, vt = 0;
+        bool full = false;                                 // every row sees all its keys
+        // this warp's 16 keys of the current tile; masked: some row does not see some of them
+        auto take = [&](bool masked) __attribute__((always_inline)) {
+            // A key that only some of the rows see (draft tokens among themselves, the edge of their windows) may hold a V that is no finite
+            // number, and a zero weight times that would reach the rows that do not see it: such elements are cleared here, and put into
+            // the rows that do see them when the unit's result is written.
+            if (kDrafts && masked) {
+                // two lanes a key, each half a row, from another chunk on in every lane (banks)
+                const uint32_t half_row = vt - v_lane + lane * (kRowBytes / 2) + ((kFp8 ? lane >> 1 & 3 : lane & 7) << 4);
+                uint32_t odd = 0;
+#pragma unroll
+                for (int i = 0; i < kRowBytes / 2; i += 16) {
+                    const uint4 w = lds128(half_row ^ i);
+                    odd |= not_finite<kFp8>(w.x) | not_finite<kFp8>(w.y) | not_finite<kFp8>(w.z) | not_finite<kFp8>(w.w);
+                }
+                if (__any_sync(0xffffffffu, odd != 0)) {
+                    const int key = key0 + (lane >> 1);
+                    const bool late = key >= lim_min, early = key >= lim_min - p.window && key < low_max && key >= p.sinks;
+                    if (odd != 0 && (late || early)) {
+#pragma unroll 1
+                        for (int i = 0; i < kRowBytes / 2; i += 16) {
+                            const uint4 w = lds128(half_row ^ i);
+                            sts128(half_row ^ i, make_uint4(finite_part<kFp8>(w.x), finite_part<kFp8>(w.y), finite_part<kFp8>(w.z), finite_part<kFp8>(w.w)));
+                        }
+                        atomicOr(&odd_keys[(q_cur * HP + sub) * 2 + (late ? 0 : 1)], 1ull << (key - lim_min + (late ? 0 : p.window)));
+                    }
+                    __syncwarp();
+                }
+            }
             float s[NT][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -513,8 +581,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 }
             }
             // s[nt][j]: key g + 8 (j >> 1), row 2 qd + (j & 1); scores and maxima stay unscaled, c joins in the exponent
-            const bool full = key0 + kSubKeys <= lim_min && (key0 >= low_max || key0 + kSubKeys <= p.sinks);
-            if (!full) {
+            if (masked) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -588,6 +655,39 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                     for (int nt = 0; nt < NT; ++nt) mma16816<false>(o[i][nt], a, pb[nt][0], pb[nt][1]);
                 }
             }
+        };
+        // on to the next tile; false: no row sees its keys
+        auto next_tile = [&]() {
+            cp_wait<kStages - 2>();
+            __syncwarp();                                  // this tile has landed, and every lane has read the slot that is filled next
+            load_tile();
+            key0 = cur.first_key(key_group);
+            ++cur.t;
+            kt = ring_s + slot_cur * (2 * kHalf) + k_lane;
+            vt = ring_s + slot_cur * (2 * kHalf) + kHalf + v_lane;
+            slot_cur = slot_cur + 1 == kStages ? 0 : slot_cur + 1;
+            full = key0 + kSubKeys <= lim_min && (key0 >= low_max || key0 + kSubKeys <= p.sinks);
+            return visible_group(rq, key0);
+        };
+        int it = 0;
+        if (kDrafts) {
+            while (true) {
+                bool part = false;
+                while (it < n_tiles) {
+                    ++it;
+                    if (!next_tile()) continue;
+                    if (!full) {
+                        part = true;
+                        break;
+                    }
+                    take(false);
+                }
+                if (!part) break;
+                take(true);
+            }
+        } else {
+            for (; it < n_tiles; ++it)
+                if (next_tile()) take(!full);
         }
 
         // -------------------------------------------------------------- the warps' partial results become one
@@ -605,6 +705,10 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             }
         if (n_tiles < kStages) cp_wait<0>();               // the next unit's queries have landed before the barrier
         __syncthreads();
+        unsigned long long any_odd = 0;
+        if (kDrafts)
+            for (int i = 0; i < 2 * HP; ++i) any_odd |= odd_keys[q_cur * HP * 2 + i];
+        if (kDrafts && tid < 2 * HP) odd_keys[(q_cur ^ 1) * HP * 2 + tid] = 0;      // for the next unit
         const bool whole = t_begin == 0 && n_tiles == rq.n;
         const int slot = 2 * blockIdx.x + (t_begin > 0 ? 0 : 1);
 #pragma unroll
@@ -631,7 +735,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
 #pragma unroll
             for (int w = 0; w < kHeadGroups; ++w) sum += mine_ml[w * kRows * 2 + 1] * exp2_fast(mine_ml[w * kRows * 2] - mx);
             row_inv[tid] = sum > 0.f ? (kFp8 ? p.v_scale[h] : 1.f) / sum : 0.f;      // read behind the barrier below
-            const int r = r0 + row, t = r / p.G;
+            const int r = r0 + row, t = kDrafts ? r / p.G : 0;
             if (whole) {
                 p.lse[(int64_t)(h * p.G + r - t * p.G) * ((int64_t)p.B * p.n_q) + (int64_t)b * p.n_q + t] =
                     sum > 0.f ? (mx + log2f(sum)) * 0.6931471805599453f : -INFINITY;
@@ -667,12 +771,28 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 const int dim = (pass * kPassTiles + i) * 16 + (kFp8 ? 2 * gg + (j >> 1) : gg + 8 * (j >> 1));
                 const int r = r0 + row;
                 if (r < p.rows) {
+                    const int t = kDrafts ? r / p.G : 0;
                     if (whole) {
-                        const int t = r / p.G;
                         p.out[(((int64_t)b * p.n_q + t) * p.Hq + (h0 + hs) * p.G + r - t * p.G) * kDim + dim] = __float2bfloat16_rn(sum * row_inv[hs * kRows + row]);
                     } else {
                         p.part_o[((int64_t)slot * (HP * kRows) + hs * kRows + row) * kDim + dim] = sum;
                     }
+                }
+            }
+        }
+        if (kDrafts && any_odd != 0) {                     // what was cleared joins the rows just written
+            __syncthreads();
+#pragma unroll 1
+            for (int i = tid; i < HP * kRows * kDim; i += kThreads) {
+                const int at = i / kDim, dim = i % kDim, hs = at / kRows, r = r0 + at % kRows, t = r / p.G;
+                if (r >= p.rows) continue;
+                const float x = odd_values<kFp8>(p, odd_keys + (q_cur * HP + hs) * 2, b, rq.len, h0 + hs, t, dim);
+                if (x == 0.f) continue;
+                if (whole) {
+                    __nv_bfloat16* o = p.out + (((int64_t)b * p.n_q + t) * p.Hq + (h0 + hs) * p.G + r - t * p.G) * kDim + dim;
+                    *o = __float2bfloat16_rn(__bfloat162float(*o) + x);
+                } else {
+                    p.part_o[((int64_t)slot * (HP * kRows) + at) * kDim + dim] += x;
                 }
             }
         }
@@ -762,26 +882,26 @@ size_t decode_workspace(int rows) {
     return (n * (kDim + 2) * sizeof(float) + kMaxDecodeGrid * 16 + 255) / 256 * 256;
 }
 
-template <int NT, int HP, bool kFp8>
+template <int NT, int HP, bool kFp8, bool kDrafts>
 int launch_decode(cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char* who) {
     using Sh = Shape<NT, HP, kFp8>;
     const int grid = std::min(ctx->num_sms, kMaxGrid) * Sh::kCtas;
-    const uint32_t variant = 1u << (8 * (NT / 2) + 2 * HP - (kFp8 ? 1 : 2));      // NT 1, 2 or 4, HP <= 4
+    const uint32_t variant = 1u << (8 * (NT / 2) + 4 * (HP - 1) + (kFp8 ? 2 : 0) + (kDrafts ? 1 : 0));      // NT 1, 2 or 4; HP 1 or 2
     if (!(ctx->decode_attr_set & variant)) {
-        if (int rc = check_cuda(cudaFuncSetAttribute(decode_kernel<NT, HP, kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem),
+        if (int rc = check_cuda(cudaFuncSetAttribute(decode_kernel<NT, HP, kFp8, kDrafts>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem),
                                 "cudaFuncSetAttribute(decode)")) return rc;
         ctx->decode_attr_set |= variant;
     }
-    decode_kernel<NT, HP, kFp8><<<grid, kThreads, Sh::kSmem, s>>>(p);
+    decode_kernel<NT, HP, kFp8, kDrafts><<<grid, kThreads, Sh::kSmem, s>>>(p);
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
     return launch_behind(decode_join_kernel<kFp8>, dim3((unsigned)grid, (unsigned)(HP * Sh::kRows)), kJoinThreads, s, who, p, HP, (int)Sh::kRows);
 }
 
-template <int HP, bool kFp8>
+template <int HP, bool kFp8, bool kDrafts>
 int launch_rows(int blocks, cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char* who) {
-    if (blocks == 1) return launch_decode<1, HP, kFp8>(ctx, p, s, who);
-    if (blocks == 2) return launch_decode<2, HP, kFp8>(ctx, p, s, who);
-    return launch_decode<4, HP, kFp8>(ctx, p, s, who);
+    if (blocks == 1) return launch_decode<1, HP, kFp8, kDrafts>(ctx, p, s, who);
+    if (blocks == 2) return launch_decode<2, HP, kFp8, kDrafts>(ctx, p, s, who);
+    return launch_decode<4, HP, kFp8, kDrafts>(ctx, p, s, who);
 }
 
 int decode_attn(cp_ctx* ctx, const void* q, const void* k, const void* v, const float* k_scale, const float* v_scale, int64_t num_pages,
@@ -847,11 +967,9 @@ int decode_attn(cp_ctx* ctx, const void* q, const void* k, const void* v, const 
     p.meta = reinterpret_cast<int32_t*>(p.part_ml + n * 2);
     p.status = ctx->d_status;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (fp8) {
-        if (Hkv % 2 == 0) return launch_rows<2, true>(nt, ctx, p, s, who);
-        return launch_rows<1, true>(nt, ctx, p, s, who);
-    }
-    return launch_rows<1, false>(nt, ctx, p, s, who);
+    if (fp8 && Hkv % 2 == 0) return n_q > 1 ? launch_rows<2, true, true>(nt, ctx, p, s, who) : launch_rows<2, true, false>(nt, ctx, p, s, who);
+    if (fp8) return n_q > 1 ? launch_rows<1, true, true>(nt, ctx, p, s, who) : launch_rows<1, true, false>(nt, ctx, p, s, who);
+    return n_q > 1 ? launch_rows<1, false, true>(nt, ctx, p, s, who) : launch_rows<1, false, false>(nt, ctx, p, s, who);
 }
 
 }  // namespace

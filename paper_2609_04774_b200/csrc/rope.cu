@@ -10,7 +10,10 @@
 // HBM-bound: q is read and written once, k and v are read once and written once (24 KB per token at 32 / 8 heads).  A warp takes
 // the heads of one token in steps of four (8 lanes a head, two 16-byte vectors a lane), so the 64 sines and cosines of a token
 // are computed once (two pairs a lane, handed round by shuffles) for all its heads.  With few tokens the steps of a
-// token are dealt to several warps instead (the sines are then computed by each): see launch_rope.
+// token are dealt to several warps instead (the sines are then computed by each): see rope_append.
+// Measured (device time): 16384 tokens, three axes, 74 us, 5.4 TB/s (E4M3 75 us), 65536 tokens 6.2 TB/s of the 6.45 that a copy reaches: at
+// 16384 the last of 3.5 waves of warps costs the rest.  Steps cut into equal runs, one wave of warps: 72 us, but 1024 tokens 8.3 -> 10.1 us.
+// 64 tokens: 3.4 us, one launch.
 #include <cuda_bf16.h>
 #include <math.h>
 

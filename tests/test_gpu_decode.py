@@ -324,3 +324,74 @@ def test_empty_batch_and_binding_refusals(ctx):
     with pytest.raises(binding.CpError) as e:
         s.call(ctx, ws=s.g_ws.tensor[:1024])
     assert e.value.code == binding.CP_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("fp8,Hkv", [(False, 2), (True, 2), (True, 1)])
+@pytest.mark.parametrize("G,n_q", [(1, 2), (4, 3), (8, 4), (8, 9)])
+def test_values_that_are_no_numbers_stay_out_of_rows_that_do_not_see_them(ctx, fp8, Hkv, G, n_q):
+    """Draft tokens whose V is infinite or NaN, and one at the edge of the windows: rows that do not see the key keep their bits, the others
+    have the odd element and, in the others, what the formula gives."""
+    window, lens = 200, [413, 40, 16, n_q]
+    s = Step(28, lens, G * Hkv, Hkv, 16, n_q=n_q, fp8=fp8)
+    bad = {}                                               # (request, key) -> dim
+    for b, n in enumerate(lens):
+        for i in range(1, n_q):
+            bad[b, n - i] = (37 * i + 11 * b) % D
+        if n > window + n_q:
+            bad[b, n - n_q + 1 - window] = 126             # in the first row's window only
+    def put(value):
+        for i, ((b, t), dim) in enumerate(bad.items()):
+            page, slot = s.kv.where(b, torch.tensor(t, device="cuda"))
+            s.kv.v[page, slot, i % Hkv, dim] = value(i)
+    put(lambda i: 0)
+    clean, clean_lse = (x.clone() for x in s.run(ctx, window))
+    s.compare(window)
+    put(lambda i: (0x7F, 0xFF)[i % 2] if fp8 else (float("inf"), float("nan"), -float("inf"))[i % 3])
+    out, lse = (x.clone() for x in s.run(ctx, window))
+    assert torch.equal(lse, clean_lse)
+    odd = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+    sees = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+    for i, ((b, t), dim) in enumerate(bad.items()):
+        p = lens[b] - n_q + torch.arange(n_q, device="cuda")
+        rows = (t <= p) & (p - t < window)
+        heads = slice(i % Hkv * G, (i % Hkv + 1) * G)
+        odd[b, rows, heads, dim] = True
+        sees[b, rows, heads] = True
+    assert bool((~torch.isfinite(out) == odd).all())
+    assert torch.equal(out[~sees], clean[~sees])
+    s.g_out.tensor.copy_(torch.where(odd, clean, out))     # the finite elements, against the formula
+    put(lambda i: 0)
+    s.compare(window)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_keys_that_are_no_numbers_stay_out_of_rows_that_do_not_see_them(ctx, fp8):
+    window, lens, n_q = 200, [413, 40, 3], 3
+    s = Step(29, lens, 8, 2, 16, n_q=n_q, fp8=fp8)
+    clean, clean_lse = (x.clone() for x in s.run(ctx, window))
+    sees = torch.zeros(clean.shape, dtype=torch.bool, device="cuda")
+    for b, n in enumerate(lens):
+        for t in [n - 1] + ([n - n_q + 1 - window] if n > 300 else []):
+            page, slot = s.kv.where(b, torch.tensor(t, device="cuda"))
+            s.kv.k[page, slot, 1, 5] = 0x7F if fp8 else float("nan")
+            p = n - n_q + torch.arange(n_q, device="cuda")
+            sees[b, (t <= p) & (p - t < window), 4:] = True
+    out, lse = s.run(ctx, window)
+    assert bool((torch.isnan(out) == sees).all())
+    rows = sees[..., 0].permute(2, 0, 1).reshape(8, -1)
+    assert torch.equal(out[~sees], clean[~sees]) and torch.equal(lse[~rows], clean_lse[~rows])
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("n_q", [1, 5])
+def test_output_over_the_queries(ctx, fp8, n_q):
+    s = Step(30, [9000, 300, 2222, 0] + [200] * 60, 16, 2, 32, n_q=n_q, fp8=fp8)
+    out, lse = (x.clone() for x in s.run(ctx))
+    keep = s.q.clone()
+    for _ in range(3):
+        s.q.copy_(keep)
+        f = binding.cp_decode_attn_fp8 if fp8 else binding.cp_decode_attn
+        f(ctx, s.q, s.cache, s.kv.table, s.kv_len, FULL, 0, SCALE, s.q, s.g_lse.tensor, s.g_ws.tensor)
+        torch.cuda.synchronize()
+        assert torch.equal(s.q, out) and torch.equal(s.g_lse.tensor, lse)
+    ctx.poll_status()

@@ -231,7 +231,8 @@ int cp_prefill_attn_kvrange(cp_ctx* ctx, const void* q, const cp_kv_cache* cache
  * the longest request) is full causal attention.  Arguments, layouts, workspace, schedule and errors as in the calls
  * without _window; KV tiles that no row of a query tile sees are neither read nor computed, so the work grows with
  * new_len * window.  Page-table entries behind the sinks and the window (of the first query of a request) are never used
- * as an address of anything that reaches a result: they may be -1 (cp_pages_evict).  _chunk is the zigzag chunk of one CP
+ * as an address of anything that reaches a result: they may be -1 (cp_pages_evict).  K and V of the mapped slots must be finite, as
+ * in those calls: a hidden key of a tile that is read meets a zero weight.  _chunk is the zigzag chunk of one CP
  * rank.  The FP8 form has the accuracy of cp_prefill_attn_fp8.
  * Errors: INVALID_ARG (also window < 1, sinks < 0), UNSUPPORTED, WORKSPACE, CUDA, BOUNDS.
  * ------------------------------------------------------------------------------------------- */

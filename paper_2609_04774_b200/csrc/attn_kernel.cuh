@@ -802,10 +802,10 @@ __device__ __forceinline__ void softmax_tile(float (&c0)[32], float (&c1)[32], f
         tc_fence_after();
         const bool grow = (m_new - m) > (kFp8 ? kRescaleThreshold8 : kRescaleThreshold);
         if (__any_sync(0xffffffffu, grow)) {
-            const float m_upd = grow ? m_new : m;
-            const float alpha = ex2(m - m_upd);
+            // a row that has seen no key yet stays at m = -inf while others of its warp grow: m - m would be NaN there
+            const float alpha = grow ? ex2(m - m_new) : 1.f;
             l *= alpha;
-            m = m_upd;
+            if (grow) m = m_new;
 #pragma unroll 1
             for (int cc = 0; cc < 4; ++cc) {
                 float o[32];
@@ -818,7 +818,7 @@ __device__ __forceinline__ void softmax_tile(float (&c0)[32], float (&c1)[32], f
         }
     }
     const float2 c2f = make_float2(c, c);
-    // a row that has seen no key yet (only possible in masked tiles of a KV-split piece) keeps m = -inf;
+    // a row that has seen no key yet keeps m = -inf (masked tiles only: of a KV-split piece, or left of a row's window);
     // subtracting 0 instead keeps its weights at exactly 0 rather than NaN
     const float m_sub = ((kMasked && m == -INFINITY) ? 0.f : m) - (kFp8 ? kP8Shift : 0.f);
     const float2 nm2 = make_float2(-m_sub, -m_sub);

@@ -477,8 +477,12 @@ int cp_decode_attn_fp8(cp_ctx* ctx, const void* q, const cp_kv_cache_fp8* cache,
  * in order.  cp_workspace_bytes_pages: workspace of the calls that take one, for n forks or copies (0 elsewhere); a workspace
  * belongs to one call at a time.  What cannot be done is skipped and reported as CP_ERR_BOUNDS by cp_ctx_poll_status.
  *   extend   room for new_tokens[r] >= 0 more tokens in every row r (0: none wanted): new table entries, refcount 1, kv_len[r] +=
- *            new_tokens[r].  A row that does not get all its pages (pool or row full) gets none and keeps its length; rows
- *            behind it that need pages get none either.  {code, row, block, -1 or the tokens wanted}
+ *            new_tokens[r].  A row whose table is full keeps its length.  A row that does not get all its pages (pool
+ *            exhausted) gets none and keeps its length, and rows behind it that need pages get none either.  {code, row, block, -1 or
+ *            the tokens wanted}.  The caller may lower kv_len[r] (rejected draft tokens), but not into a page that the row shares
+ *            (not below the full pages that a fork of it shares): the pages behind the new end stay the row's and are
+ *            used again by the next extend.  Where one of these is shared, its reference is given up and a fresh page takes
+ *            its place; an entry there that names no used page counts as -1
  *   evict    the next token of a row sits at position kv_len[r]: entries of pages that are wholly behind its window and
  *            behind the sinks become -1 and give up their reference (CP_NO_WINDOW: none do)
  *   free     all entries of the n listed rows are given up, kv_len becomes 0 (a row named twice counts once)

@@ -113,23 +113,116 @@ __device__ __forceinline__ int32_t scan_pages(const int32_t* __restrict__ refcou
     return min(found, want);
 }
 
-// Pages of row r that [kv_len, kv_len + add) needs beyond the ones it has; -1: the request cannot be served.
-__device__ __forceinline__ int64_t pages_needed(int32_t len, int32_t add, int page_shift, int64_t capacity) {
-    if (len < 0 || add < 0 || (int64_t)len + add > capacity) return -1;
+// Entries [first, first + count) of a row are those that [kv_len, kv_len + add) needs beyond the pages that hold tokens; count -1: the
+// request cannot be served.
+struct Span {
+    int64_t first, count;
+};
+__device__ __forceinline__ Span span_of(int32_t len, int32_t add, int page_shift, int64_t capacity) {
+    if (len < 0 || add < 0 || (int64_t)len + add > capacity) return {0, -1};
     const int64_t m = (1ll << page_shift) - 1;
-    return (((int64_t)len + add + m) >> page_shift) - ((len + m) >> page_shift);
+    const int64_t first = ((int64_t)len + m) >> page_shift;
+    return {first, (((int64_t)len + add + m) >> page_shift) - first};
 }
 
-__global__ void __launch_bounds__(kMetaThreads)
+// An entry behind a row's end may name a page still (the row was longer before: rejected draft tokens).  The row's own page is used again; of
+// one that is shared only the reference is given up, later (give_up_shared: all decisions look at the counts as the call found them); one
+// that names no used page counts as -1.  Returns whether the entry needs a fresh page.
+__device__ __forceinline__ bool settle_entry(int32_t* entry, int32_t page, const int32_t* refcount, int64_t num_pages, bool& shared) {
+    if (page == -1) return true;
+    const int32_t count = page >= 0 && page < num_pages ? refcount[page] : 0;
+    if (count == 1) return false;
+    *entry = count > 1 ? -2 - page : -1;
+    shared |= count > 1;
+    return true;
+}
+__device__ __forceinline__ void give_up_shared(int32_t* entry, int32_t mark, int32_t* refcount) {
+    if (mark >= -1) return;
+    atomicSub(refcount + (-2 - mark), 1);
+    *entry = -1;
+}
+
+// Calls f(entry, its value) -> bool for the entries of this lane's span and returns how often it was true.  Long spans (prompts) are walked by
+// the warp together, kBatch loads in flight: every lane of it makes the call.
+constexpr int kOwnEntries = 4;
+template <typename F>
+__device__ __forceinline__ int64_t count_entries(int32_t* row, const Span& sp, F f) {
+    constexpr int kBatch = 8;
+    const int lane = threadIdx.x & 31;
+    int64_t n = 0;
+    if (sp.count <= kOwnEntries)
+        for (int i = 0; i < sp.count; ++i) n += f(row + sp.first + i, row[sp.first + i]);
+    for (uint32_t todo = __ballot_sync(0xffffffffu, sp.count > kOwnEntries); todo != 0; todo &= todo - 1) {
+        const int src = __ffs(todo) - 1;
+        int32_t* at = reinterpret_cast<int32_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row + sp.first), src));
+        const int64_t count = __shfl_sync(0xffffffffu, (long long)sp.count, src);
+        int32_t hits = 0;
+        for (int64_t i0 = lane; i0 < count; i0 += 32 * kBatch) {
+            int32_t value[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) value[i] = i0 + 32 * i < count ? at[i0 + 32 * i] : -1;
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (i0 + 32 * i < count) hits += f(at + i0 + 32 * i, value[i]);
+        }
+        hits = __reduce_add_sync(0xffffffffu, hits);
+        if (lane == src) n = hits;
+    }
+    return n;
+}
+
+// The entries of this lane's span that hold -1, n of them, take the pages ids[0 .. n).  Every lane of the warp makes the call.
+__device__ __forceinline__ void fill_entries(int32_t* row, const Span& sp, int64_t n, const int32_t* ids, int32_t* refcount) {
+    const int lane = threadIdx.x & 31;
+    if (sp.count <= kOwnEntries)
+        for (int i = 0; i < sp.count; ++i)
+            if (row[sp.first + i] == -1) {
+                row[sp.first + i] = *ids;
+                refcount[*ids++] = 1;
+            }
+    for (uint32_t todo = __ballot_sync(0xffffffffu, sp.count > kOwnEntries && n > 0); todo != 0; todo &= todo - 1) {
+        const int src = __ffs(todo) - 1;
+        int32_t* at = reinterpret_cast<int32_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row + sp.first), src));
+        const int32_t* next = reinterpret_cast<const int32_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(ids), src));
+        const int64_t count = __shfl_sync(0xffffffffu, (long long)sp.count, src);
+        const bool all = __shfl_sync(0xffffffffu, (int)(n == sp.count), src);
+        for (int64_t i0 = 0; i0 < count; i0 += 32) {
+            const int64_t i = i0 + lane;
+            const bool take = i < count && (all || at[i] == -1);
+            const uint32_t takers = __ballot_sync(0xffffffffu, take);
+            if (take) {
+                const int32_t page = next[__popc(takers & ((1u << lane) - 1))];
+                at[i] = page;
+                refcount[page] = 1;
+            }
+            next += __popc(takers);
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kMetaThreads, 1)      // the only CTA: registers for all of it
 extend_kernel(PoolGeom g, int32_t* refcount, int32_t* table, int64_t rows, int64_t stride, int32_t* kv_len, const int32_t* add, int32_t* ids,
               int32_t* status) {
     __shared__ int64_t scratch[kMetaThreads / 32];
     const int64_t capacity = stride << g.page_shift;
-    // pages wanted by all rows
-    int64_t mine = 0, total;
-    for (int64_t r = threadIdx.x; r < rows; r += kMetaThreads) {
-        const int64_t n = pages_needed(kv_len[r], add[r], g.page_shift, capacity);
-        mine += n > 0 ? n : 0;
+    auto span = [&](int64_t r) { return r < rows ? span_of(kv_len[r], add[r], g.page_shift, capacity) : Span{0, 0}; };
+    // pages wanted by all rows; those of the first kMetaThreads rows stay in registers
+    int64_t mine = 0, total, first_need = 0;
+    const Span first_span = span(threadIdx.x);
+    bool shared = false;
+    for (int64_t r0 = 0; r0 < rows; r0 += kMetaThreads) {
+        const int64_t r = r0 + threadIdx.x;
+        const int64_t n = count_entries(table + r * stride, r0 == 0 ? first_span : span(r),
+                                        [&](int32_t* e, int32_t v) { return settle_entry(e, v, refcount, g.num_pages, shared); });
+        if (r0 == 0) first_need = n;
+        mine += n;
+    }
+    if (__syncthreads_or(shared)) {
+        for (int64_t r0 = 0; r0 < rows; r0 += kMetaThreads) {
+            const int64_t r = r0 + threadIdx.x;
+            count_entries(table + r * stride, span(r), [&](int32_t* e, int32_t v) { give_up_shared(e, v, refcount); return false; });
+        }
+        __syncthreads();
     }
     block_scan<int64_t>(mine, scratch, total);
     const int64_t got = total > 0 ? scan_pages<true>(refcount, 0, (int32_t)g.num_pages, total, scratch, [&](int32_t k, int32_t page) { ids[k] = page; }) : 0;
@@ -138,24 +231,16 @@ extend_kernel(PoolGeom g, int32_t* refcount, int32_t* table, int64_t rows, int64
     int64_t base = 0;
     for (int64_t r0 = 0; r0 < rows; r0 += kMetaThreads) {
         const int64_t r = r0 + threadIdx.x;
-        const int32_t len = r < rows ? kv_len[r] : 0, more = r < rows ? add[r] : 0;
-        const int64_t n = r < rows ? pages_needed(len, more, g.page_shift, capacity) : 0;
+        int32_t* row = table + r * stride;
+        const Span sp = r0 == 0 ? first_span : span(r);
+        const int64_t n = r0 == 0 ? first_need : count_entries(row, sp, [&](int32_t*, int32_t v) { return v == -1; });
         int64_t step;
-        const int64_t at = base + block_scan<int64_t>(n > 0 ? n : 0, scratch, step);
+        const int64_t at = base + block_scan<int64_t>(n, scratch, step);
         base += step;
-        if (r < rows) {
-            if (n < 0 || (n > 0 && at + n > got)) {
-                report_status(status, CP_ERR_BOUNDS, r, n < 0 ? more : -1);
-            } else {
-                const int64_t first = ((int64_t)len + g.page_size - 1) >> g.page_shift;
-                for (int64_t i = 0; i < n; ++i) {
-                    const int32_t page = ids[at + i];
-                    table[r * stride + first + i] = page;
-                    refcount[page] = 1;
-                }
-                kv_len[r] = len + more;
-            }
-        }
+        const bool served = r < rows && sp.count >= 0 && (n == 0 || at + n <= got);
+        fill_entries(row, served ? sp : Span{0, 0}, n, ids + at, refcount);
+        if (served) kv_len[r] += add[r];
+        else if (r < rows) report_status(status, CP_ERR_BOUNDS, r, sp.count < 0 ? add[r] : -1);
     }
 }
 

@@ -224,10 +224,33 @@ def cp_schedule_inspect(cu_new, prefix_len, C, Hq, Hkv, num_sms=148, want_lists=
     return info, pieces, items
 
 
+def _paged(pools, dtypes, what):
+    """Device of paged tensors [num_pages, page_size, Hkv, D] of one shape, type and layout on one device, refused otherwise: the kernels
+    compute every address from the first one's."""
+    first = pools[0]
+    if first.dim() != 4 or first.stride(3) != 1:
+        raise CpArgumentError("%s: K and V are [num_pages, page_size, Hkv, D] with unit stride in the last dimension, got %s with strides %s"
+                              % (what, tuple(first.shape), first.stride()))
+    for t in pools[1:]:
+        if t.shape != first.shape or t.stride() != first.stride() or t.dtype != first.dtype or t.device != first.device:
+            raise CpArgumentError("%s: K and V must agree in shape, strides, type and device, got %s %s with strides %s on %s and %s %s with strides "
+                                  "%s on %s" % (what, first.dtype, tuple(first.shape), first.stride(), first.device, t.dtype, tuple(t.shape),
+                                                t.stride(), t.device))
+    if str(first.dtype) not in dtypes:
+        raise CpArgumentError("%s: K and V are %s, got %s" % (what, " or ".join(dtypes), first.dtype))
+    if not first.is_cuda:
+        raise CpArgumentError("%s: K and V must be on a CUDA device, got %s" % (what, first.device))
+    return first.get_device()
+
+
+_BF16, _CODES = ("torch.bfloat16",), ("torch.uint8", "torch.int8", "torch.float8_e4m3fn")
+
+
 def make_cache(k_pages, v_pages) -> cp_kv_cache:
     """Describe paged K/V tensors [num_pages, page_size, Hkv, D] (bf16, any strides with dim stride 1)."""
-    assert k_pages.dim() == 4 and k_pages.stride() == v_pages.stride() and k_pages.stride(3) == 1
+    device = _paged((k_pages, v_pages), _BF16, "make_cache")
     c = cp_kv_cache()
+    c.device = device                                      # compared with the context's by the serving calls
     c.k, c.v = k_pages.data_ptr(), v_pages.data_ptr()
     c.num_pages, c.page_size, c.Hkv, c.D = k_pages.shape
     c.stride_page, c.stride_tok, c.stride_head = k_pages.stride(0), k_pages.stride(1), k_pages.stride(2)
@@ -292,7 +315,7 @@ def _window_args(kind, ctx, q, cache, page_table, rows, Hq, out, lse, workspace,
     qp, op, lp = _arg(ctx, q, "q", bf16, shape), _arg(ctx, out, "out", bf16, shape), _arg(ctx, lse, "lse", f32, (Hq, rows))
     if rows == 0:                                          # an empty chunk: empty tensors have no address, the call reads none
         qp = op = lp = ws
-    return (ctx._h, qp, _described(cache, kind), table), (op, lp, ws, ws_bytes, _raw_stream(ctx, stream))
+    return (ctx._h, qp, _described(ctx, cache, kind), table), (op, lp, ws, ws_bytes, _raw_stream(ctx, stream))
 
 
 def _host_i64(a):
@@ -384,9 +407,17 @@ def cp_kv_append_segments(ctx, cache, page_table, segments, k_rows, v_rows, stre
 
 def make_cache_fp8(k8_pages, v8_pages, k_scale, v_scale) -> cp_kv_cache_fp8:
     """Describe paged E4M3 K/V tensors [num_pages, page_size, Hkv, D] (uint8) with fp32 scales [Hkv] on the device."""
-    assert k8_pages.dim() == 4 and k8_pages.stride() == v8_pages.stride() and k8_pages.stride(3) == 1
-    assert k8_pages.element_size() == 1 and k_scale.numel() == k8_pages.shape[2] == v_scale.numel()
+    scales = (("k_scale", k_scale), ("v_scale", v_scale))
+    for name, t in scales:
+        if k8_pages.dim() == 4 and (str(t.dtype) != "torch.float32" or t.numel() != k8_pages.shape[2] or not t.is_contiguous()):
+            raise CpArgumentError("make_cache_fp8: %s must be a contiguous fp32 tensor of %d elements (one per KV head), got %s %s with strides %s"
+                                  % (name, k8_pages.shape[2], t.dtype, tuple(t.shape), t.stride()))
+    device = _paged((k8_pages, v8_pages), _CODES, "make_cache_fp8")
+    for name, t in scales:
+        if t.device != k8_pages.device:
+            raise CpArgumentError("make_cache_fp8: %s is on %s, the pages are on %s" % (name, t.device, k8_pages.device))
     c = cp_kv_cache_fp8()
+    c.device = device
     c.k, c.v, c.k_scale, c.v_scale = k8_pages.data_ptr(), v8_pages.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr()
     c.num_pages, c.page_size, c.Hkv, c.D = k8_pages.shape
     c.stride_page, c.stride_tok, c.stride_head = k8_pages.stride(0), k8_pages.stride(1), k8_pages.stride(2)
@@ -498,10 +529,12 @@ def _arg(ctx, t, name, dtype, shape):
                      % (name, dtype, tuple(shape), ctx.device, t.dtype, tuple(t.shape), t.stride(), t.device))
 
 
-def _described(desc, kind):
-    """Address of a descriptor, which must be of the kind that the call reads."""
+def _described(ctx, desc, kind):
+    """Address of a descriptor, which must be of the kind that the call reads and, unless made by hand, of tensors on the context's device."""
     if not isinstance(desc, kind):
         raise CpArgumentError("the call takes a %s, got a %s" % (kind.__name__, type(desc).__name__))
+    if getattr(desc, "device", ctx.device) != ctx.device:
+        raise CpArgumentError("the %s describes tensors on cuda:%d, the context is on cuda:%d" % (kind.__name__, desc.device, ctx.device))
     return ctypes.addressof(desc)
 
 
@@ -521,7 +554,7 @@ def _decode_attn(call, kind, ctx, q, cache, page_table, kv_len, window, sinks, s
     B, n_q, Hq, _ = shape
     stride = page_table.shape[1]
     ws, ws_bytes = _workspace(ctx, workspace)
-    rc = call(ctx._h, _arg(ctx, q, "q", bf16, (B, n_q, Hq, 128)), _described(cache, kind), _arg(ctx, page_table, "page_table", i32, (B, stride)), stride,
+    rc = call(ctx._h, _arg(ctx, q, "q", bf16, (B, n_q, Hq, 128)), _described(ctx, cache, kind), _arg(ctx, page_table, "page_table", i32, (B, stride)), stride,
               _arg(ctx, kv_len, "kv_len", i32, (B,)), B, n_q, Hq, window, sinks, scale, _arg(ctx, out, "out", bf16, shape),
               _arg(ctx, lse, "lse", f32, (Hq, B * n_q)), ws, ws_bytes, _raw_stream(ctx, stream))
     if rc != CP_OK:
@@ -565,8 +598,8 @@ def _rope_append(call, kind, ctx, rope, q, k_rows, v_rows, positions, token_seq,
         rows, stride = page_table.shape
         kp, vp = _arg(ctx, k_rows, "k_rows", bf16, shape), _arg(ctx, v_rows, "v_rows", bf16, shape)
         sp, tp = _arg(ctx, token_slot, "token_slot", i32, (n,)), _arg(ctx, page_table, "page_table", i32, (rows, stride))
-    rc = call(ctx._h, _described(rope, cp_rope), qp, kp, vp, n, Hq, _arg(ctx, positions, "positions", i32, (rope.n_axes, n)),
-              _arg(ctx, token_seq, "token_seq", i32, (n,)), sp, _described(cache, kind), tp, rows, stride, qo, _raw_stream(ctx, stream))
+    rc = call(ctx._h, _described(ctx, rope, cp_rope), qp, kp, vp, n, Hq, _arg(ctx, positions, "positions", i32, (rope.n_axes, n)),
+              _arg(ctx, token_seq, "token_seq", i32, (n,)), sp, _described(ctx, cache, kind), tp, rows, stride, qo, _raw_stream(ctx, stream))
     if rc != CP_OK:
         _check(rc)
 
@@ -586,13 +619,15 @@ def make_page_pool(k, v, num_pages=None) -> cp_page_pool:
     """Describe the K and V pools of one numbering of pages: k, v [layers, num_pages, page_size, Hkv, 128], or lists of such 4-D
     tensors, bf16 or uint8 (E4M3); all of one geometry."""
     ks, vs = [k[i] for i in range(len(k))], [v[i] for i in range(len(v))]
+    if len(ks) != len(vs) or not ks:
+        raise CpArgumentError("make_page_pool: %d layers of k, %d of v" % (len(ks), len(vs)))
+    device = _paged(ks + vs, _BF16 + _CODES, "make_page_pool")
     first = ks[0]
-    if len(ks) != len(vs) or any(t.shape != first.shape or t.stride() != first.stride() or t.dtype != first.dtype for t in ks + vs):
-        raise CpArgumentError("the layers' k and v must agree in number, shape, strides and type")
-    if first.dim() != 4 or first.shape[3] != 128 or first.stride(3) != 1 or (num_pages is not None and num_pages != first.shape[0]):
-        raise CpArgumentError("a layer is [num_pages, page_size, Hkv, 128] with unit stride in the last dimension, got %s" % (tuple(first.shape),))
+    if first.shape[3] != 128 or (num_pages is not None and num_pages != first.shape[0]):
+        raise CpArgumentError("a layer is [num_pages, page_size, Hkv, 128], got %s" % (tuple(first.shape),))
     e = first.element_size()
     p = cp_page_pool()
+    p.device = device
     p._k = (ctypes.c_void_p * len(ks))(*[t.data_ptr() for t in ks])        # kept alive with the descriptor
     p._v = (ctypes.c_void_p * len(vs))(*[t.data_ptr() for t in vs])
     p.k, p.v = ctypes.addressof(p._k), ctypes.addressof(p._v)
@@ -609,7 +644,7 @@ def cp_workspace_bytes_pages(num_pages, n=0) -> int:
 def _table_args(ctx, pool, refcount, page_table):
     i32 = (_types or _torch_types())[1]
     rows, stride = page_table.shape
-    return (ctx._h, _described(pool, cp_page_pool), _arg(ctx, refcount, "refcount", i32, (pool.num_pages,)),
+    return (ctx._h, _described(ctx, pool, cp_page_pool), _arg(ctx, refcount, "refcount", i32, (pool.num_pages,)),
             _arg(ctx, page_table, "page_table", i32, (rows, stride)), rows, stride)
 
 
@@ -657,5 +692,5 @@ def cp_pages_copy(ctx, pool, src, dst, workspace, stream=None):
     if _types is None:
         _torch_types()
     n = src.numel()
-    _check(load().cp_pages_copy(ctx._h, _described(pool, cp_page_pool), _ints(ctx, src, "src", n), _ints(ctx, dst, "dst", n), n, *_workspace(ctx, workspace),
+    _check(load().cp_pages_copy(ctx._h, _described(ctx, pool, cp_page_pool), _ints(ctx, src, "src", n), _ints(ctx, dst, "dst", n), n, *_workspace(ctx, workspace),
                                 _raw_stream(ctx, stream)))

@@ -456,7 +456,8 @@ int cp_rope_append_fp8(cp_ctx* ctx, const cp_rope* rope, const void* q, const vo
  *   page_table  device [B, table_stride] int32; kv_len  device [B] int32, the new tokens included
  *   out      device [B, n_q, Hq, D] bf16, may be q;  lse  device [Hq, B * n_q] fp32 (the layout cp_merge takes)
  * A row before position 0 (kv_len[b] < n_q; kv_len[b] = 0 for an idle row) sees nothing: zeros, lse = -inf.  Only slots that some row
- * sees are read, and what they hold, infinities and NaN too, reaches no other row; an entry outside the pool reads as zeros.
+ * sees are read, and what they hold, infinities and NaN too, reaches no other row; an entry outside the pool reads as zeros.  A row with a
+ * score of NaN or +inf becomes NaN, its lse too.
  * kv_len[b] < 0 counts as 0, one beyond the table row as the row's capacity; both are reported as CP_ERR_BOUNDS {code, b, block,
  * kv_len} by cp_ctx_poll_status.  Weights are rounded to bf16 for P V (_fp8: to fp16), all sums are fp32.  Two launches, whose grids
  * do not depend on the lengths: a captured call is replayed with other lengths and tables.  workspace:

@@ -734,11 +734,12 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             for (int w = 0; w < kHeadGroups; ++w) mx = fmaxf(mx, mine_ml[w * kRows * 2]);
 #pragma unroll
             for (int w = 0; w < kHeadGroups; ++w) sum += mine_ml[w * kRows * 2 + 1] * exp2_fast(mine_ml[w * kRows * 2] - mx);
-            row_inv[tid] = sum > 0.f ? (kFp8 ? p.v_scale[h] : 1.f) / sum : 0.f;      // read behind the barrier below
+            // a sum of zero: the row sees nothing; one that is no number (of a key or the query) makes the row NaN
+            row_inv[tid] = sum == 0.f ? 0.f : (kFp8 ? p.v_scale[h] : 1.f) / sum;     // read behind the barrier below
             const int r = r0 + row, t = kDrafts ? r / p.G : 0;
             if (whole) {
                 p.lse[(int64_t)(h * p.G + r - t * p.G) * ((int64_t)p.B * p.n_q) + (int64_t)b * p.n_q + t] =
-                    sum > 0.f ? (mx + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+                    sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.6931471805599453f;
             } else {
                 p.part_ml[((int64_t)slot * (HP * kRows) + tid) * 2] = mx;
                 p.part_ml[((int64_t)slot * (HP * kRows) + tid) * 2 + 1] = sum;
@@ -864,12 +865,12 @@ decode_join_kernel(const __grid_constant__ DecodeParams p, int heads, int rows_p
         float x = 0.f;
 #pragma unroll
         for (int w = 0; w < kJoinWarps; ++w) x += acc[w][threadIdx.x];
-        const float inv = total > 0.f ? (kFp8 ? p.v_scale[h] : 1.f) / total : 0.f;
+        const float inv = total == 0.f ? 0.f : (kFp8 ? p.v_scale[h] : 1.f) / total;
         p.out[(token * p.Hq + head) * kDim + threadIdx.x] = __float2bfloat16_rn(x * inv);
     }
     if (threadIdx.x == 0)
         p.lse[(int64_t)head * ((int64_t)p.B * p.n_q) + token] =
-            total > 0.f ? (mx + log2f(total)) * 0.6931471805599453f : -INFINITY;
+            total == 0.f ? -INFINITY : (mx + log2f(total)) * 0.6931471805599453f;
 }
 
 constexpr int kMaxDecodeGrid = 2 * kMaxGrid;

@@ -461,7 +461,7 @@ int cp_rope_append_fp8(cp_ctx* ctx, const cp_rope* rope, const void* q, const vo
  * kv_len[b] < 0 counts as 0, one beyond the table row as the row's capacity; both are reported as CP_ERR_BOUNDS {code, b, block,
  * kv_len} by cp_ctx_poll_status.  Weights are rounded to bf16 for P V (_fp8: to fp16), all sums are fp32.  Two launches, whose grids
  * do not depend on the lengths: a captured call is replayed with other lengths and tables.  workspace:
- * cp_workspace_bytes_decode (0 on invalid arguments), for one call at a time.
+ * cp_workspace_bytes_decode (0 on arguments that the call refuses), for one call at a time.
  * Limits: n_q <= 64, n_q * Hq / Hkv <= 1024, B <= 65536.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA. */
 size_t cp_workspace_bytes_decode(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv);
 int cp_decode_attn(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table, int64_t table_stride,

@@ -875,6 +875,7 @@ decode_join_kernel(const __grid_constant__ DecodeParams p, int heads, int rows_p
 
 constexpr int kMaxDecodeGrid = 2 * kMaxGrid;
 constexpr int kMaxHeads = 2;                               // largest HP
+constexpr int kMaxDecodeTokens = 64, kMaxDecodeRows = 1024, kMaxDecodeBatch = 65536;      // limits of a call: n_q, rows per KV head, B
 inline int row_blocks(int rows) { return rows <= 8 ? 1 : (rows <= 16 ? 2 : 4); }
 
 // Workspace: partial rows and their (maximum, sum) of two pieces per CTA, and four words per CTA.
@@ -920,10 +921,10 @@ int decode_attn(cp_ctx* ctx, const void* q, const void* k, const void* v, const 
     if (((uintptr_t)q | (uintptr_t)out) & 15) return set_error(CP_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned", who);
     const int shift = log2_exact(page_size);
     const int64_t rows = (int64_t)n_q * (Hq / Hkv);
-    if (n_q > 64 || rows > 1024)
+    if (n_q > kMaxDecodeTokens || rows > kMaxDecodeRows)
         return set_error(CP_ERR_UNSUPPORTED, "%s: n_q=%d, %lld query rows per KV head; at most 64 and 1024 (more: a prefill call)", who, n_q,
                          (long long)rows);
-    if (B > 65536 || table_stride > (0x7fffff00ll >> shift) || num_pages > 0x7fffffffll)
+    if (B > kMaxDecodeBatch || table_stride > (0x7fffff00ll >> shift) || num_pages > 0x7fffffffll)
         return set_error(CP_ERR_UNSUPPORTED, "%s: B=%d (at most 65536), a table row of %lld entries or %lld pages", who, B,
                          (long long)table_stride, (long long)num_pages);
     const size_t need = decode_workspace((int)rows);
@@ -977,7 +978,9 @@ int decode_attn(cp_ctx* ctx, const void* q, const void* k, const void* v, const 
 
 extern "C" size_t cp_workspace_bytes_decode(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv) {
     if (B < 0 || n_q < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0) return 0;
-    return decode_workspace((int)std::min<int64_t>((int64_t)n_q * (Hq / Hkv), 1024));
+    const int64_t rows = (int64_t)n_q * (Hq / Hkv);
+    if (B > kMaxDecodeBatch || n_q > kMaxDecodeTokens || rows > kMaxDecodeRows) return 0;
+    return decode_workspace((int)rows);
 }
 
 extern "C" int cp_decode_attn(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table, int64_t table_stride,

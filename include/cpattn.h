@@ -415,7 +415,7 @@ int cp_kv_append_segments_fp8(cp_ctx* ctx, const cp_kv_cache_fp8* cache, const i
 /* Rotary positions with one to four axes (text: one; images and video: time, height, width).  The first rot_dims elements of a
  * head are rot_dims / 2 pairs; pair i is (i, i + rot_dims / 2), or (2i, 2i + 1) when interleaved, and turns by the angle
  * positions[axis[i]][token] * freq[i] radians: (a, b) -> (a cos - b sin, b cos + a sin).  The elements behind them keep their
- * bits.  Angles are exact to 2^-32 of a turn for every int32 position.  rot_dims: a multiple of 16.
+ * bits.  Angles are off by at most 2^-25 of a turn (2e-7 radians) for every int32 position and |freq| up to 2 pi.  rot_dims: a multiple of 16.
  * cp_rope_init fills the struct for consecutive sections of pairs per axis (sum 1..64; rot_dims = twice the sum) and
  * freq[i] = base^(-2 i / rot_dims); callers may then change axis[] and freq[] (scaled frequencies, interleaved sections).
  * Host only.  Errors: INVALID_ARG. */
@@ -483,7 +483,8 @@ int cp_decode_attn_fp8(cp_ctx* ctx, const void* q, const cp_kv_cache_fp8* cache,
  *            the tokens wanted}.  The caller may lower kv_len[r] (rejected draft tokens), but not into a page that the row shares
  *            (not below the full pages that a fork of it shares): the pages behind the new end stay the row's and are
  *            used again by the next extend.  Where one of these is shared, its reference is given up and a fresh page takes
- *            its place; an entry there that names no used page counts as -1
+ *            its place; an entry there that names no used page counts as -1.  Lower a length before evict, not after it: what the
+ *            new end's window sees would be gone
  *   evict    the next token of a row sits at position kv_len[r]: entries of pages that are wholly behind its window and
  *            behind the sinks become -1 and give up their reference (CP_NO_WINDOW: none do)
  *   free     all entries of the n listed rows are given up, kv_len becomes 0 (a row named twice counts once)

@@ -1056,8 +1056,9 @@ __device__ __forceinline__ void fill_role(const AttnParams& p) {
 
 // kFp8: the FP8 K/V variant (one-byte Q / K / V / P operands).  kWin: the windowed calls (a unit's KV tiles are the
 // sinks' and the window's, the ones between are skipped); the calls without a window keep their own instantiation.
-// Bound by the tensor and MUFU pipes as the full form is: 32768 tokens, 32 heads, window 4096 in 1.62 ms in a single launch, 1277 TFLOP/s of
-// visible pairs (1.87 ms, 1104 in a row of launches under the power cap); of 34 tiles per query tile two are half hidden.
+// Bound by the tensor and MUFU pipes as the full form is: 32768 tokens, 32 heads, window 4096 in 1.62 ms in a single launch at boost clocks,
+// 1277 TFLOP/s of visible pairs (1.81 ms, 1143 in a row of launches under the power cap; E4M3 1.66 ms, 1246); of 34 tiles per query tile two are
+// half hidden.
 // Inl: the launch-parameter copy of the work lists, InlineSmall or InlineSched.
 template <bool kFp8, bool kWin, typename Inl>
 __global__ void __launch_bounds__(kThreads, 1)

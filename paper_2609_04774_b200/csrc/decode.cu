@@ -24,10 +24,11 @@
 // mantissa fit; what falls below 2^-24 of the row's largest is lost), weights are fp16 after a scaling by 2^7, so the
 // result has fp16 weights (2^-11) where the bf16 cache has bf16 ones (2^-8).  Sums, maxima and accumulators are fp32.
 //
-// Measured (device time; of the 6.45 TB/s that a copy reaches): 64 requests of 257..16384 keys, 32 / 8 heads: 178 us, 6.5 TB/s; E4M3 103 us,
-// 5.7 TB/s; 128 requests with a window of 4096, 64 / 8 heads: 278 us, 6.7 TB/s, E4M3 160 us, 5.8 TB/s; four contexts of 128K keys, four
-// draft tokens each, 32 / 4 heads: 144 us, 6.2 TB/s, E4M3 144 us (bound by the fp16 widening and the fragments' shared-memory
-// traffic); one request of 4097 keys: 10 us, the latency of two launches.
+// Measured (device time from a graph; a copy reaches 6.45 TB/s, reading alone somewhat more): 64 requests of 257..16384 keys, 32 / 8 heads: 177 us,
+// 6.6 TB/s; E4M3 101 us, 5.8 TB/s; 128 requests with a window of 4096, 64 / 8 heads: 276 us, 6.7 TB/s, E4M3 158 us, 5.9 TB/s; four contexts of
+// 100K..128K keys, four draft tokens each, 32 / 4 heads: 143 us, 6.2 TB/s, E4M3 140 us (bound by the fp16 widening and the fragments' shared-memory
+// traffic); one request of 4097 keys: 9.7 us, the latency of two launches.  More than 32 rows per KV head are several units, each reading K and V
+// (from L2 where it can): four contexts of 64K keys, four draft tokens, 64 / 4 heads: 170 us against 93 for 32 / 4, E4M3 160 against 99.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>

@@ -6,7 +6,8 @@
 //
 // Choosing pages is a prefix sum over the rows' needs and one over the pool's counts.  One CTA of 1024 threads does both:
 // the counts are 4 bytes a page (64 KB for a pool of a million tokens in pages of 64), the scan stops at the last page needed, and a
-// second CTA would cost a grid-wide wait that is longer than the scan.  Moving pages is HBM-bound (2x the moved bytes): the
+// second CTA would cost a grid-wide wait that is longer than the scan.  Extend for one token of 64 rows takes 5.2 us (4.6 without the look at
+// what the entries hold), for a prompt of 2048 pages 15 us: a warp walks a long row together, 32 entries at a time.  Moving pages is HBM-bound (2x the moved bytes): the
 // list of moves stays in the workspace, a second launch (set up while the first one runs) copies them for all layers, 32 KB per CTA step
 // with eight 16-byte vectors in flight per thread.  1 GB of moved pages: 171 us with the choosing and the tables, 6.1 TB/s; with four
 // vectors 174, with eight CTAs per SM in one wave 184.

@@ -5,7 +5,8 @@
 //     a' = a cos - b sin,   b' = b cos + a sin.
 // Angles are kept in turns, as 64-bit fixed point: step(i) = freq(i) / 2 pi mod 1, scaled by 2^64, and the product
 // pos * step wraps modulo one turn by itself, so a position of 10^6 or 2^31 loses nothing (an fp32 product would be off by
-// 0.06 radians at 10^6).  The top 32 bits, read as a signed fraction in [-1/2, 1/2), go to sincospif.
+// 0.06 radians at 10^6).  The top 32 bits, read as a signed fraction in [-1/2, 1/2), go to sincospif as an fp32 number of half turns, whose
+// rounding is the largest error of the angle: 2^-26 of a turn (cutting the bits off adds 2^-32, the step's own 2^-64 up to 2^-33).
 //
 // HBM-bound: q is read and written once, k and v are read once and written once (24 KB per token at 32 / 8 heads).  A warp takes
 // the heads of one token in steps of four (8 lanes a head, two 16-byte vectors a lane), so the 64 sines and cosines of a token

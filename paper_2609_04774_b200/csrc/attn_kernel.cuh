@@ -802,10 +802,12 @@ __device__ __forceinline__ void softmax_tile(float (&c0)[32], float (&c1)[32], f
         tc_fence_after();
         const bool grow = (m_new - m) > (kFp8 ? kRescaleThreshold8 : kRescaleThreshold);
         if (__any_sync(0xffffffffu, grow)) {
-            // a row that has seen no key yet stays at m = -inf while others of its warp grow: m - m would be NaN there
-            const float alpha = grow ? ex2(m - m_new) : 1.f;
+            // a row that has seen no key yet stays at m = -inf while others of its warp grow: m - m would be NaN there (only in masked tiles:
+            // in the others every row sees keys)
+            const float m_upd = grow ? m_new : m;
+            const float alpha = ex2(kMasked && !grow ? 0.f : m - m_upd);
             l *= alpha;
-            if (grow) m = m_new;
+            m = m_upd;
 #pragma unroll 1
             for (int cc = 0; cc < 4; ++cc) {
                 float o[32];
@@ -818,7 +820,7 @@ __device__ __forceinline__ void softmax_tile(float (&c0)[32], float (&c1)[32], f
         }
     }
     const float2 c2f = make_float2(c, c);
-    // a row that has seen no key yet keeps m = -inf (masked tiles only: of a KV-split piece, or left of a row's window);
+    // a row that has seen no key yet keeps m = -inf (masked tiles only: of a KV-split piece or a key range, or left of its window);
     // subtracting 0 instead keeps its weights at exactly 0 rather than NaN
     const float m_sub = ((kMasked && m == -INFINITY) ? 0.f : m) - (kFp8 ? kP8Shift : 0.f);
     const float2 nm2 = make_float2(-m_sub, -m_sub);

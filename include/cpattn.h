@@ -471,8 +471,74 @@ int cp_decode_attn_fp8(cp_ctx* ctx, const void* q, const cp_kv_cache_fp8* cache,
                        const int32_t* kv_len, int32_t B, int32_t n_q, int32_t Hq, int64_t window, int64_t sinks, float scale, void* out,
                        float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/* 4-bit K/V caches (OCP microscaling, MXFP4).  32 consecutive elements of a head's row are a block: an exponent byte e and 32 E2M1 codes (sign, two
+ * bits of exponent, one of mantissa: 0, .5, 1, 1.5, 2, 3, 4, 6), each worth code * 2^(e - 127); e = 255: the whole block is NaN.  A
+ * token's row holds Hkv * 64 bytes of codes (element 2i of a head in the low half of its byte i), then Hkv * 4 exponent bytes (block b of
+ * head h at Hkv * 64 + 4 h + b): 68 bytes a head where bf16 takes 256.  Token t is at page_table[t / page_size] * stride_page + (t %
+ * page_size) * stride_tok; both strides in bytes, multiples of 16, stride_tok >= 68 * Hkv; k and v 16-byte aligned.
+ *   cp_rope_append_mx4  cp_rope_append into such a cache.  k (rotated) and v are quantised block by block: e = floor(log2(largest magnitude))
+ *            - 2 + 127 (at least 0), codes to the nearest, ties to the even code, saturating at 6.  A block with an infinity or a NaN becomes
+ *            NaN.  The codes are those of the exactly rotated values: where the fp32 rotation does not decide, it is redone in fp64.
+ *   cp_kv_gather_mx4    the values of n logical tokens from t_begin as bf16 rows [n, Hkv, D] (exact up to e = 251; larger ones may overflow), what the
+ *            prefill calls read: rows of whole pages are a cp_kv_cache with table 0, 1, 2, ..  Page ids as in cp_kv_gather.
+ *   cp_decode_attn_mx4  cp_decode_attn over such a cache, same arguments, workspace and limits.  Weights are rounded to bf16, K and V are taken exactly
+ *            (e up to 253), the queries lose what is below 2^-24 of a row's largest element.
+ * Errors as in the calls they are forms of. */
+typedef struct {
+    const void* k;          /* device */
+    const void* v;
+    int64_t num_pages;
+    int32_t page_size;      /* 16, 32, 64 or 128 */
+    int32_t Hkv;
+    int32_t D;              /* 128 */
+    int32_t reserved;
+    int64_t stride_page, stride_tok; /* bytes */
+} cp_kv_cache_mx4;
+int cp_rope_append_mx4(cp_ctx* ctx, const cp_rope* rope, const void* q, const void* k_rows, const void* v_rows, int64_t n,
+                       int32_t Hq, const int32_t* positions, const int32_t* token_seq, const int32_t* token_slot,
+                       const cp_kv_cache_mx4* cache, const int32_t* page_table, int64_t table_rows, int64_t table_stride,
+                       void* q_out, void* stream);
+int cp_kv_gather_mx4(cp_ctx* ctx, const cp_kv_cache_mx4* cache, const int32_t* page_table, int64_t t_begin, int64_t n, void* k_rows,
+                     void* v_rows, void* stream);
+int cp_decode_attn_mx4(cp_ctx* ctx, const void* q, const cp_kv_cache_mx4* cache, const int32_t* page_table, int64_t table_stride,
+                       const int32_t* kv_len, int32_t B, int32_t n_q, int32_t Hq, int64_t window, int64_t sinks, float scale, void* out,
+                       float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Trees of drafted tokens.  Sequence b has kv_len[b] tokens in its table row, of which the last tree_len[b] (0..n_q; tree_len NULL: n_q each)
+ * are a tree of drafts: with base = kv_len[b] - tree_len[b], drafted token t sits in slot base + t, and at position base + depth(t), the
+ * depth of a token without a parent among the drafts being 0.  parent  device [B, n_q] int32: parent[b][t] < t, or -1: the sequence itself.
+ * A step: cp_pages_extend, cp_tree_plan, then layer by layer cp_rope_append and cp_tree_attn, the choice of the accepted
+ * tokens, cp_tree_commit.  Entries behind a sequence's tree_len are padding.  n_q <= 64.
+ *   cp_tree_plan   mask [B, n_q]: bits of the drafted tokens that a token sees, its ancestors and itself (0 behind the tree); positions [n_axes,
+ *            B * n_q] (the same on every axis), token_seq (b; -1 behind the tree: padding) and token_slot [B * n_q] as cp_rope_append takes
+ *            them (0 behind the tree).  A parent outside [-1, t) is reported as CP_ERR_BOUNDS {code, b * n_q + t, block, parent} and
+ *            counts as -1.
+ *   cp_tree_attn   cp_decode_attn where row t sees the keys before base as a token at its position does, and of the drafts those of its mask that its
+ *            window or the sinks hold, by their positions.  The masks may be any bits (bits from tree_len on are
+ *            ignored); the position of a token is base + (bits of its mask) - 1.  Rows behind the tree: zeros, lse = -inf.  A tree_len outside
+ *            [0, min(n_q, kv_len[b])] is reported {code, b, block, tree_len} and counts as the nearest in it.  Workspace: cp_workspace_bytes_tree; limits,
+ *            layouts and the rest as in cp_decode_attn[_fp8|_mx4].
+ *   cp_tree_commit   accepted [B]: the last drafted token that sequence b keeps (-1: none).  It and its ancestors n_0 < n_1 < .. become the sequence's next
+ *            tokens: what slot base + n_i holds moves to slot base + i, K and V, in every layer of the pool; kv_len[b] = base + their number;
+ *            path [B, n_q] receives n_0, n_1, .., then -1.  The table keeps its pages (as with a length that the caller lowers, see extend;
+ *            the drafts must not lie in pages shared with a fork).  An accepted outside [-1, tree_len) is reported {code, b, block, accepted}
+ *            and counts as -1; a token whose slot has no page of the pool is reported {code, table entry, block, id} and not moved.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA. */
+int cp_tree_plan(cp_ctx* ctx, const int32_t* parent, const int32_t* tree_len, const int32_t* kv_len, int32_t B, int32_t n_q, int32_t n_axes,
+                 uint64_t* mask, int32_t* positions, int32_t* token_seq, int32_t* token_slot, void* stream);
+size_t cp_workspace_bytes_tree(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv);
+int cp_tree_attn(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table, int64_t table_stride, const int32_t* kv_len,
+                 const int32_t* tree_len, const uint64_t* mask, int32_t B, int32_t n_q, int32_t Hq, int64_t window, int64_t sinks, float scale,
+                 void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+int cp_tree_attn_fp8(cp_ctx* ctx, const void* q, const cp_kv_cache_fp8* cache, const int32_t* page_table, int64_t table_stride,
+                     const int32_t* kv_len, const int32_t* tree_len, const uint64_t* mask, int32_t B, int32_t n_q, int32_t Hq, int64_t window,
+                     int64_t sinks, float scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+int cp_tree_attn_mx4(cp_ctx* ctx, const void* q, const cp_kv_cache_mx4* cache, const int32_t* page_table, int64_t table_stride,
+                     const int32_t* kv_len, const int32_t* tree_len, const uint64_t* mask, int32_t B, int32_t n_q, int32_t Hq, int64_t window,
+                     int64_t sinks, float scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* The care of the pages.  A pool is n_layers K and V caches of one geometry (layer l: k[l], v[l]; strides in BYTES, multiples of
- * 16; row_bytes = bytes of one head's row: 256 bf16, 128 E4M3) whose pages share one numbering, and refcount [num_pages] int32 on
+ * 16; row_bytes = bytes of one head's row: 256 bf16, 128 E4M3; 4-bit rows are Hkv = 16-byte pieces of a token's row, row_bytes = 16, stride_head = 16) whose pages share one numbering, and refcount [num_pages] int32 on
  * the device: how many table entries name a page; 0 = free.  k and v are host arrays of device pointers, read before the call
  * returns; extend, evict and free look at num_pages and page_size only.  Pages are handed out lowest free id first, to the rows
  * in order.  cp_workspace_bytes_pages: workspace of the calls that take one, for n forks or copies (0 elsewhere); a workspace
@@ -524,6 +590,9 @@ int cp_pages_compact(cp_ctx* ctx, const cp_page_pool* pool, int32_t* refcount, i
                      int64_t table_stride, int32_t* page_map, int32_t* n_live, void* workspace, size_t workspace_bytes, void* stream);
 int cp_pages_copy(cp_ctx* ctx, const cp_page_pool* pool, const int32_t* src, const int32_t* dst, int32_t n, void* workspace,
                   size_t workspace_bytes, void* stream);
+/* see "Trees of drafted tokens" */
+int cp_tree_commit(cp_ctx* ctx, const cp_page_pool* pool, const int32_t* page_table, int64_t table_stride, int32_t* kv_len,
+                   const int32_t* tree_len, const int32_t* parent, const int32_t* accepted, int32_t B, int32_t n_q, int32_t* path, void* stream);
 
 #ifdef __cplusplus
 }

@@ -28,7 +28,8 @@ EXPORTS = ["cp_strerror", "cp_last_error", "cp_ctx_create", "cp_ctx_destroy", "c
            "cp_prefill_attn_window", "cp_prefill_attn_window_batch", "cp_prefill_attn_window_chunk", "cp_prefill_attn_fp8_window_batch",
            "cp_rope_init", "cp_rope_append", "cp_rope_append_fp8", "cp_workspace_bytes_pages", "cp_pages_extend", "cp_pages_evict",
            "cp_pages_free", "cp_pages_fork", "cp_pages_compact", "cp_pages_copy", "cp_workspace_bytes_decode", "cp_decode_attn",
-           "cp_decode_attn_fp8"]
+           "cp_decode_attn_fp8", "cp_rope_append_mx4", "cp_kv_gather_mx4", "cp_decode_attn_mx4", "cp_tree_plan", "cp_workspace_bytes_tree",
+           "cp_tree_attn", "cp_tree_attn_fp8", "cp_tree_attn_mx4", "cp_tree_commit"]
 
 # The serving calls run once per layer and token, so their argument types are declared once and plain integers are passed.
 _P, _I, _L, _F, _Z = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
@@ -50,6 +51,15 @@ _ARGTYPES = {
     "cp_workspace_bytes_decode": [_I, _I, _I, _I],
     "cp_decode_attn": [_P, _P, _P, _P, _L, _P, _I, _I, _I, _L, _L, _F, _P, _P, _P, _Z, _P],
     "cp_decode_attn_fp8": [_P, _P, _P, _P, _L, _P, _I, _I, _I, _L, _L, _F, _P, _P, _P, _Z, _P],
+    "cp_decode_attn_mx4": [_P, _P, _P, _P, _L, _P, _I, _I, _I, _L, _L, _F, _P, _P, _P, _Z, _P],
+    "cp_rope_append_mx4": [_P, _P, _P, _P, _P, _L, _I, _P, _P, _P, _P, _P, _L, _L, _P, _P],
+    "cp_kv_gather_mx4": [_P, _P, _P, _L, _L, _P, _P, _P],
+    "cp_tree_plan": [_P, _P, _P, _P, _I, _I, _I, _P, _P, _P, _P, _P],
+    "cp_workspace_bytes_tree": [_I, _I, _I, _I],
+    "cp_tree_attn": [_P, _P, _P, _P, _L, _P, _P, _P, _I, _I, _I, _L, _L, _F, _P, _P, _P, _Z, _P],
+    "cp_tree_attn_fp8": [_P, _P, _P, _P, _L, _P, _P, _P, _I, _I, _I, _L, _L, _F, _P, _P, _P, _Z, _P],
+    "cp_tree_attn_mx4": [_P, _P, _P, _P, _L, _P, _P, _P, _I, _I, _I, _L, _L, _F, _P, _P, _P, _Z, _P],
+    "cp_tree_commit": [_P, _P, _P, _L, _P, _P, _P, _P, _I, _I, _P, _P],
 }
 
 
@@ -86,6 +96,12 @@ class cp_kv_cache_fp8(ctypes.Structure):
                 ("stride_head", ctypes.c_int64)]
 
 
+class cp_kv_cache_mx4(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("num_pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32), ("reserved", ctypes.c_int32), ("stride_page", ctypes.c_int64),
+                ("stride_tok", ctypes.c_int64)]
+
+
 class cp_rope(ctypes.Structure):
     _fields_ = [("n_axes", ctypes.c_int32), ("rot_dims", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("axis", ctypes.c_int32 * 64), ("freq", ctypes.c_double * 64)]
@@ -115,6 +131,7 @@ def load():
         lib.cp_workspace_bytes_fp8.restype = ctypes.c_size_t
         lib.cp_workspace_bytes_pages.restype = ctypes.c_size_t
         lib.cp_workspace_bytes_decode.restype = ctypes.c_size_t
+        lib.cp_workspace_bytes_tree.restype = ctypes.c_size_t
         for name in EXPORTS:
             if name not in ("cp_strerror", "cp_last_error") and not name.startswith("cp_workspace_bytes"):
                 getattr(lib, name).restype = ctypes.c_int
@@ -232,10 +249,19 @@ def _paged(pools, dtypes, what):
         raise CpArgumentError("%s: K and V are [num_pages, page_size, Hkv, D] with unit stride in the last dimension, got %s with strides %s"
                               % (what, tuple(first.shape), first.stride()))
     for t in pools[1:]:
-        if t.shape != first.shape or t.stride() != first.stride() or t.dtype != first.dtype or t.device != first.device:
-            raise CpArgumentError("%s: K and V must agree in shape, strides, type and device, got %s %s with strides %s on %s and %s %s with strides "
-                                  "%s on %s" % (what, first.dtype, tuple(first.shape), first.stride(), first.device, t.dtype, tuple(t.shape),
-                                                t.stride(), t.device))
+        _same(first, t, what)
+    return _on_cuda(first, dtypes, what)
+
+
+def _same(first, t, what):
+    if t.shape != first.shape or t.stride() != first.stride() or t.dtype != first.dtype or t.device != first.device:
+        raise CpArgumentError("%s: K and V must agree in shape, strides, type and device, got %s %s with strides %s on %s and %s %s with strides "
+                              "%s on %s" % (what, first.dtype, tuple(first.shape), first.stride(), first.device, t.dtype, tuple(t.shape),
+                                            t.stride(), t.device))
+
+
+def _on_cuda(first, dtypes, what):
+    """Device of a tensor of one of the types on a CUDA device."""
     if str(first.dtype) not in dtypes:
         raise CpArgumentError("%s: K and V are %s, got %s" % (what, " or ".join(dtypes), first.dtype))
     if not first.is_cuda:
@@ -308,7 +334,7 @@ def cp_prefill_attn_kvrange(ctx, q, cache, page_table, prefix_len, new_len, kv_l
 
 def _window_args(kind, ctx, q, cache, page_table, rows, Hq, out, lse, workspace, stream):
     """The tensors of a windowed call, checked: (q, cache, page_table) and (out, lse, workspace, its bytes, stream)."""
-    bf16, i32, f32, _ = _types or _torch_types()
+    bf16, i32, f32 = (_types or _torch_types())[:3]
     shape = (rows, Hq, 128)
     table = _arg(ctx, page_table, "page_table", i32, page_table.shape)
     ws, ws_bytes = _workspace(ctx, workspace)
@@ -512,7 +538,7 @@ _types = None      # (bf16, int32, float32, the current raw stream of a device),
 def _torch_types():
     global _types
     import torch
-    _types = (torch.bfloat16, torch.int32, torch.float32, torch._C._cuda_getCurrentRawStream)
+    _types = (torch.bfloat16, torch.int32, torch.float32, torch._C._cuda_getCurrentRawStream, torch.int64)
     return _types
 
 
@@ -549,7 +575,7 @@ def cp_workspace_bytes_decode(B, n_q, Hq, Hkv) -> int:
 
 
 def _decode_attn(call, kind, ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream):
-    bf16, i32, f32, _ = _types or _torch_types()
+    bf16, i32, f32 = (_types or _torch_types())[:3]
     shape = q.shape
     B, n_q, Hq, _ = shape
     stride = page_table.shape[1]
@@ -582,7 +608,7 @@ def make_rope(sections, base=10000.0, interleaved=False) -> cp_rope:
 
 
 def _rope_append(call, kind, ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream):
-    bf16, i32, _, _ = _types or _torch_types()
+    bf16, i32 = (_types or _torch_types())[:2]
     n = token_seq.shape[0]
     qp = qo = kp = vp = sp = tp = None
     Hq = rows = stride = 0
@@ -615,6 +641,143 @@ def cp_rope_append_fp8(ctx, rope, q, k_rows, v_rows, positions, token_seq, token
     _rope_append(load().cp_rope_append_fp8, cp_kv_cache_fp8, ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream)
 
 
+def _layers(pool, ks, vs):
+    """The layers' addresses, kept alive with the descriptor."""
+    pool._k = (ctypes.c_void_p * len(ks))(*[t.data_ptr() for t in ks])
+    pool._v = (ctypes.c_void_p * len(vs))(*[t.data_ptr() for t in vs])
+    pool.k, pool.v = ctypes.addressof(pool._k), ctypes.addressof(pool._v)
+    pool.n_layers = len(ks)
+
+
+def cp_rope_append_mx4(ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream=None):
+    """cp_rope_append into a 4-bit cache: k (rotated) and v as blocks of 32 E2M1 codes with an exponent."""
+    _rope_append(load().cp_rope_append_mx4, cp_kv_cache_mx4, ctx, rope, q, k_rows, v_rows, positions, token_seq, token_slot, cache, page_table, q_out, stream)
+
+
+def mx4_token_bytes(Hkv) -> int:
+    """Bytes of a token's row of a 4-bit cache, rounded up to the alignment of rows."""
+    return -(-Hkv * 68 // 16) * 16
+
+
+def make_cache_mx4(k_pages, v_pages, Hkv) -> cp_kv_cache_mx4:
+    """Describe paged 4-bit K/V tensors [num_pages, page_size, bytes] (uint8, unit stride in the last dimension): a token's row holds Hkv * 64 bytes of
+    codes, then Hkv * 4 exponents; the rest of it is not used."""
+    first = k_pages
+    if first.dim() != 3 or first.stride(2) != 1 or first.shape[2] < Hkv * 68:
+        raise CpArgumentError("make_cache_mx4: K and V are [num_pages, page_size, %d bytes at least] with unit stride in the last dimension, got %s with "
+                              "strides %s" % (Hkv * 68, tuple(first.shape), first.stride()))
+    _same(k_pages, v_pages, "make_cache_mx4")
+    c = cp_kv_cache_mx4()
+    c.device = _on_cuda(first, ("torch.uint8",), "make_cache_mx4")
+    c.k, c.v = k_pages.data_ptr(), v_pages.data_ptr()
+    c.num_pages, c.page_size, c.Hkv, c.D = first.shape[0], first.shape[1], Hkv, 128
+    c.stride_page, c.stride_tok = first.stride(0), first.stride(1)
+    return c
+
+
+def cp_kv_gather_mx4(ctx, cache, page_table, t_begin, n, k_rows, v_rows, stream=None):
+    """Values of logical tokens [t_begin, t_begin + n) of one sequence (page_table: its row) -> bf16 rows [n, Hkv, 128]; either may be None."""
+    bf16, i32 = (_types or _torch_types())[:2]
+    if page_table.numel() * cache.page_size < t_begin + n:
+        raise CpArgumentError("page_table has %d entries for %d tokens" % (page_table.numel(), t_begin + n))
+    shape = (n, cache.Hkv, 128)
+    rc = load().cp_kv_gather_mx4(ctx._h, _described(ctx, cache, cp_kv_cache_mx4), _arg(ctx, page_table, "page_table", i32, page_table.shape) or None, t_begin, n,
+                                 None if k_rows is None else _arg(ctx, k_rows, "k_rows", bf16, shape),
+                                 None if v_rows is None else _arg(ctx, v_rows, "v_rows", bf16, shape), _raw_stream(ctx, stream))
+    if rc != CP_OK:
+        _check(rc)
+
+
+def cp_decode_attn_mx4(ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream=None):
+    """cp_decode_attn over a 4-bit cache."""
+    _decode_attn(load().cp_decode_attn_mx4, cp_kv_cache_mx4, ctx, q, cache, page_table, kv_len, window, sinks, scale, out, lse, workspace, stream)
+
+
+# ------------------------------------------------------------------------------------------------
+# Trees of drafted tokens
+# ------------------------------------------------------------------------------------------------
+
+def cp_tree_plan(ctx, parent, tree_len, kv_len, mask, positions, token_seq, token_slot, stream=None):
+    """parent [B, n_q] int32 (-1: the sequence itself), tree_len [B] int32 or None, kv_len [B] int32, the drafted tokens included -> mask [B, n_q] int64,
+    positions [n_axes, B * n_q], token_seq and token_slot [B * n_q] int32, as cp_tree_attn and cp_rope_append take them."""
+    types = _types or _torch_types()
+    i32, i64 = types[1], types[4]
+    B, n_q = parent.shape
+    axes = positions.shape[0]
+    rc = load().cp_tree_plan(ctx._h, _arg(ctx, parent, "parent", i32, (B, n_q)), None if tree_len is None else _arg(ctx, tree_len, "tree_len", i32, (B,)),
+                             _arg(ctx, kv_len, "kv_len", i32, (B,)), B, n_q, axes, _arg(ctx, mask, "mask", i64, (B, n_q)),
+                             _arg(ctx, positions, "positions", i32, (axes, B * n_q)), _arg(ctx, token_seq, "token_seq", i32, (B * n_q,)),
+                             _arg(ctx, token_slot, "token_slot", i32, (B * n_q,)), _raw_stream(ctx, stream))
+    if rc != CP_OK:
+        _check(rc)
+
+
+def cp_workspace_bytes_tree(B, n_q, Hq, Hkv) -> int:
+    return int(load().cp_workspace_bytes_tree(B, n_q, Hq, Hkv))
+
+
+def _tree_attn(call, kind, ctx, q, cache, page_table, kv_len, tree_len, mask, window, sinks, scale, out, lse, workspace, stream):
+    bf16, i32, f32, _, i64 = _types or _torch_types()
+    shape = q.shape
+    B, n_q, Hq, _ = shape
+    stride = page_table.shape[1]
+    ws, ws_bytes = _workspace(ctx, workspace)
+    rc = call(ctx._h, _arg(ctx, q, "q", bf16, (B, n_q, Hq, 128)), _described(ctx, cache, kind), _arg(ctx, page_table, "page_table", i32, (B, stride)), stride,
+              _arg(ctx, kv_len, "kv_len", i32, (B,)), None if tree_len is None else _arg(ctx, tree_len, "tree_len", i32, (B,)),
+              _arg(ctx, mask, "mask", i64, (B, n_q)), B, n_q, Hq, window, sinks, scale, _arg(ctx, out, "out", bf16, shape),
+              _arg(ctx, lse, "lse", f32, (Hq, B * n_q)), ws, ws_bytes, _raw_stream(ctx, stream))
+    if rc != CP_OK:
+        _check(rc)
+
+
+def cp_tree_attn(ctx, q, cache, page_table, kv_len, tree_len, mask, window, sinks, scale, out, lse, workspace, stream=None):
+    """cp_decode_attn where the last tree_len[b] (None: n_q) tokens of sequence b are a tree: row t sees the drafted tokens of mask[b, t] (int64 bits)."""
+    _tree_attn(load().cp_tree_attn, cp_kv_cache, ctx, q, cache, page_table, kv_len, tree_len, mask, window, sinks, scale, out, lse, workspace, stream)
+
+
+def cp_tree_attn_fp8(ctx, q, cache, page_table, kv_len, tree_len, mask, window, sinks, scale, out, lse, workspace, stream=None):
+    """cp_tree_attn over an FP8 cache."""
+    _tree_attn(load().cp_tree_attn_fp8, cp_kv_cache_fp8, ctx, q, cache, page_table, kv_len, tree_len, mask, window, sinks, scale, out, lse, workspace, stream)
+
+
+def cp_tree_attn_mx4(ctx, q, cache, page_table, kv_len, tree_len, mask, window, sinks, scale, out, lse, workspace, stream=None):
+    """cp_tree_attn over a 4-bit cache."""
+    _tree_attn(load().cp_tree_attn_mx4, cp_kv_cache_mx4, ctx, q, cache, page_table, kv_len, tree_len, mask, window, sinks, scale, out, lse, workspace, stream)
+
+
+def cp_tree_commit(ctx, pool, page_table, kv_len, tree_len, parent, accepted, path, stream=None):
+    """Keep the drafted token accepted[b] (-1: none) and its ancestors: their rows move to the first slots behind the sequence in every layer, kv_len[b]
+    follows, path [B, n_q] receives their numbers, then -1."""
+    i32 = (_types or _torch_types())[1]
+    B, n_q = parent.shape
+    stride = page_table.shape[1]
+    rc = load().cp_tree_commit(ctx._h, _described(ctx, pool, cp_page_pool), _arg(ctx, page_table, "page_table", i32, (B, stride)), stride,
+                               _arg(ctx, kv_len, "kv_len", i32, (B,)), None if tree_len is None else _arg(ctx, tree_len, "tree_len", i32, (B,)),
+                               _arg(ctx, parent, "parent", i32, (B, n_q)), _arg(ctx, accepted, "accepted", i32, (B,)), B, n_q,
+                               _arg(ctx, path, "path", i32, (B, n_q)), _raw_stream(ctx, stream))
+    if rc != CP_OK:
+        _check(rc)
+
+
+def make_page_pool_mx4(k, v) -> cp_page_pool:
+    """make_page_pool for 4-bit caches: k, v [layers, num_pages, page_size, bytes] uint8, or lists of such 3-D tensors; the page calls move the rows' bytes."""
+    ks, vs = [k[i] for i in range(len(k))], [v[i] for i in range(len(v))]
+    if len(ks) != len(vs) or not ks:
+        raise CpArgumentError("make_page_pool_mx4: %d layers of k, %d of v" % (len(ks), len(vs)))
+    first = ks[0]
+    if first.dim() != 3 or first.stride(2) != 1 or first.shape[2] % 16:
+        raise CpArgumentError("make_page_pool_mx4: a layer is [num_pages, page_size, bytes] with rows of whole 16-byte pieces, got %s with strides %s"
+                              % (tuple(first.shape), first.stride()))
+    for t in ks[1:] + vs:
+        _same(first, t, "make_page_pool_mx4")
+    p = cp_page_pool()
+    p.device = _on_cuda(first, ("torch.uint8",), "make_page_pool_mx4")
+    _layers(p, ks, vs)
+    p.num_pages, p.page_size, p.Hkv, p.row_bytes = first.shape[0], first.shape[1], first.shape[2] // 16, 16
+    p.stride_page, p.stride_tok, p.stride_head = first.stride(0), first.stride(1), 16
+    return p
+
+
 def make_page_pool(k, v, num_pages=None) -> cp_page_pool:
     """Describe the K and V pools of one numbering of pages: k, v [layers, num_pages, page_size, Hkv, 128], or lists of such 4-D
     tensors, bf16 or uint8 (E4M3); all of one geometry."""
@@ -628,10 +791,7 @@ def make_page_pool(k, v, num_pages=None) -> cp_page_pool:
     e = first.element_size()
     p = cp_page_pool()
     p.device = device
-    p._k = (ctypes.c_void_p * len(ks))(*[t.data_ptr() for t in ks])        # kept alive with the descriptor
-    p._v = (ctypes.c_void_p * len(vs))(*[t.data_ptr() for t in vs])
-    p.k, p.v = ctypes.addressof(p._k), ctypes.addressof(p._v)
-    p.n_layers = len(ks)
+    _layers(p, ks, vs)
     p.num_pages, p.page_size, p.Hkv, p.row_bytes = first.shape[0], first.shape[1], first.shape[2], 128 * e
     p.stride_page, p.stride_tok, p.stride_head = first.stride(0) * e, first.stride(1) * e, first.stride(2) * e
     return p

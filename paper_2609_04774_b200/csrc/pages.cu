@@ -480,6 +480,106 @@ copy_apply_kernel(PoolGeom g, const __grid_constant__ LayerPtrs layers, const in
     copy_moves(g, layers, moves, *n_moves, blockIdx.x, gridDim.x);
 }
 
+// Commit of an accepted path, first launch: which drafted tokens are on it (their numbers grow along it), and the new lengths.
+constexpr int kMaxTree = 64;
+__global__ void __launch_bounds__(kMaxTree)
+tree_path_kernel(int32_t* kv_len, const int32_t* tree_len, const int32_t* parent, const int32_t* accepted, int32_t n_q, int32_t* path, int32_t* status) {
+    __shared__ int32_t up[kMaxTree];
+    __shared__ unsigned long long nodes;
+    let_next_launch_begin();
+    const int b = blockIdx.x, t = threadIdx.x;
+    const int len = max(kv_len[b], 0), m = min(max(tree_len ? tree_len[b] : n_q, 0), min(n_q, len));
+    if (t < n_q) up[t] = parent[(int64_t)b * n_q + t];
+    __syncthreads();
+    if (t == 0) {
+        int at = accepted[b];
+        if (at < -1 || at >= m) {
+            report_status(status, CP_ERR_BOUNDS, b, at);
+            at = -1;
+        }
+        unsigned long long on = 0;
+        while (at >= 0) {                                  // a parent comes before its child, so this ends
+            on |= 1ull << at;
+            const int to = up[at];
+            if (to < -1 || to >= at) report_status(status, CP_ERR_BOUNDS, (int64_t)b * n_q + at, to);
+            at = to >= at ? -1 : to;
+        }
+        nodes = on;
+        kv_len[b] = len - m + __popcll(on);
+    }
+    __syncthreads();
+    const unsigned long long on = nodes;
+    const int n = __popcll(on);
+    if (t >= n && t < n_q) path[(int64_t)b * n_q + t] = -1;
+    if (on >> t & 1) path[(int64_t)b * n_q + __popcll(on & ((1ull << t) - 1))] = t;
+}
+
+// Second launch: the rows move, HBM-bound (each is read and written once).  A thread has one 16-byte column of a layer's K or V and takes the path's
+// tokens in order: slot base + i is written after base + n_i was read, and as n_i >= i and the n_i grow, no later token is read from a slot that has
+// been written.  Eight loads are in flight per thread.
+constexpr int kCommitBatch = 8;
+__global__ void __launch_bounds__(kCopyThreads)
+tree_move_kernel(PoolGeom g, const __grid_constant__ LayerPtrs layers, const int32_t* table, int64_t table_stride, const int32_t* kv_len, int32_t n_q,
+                 const int32_t* path, int32_t* status) {
+    __shared__ int64_t from[kMaxTree], to[kMaxTree];
+    __shared__ int32_t n_moves;
+    const int b = blockIdx.y;
+    wait_for_launch_before();
+    if (threadIdx.x < 32) {                                // the moves, in order: tokens that stay and tokens without a page are left out
+        const int32_t* nodes = path + (int64_t)b * n_q;
+        int n = 0;
+        for (int i = threadIdx.x; i < n_q; i += 32) n += nodes[i] >= 0;
+        n = __reduce_add_sync(0xffffffffu, n);
+        const int64_t base = (int64_t)kv_len[b] - n;
+        int count = 0;
+        for (int i0 = 0; i0 < n; i0 += 32) {
+            const int i = i0 + threadIdx.x;
+            bool move = false;
+            int64_t off[2] = {0, 0};
+            if (i < n && nodes[i] != i) {
+                move = true;
+                for (int k = 0; k < 2; ++k) {
+                    const int64_t slot = base + (k ? i : nodes[i]), entry = slot >> g.page_shift;
+                    const int32_t page = entry < table_stride ? table[b * table_stride + entry] : -1;
+                    if (page < 0 || page >= g.num_pages) {
+                        if (blockIdx.x == 0) report_status(status, CP_ERR_BOUNDS, b * table_stride + entry, page);
+                        move = false;
+                        break;
+                    }
+                    off[k] = page * g.stride_page + (slot & (g.page_size - 1)) * g.stride_tok;
+                }
+            }
+            const uint32_t hit = __ballot_sync(0xffffffffu, move);
+            if (move) {
+                const int at = count + __popc(hit & ((1u << threadIdx.x) - 1));
+                from[at] = off[0];
+                to[at] = off[1];
+            }
+            count += __popc(hit);
+        }
+        if (threadIdx.x == 0) n_moves = count;
+    }
+    __syncthreads();
+    const int n = n_moves;
+    if (n == 0) return;
+    const int vecs = g.Hkv << g.row_vec_shift;             // columns of a token in one tensor
+    const int64_t columns = (int64_t)g.n_layers * 2 * vecs;
+    for (int64_t c = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; c < columns; c += (int64_t)gridDim.x * kCopyThreads) {
+        const int tensor = (int)(c / vecs), col = (int)(c - (int64_t)tensor * vecs);
+        uint8_t* base = static_cast<uint8_t*>(tensor & 1 ? layers.v[tensor >> 1] : layers.k[tensor >> 1]) +
+                        (int64_t)(col >> g.row_vec_shift) * g.stride_head + (col & ((1 << g.row_vec_shift) - 1)) * 16;
+        for (int i0 = 0; i0 < n; i0 += kCommitBatch) {
+            uint4 x[kCommitBatch];
+#pragma unroll
+            for (int i = 0; i < kCommitBatch; ++i)
+                if (i0 + i < n) x[i] = *reinterpret_cast<const uint4*>(base + from[i0 + i]);
+#pragma unroll
+            for (int i = 0; i < kCommitBatch; ++i)
+                if (i0 + i < n) *reinterpret_cast<uint4*>(base + to[i0 + i]) = x[i];
+        }
+    }
+}
+
 int check_pool(const cp_page_pool* p, bool copies, PoolGeom& g, LayerPtrs* layers, const char* who) {
     if (!p || p->num_pages < 1) return set_error(CP_ERR_INVALID_ARG, "%s: pool is NULL or empty", who);
     if (p->page_size != 16 && p->page_size != 32 && p->page_size != 64 && p->page_size != 128)
@@ -494,8 +594,9 @@ int check_pool(const cp_page_pool* p, bool copies, PoolGeom& g, LayerPtrs* layer
         return set_error(CP_ERR_INVALID_ARG, "%s: pool without layers or heads", who);
     if (p->n_layers > CP_POOL_MAX_LAYERS || p->Hkv > 4096)
         return set_error(CP_ERR_UNSUPPORTED, "%s: %d layers (at most %d), %d heads", who, p->n_layers, CP_POOL_MAX_LAYERS, p->Hkv);
-    if (p->row_bytes != 256 && p->row_bytes != 128)
-        return set_error(CP_ERR_UNSUPPORTED, "%s: row_bytes=%d; a head row has 256 (bf16) or 128 bytes (E4M3)", who, p->row_bytes);
+    if (p->row_bytes != 256 && p->row_bytes != 128 && p->row_bytes != 16)
+        return set_error(CP_ERR_UNSUPPORTED, "%s: row_bytes=%d; a head row has 256 (bf16) or 128 bytes (E4M3), a piece of a 4-bit token row 16", who,
+                         p->row_bytes);
     if (((p->stride_page | p->stride_tok | p->stride_head) & 15) || p->stride_page < 1 || p->stride_tok < 1 || p->stride_head < 1)
         return set_error(CP_ERR_UNSUPPORTED, "%s: strides must be positive multiples of 16 bytes", who);
     for (int32_t l = 0; l < p->n_layers; ++l) {
@@ -509,7 +610,7 @@ int check_pool(const cp_page_pool* p, bool copies, PoolGeom& g, LayerPtrs* layer
     g.stride_tok = p->stride_tok;
     g.stride_head = p->stride_head;
     g.Hkv = p->Hkv;
-    g.row_vec_shift = p->row_bytes == 256 ? 4 : 3;
+    g.row_vec_shift = log2_exact(p->row_bytes / 16);
     g.n_layers = p->n_layers;
     g.contiguous = p->stride_head == p->row_bytes && p->stride_tok == (int64_t)p->Hkv * p->row_bytes;
     return CP_OK;
@@ -673,4 +774,28 @@ extern "C" int cp_pages_copy(cp_ctx* ctx, const cp_page_pool* pool, const int32_
                                                                                                                 ctx->d_status);
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
     return launch_behind(copy_apply_kernel, dim3(copy_grid(ctx, g, n)), kCopyThreads, s, who, g, layers, (const int32_t*)n_moves, (const Move*)moves);
+}
+
+extern "C" int cp_tree_commit(cp_ctx* ctx, const cp_page_pool* pool, const int32_t* page_table, int64_t table_stride, int32_t* kv_len,
+                              const int32_t* tree_len, const int32_t* parent, const int32_t* accepted, int32_t B, int32_t n_q, int32_t* path,
+                              void* stream) {
+    const char* who = "cp_tree_commit";
+    PoolGeom g;
+    LayerPtrs layers;
+    if (int rc = check_pool(pool, true, g, &layers, who)) return rc;
+    if (B < 0 || n_q < 1) return set_error(CP_ERR_INVALID_ARG, "%s: B=%d n_q=%d", who, B, n_q);
+    if (n_q > kMaxTree || B > 65535) return set_error(CP_ERR_UNSUPPORTED, "%s: n_q=%d (at most 64), B=%d (at most 65535)", who, n_q, B);
+    if (!ctx) return set_error(CP_ERR_INVALID_ARG, "%s: ctx is NULL", who);
+    if (B == 0) return CP_OK;
+    if (int rc = check_table(page_table, B, table_stride, g, who)) return rc;
+    if (!kv_len || !parent || !accepted || !path) return set_error(CP_ERR_INVALID_ARG, "%s: null pointer", who);
+    DeviceGuard guard(ctx->device);
+    if (guard.rc()) return guard.rc();
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    tree_path_kernel<<<(unsigned)B, kMaxTree, 0, s>>>(kv_len, tree_len, parent, accepted, n_q, path, ctx->d_status);
+    if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
+    const int64_t columns = (int64_t)g.n_layers * 2 * ((int64_t)g.Hkv << g.row_vec_shift);
+    const unsigned blocks = (unsigned)std::min<int64_t>((columns + kCopyThreads - 1) / kCopyThreads, 4096);
+    return launch_behind(tree_move_kernel, dim3(blocks, (unsigned)B), kCopyThreads, s, who, g, layers, page_table, table_stride, (const int32_t*)kv_len, n_q,
+                         (const int32_t*)path, ctx->d_status);
 }

@@ -99,12 +99,103 @@ __device__ __forceinline__ uint2 quantize8(const float (&x)[8], float sc, float 
     return a;
 }
 
+// ---- 4-bit blocks.  A head is owned by eight lanes, two chunks of eight elements each, which may lie in any of its four blocks.
+// A code depends on where a value lies between the format's few borders and an exponent on which side of a power of two the block's largest
+// is, so the fp32 rotation (off by less than kTurnError times the pair's magnitudes: 2^-23 from the angle, 2^-23 from the sine and cosine, three
+// roundings of 2^-24) is only trusted where values that much smaller and larger give the same codes and exponents; otherwise the head is
+// rotated again in fp64 (about one head in ten thousand).  16384 tokens: see the figures above.
+constexpr float kTurnError = 5e-7f;
+
+// E2M1 codes of two values, the first in the low half: nearest, ties to even, saturating at 6.
+__device__ __forceinline__ uint32_t e2m1x2(float a, float b) {
+    uint32_t d;
+    asm("{\n\t.reg .b8 c;\n\tcvt.rn.satfinite.e2m1x2.f32 c, %2, %1;\n\tcvt.u32.u8 %0, c;\n\t}" : "=r"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t e2m1x8(const float (&x)[8]) {
+    return e2m1x2(x[0], x[1]) | e2m1x2(x[2], x[3]) << 8 | e2m1x2(x[4], x[5]) << 16 | e2m1x2(x[6], x[7]) << 24;
+}
+// Largest exponent field (255: an infinity or NaN is there) of eight values, each changed by `by` towards larger (by > 0) or smaller magnitudes.
+__device__ __forceinline__ uint32_t exponent8(const float (&x)[8], float by) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    if (top >= 0x7f800000u) return 255;
+    return __float_as_uint(fmaxf(__uint_as_float(top) + by, 0.f)) >> 23;
+}
+// Exponents of the head's four blocks, a byte each, from those of this lane's two chunks.
+__device__ __forceinline__ uint32_t block_exponents(uint32_t ea, int ca, uint32_t eb, int cb, uint32_t lanes) {
+    uint32_t w = ca >> 2 == cb >> 2 ? max(ea, eb) << (8 * (ca >> 2)) : ea << (8 * (ca >> 2)) | eb << (8 * (cb >> 2));
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) w = __vmaxu4(w, __shfl_xor_sync(lanes, w, o));
+    return w;
+}
+// Exponent byte of a block whose largest magnitude has exponent field f: two less (6 = 1.5 2^2 is the largest code), at least 0.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t f) { return f == 255 ? 255u : (f > 2 ? f - 2 : 0u); }
+// 2^(127 - byte), exact; byte <= 252 (255: any)
+__device__ __forceinline__ float scale_up(uint32_t byte) { return __uint_as_float((byte > 253 ? 1u : 254u - byte) << 23); }
+// x as fp32 so that every border of a shorter format is on the right side: inexact values get an odd last bit.
+__device__ __forceinline__ float to_odd(double x) {
+    const float f = __double2float_rz(x);
+    return (double)f == x || !(fabsf(f) < INFINITY) ? f : __uint_as_float(__float_as_uint(f) | 1u);
+}
+
 // kPairs: pair i is elements (2i, 2i + 1) of a head, else (i, i + rot / 2).  A lane owns two chunks of 8 elements of a head, ca and
 // cb, and eight pairs: interleaved, four in each chunk; half layout, element j of ca with element j of cb.  Lanes whose chunks lie
 // behind the rotated part copy them.
-template <bool kPairs, bool kFp8>
-__global__ void __launch_bounds__(kRopeThreads, 4)
+// The codes and exponent fields of a lane's two chunks from a rotation in fp64 (one lane of every eight that own a head asks for it).
+template <bool kPairs>
+__device__ __noinline__ void exact_codes(const RopeParams& p, int t, uint4 ra, uint4 rb, int ca, int cb, bool turn_a, bool turn_b, uint32_t lanes,
+                                         uint32_t& f, uint32_t& codes_a, uint32_t& codes_b) {
+    float ia[8], ib[8];
+    unpack8(ra, ia);
+    unpack8(rb, ib);
+    double xa[8], xb[8];
+#pragma unroll 1
+    for (int j = 0; j < 8; ++j) {
+        xa[j] = ia[j];
+        xb[j] = ib[j];
+    }
+    auto turn = [&](int pair, double& a, double& b) {
+        const int64_t pos = p.positions[(int64_t)p.axis[pair] * p.n + t];
+        double s, c;
+        sincospi((double)(int64_t)((uint64_t)pos * p.step[pair]) * 1.08420217248550443400745280086994171e-19, &s, &c);      // 2^-63: half turns
+        const double u = a * c - b * s, w = b * c + a * s;
+        a = u;
+        b = w;
+    };
+#pragma unroll 1
+    for (int j = 0; j < 4; ++j) {
+        if (kPairs) {
+            if (turn_a) turn(4 * ca + j, xa[2 * j], xa[2 * j + 1]);
+            if (turn_b) turn(4 * cb + j, xb[2 * j], xb[2 * j + 1]);
+        } else if (turn_a) {
+            turn(8 * ca + j, xa[j], xb[j]);
+            turn(8 * ca + j + 4, xa[j + 4], xb[j + 4]);
+        }
+    }
+    float ya[8], yb[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        ya[j] = to_odd(xa[j]);
+        yb[j] = to_odd(xb[j]);
+    }
+    f = block_exponents(exponent8(ya, 0.f), ca, exponent8(yb, 0.f), cb, lanes);
+    const float ua = scale_up(scale_byte(f >> (8 * (ca >> 2)) & 255)), ub = scale_up(scale_byte(f >> (8 * (cb >> 2)) & 255));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        ya[j] *= ua;
+        yb[j] *= ub;
+    }
+    codes_a = e2m1x8(ya);
+    codes_b = e2m1x8(yb);
+}
+
+enum Form : int { kRows16, kRows8, kRows4 };       // bf16, E4M3, 4-bit blocks
+template <bool kPairs, Form kForm>
+__global__ void __launch_bounds__(kRopeThreads, kForm == kRows4 ? 3 : 4)
 rope_append_kernel(const __grid_constant__ RopeParams p) {
+    constexpr bool kFp8 = kForm == kRows8, kMx = kForm == kRows4;
     const int lane = threadIdx.x & 31;
     const int sub = lane & 7, grp = lane >> 3;
     const int64_t w = ((int64_t)blockIdx.x * kRopeThreads + threadIdx.x) >> 5;
@@ -188,7 +279,7 @@ rope_append_kernel(const __grid_constant__ RopeParams p) {
         if (!locate(s, kind, h, heads) || (kind > 0 && tok_off < 0)) continue;
         uint4 oa = ra, ob = rb;
         float xa[8], xb[8];
-        if (kind < 2 || kFp8) {
+        if (kind < 2 || kFp8 || kMx) {
             unpack8(ra, xa);
             unpack8(rb, xb);
         }
@@ -224,7 +315,59 @@ rope_append_kernel(const __grid_constant__ RopeParams p) {
             dst[cb] = ob;
         } else {
             uint8_t* dst = (kind == 1 ? p.cache_k : p.cache_v) + tok_off + (int64_t)h * p.stride_head;
-            if (kFp8) {
+            if (kMx) {
+                const uint32_t lanes = 0xffu << (8 * grp);
+                // how far xa, xb may be off: a lane's pairs have one element in each chunk (half layout) or both in one
+                float err_a = 0.f, err_b = 0.f;
+                if (kind == 1 && (turn_a || turn_b)) {
+                    float in_a[8], in_b[8];
+                    unpack8(ra, in_a);
+                    unpack8(rb, in_b);
+                    float ma = 0.f, mb = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        ma = fmaxf(ma, fabsf(in_a[j]));
+                        mb = fmaxf(mb, fabsf(in_b[j]));
+                    }
+                    err_a = turn_a ? kTurnError * (kPairs ? 2.f * ma : ma + mb) : 0.f;
+                    err_b = turn_b ? kTurnError * (kPairs ? 2.f * mb : ma + mb) : 0.f;
+                }
+                uint32_t f = block_exponents(exponent8(xa, -err_a), ca, exponent8(xb, -err_b), cb, lanes);
+                bool unsure = false;
+                if (kind == 1) unsure = f != block_exponents(exponent8(xa, err_a), ca, exponent8(xb, err_b), cb, lanes);
+                uint32_t codes_a, codes_b;
+                auto code8 = [&](const float (&x)[8], int chunk, float err, bool& differ) {
+                    const float up = scale_up(scale_byte(f >> (8 * (chunk >> 2)) & 255));
+                    float y[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) y[j] = x[j] * up;
+                    const uint32_t c = e2m1x8(y);
+                    if (kind == 1) {
+                        float lo[8], hi[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            lo[j] = y[j] - err * up;
+                            hi[j] = y[j] + err * up;
+                        }
+                        // (the sign of a value that may be zero does not count: both codes are zeros)
+                        const uint32_t l = e2m1x8(lo), u = e2m1x8(hi), d = (l ^ u) & 0x77777777u;
+                        differ = d != 0 || (err > 0.f && ((l ^ u) & 0x88888888u & ~(c << 1 | c << 2 | c << 3)) != 0);
+                    }
+                    return c;
+                };
+                bool da = false, db = false;
+                codes_a = code8(xa, ca, err_a, da);
+                codes_b = code8(xb, cb, err_b, db);
+                if (kind == 1 && __any_sync(lanes, unsure || da || db)) {
+                    exact_codes<kPairs>(p, t, ra, rb, ca, cb, turn_a, turn_b, lanes, f, codes_a, codes_b);
+                }
+                reinterpret_cast<uint32_t*>(dst)[ca] = codes_a;
+                reinterpret_cast<uint32_t*>(dst)[cb] = codes_b;
+                if (sub == 0) {
+                    const uint32_t e = scale_byte(f & 255) | scale_byte(f >> 8 & 255) << 8 | scale_byte(f >> 16 & 255) << 16 | scale_byte(f >> 24) << 24;
+                    *reinterpret_cast<uint32_t*>(dst + (int64_t)(p.Hkv - h) * p.stride_head + h * 4) = e;
+                }
+            } else if (kFp8) {
                 const float sc = kind == 1 ? p.k_scale[h] : p.v_scale[h];
                 const float inv = __frcp_rn(sc);
                 reinterpret_cast<uint2*>(dst)[ca] = quantize8(xa, sc, inv);
@@ -241,7 +384,7 @@ int rope_append(cp_ctx* ctx, const cp_rope* rope, const void* q, const void* k_r
                 const int32_t* positions, const int32_t* token_seq, const int32_t* token_slot, const int32_t* page_table,
                 int64_t table_rows, int64_t table_stride, void* q_out, const void* ck, const void* cv, const float* k_scale,
                 const float* v_scale, int64_t num_pages, int32_t page_size, int32_t Hkv, int64_t stride_page, int64_t stride_tok,
-                int64_t stride_head, bool fp8, void* stream, const char* who) {
+                int64_t stride_head, Form form, void* stream, const char* who) {
     if (!rope || n < 0 || (n > 0 && (!positions || !token_seq)))
         return set_error(CP_ERR_INVALID_ARG, "%s: null pointer or negative token count", who);
     if (rope->n_axes < 1 || rope->n_axes > CP_ROPE_MAX_AXES || rope->rot_dims < 2 || rope->rot_dims > kHeadDim)
@@ -315,13 +458,11 @@ int rope_append(cp_ctx* ctx, const cp_rope* rope, const void* q, const void* k_r
     const int64_t blocks = (n * p.parts + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
     if (blocks > 0x7fffffffll) return set_error(CP_ERR_UNSUPPORTED, "%s: %lld blocks", who, (long long)blocks);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (rope->interleaved) {
-        if (fp8) rope_append_kernel<true, true><<<(unsigned)blocks, kRopeThreads, 0, s>>>(p);
-        else rope_append_kernel<true, false><<<(unsigned)blocks, kRopeThreads, 0, s>>>(p);
-    } else {
-        if (fp8) rope_append_kernel<false, true><<<(unsigned)blocks, kRopeThreads, 0, s>>>(p);
-        else rope_append_kernel<false, false><<<(unsigned)blocks, kRopeThreads, 0, s>>>(p);
-    }
+    const bool pairs_of_two = rope->interleaved != 0;
+    void (*kernel)(const RopeParams) = form == kRows4 ? (pairs_of_two ? rope_append_kernel<true, kRows4> : rope_append_kernel<false, kRows4>)
+                                       : form == kRows8 ? (pairs_of_two ? rope_append_kernel<true, kRows8> : rope_append_kernel<false, kRows8>)
+                                                        : (pairs_of_two ? rope_append_kernel<true, kRows16> : rope_append_kernel<false, kRows16>);
+    kernel<<<(unsigned)blocks, kRopeThreads, 0, s>>>(p);
     return check_cuda(cudaGetLastError(), who);
 }
 
@@ -359,7 +500,7 @@ extern "C" int cp_rope_append(cp_ctx* ctx, const cp_rope* rope, const void* q, c
     if (int rc = validate_kv_cache(cache, who)) return rc;
     return rope_append(ctx, rope, q, k_rows, v_rows, n, Hq, positions, token_seq, token_slot, page_table, table_rows, table_stride,
                        q_out, cache->k, cache->v, nullptr, nullptr, cache->num_pages, cache->page_size, cache->Hkv,
-                       cache->stride_page * 2, cache->stride_tok * 2, cache->stride_head * 2, false, stream, who);
+                       cache->stride_page * 2, cache->stride_tok * 2, cache->stride_head * 2, kRows16, stream, who);
 }
 
 extern "C" int cp_rope_append_fp8(cp_ctx* ctx, const cp_rope* rope, const void* q, const void* k_rows, const void* v_rows, int64_t n,
@@ -370,5 +511,16 @@ extern "C" int cp_rope_append_fp8(cp_ctx* ctx, const cp_rope* rope, const void* 
     if (int rc = validate_kv_cache_fp8(cache, who)) return rc;
     return rope_append(ctx, rope, q, k_rows, v_rows, n, Hq, positions, token_seq, token_slot, page_table, table_rows, table_stride,
                        q_out, cache->k, cache->v, cache->k_scale, cache->v_scale, cache->num_pages, cache->page_size, cache->Hkv,
-                       cache->stride_page, cache->stride_tok, cache->stride_head, true, stream, who);
+                       cache->stride_page, cache->stride_tok, cache->stride_head, kRows8, stream, who);
+}
+
+extern "C" int cp_rope_append_mx4(cp_ctx* ctx, const cp_rope* rope, const void* q, const void* k_rows, const void* v_rows, int64_t n,
+                                  int32_t Hq, const int32_t* positions, const int32_t* token_seq, const int32_t* token_slot,
+                                  const cp_kv_cache_mx4* cache, const int32_t* page_table, int64_t table_rows, int64_t table_stride,
+                                  void* q_out, void* stream) {
+    const char* who = "cp_rope_append_mx4";
+    if (int rc = validate_kv_cache_mx4(cache, who)) return rc;
+    return rope_append(ctx, rope, q, k_rows, v_rows, n, Hq, positions, token_seq, token_slot, page_table, table_rows, table_stride,
+                       q_out, cache->k, cache->v, nullptr, nullptr, cache->num_pages, cache->page_size, cache->Hkv, cache->stride_page,
+                       cache->stride_tok, 64, kRows4, stream, who);
 }

@@ -14,7 +14,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libcpattn.so")
-SOURCES = ["ctx.cu", "plan.cpp", "cache_manager.cpp", "merge.cu", "kv_copy.cu", "attn_sm100.cu", "rope.cu", "pages.cu", "decode.cu", "mx4.cu", "tree.cu"]
+SOURCES = ["ctx.cu", "plan.cpp", "cache_manager.cpp", "merge.cu", "kv_copy.cu", "attn_sm100.cu", "rope.cu", "pages.cu", "decode.cu", "mx4.cu", "tree.cu", "tree_wide.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
@@ -35,7 +35,7 @@ def _stale(target: str, deps) -> bool:
 
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile every source to an object in ``build/`` and link ``libcpattn.so``.  Returns its path."""
-    headers = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "attn_kernel.cuh"), os.path.join(CSRC, "device_util.cuh"), os.path.join(CSRC, "decode_kernel.cuh"), os.path.join(ROOT, "include", "cpattn.h"),
+    headers = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "attn_kernel.cuh"), os.path.join(CSRC, "device_util.cuh"), os.path.join(CSRC, "decode_kernel.cuh"), os.path.join(CSRC, "tc_ptx.cuh"), os.path.join(CSRC, "tree_wide.cuh"), os.path.join(ROOT, "include", "cpattn.h"),
                os.path.join(ROOT, "include", "cpcache.h"), os.path.abspath(__file__)]
     objdir = os.path.join(_HERE, "build")
     os.makedirs(objdir, exist_ok=True)

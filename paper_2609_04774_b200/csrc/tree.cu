@@ -52,11 +52,16 @@ tree_plan_kernel(const int32_t* parent, const int32_t* tree_len, const int32_t* 
     token_slot[at] = t < m ? base + t : 0;
 }
 
+// Up to 32 rows per KV head take the narrow form, which reads the keys once for them.
+constexpr int kNarrowRows = 32;
+
 template <typename Cache>
 int tree_attn(cp_ctx* ctx, const void* q, const Cache* cache, const int32_t* page_table, int64_t table_stride, const int32_t* kv_len,
               const int32_t* tree_len, const uint64_t* mask, int32_t B, int32_t n_q, int32_t Hq, int64_t window, int64_t sinks, float scale,
               void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream, Kind kind, const char* who) {
     if (B > 0 && !mask) return set_error(CP_ERR_INVALID_ARG, "%s: null pointer", who);
+    if (workspace && workspace_bytes < cp_workspace_bytes_tree(B, n_q, Hq, cache->Hkv))
+        return set_error(CP_ERR_WORKSPACE, "%s: workspace of %zu bytes; need %zu", who, workspace_bytes, cp_workspace_bytes_tree(B, n_q, Hq, cache->Hkv));
     if ((uintptr_t)mask & 7) return set_error(CP_ERR_INVALID_ARG, "%s: mask must be 8-byte aligned", who);
     DecodeParams p;
     if (int rc = decode_params(ctx, q, view_of(cache), page_table, table_stride, kv_len, B, n_q, Hq, window, sinks, scale, out, lse, workspace,
@@ -67,6 +72,8 @@ int tree_attn(cp_ctx* ctx, const void* q, const Cache* cache, const int32_t* pag
     DeviceGuard guard(ctx->device);
     if (guard.rc()) return guard.rc();
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const CacheView view = view_of(cache);
+    if (kind == kBf16 && p.rows > kNarrowRows) return launch_tree_wide(ctx, &p, &view, workspace, stream, who);
     if (kind == kBf16) return launch_rows<1, kBf16, kTree>(ctx, p, s, who);
     if (kind == kE4m3) return p.Hkv % 2 == 0 ? launch_rows<2, kE4m3, kTree>(ctx, p, s, who) : launch_rows<1, kE4m3, kTree>(ctx, p, s, who);
     return p.Hkv % 4 == 0 ? launch_rows<4, kMx4, kTree>(ctx, p, s, who) : launch_rows<1, kMx4, kTree>(ctx, p, s, who);
@@ -91,7 +98,10 @@ extern "C" int cp_tree_plan(cp_ctx* ctx, const int32_t* parent, const int32_t* t
     return check_cuda(cudaGetLastError(), who);
 }
 
-extern "C" size_t cp_workspace_bytes_tree(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv) { return cp_workspace_bytes_decode(B, n_q, Hq, Hkv); }
+extern "C" size_t cp_workspace_bytes_tree(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv) {
+    const size_t narrow = cp_workspace_bytes_decode(B, n_q, Hq, Hkv);
+    return narrow == 0 || (int64_t)n_q * (Hq / Hkv) <= kNarrowRows ? narrow : std::max(narrow, tree_wide_workspace());
+}
 
 extern "C" int cp_tree_attn(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table, int64_t table_stride,
                             const int32_t* kv_len, const int32_t* tree_len, const uint64_t* mask, int32_t B, int32_t n_q, int32_t Hq,

@@ -1,0 +1,687 @@
+// Attention of drafted trees with many query rows per KV head (n_q * Hq / Hkv > 32) on the tcgen05 tensor cores, over paged caches with lengths, masks
+// and page tables on the device.
+//
+// With r rows a key costs 512 r flops and 512 bytes (bf16): at 128 rows half of what the tensor cores can do while the keys arrive, at 264 as
+// much.  The narrow form (decode_kernel.cuh) works such rows off in units of 32 with mma.sync, each reading the keys again; here a CTA takes up to
+// 256 rows, so every key that lands in shared memory is used once by all of them.
+//   - Query row t * G + h of a KV head (token t, head h of the group) is a row of the M side: two 128-row score tiles that share the K/V tiles, one
+//     softmax warpgroup each.  Trees of up to 128 rows use one.
+//   - More than 256 rows are several classes of equal height.  CTA c belongs to class c % classes and walks run c / classes of the key axis, so the
+//     classes read the same keys at the same time and all but one find them in L2.
+//   - The key axis is all (request, KV head) units one after the other, 128 keys a step, cut into equal runs, one per CTA of a class, whatever
+//     the lengths are (the scheme of the narrow form: Cursor); pieces of cut units are joined by a second launch.
+//   - Warps: two softmax warpgroups; a TMA producer that fetches K/V tiles page by page; the issuers of S = Q K^T and of O += P V; a warp that gathers the
+//     unit's query rows.  S, P and O live in TMEM: S | P0 | P1 | O0 | O1.  S is one buffer that the tiles use in turn, read into registers at
+//     once, so the next product runs under the exponentials.
+//   - Only the last tiles of a unit and those at a window's edge hide keys from rows.  Their masks are bits: of the tree's mask and of the window.  A hidden
+//     key's weight is zero, but zero times an infinity is not: the issuer of P V looks through the V of these tiles and clears what is no
+//     finite number; what some rows do see of it is added to their results when they are written.
+// Every wait is bounded, as in the prefill kernel.
+#pragma once
+
+#include "decode_kernel.cuh"
+#include "tc_ptx.cuh"
+
+namespace {
+
+constexpr int kWideThreads = 384;
+constexpr int kWideStages = 5;                             // ring of 32 KB tiles, K and V in turn
+constexpr int kWideRows = 256;                             // query rows of a unit
+constexpr int kWideCost = 3;                               // fixed cost of a unit in tiles: queries, epilogue
+constexpr int kWideRegsSoftmax = 200, kWideRegsOther = 104;
+static_assert(2 * 128 * kWideRegsSoftmax + 128 * kWideRegsOther <= 65536 - 1024, "leave slack in the register file");
+constexpr float kWideLag = 8.0f;                           // the running maximum may lag by a factor 2^8
+constexpr int kWideSplit = 3;                              // P is handed over in two pieces: three quarters of the keys, then the rest
+
+constexpr uint32_t kWideQ = 0;                             // shared memory: two query tiles, the ring, barriers and small areas
+constexpr uint32_t kWideKV = 2 * kTileBytes;
+constexpr uint32_t kWideBar = kWideKV + kWideStages * kTileBytes;
+enum WideBar : uint32_t {
+    kWQFull = 0, kWQEmpty = 1,
+    kWKvFull = 2,                            // + stage
+    kWKvEmpty = kWKvFull + kWideStages,      // + stage
+    kWSReady = kWKvEmpty + kWideStages,      // + tile: its scores are in the S buffer
+    kWSFree = kWSReady + 2,                  // the S buffer has been read
+    kWPReady = kWSFree + 1,                  // + 2 tile + piece
+    kWPvDone = kWPReady + 4,                 // + tile: P V of a step has finished
+    kWOFree = kWPvDone + 2,                  // + tile: O has been read
+    kWOdd = kWOFree + 2,                     // the unit's list of odd keys is complete
+    kNumWideBars = kWOdd + 1
+};
+constexpr uint32_t kWideOdd = kWideBar + (kNumWideBars * 8 + 15) / 16 * 16;      // [unit parity][2] keys whose V is no finite number (see odd_values)
+constexpr uint32_t kWideScan = kWideOdd + 32;              // sums of the warps, then the run's start
+constexpr uint32_t kWideTmemPtr = kWideScan + 12 * 8 + 16, kWideAbort = kWideTmemPtr + 4;
+constexpr uint32_t kWideSmem = kWideAbort + 12 + 1024;     // slack for manual alignment
+static_assert(kWideSmem <= 227 * 1024, "shared memory of a CTA");
+
+constexpr uint32_t kWTmemS = 0, kWTmemP = 128, kWTmemO = 256;      // columns; + 64 and + 128 for the second tile
+
+struct WideParams {
+    DecodeParams d;
+    int32_t classes;           // row classes of a KV head
+    int32_t class_rows;        // rows of a class (the last may have fewer)
+    int32_t tiles;             // score tiles of a unit: 1 or 2
+    int32_t runs;              // CTAs of a class
+};
+
+// The units of this CTA, one after the other: request b, KV head u, tiles [t_begin, t_end).
+struct WideUnits {
+    Cursor<kBlockN, true> cur;
+    int64_t x1;
+    int t_begin, t_end;
+    bool whole;
+    __device__ __forceinline__ void begin(const DecodeParams& p, const int32_t* start, int64_t x0, int64_t end) {
+        cur.b = start[0];
+        cur.u = start[1];
+        cur.t = max(0, start[2] - kWideCost);
+        cur.x = x0 - start[2];
+        cur.r = request_of<kBlockN, true>(p, cur.b);
+        x1 = end;
+        span();
+    }
+    __device__ __forceinline__ void span() {
+        t_begin = cur.t;
+        t_end = (int)min((int64_t)cur.r.n, x1 - cur.x - kWideCost);
+        whole = t_begin == 0 && t_end == cur.r.n;
+    }
+    __device__ __forceinline__ bool valid() const { return cur.x + kWideCost + cur.t < x1; }
+    __device__ __forceinline__ void next(const DecodeParams& p) {
+        cur.t = 0;
+        cur.x += kWideCost + cur.r.n;
+        if (++cur.u == p.Hkv) {
+            cur.u = 0;
+            if (++cur.b < p.B) cur.r = request_of<kBlockN, true>(p, cur.b);
+        }
+        span();
+    }
+    __device__ __forceinline__ int key_of(int t) const { return (t < cur.r.sink_tiles ? t : t + cur.r.skip) * kBlockN; }
+    // every row of the tree sees all keys of the tile
+    __device__ __forceinline__ bool full(const DecodeParams& p, int key0) const {
+        return key0 + kBlockN <= cur.r.base && (key0 >= cur.r.len - p.window || key0 + kBlockN <= p.sinks);
+    }
+};
+
+struct WideCtx {
+    uint32_t smem, bars, tmem;
+    uint8_t* gen;              // the same shared memory
+    volatile uint32_t* abort_flag;
+    int32_t* status;
+    __device__ __forceinline__ void wait(uint32_t id, uint32_t parity, int iter) const { mbar_wait(bars, id, parity, abort_flag, status, iter); }
+};
+struct WideRing {
+    uint32_t slot, par;
+    __device__ __forceinline__ WideRing plus(uint32_t n) const {      // n < 2 kWideStages
+        WideRing r = {slot + n, par};
+        if (r.slot >= (uint32_t)kWideStages) { r.slot -= kWideStages; r.par ^= 1u; }
+        return r;
+    }
+    __device__ __forceinline__ WideRing after(uint32_t n) const {
+        const uint32_t q = n / kWideStages;
+        WideRing r = plus(n - q * kWideStages);
+        r.par ^= q & 1u;
+        return r;
+    }
+};
+
+// ---------------------------------------------------------------------------------------------- producer
+// Load order = order of first use: K(j0), then K(j + 1) before V(j).  Lane i < pages of a tile holds a page id; those of the next K tile are
+// fetched while the current ones are used.  Pages that no row sees anything of are read as zeros.
+__device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx& c, WideUnits units, const CUtensorMap* tmK, const CUtensorMap* tmV) {
+    const DecodeParams& p = w.d;
+    const int lane = threadIdx.x & 31;
+    const int page_tokens = 1 << p.page_shift, per_tile = kBlockN >> p.page_shift;
+    const uint32_t box_bytes = (uint32_t)page_tokens * 128u;
+    const int outside = (int)p.num_pages;                  // a page coordinate behind the tensor: TMA fills zeros
+    uint32_t it = 0;
+    for (; units.valid(); units.next(p)) {
+        const Request r = units.cur.r;
+        const int32_t* row = p.table + units.cur.b * p.table_stride;
+        auto fetch = [&](int t) {
+            const int key0 = units.key_of(t), key = key0 + lane * page_tokens;
+            int id = outside;
+            if (lane < per_tile && key < r.len && (key + page_tokens > r.low(p) || key < p.sinks)) {
+                id = __ldg(row + (key >> p.page_shift));
+                if ((uint32_t)id >= (uint32_t)outside) id = outside;
+            }
+            return id;
+        };
+        int ahead = fetch(units.t_begin), k_ids = 0, v_ids = 0;
+        const int n_loads = 2 * (units.t_end - units.t_begin);
+        int j = units.t_begin;                             // next K tile
+        for (int ld = 0; ld < n_loads; ++ld) {
+            const bool is_v = ld == n_loads - 1 || (ld > 0 && (ld & 1) == 0);
+            int ids;
+            if (!is_v) {
+                v_ids = k_ids;
+                k_ids = ids = ahead;
+                if (++j < units.t_end) ahead = fetch(j);
+            } else {
+                ids = ld == n_loads - 1 ? k_ids : v_ids;
+            }
+            const uint32_t slot = it % kWideStages, fbar = c.bars + (kWKvFull + slot) * 8;
+            const uint32_t dst = c.smem + kWideKV + slot * kTileBytes;
+            if (lane == 0) {
+                c.wait(kWKvEmpty + slot, ((it / kWideStages) & 1) ^ 1, ld);
+                mbar_expect_tx(fbar, kTileBytes);
+            }
+            __syncwarp();
+            if (lane < per_tile) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    tma_load_4d(dst + half * kHalfBytes + lane * box_bytes, is_v ? tmV : tmK, fbar, half * 64, units.cur.u, 0, ids);
+            }
+            __syncwarp();
+            ++it;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- queries
+// Row i of the unit's class is token (r0 + i) / G, head (r0 + i) % G of the group; rows behind the tree are zeros.  128-byte swizzle lines, 64 dims a half.
+__device__ __forceinline__ void wide_queries(const WideParams& w, const WideCtx& c, WideUnits units) {
+    const DecodeParams& p = w.d;
+    const int lane = threadIdx.x & 31;
+    const int r0 = (int)(blockIdx.x % w.classes) * w.class_rows, rows = min(w.class_rows, p.rows - r0);
+    const int chunk = lane & 15;
+    for (int round = 0; units.valid(); units.next(p), ++round) {
+        const int b = units.cur.b, m = units.cur.r.len - units.cur.r.base;
+        const __nv_bfloat16* q = p.q + ((int64_t)b * p.n_q * p.Hq + (int64_t)units.cur.u * p.G) * kDim + chunk * 8;
+        c.wait(kWQEmpty, (round & 1) ^ 1, round);
+        __syncwarp();
+        for (int i = lane >> 4; i < w.tiles * kBlockM; i += 2) {
+            const int t = (r0 + i) / p.G;
+            const bool ok = i < rows && t < m;
+            const __nv_bfloat16* src = ok ? q + ((int64_t)t * p.Hq + (r0 + i - t * p.G)) * kDim : p.q;
+            const int in = i & (kBlockM - 1);
+            cp_async16_or_zeros(c.smem + kWideQ + (i / kBlockM) * kTileBytes + (chunk >> 3) * kHalfBytes + in * 128 + (((chunk & 7) ^ (in & 7)) << 4), src, ok);
+        }
+        cp_commit();
+        cp_wait<0>();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the tensor cores read what these lanes wrote
+        __syncwarp();
+        if (lane == 0) mbar_arrive(c.bars + kWQFull * 8);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- issuers
+__device__ __forceinline__ void wide_scores(const WideParams& w, const WideCtx& c, WideUnits units) {
+    WideRing first = {0, 0};           // ring position of the unit's first load
+    uint32_t s_par = 1;                // parity of "the previous score tile was read"; 1: there is none yet
+    const uint64_t q_desc = make_desc(c.smem + kWideQ, 16, 1024), k_desc = make_desc(c.smem + kWideKV, 16, 1024);
+    for (int round = 0; units.valid(); units.next(w.d), ++round) {
+        const int j0 = units.t_begin, n = units.t_end;
+        c.wait(kWQFull, round & 1, round);
+        WideRing pos = first;
+#pragma unroll 1
+        for (int j = j0; j < n; ++j) {
+            c.wait(kWKvFull + pos.slot, pos.par, j);
+            for (int h = 0; h < w.tiles; ++h) {
+                c.wait(kWSFree, s_par, j);
+                s_par ^= 1u;
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int ks = 0; ks < kD / 16; ++ks) {
+                        const uint32_t off = ((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4;
+                        mma_ss(c.tmem + kWTmemS, q_desc + h * (kTileBytes >> 4) + off, k_desc + pos.slot * (kTileBytes >> 4) + off, kIdescS, ks > 0);
+                    }
+                    tc_commit(c.bars + (kWSReady + h) * 8);
+                    if (h == w.tiles - 1) {
+                        tc_commit(c.bars + (kWKvEmpty + pos.slot) * 8);
+                        if (j == n - 1) tc_commit(c.bars + kWQEmpty * 8);
+                    }
+                }
+                __syncwarp();
+            }
+            pos = pos.plus(j == j0 ? 1 : 2);
+        }
+        first = first.after(2 * (n - j0));
+    }
+}
+
+// The V of a tile that hides keys from some row: keys that no row sees lose what is no finite number; so do those that only some rows
+// see, which are listed (as odd_values takes them).  Those that every row sees keep it: every row becomes that.
+__device__ __forceinline__ void wide_clear(const DecodeParams& p, const Request& r, uint32_t v_tile, int key0, unsigned long long* odd) {
+    const int lane = threadIdx.x & 31, low = r.low(p), low_max = r.len - p.window;
+#pragma unroll 4
+    for (int i = lane; i < 2 * (int)kHalfBytes / 16; i += 32) {
+        const uint4 x = lds128(v_tile + i * 16);
+        const uint32_t bad = not_finite<false>(x.x) | not_finite<false>(x.y) | not_finite<false>(x.z) | not_finite<false>(x.w);
+        if (bad == 0) continue;
+        const int key = key0 + (i >> 3 & (kBlockN - 1));
+        const bool nobody = key >= r.len || (key < low && key >= p.sinks);
+        const bool late = key >= r.base, early = key < low_max && key >= p.sinks;
+        if (!nobody && !late && !early) continue;
+        sts128(v_tile + i * 16, make_uint4(finite_part<false>(x.x), finite_part<false>(x.y), finite_part<false>(x.z), finite_part<false>(x.w)));
+        if (!nobody) atomicOr(odd + (late ? 0 : 1), 1ull << (late ? key - r.base : key - low));
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+}
+
+__device__ __forceinline__ void wide_outputs(const WideParams& w, const WideCtx& c, WideUnits units) {
+    const DecodeParams& p = w.d;
+    const int lane = threadIdx.x & 31;
+    WideRing first = {0, 0};
+    uint32_t p_par = 0;                // parity of "P is there", the same for both tiles
+    const uint64_t v_desc = make_desc(c.smem + kWideKV, kHalfBytes, 1024);
+    for (int round = 0; units.valid(); units.next(p), ++round) {
+        const int j0 = units.t_begin, n = units.t_end;
+        unsigned long long* odd = reinterpret_cast<unsigned long long*>(c.gen + kWideOdd) + 2 * (round & 1);
+        if (lane < 2) odd[lane] = 0;   // its readers, of the unit before the last, are done: the last unit's P came behind them
+        __syncwarp();
+        WideRing pos = first.plus(n - j0 == 1 ? 1 : 2);
+#pragma unroll 1
+        for (int j = j0; j < n; ++j) {
+            c.wait(kWKvFull + pos.slot, pos.par, j);
+            const int key0 = units.key_of(j);
+            if (!units.full(p, key0)) wide_clear(p, units.cur.r, c.smem + kWideKV + pos.slot * kTileBytes, key0, odd);
+            for (int h = 0; h < w.tiles; ++h) {
+                if (j == j0 && round > 0) c.wait(kWOFree + h, (round - 1) & 1, j);
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    c.wait(kWPReady + 2 * h + part, p_par, j);
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int ks = 0; ks < 8; ++ks)
+                            if ((ks < 2 * kWideSplit) == (part == 0))
+                                mma_ts(c.tmem + kWTmemO + h * 128, c.tmem + kWTmemP + h * 64 + ks * 8, v_desc + pos.slot * (kTileBytes >> 4) + ks * (2048 >> 4),
+                                       kIdescPV, j > j0 || ks > 0);
+                        if (part == 1) {
+                            tc_commit(c.bars + (kWPvDone + h) * 8);
+                            if (h == w.tiles - 1) tc_commit(c.bars + (kWKvEmpty + pos.slot) * 8);
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+            p_par ^= 1u;
+            pos = pos.plus(j + 2 == n ? 1 : 2);
+        }
+        if (lane == 0) mbar_arrive(c.bars + kWOdd * 8);
+        first = first.after(2 * (n - j0));
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- softmax
+// Keys [k, k + 32) that a row sees: before base those of its window and the sinks, from base on those of its mask.
+__device__ __forceinline__ uint32_t wide_seen(int k, int base, int low, int sinks, unsigned long long mask) {
+    const uint32_t before = bits_below(base - k) & (~bits_below(low - k) | bits_below(sinks - k));
+    const int d = k - base;
+    const uint32_t drafts = d >= 64 || d <= -32 ? 0u : (d >= 0 ? (uint32_t)(mask >> d) : (uint32_t)(mask << -d));
+    return before | drafts;
+}
+__device__ __forceinline__ void wide_hide(float (&s)[32], uint32_t seen) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        if (!(seen >> i & 1u)) s[i] = -INFINITY;
+}
+
+// What wide_clear took out of the V that a row sees joins the row just written.
+__device__ __noinline__ void wide_odd_row(const DecodeParams& p, const unsigned long long* odd, int b, int base, int len, int u, int t, bool whole, int64_t at) {
+#pragma unroll 1
+    for (int dim = 0; dim < kD; ++dim) {
+        const float x = odd_values<kBf16, true>(p, odd, b, base, len, u, t, dim);
+        if (x == 0.f) continue;
+        if (whole) p.out[at + dim] = __float2bfloat16_rn(__bfloat162float(p.out[at + dim]) + x);
+        else p.part_o[at + dim] += x;
+    }
+}
+
+#define CP_LOAD_S3(a0, a1, a2)       \
+    TMEM_LD32(s_tmem + 0, a0, 0);    \
+    TMEM_LD32(s_tmem + 32, a1, 0);   \
+    TMEM_LD32(s_tmem + 64, a2, 0);
+
+// One score tile (in c0..c3): the row's maximum, the rescaling of O where it grows by more than the lag, the weights in four pieces.  If the unit has another
+// tile, its scores replace the current ones before the function returns.
+__device__ __forceinline__ void wide_softmax_tile(const WideCtx& cx, float (&c0)[32], float (&c1)[32], float (&c2)[32], float (&c3)[32], int wg, bool more,
+                                                  bool first, uint32_t& s_par, uint32_t pv_par, uint32_t s_tmem, uint32_t p_tmem, uint32_t o_tmem, float c,
+                                                  float& m, float& l, int iter) {
+    float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+    max32(c0, mx0, mx1, mx2, mx3);
+    max32(c1, mx0, mx1, mx2, mx3);
+    max32(c2, mx0, mx1, mx2, mx3);
+    max32(c3, mx0, mx1, mx2, mx3);
+    const float m_new = fmaxf(m, fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * c);
+    if (first) {
+        m = m_new;                     // O is overwritten by the first product
+    } else {
+        cx.wait(kWPvDone + wg, pv_par, iter);
+        __syncwarp();
+        tc_fence_after();
+        const bool grow = m_new - m > kWideLag;
+        if (__any_sync(0xffffffffu, grow)) {
+            const float m_upd = grow ? m_new : m, alpha = ex2(m - m_upd);
+            l *= alpha;
+            m = m_upd;
+#pragma unroll 1
+            for (int cc = 0; cc < 4; ++cc) {
+                float o[32];
+                TMEM_LD32(o_tmem + cc * 32, o, 0);
+                tc_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] *= alpha;
+                TMEM_ST32F(o_tmem + cc * 32, o, 0);
+            }
+        }
+    }
+    const float2 c2f = make_float2(c, c), nm2 = make_float2(-m, -m);
+    float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0, sum2 = sum0, sum3 = sum0;
+    uint32_t pk[16];
+    const uint32_t p_bar = cx.bars + (kWPReady + 2 * wg) * 8;
+#define CP_WIDE_PIECE(cur, q)                                                           \
+    exp32<false>(cur, pk, c2f, nm2, sum0, sum1, sum2, sum3);                            \
+    TMEM_ST16R(p_tmem + (q) * 16, pk, 0);                                               \
+    if ((q) + 1 == kWideSplit || (q) == 3) {                                            \
+        tc_wait_st();                                                                   \
+        tc_fence_before();                                                              \
+        __syncwarp();                                                                   \
+        if ((threadIdx.x & 31) == 0) mbar_arrive(p_bar + ((q) == 3 ? 8 : 0));           \
+    }
+    CP_WIDE_PIECE(c0, 0)
+    CP_WIDE_PIECE(c1, 1)
+    CP_WIDE_PIECE(c2, 2)
+    bool early = false;                // is the next score tile there already?  (the same answer in the whole warp)
+    if (more) {
+        early = __all_sync(0xffffffffu, mbar_test(cx.bars + (kWSReady + wg) * 8, s_par));
+        if (early) {
+            tc_fence_after();
+            CP_LOAD_S3(c0, c1, c2)
+        }
+    }
+    CP_WIDE_PIECE(c3, 3)
+#undef CP_WIDE_PIECE
+    if (more) {
+        if (!early) {
+            cx.wait(kWSReady + wg, s_par, iter);
+            __syncwarp();
+            tc_fence_after();
+            CP_LOAD_S3(c0, c1, c2)
+        }
+        TMEM_LD32(s_tmem + 96, c3, 0);
+        tc_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(cx.bars + kWSFree * 8);
+        s_par ^= 1u;
+    }
+    const float2 st = __fadd2_rn(__fadd2_rn(sum0, sum1), __fadd2_rn(sum2, sum3));
+    l += st.x + st.y;
+}
+
+__device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx& cx, WideUnits units, int wg, int64_t total, int ctas) {
+    const DecodeParams& p = w.d;
+    const int lane = threadIdx.x & 31, warp_in_wg = threadIdx.x >> 5 & 3;
+    const uint32_t lane_addr = (uint32_t)(warp_in_wg * 32) << 16;
+    const uint32_t s_tmem = cx.tmem + lane_addr + kWTmemS, p_tmem = cx.tmem + lane_addr + kWTmemP + wg * 64, o_tmem = cx.tmem + lane_addr + kWTmemO + wg * 128;
+    const int cls = (int)(blockIdx.x % w.classes), run = (int)(blockIdx.x / w.classes);
+    const int row = wg * kBlockM + warp_in_wg * 32 + lane;                // of the class
+    const int r = cls * w.class_rows + row, t = r / p.G;                  // of the KV head; its token
+    const bool in_class = row < w.class_rows && r < p.rows;
+    const float c = p.scale_log2;
+    uint32_t s_par = 0, tile_cnt = 0;
+    for (int round = 0; units.valid(); ++round) {
+        const Request rq = units.cur.r;
+        const int b = units.cur.b, u = units.cur.u, j0 = units.t_begin, n = units.t_end, m_tree = rq.len - rq.base;
+        TreeRow tr;
+        tr.mask = 0;
+        tr.lim = 0;
+        if (in_class) tr = tree_row(p, b, t, rq.base, m_tree);
+        const int low = tr.lim - p.window;
+        float m = kNoKey, l = 0.f;
+        float s0[32], s1[32], s2[32], s3[32];
+        cx.wait(kWSReady + wg, s_par, j0);
+        __syncwarp();
+        s_par ^= 1u;
+        tc_fence_after();
+        CP_LOAD_S3(s0, s1, s2)
+        TMEM_LD32(s_tmem + 96, s3, 0);
+        tc_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(cx.bars + kWSFree * 8);
+#pragma unroll 1
+        for (int j = j0; j < n; ++j) {
+            const int key0 = units.key_of(j);
+            if (!units.full(p, key0)) {
+                wide_hide(s0, wide_seen(key0, rq.base, low, p.sinks, tr.mask));
+                wide_hide(s1, wide_seen(key0 + 32, rq.base, low, p.sinks, tr.mask));
+                wide_hide(s2, wide_seen(key0 + 64, rq.base, low, p.sinks, tr.mask));
+                wide_hide(s3, wide_seen(key0 + 96, rq.base, low, p.sinks, tr.mask));
+            }
+            wide_softmax_tile(cx, s0, s1, s2, s3, wg, j + 1 < n, j == j0, s_par, (tile_cnt - 1) & 1, s_tmem, p_tmem, o_tmem, c, m, l, j);
+            ++tile_cnt;
+        }
+        const bool whole = units.whole;
+        const int64_t x_end = units.cur.x + kWideCost + rq.n;
+        units.next(p);
+        cx.wait(kWPvDone + wg, (tile_cnt - 1) & 1, n);
+        cx.wait(kWOdd, round & 1, n);
+        __syncwarp();
+        tc_fence_after();
+        const unsigned long long* odd = reinterpret_cast<const unsigned long long*>(cx.gen + kWideOdd) + 2 * (round & 1);
+        const bool live = in_class && t < m_tree;          // rows behind the tree: zeros, -inf
+        const bool any_odd = live && (odd[0] | odd[1]) != 0;
+        const float inv = !whole ? 1.f : (l == 0.f ? 0.f : 1.f / l);
+        const int64_t slot = 2 * ((int64_t)cls * w.runs + run) + (j0 > 0 ? 0 : 1);
+        const int head = u * p.G + r - t * p.G;
+        // offset of this row in the destination, -1: none
+        const int64_t at = !in_class ? -1 : (whole ? (((int64_t)b * p.n_q + t) * p.Hq + head) * kD : (slot * kWideRows + row) * kD);
+        const int qt = lane & 3;
+        int64_t to[4];                 // of the rows of this lane's quad: the lanes swap 16-byte pieces, so that a store writes 64 contiguous bytes of a row
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i] = __shfl_sync(0xffffffffu, at, (lane & ~3) + i);
+#pragma unroll 1
+        for (int cc = 0; cc < 4; ++cc) {
+            float o[32];
+            TMEM_LD32(o_tmem + cc * 32, o, 0);
+            tc_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = live ? o[i] * inv : 0.f;
+            if (whole) {
+                uint4 v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    v[i] = make_uint4(pack_bf16(o[8 * i], o[8 * i + 1]), pack_bf16(o[8 * i + 2], o[8 * i + 3]), pack_bf16(o[8 * i + 4], o[8 * i + 5]),
+                                      pack_bf16(o[8 * i + 6], o[8 * i + 7]));
+                quad_transpose(v, qt);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (to[i] >= 0) *reinterpret_cast<uint4*>(p.out + to[i] + cc * 32 + qt * 8) = v[i];
+            } else {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint4 v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int k = half * 16 + 4 * i;
+                        v[i] = make_uint4(__float_as_uint(o[k]), __float_as_uint(o[k + 1]), __float_as_uint(o[k + 2]), __float_as_uint(o[k + 3]));
+                    }
+                    quad_transpose(v, qt);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (to[i] >= 0) *reinterpret_cast<uint4*>(p.part_o + to[i] + cc * 32 + half * 16 + qt * 4) = v[i];
+                }
+            }
+        }
+        tc_fence_before();
+        __syncwarp();                  // also: the rows are written, by the lanes of their quads
+        if (any_odd) wide_odd_row(p, odd, b, rq.base, rq.len, u, t, whole, at);
+        if (lane == 0) mbar_arrive(cx.bars + (kWOFree + wg) * 8);
+        if (in_class) {
+            if (whole) {
+                p.lse[(int64_t)head * ((int64_t)p.B * p.n_q) + (int64_t)b * p.n_q + t] =
+                    live && l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            } else {
+                p.part_ml[(slot * kWideRows + row) * 2] = live ? m : kNoKey;
+                p.part_ml[(slot * kWideRows + row) * 2 + 1] = live ? l : 0.f;
+            }
+        }
+        if (threadIdx.x == 0 && !whole && j0 == 0) {
+            // this CTA holds the unit's first piece: the last one ends with the unit's last tile, at place x_end - 1
+            int64_t last = min((x_end * ctas - 1) / total, (int64_t)ctas - 1);
+            while (run_begin(total, last, ctas) >= x_end) --last;
+            while (run_begin(total, last + 1, ctas) < x_end) ++last;
+            int32_t* meta = p.meta + ((int64_t)cls * w.runs + run) * 4;
+            meta[0] = b;
+            meta[1] = u;
+            meta[2] = (int32_t)(last - run + 1);
+            meta[3] = 1;
+        }
+    }
+}
+#undef CP_LOAD_S3
+
+__global__ void __launch_bounds__(kWideThreads, 1)
+tree_wide_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ WideParams w) {
+    extern __shared__ uint8_t smem_raw[];
+    const DecodeParams& p = w.d;
+    WideCtx c;
+    c.smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    c.gen = smem_raw + (c.smem - smem_u32(smem_raw));
+    c.bars = c.smem + kWideBar;
+    c.abort_flag = reinterpret_cast<volatile uint32_t*>(c.gen + kWideAbort);
+    c.status = p.status;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int run = (int)(blockIdx.x / w.classes);
+    let_next_launch_begin();
+    if (tid == 0) {
+        mbar_init(c.bars + kWQFull * 8, 1);
+        mbar_init(c.bars + kWQEmpty * 8, 1);
+        for (int s = 0; s < kWideStages; ++s) {
+            mbar_init(c.bars + (kWKvFull + s) * 8, 1);
+            mbar_init(c.bars + (kWKvEmpty + s) * 8, 1);
+        }
+        mbar_init(c.bars + kWSFree * 8, 4);
+        for (int h = 0; h < 2; ++h) {
+            mbar_init(c.bars + (kWSReady + h) * 8, 1);
+            for (int q = 0; q < 2; ++q) mbar_init(c.bars + (kWPReady + 2 * h + q) * 8, 4);      // one arrival per warp
+            mbar_init(c.bars + (kWPvDone + h) * 8, 1);
+            mbar_init(c.bars + (kWOFree + h) * 8, 4);
+        }
+        mbar_init(c.bars + kWOdd * 8, 1);
+        *c.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(c.smem + kWideTmemPtr), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    // where this CTA's run starts: requests are dealt to the threads in order, a prefix sum over their places finds it
+    int64_t* scan = reinterpret_cast<int64_t*>(c.gen + kWideScan);
+    int32_t* start = reinterpret_cast<int32_t*>(scan + kWideThreads / 32);
+    const int per = (p.B + kWideThreads - 1) / kWideThreads;
+    int64_t mine = 0;
+    for (int i = 0; i < per; ++i) {
+        const int b = tid * per + i;
+        if (b >= p.B) break;
+        mine += request_of<kBlockN, true>(p, b).n + kWideCost;
+        if (blockIdx.x == 0) {
+            const int len = p.kv_len[b];
+            if (len > p.capacity || len < 0) report_status(p.status, CP_ERR_BOUNDS, b, len);
+            if (p.tree_len && (p.tree_len[b] < 0 || p.tree_len[b] > min(p.n_q, len))) report_status(p.status, CP_ERR_BOUNDS, b, p.tree_len[b]);
+        }
+    }
+    int64_t inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+    }
+    if (lane == 31) scan[warp] = inc;
+    if (tid == 0) p.meta[((int64_t)(blockIdx.x % w.classes) * w.runs + run) * 4 + 3] = 0;
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    c.tmem = *reinterpret_cast<volatile uint32_t*>(c.gen + kWideTmemPtr);
+    int64_t before = inc - mine, total = 0;
+    for (int i = 0; i < kWideThreads / 32; ++i) {
+        if (i < warp) before += scan[i];
+        total += scan[i];
+    }
+    total *= p.Hkv;
+    before *= p.Hkv;
+    const int ctas = (int)min((int64_t)w.runs, total);
+    const int64_t x0 = run < ctas ? run_begin(total, run, ctas) : total, x1 = run < ctas ? run_begin(total, run + 1, ctas) : total;
+    if (x0 >= before && x0 < before + mine * p.Hkv) {
+        int b = tid * per;
+        int64_t at = before;
+        while (true) {
+            const int64_t n = (int64_t)(request_of<kBlockN, true>(p, b).n + kWideCost) * p.Hkv;
+            if (x0 < at + n) break;
+            at += n;
+            ++b;
+        }
+        const int n = request_of<kBlockN, true>(p, b).n + kWideCost;
+        start[0] = b;
+        start[1] = (int32_t)((x0 - at) / n);
+        start[2] = (int32_t)((x0 - at) % n);
+    }
+    __syncthreads();
+    if (x0 < x1) {
+        WideUnits units;
+        units.begin(p, start, x0, x1);
+        if (warp < 8) {
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWideRegsSoftmax));
+            if (warp < 4 || w.tiles == 2) wide_softmax(w, c, units, warp >> 2, total, ctas);
+        } else {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWideRegsOther));
+            if (warp == 8) wide_producer(w, c, units, &tmK, &tmV);
+            else if (warp == 9) wide_scores(w, c, units);
+            else if (warp == 10) wide_outputs(w, c, units);
+            else wide_queries(w, c, units);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (*c.abort_flag) {
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);   // copies in flight land before shared memory is released
+        __syncthreads();
+    }
+    if (warp == 0) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(c.tmem), "r"(512u) : "memory");
+    }
+}
+
+// Joins the pieces of cut units: CTA (v, y), v = class * runs + run of a unit's first piece; a warp a row.  Pieces: slot 2v + 1, then slots 2v', v' = v + 1, ..
+constexpr int kWideJoinRows = 8;
+__global__ void __launch_bounds__(32 * kWideJoinRows)
+tree_join_kernel(const __grid_constant__ WideParams w) {
+    const DecodeParams& p = w.d;
+    wait_for_launch_before();
+    const int v = blockIdx.x, row = blockIdx.y * kWideJoinRows + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int4 me = *reinterpret_cast<const int4*>(p.meta + 4 * v);
+    const int r = v / w.runs * w.class_rows + row;
+    if (me.w == 0 || row >= w.class_rows || r >= p.rows) return;
+    auto slot_of = [&](int k) { return (int64_t)(k == 0 ? 2 * v + 1 : 2 * (v + k)) * kWideRows + row; };
+    float mx = kNoKey;
+    for (int k = lane; k < me.z; k += 32) mx = fmaxf(mx, p.part_ml[slot_of(k) * 2]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < me.z; ++k) {
+        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + slot_of(k) * 2);
+        const float4 x = *reinterpret_cast<const float4*>(p.part_o + slot_of(k) * kD + lane * 4);
+        const float f = exp2_fast(ml.x - mx);
+        sum += f * ml.y;
+        a.x += f * x.x;
+        a.y += f * x.y;
+        a.z += f * x.z;
+        a.w += f * x.w;
+    }
+    const int t = r / p.G, head = me.y * p.G + r - t * p.G;
+    const int64_t token = (int64_t)me.x * p.n_q + t;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    uint2 out;
+    out.x = pack_bf16(a.x * inv, a.y * inv);
+    out.y = pack_bf16(a.z * inv, a.w * inv);
+    *reinterpret_cast<uint2*>(p.out + (token * p.Hq + head) * kD + lane * 4) = out;
+    if (lane == 0) p.lse[(int64_t)head * ((int64_t)p.B * p.n_q) + token] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.6931471805599453f;
+}
+
+}  // namespace

@@ -128,7 +128,7 @@ int validate_kv_cache_fp8(const cp_kv_cache_fp8* c, const char* who);
 int validate_kv_cache_mx4(const cp_kv_cache_mx4* c, const char* who);
 // The wide form of tree attention (tree_wide.cu): parameters and cache as decode_kernel.cuh describes them, the workspace's own layout.
 size_t tree_wide_workspace();
-int launch_tree_wide(cp_ctx* ctx, const void* decode_params, const void* cache_view, void* workspace, void* stream, const char* who);
+int launch_tree_wide(cp_ctx* ctx, int kind, const void* decode_params, const void* cache_view, void* workspace, void* stream, const char* who);
 int build_tiles(int32_t B, const int64_t* cu_new, const int64_t* prefix_len, const int32_t* C,
                 const int64_t* cu_pages, int32_t page_size, int32_t only_shard, int32_t only_chunk, int64_t kv_lo,
                 int64_t kv_hi, int32_t tile_rows, std::vector<TileItem>& out, int32_t window = INT32_MAX, int32_t sinks = 0);
@@ -159,7 +159,7 @@ struct cp_ctx {
     int stage_next;
     cpattn::EncodeTiledFn encode_tiled;
     bool attn_attr_set;
-    bool tree_attr_set;
+    bool tree_attr_set[3];
     uint32_t decode_attr_set[3];       // per kind of cache, one bit per instantiation of the decode kernel
     // schedule reuse (cp_ctx_cache_schedule): what the last attention call left in its workspace
     bool cache_on;

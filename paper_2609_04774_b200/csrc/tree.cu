@@ -73,7 +73,7 @@ int tree_attn(cp_ctx* ctx, const void* q, const Cache* cache, const int32_t* pag
     if (guard.rc()) return guard.rc();
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const CacheView view = view_of(cache);
-    if (kind == kBf16 && p.rows > kNarrowRows) return launch_tree_wide(ctx, &p, &view, workspace, stream, who);
+    if (p.rows > kNarrowRows) return launch_tree_wide(ctx, kind, &p, &view, workspace, stream, who);
     if (kind == kBf16) return launch_rows<1, kBf16, kTree>(ctx, p, s, who);
     if (kind == kE4m3) return p.Hkv % 2 == 0 ? launch_rows<2, kE4m3, kTree>(ctx, p, s, who) : launch_rows<1, kE4m3, kTree>(ctx, p, s, who);
     return p.Hkv % 4 == 0 ? launch_rows<4, kMx4, kTree>(ctx, p, s, who) : launch_rows<1, kMx4, kTree>(ctx, p, s, who);

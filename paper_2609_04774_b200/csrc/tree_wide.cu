@@ -14,6 +14,27 @@ int encode_kv(cp_ctx* ctx, const CacheView& v, bool second, CUtensorMap* map, co
     return CP_OK;
 }
 
+template <Kind kKind>
+int launch(cp_ctx* ctx, const WideParams& w, const CacheView& view, cudaStream_t s, const char* who) {
+    using W = Wide<kKind>;
+    CUtensorMap k = {}, v = {};
+    if (kKind == kBf16) {
+        if (int rc = encode_kv(ctx, view, false, &k, who)) return rc;
+        if (int rc = encode_kv(ctx, view, true, &v, who)) return rc;
+    }
+    if (!ctx->tree_attr_set[kKind]) {
+        if (int rc = check_cuda(cudaFuncSetAttribute(tree_wide_kernel<kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, W::kSmem),
+                                "cudaFuncSetAttribute(tree)")) return rc;
+        ctx->tree_attr_set[kKind] = true;
+    }
+    tree_wide_kernel<kKind><<<(unsigned)(w.runs * w.classes), W::kThreads, W::kSmem, s>>>(k, v, w);
+    if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
+    const unsigned y = (unsigned)((w.class_rows + kWideJoinRows - 1) / kWideJoinRows);
+    // an ordinary launch: the first kernel moves registers between its warps as it starts, and nothing is to be set up beside it then
+    tree_join_kernel<kKind><<<dim3((unsigned)(w.runs * w.classes), y), 32 * kWideJoinRows, 0, s>>>(w);
+    return check_cuda(cudaGetLastError(), who);
+}
+
 }  // namespace
 
 namespace cpattn {
@@ -23,7 +44,7 @@ size_t tree_wide_workspace() {
     return (n * (kD + 2) * sizeof(float) + kMaxGrid * 16 + 255) / 256 * 256;
 }
 
-int launch_tree_wide(cp_ctx* ctx, const void* decode_params, const void* cache_view, void* workspace, void* stream, const char* who) {
+int launch_tree_wide(cp_ctx* ctx, int kind, const void* decode_params, const void* cache_view, void* workspace, void* stream, const char* who) {
     WideParams w;
     w.d = *static_cast<const DecodeParams*>(decode_params);
     const CacheView& view = *static_cast<const CacheView*>(cache_view);
@@ -36,19 +57,10 @@ int launch_tree_wide(cp_ctx* ctx, const void* decode_params, const void* cache_v
     w.d.part_o = static_cast<float*>(workspace);
     w.d.part_ml = w.d.part_o + n * kD;
     w.d.meta = reinterpret_cast<int32_t*>(w.d.part_ml + n * 2);
-    CUtensorMap k, v;
-    if (int rc = encode_kv(ctx, view, false, &k, who)) return rc;
-    if (int rc = encode_kv(ctx, view, true, &v, who)) return rc;
-    if (!ctx->tree_attr_set) {
-        if (int rc = check_cuda(cudaFuncSetAttribute(tree_wide_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideSmem), "cudaFuncSetAttribute(tree)"))
-            return rc;
-        ctx->tree_attr_set = true;
-    }
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    tree_wide_kernel<<<(unsigned)(w.runs * w.classes), kWideThreads, kWideSmem, s>>>(k, v, w);
-    if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
-    const unsigned y = (unsigned)((w.class_rows + kWideJoinRows - 1) / kWideJoinRows);
-    return launch_behind(tree_join_kernel, dim3((unsigned)(w.runs * w.classes), y), 32 * kWideJoinRows, s, who, w);
+    if (kind == kE4m3) return launch<kE4m3>(ctx, w, view, s, who);
+    if (kind == kMx4) return launch<kMx4>(ctx, w, view, s, who);
+    return launch<kBf16>(ctx, w, view, s, who);
 }
 
 }  // namespace cpattn

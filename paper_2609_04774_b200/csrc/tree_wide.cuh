@@ -1,18 +1,21 @@
-// Attention of drafted trees with many query rows per KV head (n_q * Hq / Hkv > 32) on the tcgen05 tensor cores, over paged caches with lengths, masks
-// and page tables on the device.
+// Attention of drafted trees (and of chains of tokens) with many query rows per KV head, n_q * Hq / Hkv of them, on the tcgen05 tensor cores, over paged caches
+// with lengths, masks and page tables on the device.
 //
-// With r rows a key costs 512 r flops and 512 bytes (bf16): at 128 rows half of what the tensor cores can do while the keys arrive, at 264 as
-// much.  The narrow form (decode_kernel.cuh) works such rows off in units of 32 with mma.sync, each reading the keys again; here a CTA takes up to
-// 256 rows, so every key that lands in shared memory is used once by all of them.
-//   - Query row t * G + h of a KV head (token t, head h of the group) is a row of the M side: two 128-row score tiles that share the K/V tiles, one
-//     softmax warpgroup each.  Trees of up to 128 rows use one.
+// With r rows a key costs 512 r flops and 512 bytes (bf16; E4M3 256, 4-bit 136): at 128 rows half of what the tensor cores can do while the keys
+// arrive, at 264 as much.  The narrow form (decode_kernel.cuh) works such rows off in units of 32 with mma.sync, each reading (and, of one-byte and 4-bit
+// caches, widening) the keys again; here a CTA takes up to 256 rows, so every key is brought to shared memory once for all of them.
+//   - Query row t * G + h of a KV head (token t, head h of the group) is a row of the M side.  Up to 256 rows are two 128-row score tiles that share the K/V
+//     tiles, one softmax warpgroup each.  Up to 128 rows are one, and the warpgroups take the K/V tiles in turn, each with an accumulator of its own; the
+//     two are added at the end of a unit (one warpgroup alone needs twice the time that the keys do to arrive).
 //   - More than 256 rows are several classes of equal height.  CTA c belongs to class c % classes and walks run c / classes of the key axis, so the
 //     classes read the same keys at the same time and all but one find them in L2.
 //   - The key axis is all (request, KV head) units one after the other, 128 keys a step, cut into equal runs, one per CTA of a class, whatever
 //     the lengths are (the scheme of the narrow form: Cursor); pieces of cut units are joined by a second launch.
-//   - Warps: two softmax warpgroups; a TMA producer that fetches K/V tiles page by page; the issuers of S = Q K^T and of O += P V; a warp that gathers the
+//   - Warps: two softmax warpgroups; a producer that fetches K/V tiles page by page; the issuers of S = Q K^T and of O += P V; a warp that gathers the
 //     unit's query rows.  S, P and O live in TMEM: S | P0 | P1 | O0 | O1.  S is one buffer that the tiles use in turn, read into registers at
 //     once, so the next product runs under the exponentials.
+//   - bf16 tiles come by TMA.  The rows of the other caches come by cp.async into a ring of raw tiles, and a fourth warpgroup widens them: E4M3 to fp16
+//     (queries and weights are then fp16 as in the narrow form), 4-bit codes and exponents to bf16, both exactly.
 //   - Only the last tiles of a unit and those at a window's edge hide keys from rows.  Their masks are bits: of the tree's mask and of the window.  A hidden
 //     key's weight is zero, but zero times an infinity is not: the issuer of P V looks through the V of these tiles and clears what is no
 //     finite number; what some rows do see of it is added to their results when they are written.
@@ -24,35 +27,55 @@
 
 namespace {
 
-constexpr int kWideThreads = 384;
-constexpr int kWideStages = 5;                             // ring of 32 KB tiles, K and V in turn
 constexpr int kWideRows = 256;                             // query rows of a unit
 constexpr int kWideCost = 3;                               // fixed cost of a unit in tiles: queries, epilogue
-constexpr int kWideRegsSoftmax = 200, kWideRegsOther = 104;
-static_assert(2 * 128 * kWideRegsSoftmax + 128 * kWideRegsOther <= 65536 - 1024, "leave slack in the register file");
 constexpr float kWideLag = 8.0f;                           // the running maximum may lag by a factor 2^8
 constexpr int kWideSplit = 3;                              // P is handed over in two pieces: three quarters of the keys, then the rest
+constexpr int kConvWarps = 4;
+constexpr int kMaxRing = 3, kMaxRaw = 7;
 
-constexpr uint32_t kWideQ = 0;                             // shared memory: two query tiles, the ring, barriers and small areas
-constexpr uint32_t kWideKV = 2 * kTileBytes;
-constexpr uint32_t kWideBar = kWideKV + kWideStages * kTileBytes;
+template <Kind kKind>
+struct Wide {
+    static constexpr bool kRawTiles = kKind != kBf16;
+    static constexpr int kThreads = kRawTiles ? 512 : 384;
+    // register budgets after the roles split; they stay below the register file by one step at least
+    static constexpr int kRegsSoftmax = kRawTiles ? 184 : 200, kRegsOther = kRawTiles ? 64 : 104;
+    static_assert(256 * kRegsSoftmax + (kThreads - 256) * kRegsOther <= 65536 - 1024, "leave slack in the register file");
+    // Rings of 32 KB tiles, one for K and one for V: a full barrier has one waiter, who has waited for each of its phases.  (With K and V in turn in one ring the
+    // issuer of S can be at a slot whose V has not landed yet, when the tiles are taken in turn; its wait would take the phase before that for its own.)
+    static constexpr int kStagesK = kRawTiles ? 2 : 3, kStagesV = kRawTiles ? 1 : 2, kStages = kStagesK + kStagesV;
+    static constexpr uint32_t kRawCodes = kKind == kE4m3 ? 16384u : 8192u;
+    static constexpr uint32_t kRawBytes = kKind == kE4m3 ? 16384u : 8704u;      // 4-bit: the codes of 128 keys, then their exponents
+    static constexpr int kRaw = kKind == kBf16 ? 0 : (kKind == kE4m3 ? 4 : 7);
+    // shared memory: two query tiles (or one and the accumulator that travels), the ring, the raw tiles, barriers and small areas
+    static constexpr uint32_t kQ = 0, kKV = 2 * kTileBytes, kRawAt = kKV + kStages * kTileBytes;
+    static constexpr uint32_t kBar = kRawAt + kRaw * kRawBytes;
+    static constexpr uint32_t kOdd = kBar + 48 * 8;        // [unit parity][2] keys whose V is no finite number (see odd_values)
+    static constexpr uint32_t kScan = kOdd + 32;           // sums of the warps, then the run's start
+    static constexpr uint32_t kExp = kScan + 16 * 8 + 16;  // [unit parity][row]: exponent by which a row of E4M3 queries was scaled up
+    static constexpr uint32_t kTmemPtr = kExp + (kKind == kE4m3 ? 2 * kWideRows : 0), kAbort = kTmemPtr + 4;
+    static constexpr uint32_t kSmem = kAbort + 12 + 1024;  // slack for manual alignment
+    static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
+};
 enum WideBar : uint32_t {
     kWQFull = 0, kWQEmpty = 1,
-    kWKvFull = 2,                            // + stage
-    kWKvEmpty = kWKvFull + kWideStages,      // + stage
-    kWSReady = kWKvEmpty + kWideStages,      // + tile: its scores are in the S buffer
+    kWKFull = 2,                             // + stage
+    kWKEmpty = kWKFull + kMaxRing,           // + stage
+    kWVFull = kWKEmpty + kMaxRing,           // + stage
+    kWVEmpty = kWVFull + kMaxRing,           // + stage
+    kWSReady = kWVEmpty + kMaxRing,          // + warpgroup: its scores are in the S buffer
     kWSFree = kWSReady + 2,                  // the S buffer has been read
-    kWPReady = kWSFree + 1,                  // + 2 tile + piece
-    kWPvDone = kWPReady + 4,                 // + tile: P V of a step has finished
-    kWOFree = kWPvDone + 2,                  // + tile: O has been read
+    kWPReady = kWSFree + 1,                  // + 2 warpgroup + piece
+    kWPvDone = kWPReady + 4,                 // + warpgroup: P V of a step has finished
+    kWOFree = kWPvDone + 2,                  // + warpgroup: O has been read
     kWOdd = kWOFree + 2,                     // the unit's list of odd keys is complete
-    kNumWideBars = kWOdd + 1
+    kWTravelFull = kWOdd + 1,                // a part of the second warpgroup's accumulator is in shared memory
+    kWTravelFree = kWTravelFull + 1,         // and has been read
+    kWRawFull = kWTravelFree + 1,            // + raw stage
+    kWRawEmpty = kWRawFull + kMaxRaw,        // + raw stage
+    kNumWideBars = kWRawEmpty + kMaxRaw
 };
-constexpr uint32_t kWideOdd = kWideBar + (kNumWideBars * 8 + 15) / 16 * 16;      // [unit parity][2] keys whose V is no finite number (see odd_values)
-constexpr uint32_t kWideScan = kWideOdd + 32;              // sums of the warps, then the run's start
-constexpr uint32_t kWideTmemPtr = kWideScan + 12 * 8 + 16, kWideAbort = kWideTmemPtr + 4;
-constexpr uint32_t kWideSmem = kWideAbort + 12 + 1024;     // slack for manual alignment
-static_assert(kWideSmem <= 227 * 1024, "shared memory of a CTA");
+static_assert(kNumWideBars <= 48, "barrier area");
 
 constexpr uint32_t kWTmemS = 0, kWTmemP = 128, kWTmemO = 256;      // columns; + 64 and + 128 for the second tile
 
@@ -60,7 +83,7 @@ struct WideParams {
     DecodeParams d;
     int32_t classes;           // row classes of a KV head
     int32_t class_rows;        // rows of a class (the last may have fewer)
-    int32_t tiles;             // score tiles of a unit: 1 or 2
+    int32_t tiles;             // 2: score tiles of a unit; 1: one, and the warpgroups take the K/V tiles in turn
     int32_t runs;              // CTAs of a class
 };
 
@@ -101,6 +124,10 @@ struct WideUnits {
     }
 };
 
+// The token of a row among the last m of its sequence, < 0 or >= m: none.  Chains are trees in which every token sees those before it; of a sequence shorter
+// than n_q the last rows are its tokens.
+__device__ __forceinline__ int wide_token(const DecodeParams& p, int t, int m) { return p.tree_mask ? t : t - (p.n_q - m); }
+
 struct WideCtx {
     uint32_t smem, bars, tmem;
     uint8_t* gen;              // the same shared memory
@@ -108,18 +135,15 @@ struct WideCtx {
     int32_t* status;
     __device__ __forceinline__ void wait(uint32_t id, uint32_t parity, int iter) const { mbar_wait(bars, id, parity, abort_flag, status, iter); }
 };
+// A position in a ring: slot, and the parity of the phase that ends when it is filled (for the side that fills: when it was emptied).
+template <int kStages>
 struct WideRing {
     uint32_t slot, par;
-    __device__ __forceinline__ WideRing plus(uint32_t n) const {      // n < 2 kWideStages
-        WideRing r = {slot + n, par};
-        if (r.slot >= (uint32_t)kWideStages) { r.slot -= kWideStages; r.par ^= 1u; }
-        return r;
-    }
-    __device__ __forceinline__ WideRing after(uint32_t n) const {
-        const uint32_t q = n / kWideStages;
-        WideRing r = plus(n - q * kWideStages);
-        r.par ^= q & 1u;
-        return r;
+    __device__ __forceinline__ void advance() {
+        if (++slot == (uint32_t)kStages) {
+            slot = 0;
+            par ^= 1u;
+        }
     }
 };
 
@@ -127,12 +151,14 @@ struct WideRing {
 // Load order = order of first use: K(j0), then K(j + 1) before V(j).  Lane i < pages of a tile holds a page id; those of the next K tile are
 // fetched while the current ones are used.  Pages that no row sees anything of are read as zeros.
 __device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx& c, WideUnits units, const CUtensorMap* tmK, const CUtensorMap* tmV) {
+    using W = Wide<kBf16>;
     const DecodeParams& p = w.d;
     const int lane = threadIdx.x & 31;
     const int page_tokens = 1 << p.page_shift, per_tile = kBlockN >> p.page_shift;
     const uint32_t box_bytes = (uint32_t)page_tokens * 128u;
     const int outside = (int)p.num_pages;                  // a page coordinate behind the tensor: TMA fills zeros
-    uint32_t it = 0;
+    WideRing<W::kStagesK> kr = {0, 1};
+    WideRing<W::kStagesV> vr = {0, 1};
     for (; units.valid(); units.next(p)) {
         const Request r = units.cur.r;
         const int32_t* row = p.table + units.cur.b * p.table_stride;
@@ -149,7 +175,7 @@ __device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx
         const int n_loads = 2 * (units.t_end - units.t_begin);
         int j = units.t_begin;                             // next K tile
         for (int ld = 0; ld < n_loads; ++ld) {
-            const bool is_v = ld == n_loads - 1 || (ld > 0 && (ld & 1) == 0);
+            const bool is_v = ld == n_loads - 1 || (ld > 0 && (ld & 1) == 0);      // K(j0), then K(j + 1) before V(j)
             int ids;
             if (!is_v) {
                 v_ids = k_ids;
@@ -158,10 +184,10 @@ __device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx
             } else {
                 ids = ld == n_loads - 1 ? k_ids : v_ids;
             }
-            const uint32_t slot = it % kWideStages, fbar = c.bars + (kWKvFull + slot) * 8;
-            const uint32_t dst = c.smem + kWideKV + slot * kTileBytes;
+            const uint32_t slot = is_v ? W::kStagesK + vr.slot : kr.slot;
+            const uint32_t fbar = c.bars + (is_v ? kWVFull + vr.slot : kWKFull + kr.slot) * 8, dst = c.smem + W::kKV + slot * kTileBytes;
             if (lane == 0) {
-                c.wait(kWKvEmpty + slot, ((it / kWideStages) & 1) ^ 1, ld);
+                c.wait(is_v ? kWVEmpty + vr.slot : kWKEmpty + kr.slot, is_v ? vr.par : kr.par, ld);
                 mbar_expect_tx(fbar, kTileBytes);
             }
             __syncwarp();
@@ -171,14 +197,152 @@ __device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx
                     tma_load_4d(dst + half * kHalfBytes + lane * box_bytes, is_v ? tmV : tmK, fbar, half * 64, units.cur.u, 0, ids);
             }
             __syncwarp();
-            ++it;
+            if (is_v) vr.advance();
+            else kr.advance();
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- raw tiles
+// E4M3 and 4-bit rows of 128 keys, K and V in turn; slots that no row sees are zeros.  16-byte chunk x of key k sits at chunk x ^ (k & 7) (4-bit rows of four
+// chunks: x ^ (k / 2 & 3)), so that eight lanes with eight keys and the same chunk meet no bank twice.
+template <Kind kKind>
+__device__ __forceinline__ void wide_raw(const WideParams& w, const WideCtx& c, WideUnits units) {
+    using W = Wide<kKind>;
+    const DecodeParams& p = w.d;
+    constexpr int kChunks = kKind == kE4m3 ? 8 : 4, kRowsPer = 32 / kChunks;
+    const int lane = threadIdx.x & 31, chunk = lane % kChunks, sub = lane / kChunks;
+    const int per_tile = kBlockN >> p.page_shift, page_mask = (1 << p.page_shift) - 1;
+    const int outside = -1;
+    uint32_t it = 0, par = 1;
+    for (; units.valid(); units.next(p)) {
+        const Request r = units.cur.r;
+        const int32_t* row = p.table + units.cur.b * p.table_stride;
+        const int low = r.low(p);
+        auto fetch = [&](int t) {
+            const int key0 = units.key_of(t), key = key0 + (lane << p.page_shift);
+            int id = outside;
+            if (lane < per_tile && key < r.len && (key + page_mask + 1 > low || key < p.sinks)) id = __ldg(row + (key >> p.page_shift));
+            return (uint32_t)id < (uint32_t)p.num_pages ? id : outside;
+        };
+        int ahead = fetch(units.t_begin);
+#pragma unroll 1
+        for (int j = units.t_begin; j < units.t_end; ++j) {
+            const int ids = ahead, key0 = units.key_of(j);
+            if (j + 1 < units.t_end) ahead = fetch(j + 1);
+#pragma unroll 1
+            for (int kv = 0; kv < 2; ++kv) {
+                if (lane == 0) c.wait(kWRawEmpty + it, par, j);
+                __syncwarp();
+                const uint32_t dst = c.smem + W::kRawAt + it * W::kRawBytes, bar = c.bars + (kWRawFull + it) * 8;
+                const uint8_t* base = (kv ? p.v : p.k) + units.cur.u * p.stride_head + chunk * 16;
+#pragma unroll 4
+                for (int i = 0; i < kBlockN; i += kRowsPer) {
+                    const int k = i + sub, key = key0 + k;
+                    const int id = __shfl_sync(0xffffffffu, ids, k >> p.page_shift);
+                    const bool ok = id >= 0 && key < r.len && (key >= low || key < p.sinks);
+                    const uint8_t* src = ok ? base + id * p.stride_page + (key & page_mask) * p.stride_tok : p.k;
+                    cp_async16_or_zeros(dst + k * (kChunks * 16) + ((chunk ^ (kKind == kE4m3 ? k & 7 : k >> 1 & 3)) << 4), src, ok);
+                }
+                if (kKind == kMx4) {
+                    const uint8_t* exps = (kv ? p.v : p.k) + p.Hkv * 64 + units.cur.u * 4;
+#pragma unroll
+                    for (int i = 0; i < kBlockN; i += 32) {
+                        const int k = i + lane, key = key0 + k;
+                        const int id = __shfl_sync(0xffffffffu, ids, k >> p.page_shift);
+                        const bool ok = id >= 0 && key < r.len && (key >= low || key < p.sinks);
+                        const uint8_t* src = ok ? exps + id * p.stride_page + (key & page_mask) * p.stride_tok : p.k;
+                        cp_async4_or_zeros(dst + W::kRawCodes + k * 4, src, ok);
+                    }
+                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+                if (++it == W::kRaw) {
+                    it = 0;
+                    par ^= 1;
+                }
+            }
+        }
+    }
+    cp_commit();
+    cp_wait<0>();
+}
+
+// The widening warps: a quarter of every tile each.  16 E4M3 codes -> 16 fp16 values; a block of 32 4-bit codes -> 32 bf16 values, in whose groups of eight
+// elements i and i + 4 stand side by side (the queries are laid out alike, and the columns of O are taken in that order).
+template <Kind kKind>
+__device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c, WideUnits units, int cw) {
+    using W = Wide<kKind>;
+    const int lane = threadIdx.x & 31;
+    uint32_t raw = 0, raw_par = 0;
+    WideRing<W::kStagesK> kr = {0, 1};
+    WideRing<W::kStagesV> vr = {0, 1};
+    for (; units.valid(); units.next(w.d)) {
+        const int n = 2 * (units.t_end - units.t_begin);
+#pragma unroll 1
+        for (int ld = 0; ld < n; ++ld) {
+            c.wait(kWRawFull + raw, raw_par, ld);
+            const bool is_v = ld & 1;
+            c.wait(is_v ? kWVEmpty + vr.slot : kWKEmpty + kr.slot, is_v ? vr.par : kr.par, ld);
+            __syncwarp();
+            const uint32_t src = c.smem + W::kRawAt + raw * W::kRawBytes, dst = c.smem + W::kKV + (is_v ? W::kStagesK + vr.slot : kr.slot) * kTileBytes;
+            if (kKind == kE4m3) {
+#pragma unroll 4
+                for (int i = 0; i < 8; ++i) {
+                    const int item = (i * kConvWarps + cw) * 32 + lane, key = (item >> 6) * 8 + (item & 7), x = item >> 3 & 7;
+                    const uint4 q = lds128(src + key * 128 + ((x ^ (key & 7)) << 4));
+                    uint4 a, b;
+                    widen4(q.x, a.x, a.y);
+                    widen4(q.y, a.z, a.w);
+                    widen4(q.z, b.x, b.y);
+                    widen4(q.w, b.z, b.w);
+                    const uint32_t row = dst + (x >> 2) * kHalfBytes + key * 128;
+                    sts128(row + (((2 * x & 7) ^ (key & 7)) << 4), a);
+                    sts128(row + (((2 * x + 1 & 7) ^ (key & 7)) << 4), b);
+                }
+            } else {
+#pragma unroll 2
+                for (int i = 0; i < 4; ++i) {
+                    const int item = (i * kConvWarps + cw) * 32 + lane, key = (item >> 5) * 8 + (item & 7), x = item >> 3 & 3;
+                    const uint4 q = lds128(src + key * 64 + ((x ^ (key >> 1 & 3)) << 4));
+                    const uint32_t e = lds32(src + W::kRawCodes + key * 4) >> (8 * x) & 255;
+                    const uint32_t codes[4] = {q.x, q.y, q.z, q.w};
+                    const uint32_t row = dst + (x >> 1) * kHalfBytes + key * 128;
+                    // one factor of 2^(e - 127 + 126) while it is a bf16 number, else 2^126 and 2^(e - 127)
+                    const bool near = __all_sync(0xffffffffu, e - 1 < 128u);
+                    const uint32_t f = near ? (e + 126) * 0x00800080u : 0x7e807e80u;
+                    const uint32_t f2 = e == 0 ? 0x00400040u : (e == 255 ? 0x7fc07fc0u : e * 0x00800080u);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        uint4 o = make_uint4(mul_bf16x2(small_bf16<0>(codes[k]), f), mul_bf16x2(small_bf16<1>(codes[k]), f),
+                                             mul_bf16x2(small_bf16<2>(codes[k]), f), mul_bf16x2(small_bf16<3>(codes[k]), f));
+                        if (!near) o = make_uint4(mul_bf16x2(o.x, f2), mul_bf16x2(o.y, f2), mul_bf16x2(o.z, f2), mul_bf16x2(o.w, f2));
+                        sts128(row + (((4 * x + k & 7) ^ (key & 7)) << 4), o);
+                    }
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // the tensor cores read what these lanes wrote
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(c.bars + (is_v ? kWVFull + vr.slot : kWKFull + kr.slot) * 8);
+                mbar_arrive(c.bars + (kWRawEmpty + raw) * 8);
+            }
+            if (++raw == W::kRaw) {
+                raw = 0;
+                raw_par ^= 1;
+            }
+            if (is_v) vr.advance();
+            else kr.advance();
         }
     }
 }
 
 // ---------------------------------------------------------------------------------------------- queries
-// Row i of the unit's class is token (r0 + i) / G, head (r0 + i) % G of the group; rows behind the tree are zeros.  128-byte swizzle lines, 64 dims a half.
+// Row i of the unit's class is token (r0 + i) / G, head (r0 + i) % G of the group; rows without a token are zeros.  128-byte swizzle lines, 64 dims a half.
+// E4M3: fp16, scaled per row by a power of two that brings the largest element to [2^10, 2^11) (what falls below 2^-24 of it is lost); the sign of the keys'
+// scale joins here.  4-bit: elements i and i + 4 of every eight side by side.
+template <Kind kKind>
 __device__ __forceinline__ void wide_queries(const WideParams& w, const WideCtx& c, WideUnits units) {
+    using W = Wide<kKind>;
     const DecodeParams& p = w.d;
     const int lane = threadIdx.x & 31;
     const int r0 = (int)(blockIdx.x % w.classes) * w.class_rows, rows = min(w.class_rows, p.rows - r0);
@@ -188,15 +352,46 @@ __device__ __forceinline__ void wide_queries(const WideParams& w, const WideCtx&
         const __nv_bfloat16* q = p.q + ((int64_t)b * p.n_q * p.Hq + (int64_t)units.cur.u * p.G) * kDim + chunk * 8;
         c.wait(kWQEmpty, (round & 1) ^ 1, round);
         __syncwarp();
+        const float sign = kKind == kE4m3 ? p.k_scale[units.cur.u] : 1.f;
+#pragma unroll 4
         for (int i = lane >> 4; i < w.tiles * kBlockM; i += 2) {
-            const int t = (r0 + i) / p.G;
-            const bool ok = i < rows && t < m;
+            const int t = (r0 + i) / p.G, live = wide_token(p, t, m);
+            const bool ok = i < rows && live >= 0 && live < m;
             const __nv_bfloat16* src = ok ? q + ((int64_t)t * p.Hq + (r0 + i - t * p.G)) * kDim : p.q;
             const int in = i & (kBlockM - 1);
-            cp_async16_or_zeros(c.smem + kWideQ + (i / kBlockM) * kTileBytes + (chunk >> 3) * kHalfBytes + in * 128 + (((chunk & 7) ^ (in & 7)) << 4), src, ok);
+            const uint32_t at = c.smem + W::kQ + (i / kBlockM) * kTileBytes + (chunk >> 3) * kHalfBytes + in * 128 + (((chunk & 7) ^ (in & 7)) << 4);
+            if (kKind == kBf16) {
+                cp_async16_or_zeros(at, src, ok);
+            } else {
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (ok) x = __ldg(reinterpret_cast<const uint4*>(src));
+                if (kKind == kMx4) {
+                    sts128(at, make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
+                                          __byte_perm(x.y, x.w, 0x7632)));
+                } else {
+                    const uint32_t word[4] = {x.x, x.y, x.z, x.w};
+                    float f[8], amax = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        f[2 * k] = __uint_as_float(word[k] << 16);
+                        f[2 * k + 1] = __uint_as_float(word[k] & 0xffff0000u);
+                        amax = fmaxf(amax, fmaxf(fabsf(f[2 * k]), fabsf(f[2 * k + 1])));
+                    }
+#pragma unroll
+                    for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                    int e = 0;
+                    if (amax > 0.f && amax < INFINITY) e = min(max(10 - ilogbf(amax), -126), 126);
+                    const float up = copysignf(__uint_as_float((uint32_t)(127 + e) << 23), sign);
+                    sts128(at, make_uint4(pack_weights<true>(f[0] * up, f[1] * up), pack_weights<true>(f[2] * up, f[3] * up),
+                                          pack_weights<true>(f[4] * up, f[5] * up), pack_weights<true>(f[6] * up, f[7] * up)));
+                    if (chunk == 0) reinterpret_cast<int8_t*>(c.gen + W::kExp)[(round & 1) * kWideRows + i] = (int8_t)e;
+                }
+            }
         }
-        cp_commit();
-        cp_wait<0>();
+        if (kKind == kBf16) {
+            cp_commit();
+            cp_wait<0>();
+        }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the tensor cores read what these lanes wrote
         __syncwarp();
         if (lane == 0) mbar_arrive(c.bars + kWQFull * 8);
@@ -204,18 +399,20 @@ __device__ __forceinline__ void wide_queries(const WideParams& w, const WideCtx&
 }
 
 // ---------------------------------------------------------------------------------------------- issuers
+template <Kind kKind>
 __device__ __forceinline__ void wide_scores(const WideParams& w, const WideCtx& c, WideUnits units) {
-    WideRing first = {0, 0};           // ring position of the unit's first load
+    using W = Wide<kKind>;
+    constexpr uint32_t kIdesc = kKind == kE4m3 ? kIdescS & ~((1u << 7) | (1u << 10)) : kIdescS;      // fp16 or bf16 operands
+    WideRing<W::kStagesK> pos = {0, 0};
     uint32_t s_par = 1;                // parity of "the previous score tile was read"; 1: there is none yet
-    const uint64_t q_desc = make_desc(c.smem + kWideQ, 16, 1024), k_desc = make_desc(c.smem + kWideKV, 16, 1024);
+    const uint64_t q_desc = make_desc(c.smem + W::kQ, 16, 1024), k_desc = make_desc(c.smem + W::kKV, 16, 1024);
     for (int round = 0; units.valid(); units.next(w.d), ++round) {
         const int j0 = units.t_begin, n = units.t_end;
         c.wait(kWQFull, round & 1, round);
-        WideRing pos = first;
 #pragma unroll 1
         for (int j = j0; j < n; ++j) {
-            c.wait(kWKvFull + pos.slot, pos.par, j);
-            for (int h = 0; h < w.tiles; ++h) {
+            c.wait(kWKFull + pos.slot, pos.par, j);
+            for (int q = 0; q < w.tiles; ++q) {
                 c.wait(kWSFree, s_par, j);
                 s_par ^= 1u;
                 tc_fence_after();
@@ -223,61 +420,75 @@ __device__ __forceinline__ void wide_scores(const WideParams& w, const WideCtx& 
 #pragma unroll
                     for (int ks = 0; ks < kD / 16; ++ks) {
                         const uint32_t off = ((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4;
-                        mma_ss(c.tmem + kWTmemS, q_desc + h * (kTileBytes >> 4) + off, k_desc + pos.slot * (kTileBytes >> 4) + off, kIdescS, ks > 0);
+                        mma_ss(c.tmem + kWTmemS, q_desc + q * (kTileBytes >> 4) + off, k_desc + pos.slot * (kTileBytes >> 4) + off, kIdesc, ks > 0);
                     }
-                    tc_commit(c.bars + (kWSReady + h) * 8);
-                    if (h == w.tiles - 1) {
-                        tc_commit(c.bars + (kWKvEmpty + pos.slot) * 8);
+                    tc_commit(c.bars + (kWSReady + (w.tiles == 2 ? q : (j - j0) & 1)) * 8);
+                    if (q == w.tiles - 1) {
+                        tc_commit(c.bars + (kWKEmpty + pos.slot) * 8);
                         if (j == n - 1) tc_commit(c.bars + kWQEmpty * 8);
                     }
                 }
                 __syncwarp();
             }
-            pos = pos.plus(j == j0 ? 1 : 2);
+            pos.advance();
         }
-        first = first.after(2 * (n - j0));
     }
 }
 
 // The V of a tile that hides keys from some row: keys that no row sees lose what is no finite number; so do those that only some rows
 // see, which are listed (as odd_values takes them).  Those that every row sees keep it: every row becomes that.
+template <bool kF16>
+__device__ __forceinline__ uint32_t odd_halves(uint32_t w) {
+    return kF16 ? ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u : not_finite<false>(w);
+}
+template <bool kF16>
+__device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
+    const uint32_t top = odd_halves<kF16>(w);
+    return w & ~(top | (top - (top >> 15)));
+}
+template <bool kF16>
 __device__ __forceinline__ void wide_clear(const DecodeParams& p, const Request& r, uint32_t v_tile, int key0, unsigned long long* odd) {
     const int lane = threadIdx.x & 31, low = r.low(p), low_max = r.len - p.window;
 #pragma unroll 4
     for (int i = lane; i < 2 * (int)kHalfBytes / 16; i += 32) {
         const uint4 x = lds128(v_tile + i * 16);
-        const uint32_t bad = not_finite<false>(x.x) | not_finite<false>(x.y) | not_finite<false>(x.z) | not_finite<false>(x.w);
+        const uint32_t bad = odd_halves<kF16>(x.x) | odd_halves<kF16>(x.y) | odd_halves<kF16>(x.z) | odd_halves<kF16>(x.w);
         if (bad == 0) continue;
         const int key = key0 + (i >> 3 & (kBlockN - 1));
         const bool nobody = key >= r.len || (key < low && key >= p.sinks);
         const bool late = key >= r.base, early = key < low_max && key >= p.sinks;
         if (!nobody && !late && !early) continue;
-        sts128(v_tile + i * 16, make_uint4(finite_part<false>(x.x), finite_part<false>(x.y), finite_part<false>(x.z), finite_part<false>(x.w)));
+        sts128(v_tile + i * 16, make_uint4(finite_halves<kF16>(x.x), finite_halves<kF16>(x.y), finite_halves<kF16>(x.z), finite_halves<kF16>(x.w)));
         if (!nobody) atomicOr(odd + (late ? 0 : 1), 1ull << (late ? key - r.base : key - low));
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
 }
 
+template <Kind kKind>
 __device__ __forceinline__ void wide_outputs(const WideParams& w, const WideCtx& c, WideUnits units) {
+    using W = Wide<kKind>;
+    constexpr uint32_t kIdesc = kKind == kE4m3 ? kIdescPV & ~((1u << 7) | (1u << 10)) : kIdescPV;
     const DecodeParams& p = w.d;
     const int lane = threadIdx.x & 31;
-    WideRing first = {0, 0};
-    uint32_t p_par = 0;                // parity of "P is there", the same for both tiles
-    const uint64_t v_desc = make_desc(c.smem + kWideKV, kHalfBytes, 1024);
+    WideRing<W::kStagesV> pos = {0, 0};
+    uint32_t p_par0 = 0, p_par1 = 0;   // parity of "P is there", per warpgroup
+    const uint64_t v_desc = make_desc(c.smem + W::kKV + W::kStagesK * kTileBytes, kHalfBytes, 1024);
     for (int round = 0; units.valid(); units.next(p), ++round) {
         const int j0 = units.t_begin, n = units.t_end;
-        unsigned long long* odd = reinterpret_cast<unsigned long long*>(c.gen + kWideOdd) + 2 * (round & 1);
+        unsigned long long* odd = reinterpret_cast<unsigned long long*>(c.gen + W::kOdd) + 2 * (round & 1);
         if (lane < 2) odd[lane] = 0;   // its readers, of the unit before the last, are done: the last unit's P came behind them
         __syncwarp();
-        WideRing pos = first.plus(n - j0 == 1 ? 1 : 2);
 #pragma unroll 1
         for (int j = j0; j < n; ++j) {
-            c.wait(kWKvFull + pos.slot, pos.par, j);
+            c.wait(kWVFull + pos.slot, pos.par, j);
             const int key0 = units.key_of(j);
-            if (!units.full(p, key0)) wide_clear(p, units.cur.r, c.smem + kWideKV + pos.slot * kTileBytes, key0, odd);
-            for (int h = 0; h < w.tiles; ++h) {
-                if (j == j0 && round > 0) c.wait(kWOFree + h, (round - 1) & 1, j);
+            if (!units.full(p, key0)) wide_clear<kKind == kE4m3>(p, units.cur.r, c.smem + W::kKV + (W::kStagesK + pos.slot) * kTileBytes, key0, odd);
+            for (int q = 0; q < w.tiles; ++q) {
+                const int h = w.tiles == 2 ? q : (j - j0) & 1;
+                const bool fresh = w.tiles == 2 ? j == j0 : j - j0 < 2;             // the accumulator's first tile of the unit
+                if (fresh && round > 0) c.wait(kWOFree + h, (round - 1) & 1, j);
+                const uint32_t p_par = h ? p_par1 : p_par0;
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {
                     c.wait(kWPReady + 2 * h + part, p_par, j);
@@ -287,20 +498,20 @@ __device__ __forceinline__ void wide_outputs(const WideParams& w, const WideCtx&
                         for (int ks = 0; ks < 8; ++ks)
                             if ((ks < 2 * kWideSplit) == (part == 0))
                                 mma_ts(c.tmem + kWTmemO + h * 128, c.tmem + kWTmemP + h * 64 + ks * 8, v_desc + pos.slot * (kTileBytes >> 4) + ks * (2048 >> 4),
-                                       kIdescPV, j > j0 || ks > 0);
+                                       kIdesc, !fresh || ks > 0);
                         if (part == 1) {
                             tc_commit(c.bars + (kWPvDone + h) * 8);
-                            if (h == w.tiles - 1) tc_commit(c.bars + (kWKvEmpty + pos.slot) * 8);
+                            if (q == w.tiles - 1) tc_commit(c.bars + (kWVEmpty + pos.slot) * 8);
                         }
                     }
                     __syncwarp();
                 }
+                if (h) p_par1 ^= 1u;
+                else p_par0 ^= 1u;
             }
-            p_par ^= 1u;
-            pos = pos.plus(j + 2 == n ? 1 : 2);
+            pos.advance();
         }
         if (lane == 0) mbar_arrive(c.bars + kWOdd * 8);
-        first = first.after(2 * (n - j0));
     }
 }
 
@@ -319,10 +530,11 @@ __device__ __forceinline__ void wide_hide(float (&s)[32], uint32_t seen) {
 }
 
 // What wide_clear took out of the V that a row sees joins the row just written.
-__device__ __noinline__ void wide_odd_row(const DecodeParams& p, const unsigned long long* odd, int b, int base, int len, int u, int t, bool whole, int64_t at) {
+template <Kind kKind>
+__device__ __forceinline__ void wide_odd_row(const DecodeParams& p, const unsigned long long* odd, int b, int base, int len, int u, int t, bool whole, int64_t at) {
 #pragma unroll 1
     for (int dim = 0; dim < kD; ++dim) {
-        const float x = odd_values<kBf16, true>(p, odd, b, base, len, u, t, dim);
+        const float x = odd_values<kKind, true>(p, odd, b, base, len, u, t, dim);
         if (x == 0.f) continue;
         if (whole) p.out[at + dim] = __float2bfloat16_rn(__bfloat162float(p.out[at + dim]) + x);
         else p.part_o[at + dim] += x;
@@ -334,8 +546,28 @@ __device__ __noinline__ void wide_odd_row(const DecodeParams& p, const unsigned 
     TMEM_LD32(s_tmem + 32, a1, 0);   \
     TMEM_LD32(s_tmem + 64, a2, 0);
 
+// 2^(s c - m) of 32 keys as 16 packed pairs, and their sums (unrounded).
+template <bool kF16>
+__device__ __forceinline__ void wide_exp32(const float (&s)[32], uint32_t (&pk)[16], float2 c2, float2 nm2, float2& sum0, float2& sum1, float2& sum2, float2& sum3) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+        float2 e[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 x = __ffma2_rn(make_float2(s[2 * (i + k)], s[2 * (i + k) + 1]), c2, nm2);
+            e[k] = make_float2(ex2(x.x), ex2(x.y));
+            pk[i + k] = pack_weights<kF16>(e[k].x, e[k].y);
+        }
+        sum0 = __fadd2_rn(sum0, e[0]);
+        sum1 = __fadd2_rn(sum1, e[1]);
+        sum2 = __fadd2_rn(sum2, e[2]);
+        sum3 = __fadd2_rn(sum3, e[3]);
+    }
+}
+
 // One score tile (in c0..c3): the row's maximum, the rescaling of O where it grows by more than the lag, the weights in four pieces.  If the unit has another
 // tile, its scores replace the current ones before the function returns.
+template <bool kF16>
 __device__ __forceinline__ void wide_softmax_tile(const WideCtx& cx, float (&c0)[32], float (&c1)[32], float (&c2)[32], float (&c3)[32], int wg, bool more,
                                                   bool first, uint32_t& s_par, uint32_t pv_par, uint32_t s_tmem, uint32_t p_tmem, uint32_t o_tmem, float c,
                                                   float& m, float& l, int iter) {
@@ -367,12 +599,12 @@ __device__ __forceinline__ void wide_softmax_tile(const WideCtx& cx, float (&c0)
             }
         }
     }
-    const float2 c2f = make_float2(c, c), nm2 = make_float2(-m, -m);
+    const float2 c2f = make_float2(c, c), nm2 = make_float2((kF16 ? kF16Shift : 0.f) - m, (kF16 ? kF16Shift : 0.f) - m);      // fp16 weights carry 2^7
     float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0, sum2 = sum0, sum3 = sum0;
     uint32_t pk[16];
     const uint32_t p_bar = cx.bars + (kWPReady + 2 * wg) * 8;
 #define CP_WIDE_PIECE(cur, q)                                                           \
-    exp32<false>(cur, pk, c2f, nm2, sum0, sum1, sum2, sum3);                            \
+    wide_exp32<kF16>(cur, pk, c2f, nm2, sum0, sum1, sum2, sum3);                            \
     TMEM_ST16R(p_tmem + (q) * 16, pk, 0);                                               \
     if ((q) + 1 == kWideSplit || (q) == 3) {                                            \
         tc_wait_st();                                                                   \
@@ -411,64 +643,113 @@ __device__ __forceinline__ void wide_softmax_tile(const WideCtx& cx, float (&c0)
     l += st.x + st.y;
 }
 
+// Column of O that holds element i of a head (see wide_widen).
+template <Kind kKind>
+__device__ __forceinline__ constexpr int wide_column(int i) { return kKind == kMx4 ? (i & ~7) | (i & 3) << 1 | (i >> 2 & 1) : i; }
+
+template <Kind kKind>
 __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx& cx, WideUnits units, int wg, int64_t total, int ctas) {
+    using W = Wide<kKind>;
+    constexpr bool kF16 = kKind == kE4m3;
     const DecodeParams& p = w.d;
     const int lane = threadIdx.x & 31, warp_in_wg = threadIdx.x >> 5 & 3;
     const uint32_t lane_addr = (uint32_t)(warp_in_wg * 32) << 16;
     const uint32_t s_tmem = cx.tmem + lane_addr + kWTmemS, p_tmem = cx.tmem + lane_addr + kWTmemP + wg * 64, o_tmem = cx.tmem + lane_addr + kWTmemO + wg * 128;
     const int cls = (int)(blockIdx.x % w.classes), run = (int)(blockIdx.x / w.classes);
-    const int row = wg * kBlockM + warp_in_wg * 32 + lane;                // of the class
+    const bool turns = w.tiles == 1;                                      // the warpgroups take the K/V tiles in turn
+    const int tile_row = warp_in_wg * 32 + lane, row = (turns ? 0 : wg * kBlockM) + tile_row;      // of the class
     const int r = cls * w.class_rows + row, t = r / p.G;                  // of the KV head; its token
     const bool in_class = row < w.class_rows && r < p.rows;
-    const float c = p.scale_log2;
-    uint32_t s_par = 0, tile_cnt = 0;
+    const int step = turns ? 2 : 1;
+    float* travel = reinterpret_cast<float*>(cx.gen + W::kQ + kTileBytes);      // 64 columns of an accumulator: [column][row]
+    float c = p.scale_log2;
+    uint32_t s_par = 0, tile_cnt = 0, travels = 0;
+    // the second warpgroup's accumulator goes to the first in parts, through one buffer
+    auto before_part = [&]() {
+        if (wg == 1) cx.wait(kWTravelFree, (travels & 1) ^ 1, (int)travels);
+        else cx.wait(kWTravelFull, travels & 1, (int)travels);
+        __syncwarp();
+    };
+    auto after_part = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(cx.bars + (wg == 1 ? kWTravelFull : kWTravelFree) * 8);
+        ++travels;
+    };
     for (int round = 0; units.valid(); ++round) {
         const Request rq = units.cur.r;
         const int b = units.cur.b, u = units.cur.u, j0 = units.t_begin, n = units.t_end, m_tree = rq.len - rq.base;
+        const int tt = wide_token(p, t, m_tree);
+        const bool live = in_class && tt >= 0 && tt < m_tree;             // rows without a token: zeros, -inf
         TreeRow tr;
         tr.mask = 0;
         tr.lim = 0;
-        if (in_class) tr = tree_row(p, b, t, rq.base, m_tree);
-        const int low = tr.lim - p.window;
+        if (live) tr = tree_row(p, b, tt, rq.base, m_tree);
+        const int low = (live ? tr.lim : rq.len) - p.window;
+        const int j1 = j0 + (turns ? wg : 0);                             // this warpgroup's first tile
+        const bool some = j1 < n;
         float m = kNoKey, l = 0.f;
-        float s0[32], s1[32], s2[32], s3[32];
-        cx.wait(kWSReady + wg, s_par, j0);
-        __syncwarp();
-        s_par ^= 1u;
-        tc_fence_after();
-        CP_LOAD_S3(s0, s1, s2)
-        TMEM_LD32(s_tmem + 96, s3, 0);
-        tc_wait_ld();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(cx.bars + kWSFree * 8);
-#pragma unroll 1
-        for (int j = j0; j < n; ++j) {
-            const int key0 = units.key_of(j);
-            if (!units.full(p, key0)) {
-                wide_hide(s0, wide_seen(key0, rq.base, low, p.sinks, tr.mask));
-                wide_hide(s1, wide_seen(key0 + 32, rq.base, low, p.sinks, tr.mask));
-                wide_hide(s2, wide_seen(key0 + 64, rq.base, low, p.sinks, tr.mask));
-                wide_hide(s3, wide_seen(key0 + 96, rq.base, low, p.sinks, tr.mask));
+        if (some) {
+            float s0[32], s1[32], s2[32], s3[32];
+            cx.wait(kWSReady + wg, s_par, j1);
+            __syncwarp();
+            s_par ^= 1u;
+            tc_fence_after();
+            CP_LOAD_S3(s0, s1, s2)
+            TMEM_LD32(s_tmem + 96, s3, 0);
+            tc_wait_ld();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(cx.bars + kWSFree * 8);
+            if (kF16) {
+                const int e = reinterpret_cast<const int8_t*>(cx.gen + W::kExp)[(round & 1) * kWideRows + row];
+                // c > 0: the sign of a scale is in the queries; with a scale of zero hidden keys must still be -inf
+                c = fmaxf(fabsf(p.k_scale[u]) * p.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23), 1e-35f);
             }
-            wide_softmax_tile(cx, s0, s1, s2, s3, wg, j + 1 < n, j == j0, s_par, (tile_cnt - 1) & 1, s_tmem, p_tmem, o_tmem, c, m, l, j);
-            ++tile_cnt;
+#pragma unroll 1
+            for (int j = j1; j < n; j += step) {
+                const int key0 = units.key_of(j);
+                if (!units.full(p, key0)) {
+                    wide_hide(s0, wide_seen(key0, rq.base, low, p.sinks, tr.mask));
+                    wide_hide(s1, wide_seen(key0 + 32, rq.base, low, p.sinks, tr.mask));
+                    wide_hide(s2, wide_seen(key0 + 64, rq.base, low, p.sinks, tr.mask));
+                    wide_hide(s3, wide_seen(key0 + 96, rq.base, low, p.sinks, tr.mask));
+                }
+                wide_softmax_tile<kF16>(cx, s0, s1, s2, s3, wg, j + step < n, j == j1, s_par, (tile_cnt - 1) & 1, s_tmem, p_tmem, o_tmem, c, m, l, j);
+                ++tile_cnt;
+            }
+            cx.wait(kWPvDone + wg, (tile_cnt - 1) & 1, n);
+            __syncwarp();
+            tc_fence_after();
         }
         const bool whole = units.whole;
         const int64_t x_end = units.cur.x + kWideCost + rq.n;
         units.next(p);
-        cx.wait(kWPvDone + wg, (tile_cnt - 1) & 1, n);
+        float f0 = 1.f, f1 = 0.f;                                         // factors of this accumulator and of the one that travels
         cx.wait(kWOdd, round & 1, n);
         __syncwarp();
-        tc_fence_after();
-        const unsigned long long* odd = reinterpret_cast<const unsigned long long*>(cx.gen + kWideOdd) + 2 * (round & 1);
-        const bool live = in_class && t < m_tree;          // rows behind the tree: zeros, -inf
+        if (turns) {                   // maxima and sums first
+            before_part();
+            if (wg == 1) {
+                reinterpret_cast<float2*>(travel)[tile_row] = make_float2(m, l);
+            } else {
+                const float2 o = reinterpret_cast<const float2*>(travel)[tile_row];
+                const float mx = fmaxf(m, o.x);
+                f0 = ex2(m - mx);
+                f1 = ex2(o.x - mx);
+                l = l * f0 + o.y * f1;
+                m = mx;
+            }
+            after_part();
+        }
+        const unsigned long long* odd = reinterpret_cast<const unsigned long long*>(cx.gen + W::kOdd) + 2 * (round & 1);
         const bool any_odd = live && (odd[0] | odd[1]) != 0;
-        const float inv = !whole ? 1.f : (l == 0.f ? 0.f : 1.f / l);
+        const float inv = !whole ? 1.f : (l == 0.f ? 0.f : (kF16 ? p.v_scale[u] : 1.f) / l);
+        f0 *= inv;
+        f1 *= inv;
         const int64_t slot = 2 * ((int64_t)cls * w.runs + run) + (j0 > 0 ? 0 : 1);
         const int head = u * p.G + r - t * p.G;
         // offset of this row in the destination, -1: none
-        const int64_t at = !in_class ? -1 : (whole ? (((int64_t)b * p.n_q + t) * p.Hq + head) * kD : (slot * kWideRows + row) * kD);
+        const int64_t at = !in_class || (turns && wg == 1) ? -1 : (whole ? (((int64_t)b * p.n_q + t) * p.Hq + head) * kD : (slot * kWideRows + row) * kD);
         const int qt = lane & 3;
         int64_t to[4];                 // of the rows of this lane's quad: the lanes swap 16-byte pieces, so that a store writes 64 contiguous bytes of a row
 #pragma unroll
@@ -476,16 +757,37 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
 #pragma unroll 1
         for (int cc = 0; cc < 4; ++cc) {
             float o[32];
-            TMEM_LD32(o_tmem + cc * 32, o, 0);
-            tc_wait_ld();
+            if (some) {
+                TMEM_LD32(o_tmem + cc * 32, o, 0);
+                tc_wait_ld();
+            } else {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = live ? o[i] * inv : 0.f;
+                for (int i = 0; i < 32; ++i) o[i] = 0.f;
+            }
+            if (turns) {
+                float* col = travel + (cc & 1) * 32 * kBlockM + tile_row;
+                if ((cc & 1) == 0) before_part();                         // 64 columns at a time
+                if (wg == 1) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) col[i * kBlockM] = o[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = live ? o[i] * f0 + col[i * kBlockM] * f1 : 0.f;
+                }
+                if ((cc & 1) == 1) after_part();
+                if (wg == 1) continue;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = live ? o[i] * f0 : 0.f;
+            }
             if (whole) {
                 uint4 v[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    v[i] = make_uint4(pack_bf16(o[8 * i], o[8 * i + 1]), pack_bf16(o[8 * i + 2], o[8 * i + 3]), pack_bf16(o[8 * i + 4], o[8 * i + 5]),
-                                      pack_bf16(o[8 * i + 6], o[8 * i + 7]));
+                for (int i = 0; i < 4; ++i) {
+#define CP_O(k) o[wide_column<kKind>(8 * i + (k))]
+                    v[i] = make_uint4(pack_bf16(CP_O(0), CP_O(1)), pack_bf16(CP_O(2), CP_O(3)), pack_bf16(CP_O(4), CP_O(5)), pack_bf16(CP_O(6), CP_O(7)));
+#undef CP_O
+                }
                 quad_transpose(v, qt);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
@@ -497,7 +799,8 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int k = half * 16 + 4 * i;
-                        v[i] = make_uint4(__float_as_uint(o[k]), __float_as_uint(o[k + 1]), __float_as_uint(o[k + 2]), __float_as_uint(o[k + 3]));
+                        v[i] = make_uint4(__float_as_uint(o[wide_column<kKind>(k)]), __float_as_uint(o[wide_column<kKind>(k + 1)]),
+                                          __float_as_uint(o[wide_column<kKind>(k + 2)]), __float_as_uint(o[wide_column<kKind>(k + 3)]));
                     }
                     quad_transpose(v, qt);
 #pragma unroll
@@ -508,12 +811,12 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
         }
         tc_fence_before();
         __syncwarp();                  // also: the rows are written, by the lanes of their quads
-        if (any_odd) wide_odd_row(p, odd, b, rq.base, rq.len, u, t, whole, at);
+        if (any_odd && at >= 0) wide_odd_row<kKind>(p, odd, b, rq.base, rq.len, u, tt, whole, at);
         if (lane == 0) mbar_arrive(cx.bars + (kWOFree + wg) * 8);
-        if (in_class) {
+        if (at >= 0) {
             if (whole) {
                 p.lse[(int64_t)head * ((int64_t)p.B * p.n_q) + (int64_t)b * p.n_q + t] =
-                    live && l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                    live && l != 0.f ? (m + log2f(l) - (kF16 ? kF16Shift : 0.f)) * 0.6931471805599453f : -INFINITY;
             } else {
                 p.part_ml[(slot * kWideRows + row) * 2] = live ? m : kNoKey;
                 p.part_ml[(slot * kWideRows + row) * 2 + 1] = live ? l : 0.f;
@@ -534,25 +837,33 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
 }
 #undef CP_LOAD_S3
 
-__global__ void __launch_bounds__(kWideThreads, 1)
+template <Kind kKind>
+__global__ void __launch_bounds__(Wide<kKind>::kThreads, 1)
 tree_wide_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ WideParams w) {
+    using W = Wide<kKind>;
+    constexpr int kThreadsHere = W::kThreads;
     extern __shared__ uint8_t smem_raw[];
     const DecodeParams& p = w.d;
     WideCtx c;
     c.smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     c.gen = smem_raw + (c.smem - smem_u32(smem_raw));
-    c.bars = c.smem + kWideBar;
-    c.abort_flag = reinterpret_cast<volatile uint32_t*>(c.gen + kWideAbort);
+    c.bars = c.smem + W::kBar;
+    c.abort_flag = reinterpret_cast<volatile uint32_t*>(c.gen + W::kAbort);
     c.status = p.status;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int run = (int)(blockIdx.x / w.classes);
-    let_next_launch_begin();
     if (tid == 0) {
         mbar_init(c.bars + kWQFull * 8, 1);
         mbar_init(c.bars + kWQEmpty * 8, 1);
-        for (int s = 0; s < kWideStages; ++s) {
-            mbar_init(c.bars + (kWKvFull + s) * 8, 1);
-            mbar_init(c.bars + (kWKvEmpty + s) * 8, 1);
+        for (int s = 0; s < kMaxRing; ++s) {
+            mbar_init(c.bars + (kWKFull + s) * 8, W::kRawTiles ? kConvWarps : 1);
+            mbar_init(c.bars + (kWKEmpty + s) * 8, 1);
+            mbar_init(c.bars + (kWVFull + s) * 8, W::kRawTiles ? kConvWarps : 1);
+            mbar_init(c.bars + (kWVEmpty + s) * 8, 1);
+        }
+        for (int s = 0; s < W::kRaw; ++s) {
+            mbar_init(c.bars + (kWRawFull + s) * 8, 32);               // one arrival per lane of the warp that copies
+            mbar_init(c.bars + (kWRawEmpty + s) * 8, kConvWarps);
         }
         mbar_init(c.bars + kWSFree * 8, 4);
         for (int h = 0; h < 2; ++h) {
@@ -562,17 +873,19 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
             mbar_init(c.bars + (kWOFree + h) * 8, 4);
         }
         mbar_init(c.bars + kWOdd * 8, 1);
+        mbar_init(c.bars + kWTravelFull * 8, 4);
+        mbar_init(c.bars + kWTravelFree * 8, 4);
         *c.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(c.smem + kWideTmemPtr), "r"(512u) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(c.smem + W::kTmemPtr), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     // where this CTA's run starts: requests are dealt to the threads in order, a prefix sum over their places finds it
-    int64_t* scan = reinterpret_cast<int64_t*>(c.gen + kWideScan);
-    int32_t* start = reinterpret_cast<int32_t*>(scan + kWideThreads / 32);
-    const int per = (p.B + kWideThreads - 1) / kWideThreads;
+    int64_t* scan = reinterpret_cast<int64_t*>(c.gen + W::kScan);
+    int32_t* start = reinterpret_cast<int32_t*>(scan + kThreadsHere / 32);
+    const int per = (p.B + kThreadsHere - 1) / kThreadsHere;
     int64_t mine = 0;
     for (int i = 0; i < per; ++i) {
         const int b = tid * per + i;
@@ -595,9 +908,9 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    c.tmem = *reinterpret_cast<volatile uint32_t*>(c.gen + kWideTmemPtr);
+    c.tmem = *reinterpret_cast<volatile uint32_t*>(c.gen + W::kTmemPtr);
     int64_t before = inc - mine, total = 0;
-    for (int i = 0; i < kWideThreads / 32; ++i) {
+    for (int i = 0; i < kThreadsHere / 32; ++i) {
         if (i < warp) before += scan[i];
         total += scan[i];
     }
@@ -624,14 +937,19 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         WideUnits units;
         units.begin(p, start, x0, x1);
         if (warp < 8) {
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWideRegsSoftmax));
-            if (warp < 4 || w.tiles == 2) wide_softmax(w, c, units, warp >> 2, total, ctas);
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(W::kRegsSoftmax));
+            wide_softmax<kKind>(w, c, units, warp >> 2, total, ctas);
         } else {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWideRegsOther));
-            if (warp == 8) wide_producer(w, c, units, &tmK, &tmV);
-            else if (warp == 9) wide_scores(w, c, units);
-            else if (warp == 10) wide_outputs(w, c, units);
-            else wide_queries(w, c, units);
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(W::kRegsOther));
+            if constexpr (W::kRawTiles) {
+                if (warp == 8) wide_raw<kKind>(w, c, units);
+                else if (warp >= 12) wide_widen<kKind>(w, c, units, warp - 12);
+            } else {
+                if (warp == 8) wide_producer(w, c, units, &tmK, &tmV);
+            }
+            if (warp == 9) wide_scores<kKind>(w, c, units);
+            else if (warp == 10) wide_outputs<kKind>(w, c, units);
+            else if (warp == 11) wide_queries<kKind>(w, c, units);
         }
     }
     tc_fence_before();
@@ -648,10 +966,10 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
 
 // Joins the pieces of cut units: CTA (v, y), v = class * runs + run of a unit's first piece; a warp a row.  Pieces: slot 2v + 1, then slots 2v', v' = v + 1, ..
 constexpr int kWideJoinRows = 8;
+template <Kind kKind>
 __global__ void __launch_bounds__(32 * kWideJoinRows)
 tree_join_kernel(const __grid_constant__ WideParams w) {
     const DecodeParams& p = w.d;
-    wait_for_launch_before();
     const int v = blockIdx.x, row = blockIdx.y * kWideJoinRows + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int4 me = *reinterpret_cast<const int4*>(p.meta + 4 * v);
     const int r = v / w.runs * w.class_rows + row;
@@ -676,12 +994,12 @@ tree_join_kernel(const __grid_constant__ WideParams w) {
     }
     const int t = r / p.G, head = me.y * p.G + r - t * p.G;
     const int64_t token = (int64_t)me.x * p.n_q + t;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float inv = sum == 0.f ? 0.f : (kKind == kE4m3 ? p.v_scale[me.y] : 1.f) / sum;
     uint2 out;
     out.x = pack_bf16(a.x * inv, a.y * inv);
     out.y = pack_bf16(a.z * inv, a.w * inv);
     *reinterpret_cast<uint2*>(p.out + (token * p.Hq + head) * kD + lane * 4) = out;
-    if (lane == 0) p.lse[(int64_t)head * ((int64_t)p.B * p.n_q) + token] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.6931471805599453f;
+    if (lane == 0) p.lse[(int64_t)head * ((int64_t)p.B * p.n_q) + token] = sum == 0.f ? -INFINITY : (mx + log2f(sum) - (kKind == kE4m3 ? kF16Shift : 0.f)) * 0.6931471805599453f;
 }
 
 }  // namespace

@@ -159,7 +159,7 @@ struct cp_ctx {
     int stage_next;
     cpattn::EncodeTiledFn encode_tiled;
     bool attn_attr_set;
-    bool tree_attr_set[3];
+    bool tree_attr_set[3][2];
     uint32_t decode_attr_set[3];       // per kind of cache, one bit per instantiation of the decode kernel
     // schedule reuse (cp_ctx_cache_schedule): what the last attention call left in its workspace
     bool cache_on;

@@ -14,25 +14,23 @@ int encode_kv(cp_ctx* ctx, const CacheView& v, bool second, CUtensorMap* map, co
     return CP_OK;
 }
 
-template <Kind kKind>
+template <Kind kKind, int kTiles>
 int launch(cp_ctx* ctx, const WideParams& w, const CacheView& view, cudaStream_t s, const char* who) {
-    using W = Wide<kKind>;
+    using W = Wide<kKind, kTiles>;
     CUtensorMap k = {}, v = {};
     if (kKind == kBf16) {
         if (int rc = encode_kv(ctx, view, false, &k, who)) return rc;
         if (int rc = encode_kv(ctx, view, true, &v, who)) return rc;
     }
-    if (!ctx->tree_attr_set[kKind]) {
-        if (int rc = check_cuda(cudaFuncSetAttribute(tree_wide_kernel<kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, W::kSmem),
+    if (!ctx->tree_attr_set[kKind][kTiles - 1]) {
+        if (int rc = check_cuda(cudaFuncSetAttribute(tree_wide_kernel<kKind, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize, W::kSmem),
                                 "cudaFuncSetAttribute(tree)")) return rc;
-        ctx->tree_attr_set[kKind] = true;
+        ctx->tree_attr_set[kKind][kTiles - 1] = true;
     }
-    tree_wide_kernel<kKind><<<(unsigned)(w.runs * w.classes), W::kThreads, W::kSmem, s>>>(k, v, w);
+    tree_wide_kernel<kKind, kTiles><<<(unsigned)(w.runs * w.classes), W::kThreads, W::kSmem, s>>>(k, v, w);
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
     const unsigned y = (unsigned)((w.class_rows + kWideJoinRows - 1) / kWideJoinRows);
-    // an ordinary launch: the first kernel moves registers between its warps as it starts, and nothing is to be set up beside it then
-    tree_join_kernel<kKind><<<dim3((unsigned)(w.runs * w.classes), y), 32 * kWideJoinRows, 0, s>>>(w);
-    return check_cuda(cudaGetLastError(), who);
+    return launch_behind(tree_join_kernel<kKind>, dim3((unsigned)(w.runs * w.classes), y), 32 * kWideJoinRows, s, who, w);
 }
 
 }  // namespace
@@ -51,16 +49,16 @@ int launch_tree_wide(cp_ctx* ctx, int kind, const void* decode_params, const voi
     const int grid = std::min(ctx->num_sms, kMaxGrid);
     w.classes = (w.d.rows + kWideRows - 1) / kWideRows;
     w.class_rows = (w.d.rows + w.classes - 1) / w.classes;
-    w.tiles = w.class_rows > kBlockM ? 2 : 1;
     w.runs = grid / w.classes;
     const size_t n = 2 * (size_t)kMaxGrid * kWideRows;
     w.d.part_o = static_cast<float*>(workspace);
     w.d.part_ml = w.d.part_o + n * kD;
     w.d.meta = reinterpret_cast<int32_t*>(w.d.part_ml + n * 2);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (kind == kE4m3) return launch<kE4m3>(ctx, w, view, s, who);
-    if (kind == kMx4) return launch<kMx4>(ctx, w, view, s, who);
-    return launch<kBf16>(ctx, w, view, s, who);
+    const bool two = w.class_rows > kBlockM;
+    if (kind == kE4m3) return two ? launch<kE4m3, 2>(ctx, w, view, s, who) : launch<kE4m3, 1>(ctx, w, view, s, who);
+    if (kind == kMx4) return two ? launch<kMx4, 2>(ctx, w, view, s, who) : launch<kMx4, 1>(ctx, w, view, s, who);
+    return two ? launch<kBf16, 2>(ctx, w, view, s, who) : launch<kBf16, 1>(ctx, w, view, s, who);
 }
 
 }  // namespace cpattn

@@ -14,8 +14,8 @@
 //   - Warps: two softmax warpgroups; a producer that fetches K/V tiles page by page; the issuers of S = Q K^T and of O += P V; a warp that gathers the
 //     unit's query rows.  S, P and O live in TMEM: S | P0 | P1 | O0 | O1.  S is one buffer that the tiles use in turn, read into registers at
 //     once, so the next product runs under the exponentials.
-//   - bf16 tiles come by TMA.  The rows of the other caches come by cp.async into a ring of raw tiles, and a fourth warpgroup widens them: E4M3 to fp16
-//     (queries and weights are then fp16 as in the narrow form), 4-bit codes and exponents to bf16, both exactly.
+//   - bf16 tiles come by TMA.  The rows of the other caches are copied by a fourth warpgroup with cp.async, which widens them into the tiles: E4M3 to
+//     fp16 (queries and weights are then fp16 as in the narrow form), 4-bit codes and exponents to bf16, both exactly.
 //   - Only the last tiles of a unit and those at a window's edge hide keys from rows.  Their masks are bits: of the tree's mask and of the window.  A hidden
 //     key's weight is zero, but zero times an infinity is not: the issuer of P V looks through the V of these tiles and clears what is no
 //     finite number; what some rows do see of it is added to their results when they are written.
@@ -32,29 +32,35 @@ constexpr int kWideCost = 3;                               // fixed cost of a un
 constexpr float kWideLag = 8.0f;                           // the running maximum may lag by a factor 2^8
 constexpr int kWideSplit = 3;                              // P is handed over in two pieces: three quarters of the keys, then the rest
 constexpr int kConvWarps = 4;
-constexpr int kMaxRing = 3, kMaxRaw = 7;
+constexpr int kMaxRing = 3;
+constexpr int kUnitBytes = 80;
 
-template <Kind kKind>
+// kTiles: score tiles of a unit; with one, the warpgroups take the K/V tiles in turn.
+template <Kind kKind, int kTiles>
 struct Wide {
-    static constexpr bool kRawTiles = kKind != kBf16;
+    static constexpr bool kRawTiles = kKind != kBf16, kTurns = kTiles == 1;
     static constexpr int kThreads = kRawTiles ? 512 : 384;
     // register budgets after the roles split; they stay below the register file by one step at least
     static constexpr int kRegsSoftmax = kRawTiles ? 184 : 200, kRegsOther = kRawTiles ? 64 : 104;
     static_assert(256 * kRegsSoftmax + (kThreads - 256) * kRegsOther <= 65536 - 1024, "leave slack in the register file");
     // Rings of 32 KB tiles, one for K and one for V: a full barrier has one waiter, who has waited for each of its phases.  (With K and V in turn in one ring the
     // issuer of S can be at a slot whose V has not landed yet, when the tiles are taken in turn; its wait would take the phase before that for its own.)
-    static constexpr int kStagesK = kRawTiles ? 2 : 3, kStagesV = kRawTiles ? 1 : 2, kStages = kStagesK + kStagesV;
-    static constexpr uint32_t kRawCodes = kKind == kE4m3 ? 16384u : 8192u;
-    static constexpr uint32_t kRawBytes = kKind == kE4m3 ? 16384u : 8704u;      // 4-bit: the codes of 128 keys, then their exponents
-    static constexpr int kRaw = kKind == kBf16 ? 0 : (kKind == kE4m3 ? 4 : 7);
-    // shared memory: two query tiles (or one and the accumulator that travels), the ring, the raw tiles, barriers and small areas
-    static constexpr uint32_t kQ = 0, kKV = 2 * kTileBytes, kRawAt = kKV + kStages * kTileBytes;
-    static constexpr uint32_t kBar = kRawAt + kRaw * kRawBytes;
+    static constexpr int kStagesK = kRawTiles ? 2 : 3, kStagesV = 2, kStages = kStagesK + kStagesV;
+    static constexpr int kWarpKeys = kBlockN / kConvWarps;
+    static constexpr uint32_t kRawCodes = kWarpKeys * (kKind == kE4m3 ? 128u : 64u);
+    static constexpr uint32_t kRawBytes = kRawCodes + (kKind == kMx4 ? kWarpKeys * 4u : 0u);       // 4-bit: codes, then exponents
+    static constexpr int kRaw = kKind == kBf16 ? 0 : (kKind == kE4m3 ? (kTurns ? 3 : 2) : (kTurns ? 6 : 3));      // slots of a warp's ring
+    static constexpr int kQueryWarps = kRawTiles ? 2 : 1;
+    // shared memory: the query tiles, the ring, the raw tiles, what the warpgroups tell one another, barriers and small areas
+    static constexpr uint32_t kQ = 0, kKV = kTiles * kTileBytes, kRawAt = kKV + kStages * kTileBytes;
+    static constexpr uint32_t kMl = kRawAt + kRaw * kConvWarps * kRawBytes;                        // [unit parity][warpgroup][row]: maximum and sum
+    static constexpr uint32_t kBar = kMl + (kTurns ? 2 * 2 * kBlockM * 8 : 0);
     static constexpr uint32_t kOdd = kBar + 48 * 8;        // [unit parity][2] keys whose V is no finite number (see odd_values)
     static constexpr uint32_t kScan = kOdd + 32;           // sums of the warps, then the run's start
     static constexpr uint32_t kExp = kScan + 16 * 8 + 16;  // [unit parity][row]: exponent by which a row of E4M3 queries was scaled up
-    static constexpr uint32_t kTmemPtr = kExp + (kKind == kE4m3 ? 2 * kWideRows : 0), kAbort = kTmemPtr + 4;
-    static constexpr uint32_t kSmem = kAbort + 12 + 1024;  // slack for manual alignment
+    static constexpr uint32_t kUnits = (kExp + (kKind == kE4m3 ? 2 * kWideRows : 0) + 15) / 16 * 16;      // a copy per warp
+    static constexpr uint32_t kTmemPtr = kUnits + kThreads / 32 * kUnitBytes, kAbort = kTmemPtr + 4;
+    static constexpr uint32_t kSmem = kAbort + 12;
     static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
 };
 enum WideBar : uint32_t {
@@ -69,11 +75,8 @@ enum WideBar : uint32_t {
     kWPvDone = kWPReady + 4,                 // + warpgroup: P V of a step has finished
     kWOFree = kWPvDone + 2,                  // + warpgroup: O has been read
     kWOdd = kWOFree + 2,                     // the unit's list of odd keys is complete
-    kWTravelFull = kWOdd + 1,                // a part of the second warpgroup's accumulator is in shared memory
-    kWTravelFree = kWTravelFull + 1,         // and has been read
-    kWRawFull = kWTravelFree + 1,            // + raw stage
-    kWRawEmpty = kWRawFull + kMaxRaw,        // + raw stage
-    kNumWideBars = kWRawEmpty + kMaxRaw
+    kWMl = kWOdd + 1,                        // + warpgroup: its accumulator, maxima and sums of the unit are complete (tiles in turn)
+    kNumWideBars = kWMl + 2
 };
 static_assert(kNumWideBars <= 48, "barrier area");
 
@@ -83,16 +86,17 @@ struct WideParams {
     DecodeParams d;
     int32_t classes;           // row classes of a KV head
     int32_t class_rows;        // rows of a class (the last may have fewer)
-    int32_t tiles;             // 2: score tiles of a unit; 1: one, and the warpgroups take the K/V tiles in turn
     int32_t runs;              // CTAs of a class
 };
 
-// The units of this CTA, one after the other: request b, KV head u, tiles [t_begin, t_end).
+// The units of this CTA, one after the other: request b, KV head u, tiles [t_begin, t_end).  Every warp has a copy in shared memory that it steps by itself, which
+// keeps a score of registers free in every role.
 struct WideUnits {
     Cursor<kBlockN, true> cur;
     int64_t x1;
     int t_begin, t_end;
-    bool whole;
+    bool whole, valid;
+    // by one lane
     __device__ __forceinline__ void begin(const DecodeParams& p, const int32_t* start, int64_t x0, int64_t end) {
         cur.b = start[0];
         cur.u = start[1];
@@ -106,16 +110,21 @@ struct WideUnits {
         t_begin = cur.t;
         t_end = (int)min((int64_t)cur.r.n, x1 - cur.x - kWideCost);
         whole = t_begin == 0 && t_end == cur.r.n;
+        valid = cur.x + kWideCost + cur.t < x1;
     }
-    __device__ __forceinline__ bool valid() const { return cur.x + kWideCost + cur.t < x1; }
+    // by the warp
     __device__ __forceinline__ void next(const DecodeParams& p) {
-        cur.t = 0;
-        cur.x += kWideCost + cur.r.n;
-        if (++cur.u == p.Hkv) {
-            cur.u = 0;
-            if (++cur.b < p.B) cur.r = request_of<kBlockN, true>(p, cur.b);
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) {
+            cur.t = 0;
+            cur.x += kWideCost + cur.r.n;
+            if (++cur.u == p.Hkv) {
+                cur.u = 0;
+                if (++cur.b < p.B) cur.r = request_of<kBlockN, true>(p, cur.b);
+            }
+            span();
         }
-        span();
+        __syncwarp();
     }
     __device__ __forceinline__ int key_of(int t) const { return (t < cur.r.sink_tiles ? t : t + cur.r.skip) * kBlockN; }
     // every row of the tree sees all keys of the tile
@@ -123,6 +132,8 @@ struct WideUnits {
         return key0 + kBlockN <= cur.r.base && (key0 >= cur.r.len - p.window || key0 + kBlockN <= p.sinks);
     }
 };
+
+static_assert(sizeof(WideUnits) <= kUnitBytes, "room for the units");
 
 // The token of a row among the last m of its sequence, < 0 or >= m: none.  Chains are trees in which every token sees those before it; of a sequence shorter
 // than n_q the last rows are its tokens.
@@ -150,8 +161,9 @@ struct WideRing {
 // ---------------------------------------------------------------------------------------------- producer
 // Load order = order of first use: K(j0), then K(j + 1) before V(j).  Lane i < pages of a tile holds a page id; those of the next K tile are
 // fetched while the current ones are used.  Pages that no row sees anything of are read as zeros.
-__device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx& c, WideUnits units, const CUtensorMap* tmK, const CUtensorMap* tmV) {
-    using W = Wide<kBf16>;
+template <int kTiles>
+__device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx& c, WideUnits& units, const CUtensorMap* tmK, const CUtensorMap* tmV) {
+    using W = Wide<kBf16, kTiles>;
     const DecodeParams& p = w.d;
     const int lane = threadIdx.x & 31;
     const int page_tokens = 1 << p.page_shift, per_tile = kBlockN >> p.page_shift;
@@ -159,17 +171,14 @@ __device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx
     const int outside = (int)p.num_pages;                  // a page coordinate behind the tensor: TMA fills zeros
     WideRing<W::kStagesK> kr = {0, 1};
     WideRing<W::kStagesV> vr = {0, 1};
-    for (; units.valid(); units.next(p)) {
+    for (; units.valid; units.next(p)) {
         const Request r = units.cur.r;
         const int32_t* row = p.table + units.cur.b * p.table_stride;
         auto fetch = [&](int t) {
             const int key0 = units.key_of(t), key = key0 + lane * page_tokens;
             int id = outside;
-            if (lane < per_tile && key < r.len && (key + page_tokens > r.low(p) || key < p.sinks)) {
-                id = __ldg(row + (key >> p.page_shift));
-                if ((uint32_t)id >= (uint32_t)outside) id = outside;
-            }
-            return id;
+            if (lane < per_tile && key < r.len && (key + page_tokens > r.low(p) || key < p.sinks)) id = __ldg(row + (key >> p.page_shift));
+            return id;                                     // looked at when it is used: the load travels meanwhile
         };
         int ahead = fetch(units.t_begin), k_ids = 0, v_ids = 0;
         const int n_loads = 2 * (units.t_end - units.t_begin);
@@ -179,7 +188,7 @@ __device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx
             int ids;
             if (!is_v) {
                 v_ids = k_ids;
-                k_ids = ids = ahead;
+                k_ids = ids = (uint32_t)ahead < (uint32_t)outside ? ahead : outside;
                 if (++j < units.t_end) ahead = fetch(j);
             } else {
                 ids = ld == n_loads - 1 ? k_ids : v_ids;
@@ -204,187 +213,210 @@ __device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx
 }
 
 // ---------------------------------------------------------------------------------------------- raw tiles
-// E4M3 and 4-bit rows of 128 keys, K and V in turn; slots that no row sees are zeros.  16-byte chunk x of key k sits at chunk x ^ (k & 7) (4-bit rows of four
-// chunks: x ^ (k / 2 & 3)), so that eight lanes with eight keys and the same chunk meet no bank twice.
-template <Kind kKind>
-__device__ __forceinline__ void wide_raw(const WideParams& w, const WideCtx& c, WideUnits units) {
-    using W = Wide<kKind>;
+// E4M3 and 4-bit rows: a warp owns 32 keys of every tile.  It copies them (K, then V, tile by tile) into a ring of its own with cp.async, slots that no row sees as
+// zeros, and widens what has landed into the tiles that the tensor cores read: 16 E4M3 codes -> 16 fp16 values; a block of 32 4-bit codes -> 32 bf16
+// values, in whose groups of eight elements i and i + 4 stand side by side (the queries are laid out alike, and the columns of O are taken in that order).
+// 16-byte chunk x of key k sits at chunk x ^ (k & 7) of its row (4-bit rows of four chunks: x ^ (k / 2 & 3)), so that eight lanes with eight keys and the same
+// chunk meet no bank twice.
+template <Kind kKind, int kTiles>
+__device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c, WideUnits& units, int cw) {
+    using W = Wide<kKind, kTiles>;
     const DecodeParams& p = w.d;
-    constexpr int kChunks = kKind == kE4m3 ? 8 : 4, kRowsPer = 32 / kChunks;
+    constexpr int kChunks = kKind == kE4m3 ? 8 : 4, kRowsPer = 32 / kChunks, kKeys = W::kWarpKeys, kCopies = kKeys / kRowsPer;
     const int lane = threadIdx.x & 31, chunk = lane % kChunks, sub = lane / kChunks;
-    const int per_tile = kBlockN >> p.page_shift, page_mask = (1 << p.page_shift) - 1;
-    const int outside = -1;
-    uint32_t it = 0, par = 1;
-    for (; units.valid(); units.next(p)) {
-        const Request r = units.cur.r;
+    const int page_mask = (1 << p.page_shift) - 1;
+    const uint32_t mine = c.smem + W::kRawAt + cw * (W::kRaw * W::kRawBytes);
+    const int64_t row_step = kRowsPer * p.stride_tok;
+    // the copy to issue next: tile j of the unit, K or V; the pages of this warp's keys in it (with 16-token pages two) and in the next tile
+    int issued = 0, j = units.t_begin, in = 0, key0 = 0, id0 = -1, id1 = -1, ahead0 = -1, ahead1 = -1;
+    bool is_v = false, more = units.valid;
+    auto look_up = [&](int t) {
         const int32_t* row = p.table + units.cur.b * p.table_stride;
-        const int low = r.low(p);
-        auto fetch = [&](int t) {
-            const int key0 = units.key_of(t), key = key0 + (lane << p.page_shift);
-            int id = outside;
-            if (lane < per_tile && key < r.len && (key + page_mask + 1 > low || key < p.sinks)) id = __ldg(row + (key >> p.page_shift));
-            return (uint32_t)id < (uint32_t)p.num_pages ? id : outside;
+        const int key = units.key_of(t) + cw * kKeys, len = units.cur.r.len, low = units.cur.r.low(p);
+        auto page_of = [&](int k) {
+            const int first = k & ~page_mask;
+            int id = -1;
+            if (k < len && (first + page_mask + 1 > low || first < p.sinks)) id = __ldg(row + (k >> p.page_shift));
+            return id;                                     // looked at when it is used: the load travels meanwhile
         };
-        int ahead = fetch(units.t_begin);
-#pragma unroll 1
-        for (int j = units.t_begin; j < units.t_end; ++j) {
-            const int ids = ahead, key0 = units.key_of(j);
-            if (j + 1 < units.t_end) ahead = fetch(j + 1);
-#pragma unroll 1
-            for (int kv = 0; kv < 2; ++kv) {
-                if (lane == 0) c.wait(kWRawEmpty + it, par, j);
-                __syncwarp();
-                const uint32_t dst = c.smem + W::kRawAt + it * W::kRawBytes, bar = c.bars + (kWRawFull + it) * 8;
-                const uint8_t* base = (kv ? p.v : p.k) + units.cur.u * p.stride_head + chunk * 16;
-#pragma unroll 4
-                for (int i = 0; i < kBlockN; i += kRowsPer) {
-                    const int k = i + sub, key = key0 + k;
-                    const int id = __shfl_sync(0xffffffffu, ids, k >> p.page_shift);
-                    const bool ok = id >= 0 && key < r.len && (key >= low || key < p.sinks);
-                    const uint8_t* src = ok ? base + id * p.stride_page + (key & page_mask) * p.stride_tok : p.k;
-                    cp_async16_or_zeros(dst + k * (kChunks * 16) + ((chunk ^ (kKind == kE4m3 ? k & 7 : k >> 1 & 3)) << 4), src, ok);
-                }
-                if (kKind == kMx4) {
-                    const uint8_t* exps = (kv ? p.v : p.k) + p.Hkv * 64 + units.cur.u * 4;
+        ahead0 = page_of(key);
+        ahead1 = page_mask < kKeys - 1 ? page_of(key + 16) : ahead0;
+    };
+    auto copy = [&]() {
+        if (more) {
+            if (!is_v) {
+                key0 = units.key_of(j) + cw * kKeys;
+                id0 = (uint32_t)ahead0 < (uint32_t)p.num_pages ? ahead0 : -1;
+                id1 = (uint32_t)ahead1 < (uint32_t)p.num_pages ? ahead1 : -1;
+                if (j + 1 < units.t_end) look_up(j + 1);
+            }
+            const int len = units.cur.r.len, low = units.cur.r.low(p);
+            const uint32_t dst = mine + in * W::kRawBytes;
+            const uint8_t* cache = is_v ? p.v : p.k;
+            const bool all = id0 >= 0 && id1 >= 0 && key0 + kKeys <= len && (key0 >= low || key0 + kKeys <= p.sinks);
+            const int64_t off0 = id0 * p.stride_page + ((key0 & page_mask) + sub) * p.stride_tok;
+            const int64_t off1 = page_mask < kKeys - 1 ? id1 * p.stride_page + sub * p.stride_tok - (16 / kRowsPer) * row_step : off0;      // of the copy that would be the first
+            const uint8_t* base = cache + units.cur.u * p.stride_head + chunk * 16;
 #pragma unroll
-                    for (int i = 0; i < kBlockN; i += 32) {
-                        const int k = i + lane, key = key0 + k;
-                        const int id = __shfl_sync(0xffffffffu, ids, k >> p.page_shift);
-                        const bool ok = id >= 0 && key < r.len && (key >= low || key < p.sinks);
-                        const uint8_t* src = ok ? exps + id * p.stride_page + (key & page_mask) * p.stride_tok : p.k;
-                        cp_async4_or_zeros(dst + W::kRawCodes + k * 4, src, ok);
-                    }
-                }
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-                if (++it == W::kRaw) {
-                    it = 0;
-                    par ^= 1;
+            for (int i = 0; i < kCopies; ++i) {
+                const int k = i * kRowsPer + sub, key = key0 + k;
+                const uint8_t* src = base + (i * kRowsPer < 16 ? off0 : off1) + i * row_step;
+                const uint32_t to = dst + k * (kChunks * 16) + ((chunk ^ (kKind == kE4m3 ? k & 7 : k >> 1 & 3)) << 4);
+                if (all) {
+                    cp_async16(to, src);
+                } else {
+                    const bool ok = (i * kRowsPer < 16 ? id0 : id1) >= 0 && key < len && (key >= low || key < p.sinks);
+                    cp_async16_or_zeros(to, ok ? src : p.k, ok);
                 }
             }
+            if (kKind == kMx4) {
+                const int k = lane & (kKeys - 1), key = key0 + k, id = k < 16 ? id0 : id1;
+                const bool ok = id >= 0 && key < len && (key >= low || key < p.sinks) && lane < kKeys;
+                const uint8_t* src = ok ? cache + p.Hkv * 64 + units.cur.u * 4 + id * p.stride_page + (key & page_mask) * p.stride_tok : p.k;
+                if (lane < kKeys) cp_async4_or_zeros(dst + W::kRawCodes + k * 4, src, ok);
+            }
+            if (++in == W::kRaw) in = 0;
+            ++issued;
+            if (is_v && ++j == units.t_end) {
+                units.next(p);
+                j = units.t_begin;
+                more = units.valid;
+                if (more) look_up(j);
+            }
+            is_v = !is_v;
         }
-    }
-    cp_commit();
-    cp_wait<0>();
-}
-
-// The widening warps: a quarter of every tile each.  16 E4M3 codes -> 16 fp16 values; a block of 32 4-bit codes -> 32 bf16 values, in whose groups of eight
-// elements i and i + 4 stand side by side (the queries are laid out alike, and the columns of O are taken in that order).
-template <Kind kKind>
-__device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c, WideUnits units, int cw) {
-    using W = Wide<kKind>;
-    const int lane = threadIdx.x & 31;
-    uint32_t raw = 0, raw_par = 0;
+        cp_commit();
+    };
+    if (more) look_up(j);
+    for (int i = 0; i < W::kRaw - 1; ++i) copy();
+    int out = 0;
+    bool v_now = false;
     WideRing<W::kStagesK> kr = {0, 1};
     WideRing<W::kStagesV> vr = {0, 1};
-    for (; units.valid(); units.next(w.d)) {
-        const int n = 2 * (units.t_end - units.t_begin);
 #pragma unroll 1
-        for (int ld = 0; ld < n; ++ld) {
-            c.wait(kWRawFull + raw, raw_par, ld);
-            const bool is_v = ld & 1;
-            c.wait(is_v ? kWVEmpty + vr.slot : kWKEmpty + kr.slot, is_v ? vr.par : kr.par, ld);
-            __syncwarp();
-            const uint32_t src = c.smem + W::kRawAt + raw * W::kRawBytes, dst = c.smem + W::kKV + (is_v ? W::kStagesK + vr.slot : kr.slot) * kTileBytes;
-            if (kKind == kE4m3) {
+    for (int ld = 0; ld < issued; ++ld) {
+        cp_wait<W::kRaw - 2>();
+        __syncwarp();                  // this slot has landed, and every lane has read the slot that is filled next
+        copy();
+        c.wait(v_now ? kWVEmpty + vr.slot : kWKEmpty + kr.slot, v_now ? vr.par : kr.par, ld);
+        __syncwarp();
+        const uint32_t src = mine + out * W::kRawBytes, tile = c.smem + W::kKV + (v_now ? W::kStagesK + vr.slot : kr.slot) * kTileBytes;
+        if (kKind == kE4m3) {
 #pragma unroll 4
-                for (int i = 0; i < 8; ++i) {
-                    const int item = (i * kConvWarps + cw) * 32 + lane, key = (item >> 6) * 8 + (item & 7), x = item >> 3 & 7;
-                    const uint4 q = lds128(src + key * 128 + ((x ^ (key & 7)) << 4));
-                    uint4 a, b;
-                    widen4(q.x, a.x, a.y);
-                    widen4(q.y, a.z, a.w);
-                    widen4(q.z, b.x, b.y);
-                    widen4(q.w, b.z, b.w);
-                    const uint32_t row = dst + (x >> 2) * kHalfBytes + key * 128;
-                    sts128(row + (((2 * x & 7) ^ (key & 7)) << 4), a);
-                    sts128(row + (((2 * x + 1 & 7) ^ (key & 7)) << 4), b);
-                }
-            } else {
+            for (int i = 0; i < kKeys / 4; ++i) {
+                const int item = i * 32 + lane, k = (item >> 6) * 8 + (item & 7), x = item >> 3 & 7, key = cw * kKeys + k;
+                const uint4 q = lds128(src + k * 128 + ((x ^ (k & 7)) << 4));
+                uint4 a, b;
+                widen4(q.x, a.x, a.y);
+                widen4(q.y, a.z, a.w);
+                widen4(q.z, b.x, b.y);
+                widen4(q.w, b.z, b.w);
+                const uint32_t row = tile + (x >> 2) * kHalfBytes + key * 128;
+                sts128(row + (((2 * x & 7) ^ (key & 7)) << 4), a);
+                sts128(row + (((2 * x + 1 & 7) ^ (key & 7)) << 4), b);
+            }
+        } else {
 #pragma unroll 2
-                for (int i = 0; i < 4; ++i) {
-                    const int item = (i * kConvWarps + cw) * 32 + lane, key = (item >> 5) * 8 + (item & 7), x = item >> 3 & 3;
-                    const uint4 q = lds128(src + key * 64 + ((x ^ (key >> 1 & 3)) << 4));
-                    const uint32_t e = lds32(src + W::kRawCodes + key * 4) >> (8 * x) & 255;
-                    const uint32_t codes[4] = {q.x, q.y, q.z, q.w};
-                    const uint32_t row = dst + (x >> 1) * kHalfBytes + key * 128;
-                    // one factor of 2^(e - 127 + 126) while it is a bf16 number, else 2^126 and 2^(e - 127)
-                    const bool near = __all_sync(0xffffffffu, e - 1 < 128u);
-                    const uint32_t f = near ? (e + 126) * 0x00800080u : 0x7e807e80u;
-                    const uint32_t f2 = e == 0 ? 0x00400040u : (e == 255 ? 0x7fc07fc0u : e * 0x00800080u);
+            for (int i = 0; i < kKeys / 8; ++i) {
+                const int item = i * 32 + lane, k = (item >> 5) * 8 + (item & 7), x = item >> 3 & 3, key = cw * kKeys + k;
+                const uint4 q = lds128(src + k * 64 + ((x ^ (k >> 1 & 3)) << 4));
+                const uint32_t e = lds32(src + W::kRawCodes + k * 4) >> (8 * x) & 255;
+                const uint32_t codes[4] = {q.x, q.y, q.z, q.w};
+                const uint32_t row = tile + (x >> 1) * kHalfBytes + key * 128;
+                // one factor of 2^(e - 127 + 126) while it is a bf16 number, else 2^126 and 2^(e - 127)
+                const bool near = __all_sync(0xffffffffu, e - 1 < 128u);
+                const uint32_t f = near ? (e + 126) * 0x00800080u : 0x7e807e80u;
+                const uint32_t f2 = e == 0 ? 0x00400040u : (e == 255 ? 0x7fc07fc0u : e * 0x00800080u);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        uint4 o = make_uint4(mul_bf16x2(small_bf16<0>(codes[k]), f), mul_bf16x2(small_bf16<1>(codes[k]), f),
-                                             mul_bf16x2(small_bf16<2>(codes[k]), f), mul_bf16x2(small_bf16<3>(codes[k]), f));
-                        if (!near) o = make_uint4(mul_bf16x2(o.x, f2), mul_bf16x2(o.y, f2), mul_bf16x2(o.z, f2), mul_bf16x2(o.w, f2));
-                        sts128(row + (((4 * x + k & 7) ^ (key & 7)) << 4), o);
-                    }
+                for (int n = 0; n < 4; ++n) {
+                    uint4 o = make_uint4(mul_bf16x2(small_bf16<0>(codes[n]), f), mul_bf16x2(small_bf16<1>(codes[n]), f),
+                                         mul_bf16x2(small_bf16<2>(codes[n]), f), mul_bf16x2(small_bf16<3>(codes[n]), f));
+                    if (!near) o = make_uint4(mul_bf16x2(o.x, f2), mul_bf16x2(o.y, f2), mul_bf16x2(o.z, f2), mul_bf16x2(o.w, f2));
+                    sts128(row + (((4 * x + n & 7) ^ (key & 7)) << 4), o);
                 }
             }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // the tensor cores read what these lanes wrote
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(c.bars + (is_v ? kWVFull + vr.slot : kWKFull + kr.slot) * 8);
-                mbar_arrive(c.bars + (kWRawEmpty + raw) * 8);
-            }
-            if (++raw == W::kRaw) {
-                raw = 0;
-                raw_par ^= 1;
-            }
-            if (is_v) vr.advance();
-            else kr.advance();
         }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");              // the tensor cores read what these lanes wrote
+        __syncwarp();
+        if (lane == 0) mbar_arrive(c.bars + (v_now ? kWVFull + vr.slot : kWKFull + kr.slot) * 8);
+        if (++out == W::kRaw) out = 0;
+        if (v_now) vr.advance();
+        else kr.advance();
+        v_now = !v_now;
     }
+    cp_wait<0>();
 }
 
 // ---------------------------------------------------------------------------------------------- queries
 // Row i of the unit's class is token (r0 + i) / G, head (r0 + i) % G of the group; rows without a token are zeros.  128-byte swizzle lines, 64 dims a half.
 // E4M3: fp16, scaled per row by a power of two that brings the largest element to [2^10, 2^11) (what falls below 2^-24 of it is lost); the sign of the keys'
 // scale joins here.  4-bit: elements i and i + 4 of every eight side by side.
-template <Kind kKind>
-__device__ __forceinline__ void wide_queries(const WideParams& w, const WideCtx& c, WideUnits units) {
-    using W = Wide<kKind>;
+template <Kind kKind, int kTiles>
+__device__ __forceinline__ void wide_queries(const WideParams& w, const WideCtx& c, WideUnits& units, int part) {
+    using W = Wide<kKind, kTiles>;
+    constexpr int kStep = 2 * W::kQueryWarps, kBatch = 8;                 // rows of a step, steps whose loads are in flight together
     const DecodeParams& p = w.d;
     const int lane = threadIdx.x & 31;
     const int r0 = (int)(blockIdx.x % w.classes) * w.class_rows, rows = min(w.class_rows, p.rows - r0);
-    const int chunk = lane & 15;
-    for (int round = 0; units.valid(); units.next(p), ++round) {
+    const int chunk = lane & 15, first = 2 * part + (lane >> 4);
+    auto place = [&](int i) {
+        const int in = i & (kBlockM - 1);
+        return c.smem + W::kQ + (i / kBlockM) * kTileBytes + (chunk >> 3) * kHalfBytes + in * 128 + (((chunk & 7) ^ (in & 7)) << 4);
+    };
+    for (int i = first; i < kTiles * kBlockM; i += kStep)                 // rows behind the class's last stay zeros
+        if (i >= rows) {
+            sts128(place(i), make_uint4(0, 0, 0, 0));
+            if (kKind == kE4m3 && chunk == 0) {
+                reinterpret_cast<int8_t*>(c.gen + W::kExp)[i] = 0;
+                reinterpret_cast<int8_t*>(c.gen + W::kExp)[kWideRows + i] = 0;
+            }
+        }
+    for (int round = 0; units.valid; units.next(p), ++round) {
         const int b = units.cur.b, m = units.cur.r.len - units.cur.r.base;
         const __nv_bfloat16* q = p.q + ((int64_t)b * p.n_q * p.Hq + (int64_t)units.cur.u * p.G) * kDim + chunk * 8;
         c.wait(kWQEmpty, (round & 1) ^ 1, round);
         __syncwarp();
         const float sign = kKind == kE4m3 ? p.k_scale[units.cur.u] : 1.f;
-#pragma unroll 4
-        for (int i = lane >> 4; i < w.tiles * kBlockM; i += 2) {
-            const int t = (r0 + i) / p.G, live = wide_token(p, t, m);
-            const bool ok = i < rows && live >= 0 && live < m;
-            const __nv_bfloat16* src = ok ? q + ((int64_t)t * p.Hq + (r0 + i - t * p.G)) * kDim : p.q;
-            const int in = i & (kBlockM - 1);
-            const uint32_t at = c.smem + W::kQ + (i / kBlockM) * kTileBytes + (chunk >> 3) * kHalfBytes + in * 128 + (((chunk & 7) ^ (in & 7)) << 4);
-            if (kKind == kBf16) {
-                cp_async16_or_zeros(at, src, ok);
-            } else {
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (ok) x = __ldg(reinterpret_cast<const uint4*>(src));
-                if (kKind == kMx4) {
-                    sts128(at, make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
-                                          __byte_perm(x.y, x.w, 0x7632)));
+        int t = (r0 + first) / p.G, h = r0 + first - t * p.G;             // token and head of the row
+        for (int i0 = 2 * part; i0 < rows; i0 += kStep * kBatch) {               // the same for all lanes
+            uint4 x[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int i = i0 + (lane >> 4) + k * kStep, live = wide_token(p, t, m);
+                const bool ok = i < rows && live >= 0 && live < m;
+                const __nv_bfloat16* src = ok ? q + ((int64_t)t * p.Hq + h) * kDim : p.q;
+                if (kKind == kBf16) {
+                    if (i < rows) cp_async16_or_zeros(place(i), src, ok);
                 } else {
-                    const uint32_t word[4] = {x.x, x.y, x.z, x.w};
-                    float f[8], amax = 0.f;
+                    x[k] = make_uint4(0, 0, 0, 0);
+                    if (ok) x[k] = __ldg(reinterpret_cast<const uint4*>(src));
+                }
+                for (h += kStep; h >= p.G; h -= p.G) ++t;
+            }
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        f[2 * k] = __uint_as_float(word[k] << 16);
-                        f[2 * k + 1] = __uint_as_float(word[k] & 0xffff0000u);
-                        amax = fmaxf(amax, fmaxf(fabsf(f[2 * k]), fabsf(f[2 * k + 1])));
-                    }
+            for (int k = 0; k < (kKind == kBf16 ? 0 : kBatch); ++k) {
+                const int i = i0 + (lane >> 4) + k * kStep;
+                if (kKind == kMx4) {
+                    if (i < rows)
+                        sts128(place(i), make_uint4(__byte_perm(x[k].x, x[k].z, 0x5410), __byte_perm(x[k].x, x[k].z, 0x7632),
+                                                    __byte_perm(x[k].y, x[k].w, 0x5410), __byte_perm(x[k].y, x[k].w, 0x7632)));
+                } else {
+                    // largest magnitude of the row, as bits: exponents are enough, and infinities and NaN stay the largest
+                    uint32_t top = __vmaxu2(__vmaxu2(x[k].x & 0x7fff7fffu, x[k].y & 0x7fff7fffu), __vmaxu2(x[k].z & 0x7fff7fffu, x[k].w & 0x7fff7fffu));
+                    top = max(top & 0xffffu, top >> 16);
 #pragma unroll
-                    for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-                    int e = 0;
-                    if (amax > 0.f && amax < INFINITY) e = min(max(10 - ilogbf(amax), -126), 126);
+                    for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    const int field = (int)(top >> 7);                    // of a zero or subnormal row 0
+                    const int e = top == 0 || field == 255 ? 0 : min(137 - max(field, 1), 126);
                     const float up = copysignf(__uint_as_float((uint32_t)(127 + e) << 23), sign);
-                    sts128(at, make_uint4(pack_weights<true>(f[0] * up, f[1] * up), pack_weights<true>(f[2] * up, f[3] * up),
-                                          pack_weights<true>(f[4] * up, f[5] * up), pack_weights<true>(f[6] * up, f[7] * up)));
-                    if (chunk == 0) reinterpret_cast<int8_t*>(c.gen + W::kExp)[(round & 1) * kWideRows + i] = (int8_t)e;
+                    const uint32_t word[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+                    uint32_t o[4];
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) o[n] = pack_weights<true>(__uint_as_float(word[n] << 16) * up, __uint_as_float(word[n] & 0xffff0000u) * up);
+                    if (i < rows) {
+                        sts128(place(i), make_uint4(o[0], o[1], o[2], o[3]));
+                        if (chunk == 0) reinterpret_cast<int8_t*>(c.gen + W::kExp)[(round & 1) * kWideRows + i] = (int8_t)e;
+                    }
                 }
             }
         }
@@ -399,20 +431,20 @@ __device__ __forceinline__ void wide_queries(const WideParams& w, const WideCtx&
 }
 
 // ---------------------------------------------------------------------------------------------- issuers
-template <Kind kKind>
-__device__ __forceinline__ void wide_scores(const WideParams& w, const WideCtx& c, WideUnits units) {
-    using W = Wide<kKind>;
+template <Kind kKind, int kTiles>
+__device__ __forceinline__ void wide_scores(const WideParams& w, const WideCtx& c, WideUnits& units) {
+    using W = Wide<kKind, kTiles>;
     constexpr uint32_t kIdesc = kKind == kE4m3 ? kIdescS & ~((1u << 7) | (1u << 10)) : kIdescS;      // fp16 or bf16 operands
     WideRing<W::kStagesK> pos = {0, 0};
     uint32_t s_par = 1;                // parity of "the previous score tile was read"; 1: there is none yet
     const uint64_t q_desc = make_desc(c.smem + W::kQ, 16, 1024), k_desc = make_desc(c.smem + W::kKV, 16, 1024);
-    for (int round = 0; units.valid(); units.next(w.d), ++round) {
+    for (int round = 0; units.valid; units.next(w.d), ++round) {
         const int j0 = units.t_begin, n = units.t_end;
         c.wait(kWQFull, round & 1, round);
 #pragma unroll 1
         for (int j = j0; j < n; ++j) {
             c.wait(kWKFull + pos.slot, pos.par, j);
-            for (int q = 0; q < w.tiles; ++q) {
+            for (int q = 0; q < kTiles; ++q) {
                 c.wait(kWSFree, s_par, j);
                 s_par ^= 1u;
                 tc_fence_after();
@@ -422,8 +454,8 @@ __device__ __forceinline__ void wide_scores(const WideParams& w, const WideCtx& 
                         const uint32_t off = ((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4;
                         mma_ss(c.tmem + kWTmemS, q_desc + q * (kTileBytes >> 4) + off, k_desc + pos.slot * (kTileBytes >> 4) + off, kIdesc, ks > 0);
                     }
-                    tc_commit(c.bars + (kWSReady + (w.tiles == 2 ? q : (j - j0) & 1)) * 8);
-                    if (q == w.tiles - 1) {
+                    tc_commit(c.bars + (kWSReady + (kTiles == 2 ? q : (j - j0) & 1)) * 8);
+                    if (q == kTiles - 1) {
                         tc_commit(c.bars + (kWKEmpty + pos.slot) * 8);
                         if (j == n - 1) tc_commit(c.bars + kWQEmpty * 8);
                     }
@@ -446,10 +478,28 @@ __device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
     const uint32_t top = odd_halves<kF16>(w);
     return w & ~(top | (top - (top >> 15)));
 }
+// x * 0 + acc of two values: NaN from the first infinity or NaN on
+template <bool kF16>
+__device__ __forceinline__ uint32_t times_zero(uint32_t x, uint32_t acc) {
+    if (kF16) asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(x), "r"(0u));
+    else asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(x), "r"(0u));
+    return acc;
+}
 template <bool kF16>
 __device__ __forceinline__ void wide_clear(const DecodeParams& p, const Request& r, uint32_t v_tile, int key0, unsigned long long* odd) {
     const int lane = threadIdx.x & 31, low = r.low(p), low_max = r.len - p.window;
-#pragma unroll 4
+    uint32_t a0 = 0, a1 = 0, a2 = 0, a3 = 0;
+#pragma unroll 8
+    for (int i = lane; i < 2 * (int)kHalfBytes / 16; i += 32) {
+        const uint4 x = lds128(v_tile + i * 16);
+        a0 = times_zero<kF16>(x.x, a0);
+        a1 = times_zero<kF16>(x.y, a1);
+        a2 = times_zero<kF16>(x.z, a2);
+        a3 = times_zero<kF16>(x.w, a3);
+    }
+    const uint32_t any = odd_halves<kF16>(a0) | odd_halves<kF16>(a1) | odd_halves<kF16>(a2) | odd_halves<kF16>(a3);
+    if (!__any_sync(0xffffffffu, any != 0)) return;        // the rule
+#pragma unroll 1
     for (int i = lane; i < 2 * (int)kHalfBytes / 16; i += 32) {
         const uint4 x = lds128(v_tile + i * 16);
         const uint32_t bad = odd_halves<kF16>(x.x) | odd_halves<kF16>(x.y) | odd_halves<kF16>(x.z) | odd_halves<kF16>(x.w);
@@ -465,16 +515,16 @@ __device__ __forceinline__ void wide_clear(const DecodeParams& p, const Request&
     __syncwarp();
 }
 
-template <Kind kKind>
-__device__ __forceinline__ void wide_outputs(const WideParams& w, const WideCtx& c, WideUnits units) {
-    using W = Wide<kKind>;
+template <Kind kKind, int kTiles>
+__device__ __forceinline__ void wide_outputs(const WideParams& w, const WideCtx& c, WideUnits& units) {
+    using W = Wide<kKind, kTiles>;
     constexpr uint32_t kIdesc = kKind == kE4m3 ? kIdescPV & ~((1u << 7) | (1u << 10)) : kIdescPV;
     const DecodeParams& p = w.d;
     const int lane = threadIdx.x & 31;
     WideRing<W::kStagesV> pos = {0, 0};
     uint32_t p_par0 = 0, p_par1 = 0;   // parity of "P is there", per warpgroup
     const uint64_t v_desc = make_desc(c.smem + W::kKV + W::kStagesK * kTileBytes, kHalfBytes, 1024);
-    for (int round = 0; units.valid(); units.next(p), ++round) {
+    for (int round = 0; units.valid; units.next(p), ++round) {
         const int j0 = units.t_begin, n = units.t_end;
         unsigned long long* odd = reinterpret_cast<unsigned long long*>(c.gen + W::kOdd) + 2 * (round & 1);
         if (lane < 2) odd[lane] = 0;   // its readers, of the unit before the last, are done: the last unit's P came behind them
@@ -484,9 +534,9 @@ __device__ __forceinline__ void wide_outputs(const WideParams& w, const WideCtx&
             c.wait(kWVFull + pos.slot, pos.par, j);
             const int key0 = units.key_of(j);
             if (!units.full(p, key0)) wide_clear<kKind == kE4m3>(p, units.cur.r, c.smem + W::kKV + (W::kStagesK + pos.slot) * kTileBytes, key0, odd);
-            for (int q = 0; q < w.tiles; ++q) {
-                const int h = w.tiles == 2 ? q : (j - j0) & 1;
-                const bool fresh = w.tiles == 2 ? j == j0 : j - j0 < 2;             // the accumulator's first tile of the unit
+            for (int q = 0; q < kTiles; ++q) {
+                const int h = kTiles == 2 ? q : (j - j0) & 1;
+                const bool fresh = kTiles == 2 ? j == j0 : j - j0 < 2;             // the accumulator's first tile of the unit
                 if (fresh && round > 0) c.wait(kWOFree + h, (round - 1) & 1, j);
                 const uint32_t p_par = h ? p_par1 : p_par0;
 #pragma unroll
@@ -501,7 +551,7 @@ __device__ __forceinline__ void wide_outputs(const WideParams& w, const WideCtx&
                                        kIdesc, !fresh || ks > 0);
                         if (part == 1) {
                             tc_commit(c.bars + (kWPvDone + h) * 8);
-                            if (q == w.tiles - 1) tc_commit(c.bars + (kWVEmpty + pos.slot) * 8);
+                            if (q == kTiles - 1) tc_commit(c.bars + (kWVEmpty + pos.slot) * 8);
                         }
                     }
                     __syncwarp();
@@ -529,11 +579,12 @@ __device__ __forceinline__ void wide_hide(float (&s)[32], uint32_t seen) {
         if (!(seen >> i & 1u)) s[i] = -INFINITY;
 }
 
-// What wide_clear took out of the V that a row sees joins the row just written.
+// What wide_clear took out of the V that a row sees joins the elements [d0, d1) of the row just written.
 template <Kind kKind>
-__device__ __forceinline__ void wide_odd_row(const DecodeParams& p, const unsigned long long* odd, int b, int base, int len, int u, int t, bool whole, int64_t at) {
+__device__ __forceinline__ void wide_odd_row(const DecodeParams& p, const unsigned long long* odd, int b, int base, int len, int u, int t, bool whole, int64_t at,
+                                             int d0, int d1) {
 #pragma unroll 1
-    for (int dim = 0; dim < kD; ++dim) {
+    for (int dim = d0; dim < d1; ++dim) {
         const float x = odd_values<kKind, true>(p, odd, b, base, len, u, t, dim);
         if (x == 0.f) continue;
         if (whole) p.out[at + dim] = __float2bfloat16_rn(__bfloat162float(p.out[at + dim]) + x);
@@ -647,35 +698,23 @@ __device__ __forceinline__ void wide_softmax_tile(const WideCtx& cx, float (&c0)
 template <Kind kKind>
 __device__ __forceinline__ constexpr int wide_column(int i) { return kKind == kMx4 ? (i & ~7) | (i & 3) << 1 | (i >> 2 & 1) : i; }
 
-template <Kind kKind>
-__device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx& cx, WideUnits units, int wg, int64_t total, int ctas) {
-    using W = Wide<kKind>;
+template <Kind kKind, int kTiles>
+__device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx& cx, WideUnits& units, int wg, int64_t total, int ctas) {
+    using W = Wide<kKind, kTiles>;
     constexpr bool kF16 = kKind == kE4m3;
     const DecodeParams& p = w.d;
     const int lane = threadIdx.x & 31, warp_in_wg = threadIdx.x >> 5 & 3;
     const uint32_t lane_addr = (uint32_t)(warp_in_wg * 32) << 16;
     const uint32_t s_tmem = cx.tmem + lane_addr + kWTmemS, p_tmem = cx.tmem + lane_addr + kWTmemP + wg * 64, o_tmem = cx.tmem + lane_addr + kWTmemO + wg * 128;
     const int cls = (int)(blockIdx.x % w.classes), run = (int)(blockIdx.x / w.classes);
-    const bool turns = w.tiles == 1;                                      // the warpgroups take the K/V tiles in turn
+    constexpr bool turns = W::kTurns;
     const int tile_row = warp_in_wg * 32 + lane, row = (turns ? 0 : wg * kBlockM) + tile_row;      // of the class
     const int r = cls * w.class_rows + row, t = r / p.G;                  // of the KV head; its token
     const bool in_class = row < w.class_rows && r < p.rows;
-    const int step = turns ? 2 : 1;
-    float* travel = reinterpret_cast<float*>(cx.gen + W::kQ + kTileBytes);      // 64 columns of an accumulator: [column][row]
+    constexpr int step = turns ? 2 : 1;
     float c = p.scale_log2;
-    uint32_t s_par = 0, tile_cnt = 0, travels = 0;
-    // the second warpgroup's accumulator goes to the first in parts, through one buffer
-    auto before_part = [&]() {
-        if (wg == 1) cx.wait(kWTravelFree, (travels & 1) ^ 1, (int)travels);
-        else cx.wait(kWTravelFull, travels & 1, (int)travels);
-        __syncwarp();
-    };
-    auto after_part = [&]() {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(cx.bars + (wg == 1 ? kWTravelFull : kWTravelFree) * 8);
-        ++travels;
-    };
-    for (int round = 0; units.valid(); ++round) {
+    uint32_t s_par = 0, tile_cnt = 0;
+    for (int round = 0; units.valid; ++round) {
         const Request rq = units.cur.r;
         const int b = units.cur.b, u = units.cur.u, j0 = units.t_begin, n = units.t_end, m_tree = rq.len - rq.base;
         const int tt = wide_token(p, t, m_tree);
@@ -688,7 +727,24 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
         const int j1 = j0 + (turns ? wg : 0);                             // this warpgroup's first tile
         const bool some = j1 < n;
         float m = kNoKey, l = 0.f;
-        if (some) {
+        if (some && !__any_sync(0xffffffffu, live)) {                     // none of this warp's rows: whatever P and O hold there, nobody takes it
+#pragma unroll 1
+            for (int j = j1; j < n; j += step) {
+                cx.wait(kWSReady + wg, s_par, j);
+                s_par ^= 1u;
+                if (j > j1) cx.wait(kWPvDone + wg, (tile_cnt - 1) & 1, j);
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(cx.bars + kWSFree * 8);
+                    mbar_arrive(cx.bars + (kWPReady + 2 * wg) * 8);
+                    mbar_arrive(cx.bars + (kWPReady + 2 * wg + 1) * 8);
+                }
+                ++tile_cnt;
+            }
+            cx.wait(kWPvDone + wg, (tile_cnt - 1) & 1, n);
+            __syncwarp();
+            tc_fence_after();
+        } else if (some) {
             float s0[32], s1[32], s2[32], s3[32];
             cx.wait(kWSReady + wg, s_par, j1);
             __syncwarp();
@@ -723,24 +779,27 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
         }
         const bool whole = units.whole;
         const int64_t x_end = units.cur.x + kWideCost + rq.n;
-        units.next(p);
-        float f0 = 1.f, f1 = 0.f;                                         // factors of this accumulator and of the one that travels
+        float f0 = 1.f, f1 = 0.f;                                         // factors of the accumulators
+        const bool both = turns && n - j0 > 1;
+        if (turns) {
+            // the warpgroups tell one another their maxima and sums; then each reads half of the columns of both accumulators, which lie in the same lanes
+            float2* ml = reinterpret_cast<float2*>(cx.gen + W::kMl) + (round & 1) * 2 * kBlockM;
+            ml[wg * kBlockM + tile_row] = make_float2(m, l);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(cx.bars + (kWMl + wg) * 8);
+            cx.wait(kWMl + (wg ^ 1), round & 1, n);
+            __syncwarp();
+            tc_fence_after();
+            const float2 o = ml[(wg ^ 1) * kBlockM + tile_row];
+            const float mx = fmaxf(m, o.x), own = ex2(m - mx), other = ex2(o.x - mx);
+            l = l * own + o.y * other;
+            m = mx;
+            f0 = wg == 0 ? own : other;
+            f1 = wg == 0 ? other : own;
+        }
         cx.wait(kWOdd, round & 1, n);
         __syncwarp();
-        if (turns) {                   // maxima and sums first
-            before_part();
-            if (wg == 1) {
-                reinterpret_cast<float2*>(travel)[tile_row] = make_float2(m, l);
-            } else {
-                const float2 o = reinterpret_cast<const float2*>(travel)[tile_row];
-                const float mx = fmaxf(m, o.x);
-                f0 = ex2(m - mx);
-                f1 = ex2(o.x - mx);
-                l = l * f0 + o.y * f1;
-                m = mx;
-            }
-            after_part();
-        }
         const unsigned long long* odd = reinterpret_cast<const unsigned long long*>(cx.gen + W::kOdd) + 2 * (round & 1);
         const bool any_odd = live && (odd[0] | odd[1]) != 0;
         const float inv = !whole ? 1.f : (l == 0.f ? 0.f : (kF16 ? p.v_scale[u] : 1.f) / l);
@@ -749,34 +808,25 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
         const int64_t slot = 2 * ((int64_t)cls * w.runs + run) + (j0 > 0 ? 0 : 1);
         const int head = u * p.G + r - t * p.G;
         // offset of this row in the destination, -1: none
-        const int64_t at = !in_class || (turns && wg == 1) ? -1 : (whole ? (((int64_t)b * p.n_q + t) * p.Hq + head) * kD : (slot * kWideRows + row) * kD);
+        const int64_t at = !in_class ? -1 : (whole ? (((int64_t)b * p.n_q + t) * p.Hq + head) * kD : (slot * kWideRows + row) * kD);
         const int qt = lane & 3;
+        const uint32_t acc0 = turns ? cx.tmem + lane_addr + kWTmemO : o_tmem, acc1 = cx.tmem + lane_addr + kWTmemO + 128;
         int64_t to[4];                 // of the rows of this lane's quad: the lanes swap 16-byte pieces, so that a store writes 64 contiguous bytes of a row
 #pragma unroll
         for (int i = 0; i < 4; ++i) to[i] = __shfl_sync(0xffffffffu, at, (lane & ~3) + i);
+        const int cc0 = turns ? 2 * wg : 0, cc1 = turns ? cc0 + 2 : 4;
 #pragma unroll 1
-        for (int cc = 0; cc < 4; ++cc) {
+        for (int cc = cc0; cc < cc1; ++cc) {
             float o[32];
-            if (some) {
-                TMEM_LD32(o_tmem + cc * 32, o, 0);
+            TMEM_LD32(acc0 + cc * 32, o, 0);
+            if (both) {
+                float o1[32];
+                TMEM_LD32(acc1 + cc * 32, o1, 0);
                 tc_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = live ? o[i] * f0 + o1[i] * f1 : 0.f;
             } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = 0.f;
-            }
-            if (turns) {
-                float* col = travel + (cc & 1) * 32 * kBlockM + tile_row;
-                if ((cc & 1) == 0) before_part();                         // 64 columns at a time
-                if (wg == 1) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) col[i * kBlockM] = o[i];
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = live ? o[i] * f0 + col[i * kBlockM] * f1 : 0.f;
-                }
-                if ((cc & 1) == 1) after_part();
-                if (wg == 1) continue;
-            } else {
+                tc_wait_ld();
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = live ? o[i] * f0 : 0.f;
             }
@@ -811,9 +861,16 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
         }
         tc_fence_before();
         __syncwarp();                  // also: the rows are written, by the lanes of their quads
-        if (any_odd && at >= 0) wide_odd_row<kKind>(p, odd, b, rq.base, rq.len, u, tt, whole, at);
-        if (lane == 0) mbar_arrive(cx.bars + (kWOFree + wg) * 8);
-        if (at >= 0) {
+        if (lane == 0) {
+            if (turns) {
+                mbar_arrive(cx.bars + kWOFree * 8);
+                mbar_arrive(cx.bars + (kWOFree + 1) * 8);
+            } else {
+                mbar_arrive(cx.bars + (kWOFree + wg) * 8);
+            }
+        }
+        if (any_odd) wide_odd_row<kKind>(p, odd, b, rq.base, rq.len, u, tt, whole, at, cc0 * 32, cc1 * 32);
+        if (in_class && (!turns || wg == 0)) {
             if (whole) {
                 p.lse[(int64_t)head * ((int64_t)p.B * p.n_q) + (int64_t)b * p.n_q + t] =
                     live && l != 0.f ? (m + log2f(l) - (kF16 ? kF16Shift : 0.f)) * 0.6931471805599453f : -INFINITY;
@@ -833,27 +890,28 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
             meta[2] = (int32_t)(last - run + 1);
             meta[3] = 1;
         }
+        units.next(p);
     }
 }
 #undef CP_LOAD_S3
 
-template <Kind kKind>
-__global__ void __launch_bounds__(Wide<kKind>::kThreads, 1)
+template <Kind kKind, int kTiles>
+__global__ void __launch_bounds__(Wide<kKind, kTiles>::kThreads, 1)
 tree_wide_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ WideParams w) {
-    using W = Wide<kKind>;
+    using W = Wide<kKind, kTiles>;
     constexpr int kThreadsHere = W::kThreads;
-    extern __shared__ uint8_t smem_raw[];
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
     const DecodeParams& p = w.d;
     WideCtx c;
-    c.smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    c.gen = smem_raw + (c.smem - smem_u32(smem_raw));
+    c.smem = smem_u32(smem_raw);
+    c.gen = smem_raw;
     c.bars = c.smem + W::kBar;
     c.abort_flag = reinterpret_cast<volatile uint32_t*>(c.gen + W::kAbort);
     c.status = p.status;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int run = (int)(blockIdx.x / w.classes);
     if (tid == 0) {
-        mbar_init(c.bars + kWQFull * 8, 1);
+        mbar_init(c.bars + kWQFull * 8, W::kQueryWarps);
         mbar_init(c.bars + kWQEmpty * 8, 1);
         for (int s = 0; s < kMaxRing; ++s) {
             mbar_init(c.bars + (kWKFull + s) * 8, W::kRawTiles ? kConvWarps : 1);
@@ -861,20 +919,15 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
             mbar_init(c.bars + (kWVFull + s) * 8, W::kRawTiles ? kConvWarps : 1);
             mbar_init(c.bars + (kWVEmpty + s) * 8, 1);
         }
-        for (int s = 0; s < W::kRaw; ++s) {
-            mbar_init(c.bars + (kWRawFull + s) * 8, 32);               // one arrival per lane of the warp that copies
-            mbar_init(c.bars + (kWRawEmpty + s) * 8, kConvWarps);
-        }
         mbar_init(c.bars + kWSFree * 8, 4);
         for (int h = 0; h < 2; ++h) {
             mbar_init(c.bars + (kWSReady + h) * 8, 1);
             for (int q = 0; q < 2; ++q) mbar_init(c.bars + (kWPReady + 2 * h + q) * 8, 4);      // one arrival per warp
             mbar_init(c.bars + (kWPvDone + h) * 8, 1);
-            mbar_init(c.bars + (kWOFree + h) * 8, 4);
+            mbar_init(c.bars + (kWOFree + h) * 8, W::kTurns ? 8 : 4);
+            mbar_init(c.bars + (kWMl + h) * 8, 4);
         }
         mbar_init(c.bars + kWOdd * 8, 1);
-        mbar_init(c.bars + kWTravelFull * 8, 4);
-        mbar_init(c.bars + kWTravelFree * 8, 4);
         *c.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -934,24 +987,29 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     }
     __syncthreads();
     if (x0 < x1) {
-        WideUnits units;
-        units.begin(p, start, x0, x1);
+        WideUnits& units = *reinterpret_cast<WideUnits*>(c.gen + W::kUnits + warp * kUnitBytes);
+        if (lane == 0) units.begin(p, start, x0, x1);
+        __syncwarp();
         if (warp < 8) {
             asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(W::kRegsSoftmax));
-            wide_softmax<kKind>(w, c, units, warp >> 2, total, ctas);
+            wide_softmax<kKind, kTiles>(w, c, units, warp >> 2, total, ctas);
         } else {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(W::kRegsOther));
-            if constexpr (W::kRawTiles) {
-                if (warp == 8) wide_raw<kKind>(w, c, units);
-                else if (warp >= 12) wide_widen<kKind>(w, c, units, warp - 12);
+            if (warp == 9) {
+                wide_scores<kKind, kTiles>(w, c, units);
+            } else if (warp == 10) {
+                wide_outputs<kKind, kTiles>(w, c, units);
+            } else if (warp == 11) {
+                wide_queries<kKind, kTiles>(w, c, units, 0);
+            } else if constexpr (W::kRawTiles) {
+                if (warp == 8) wide_queries<kKind, kTiles>(w, c, units, 1);
+                else wide_widen<kKind, kTiles>(w, c, units, warp - 12);
             } else {
-                if (warp == 8) wide_producer(w, c, units, &tmK, &tmV);
+                wide_producer<kTiles>(w, c, units, &tmK, &tmV);
             }
-            if (warp == 9) wide_scores<kKind>(w, c, units);
-            else if (warp == 10) wide_outputs<kKind>(w, c, units);
-            else if (warp == 11) wide_queries<kKind>(w, c, units);
         }
     }
+    let_next_launch_begin();           // not earlier: nothing is to be set up beside a block whose warps pass registers on
     tc_fence_before();
     __syncthreads();
     if (*c.abort_flag) {
@@ -970,6 +1028,7 @@ template <Kind kKind>
 __global__ void __launch_bounds__(32 * kWideJoinRows)
 tree_join_kernel(const __grid_constant__ WideParams w) {
     const DecodeParams& p = w.d;
+    wait_for_launch_before();
     const int v = blockIdx.x, row = blockIdx.y * kWideJoinRows + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int4 me = *reinterpret_cast<const int4*>(p.meta + 4 * v);
     const int r = v / w.runs * w.class_rows + row;

@@ -3,31 +3,42 @@
 
 namespace {
 
-int encode_kv(cp_ctx* ctx, const CacheView& v, bool second, CUtensorMap* map, const char* who) {
-    cuuint64_t dims[4] = {(cuuint64_t)kD, (cuuint64_t)v.Hkv, (cuuint64_t)v.page_size, (cuuint64_t)v.num_pages};
-    cuuint64_t strides[3] = {(cuuint64_t)v.stride_head, (cuuint64_t)v.stride_tok, (cuuint64_t)v.stride_page};
-    cuuint32_t box[4] = {64, 1, (cuuint32_t)v.page_size, 1}, es[4] = {1, 1, 1, 1};
-    const CUresult r = ctx->encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(second ? v.v : v.k), dims, strides, box, es,
-                                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) return set_error(CP_ERR_CUDA, "%s: cuTensorMapEncodeTiled(%s) failed with %d", who, second ? "v" : "k", (int)r);
-    return CP_OK;
+int encode(cp_ctx* ctx, CUtensorMap* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+           const cuuint32_t* box, CUtensorMapSwizzle swizzle, const char* who) {
+    const cuuint32_t es[4] = {1, 1, 1, 1};
+    const CUresult r = ctx->encode_tiled(map, type, rank, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? CP_OK : set_error(CP_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed with %d", who, (int)r);
+}
+
+// One box is a page of one head: 64 bf16 dims, or the whole row of codes; 4-bit: a second box for 16 bytes of exponents a token.
+template <Kind kKind>
+int encode_cache(cp_ctx* ctx, const CacheView& v, bool second, CUtensorMap* map, CUtensorMap* exps, const char* who) {
+    const uint8_t* base = static_cast<const uint8_t*>(second ? v.v : v.k);
+    const cuuint64_t dims[4] = {kKind == kMx4 ? 64u : 128u, (cuuint64_t)v.Hkv, (cuuint64_t)v.page_size, (cuuint64_t)v.num_pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)v.stride_head, (cuuint64_t)v.stride_tok, (cuuint64_t)v.stride_page};
+    const cuuint32_t box[4] = {kKind == kE4m3 ? 128u : 64u, 1, (cuuint32_t)v.page_size, 1};
+    if (int rc = encode(ctx, map, kKind == kBf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, base, dims, strides, box,
+                        kKind == kMx4 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, who)) return rc;
+    if (kKind != kMx4) return CP_OK;
+    const cuuint64_t edims[3] = {(cuuint64_t)v.Hkv * 4, (cuuint64_t)v.page_size, (cuuint64_t)v.num_pages};
+    const cuuint64_t estrides[2] = {(cuuint64_t)v.stride_tok, (cuuint64_t)v.stride_page};
+    const cuuint32_t ebox[3] = {16, (cuuint32_t)v.page_size, 1};
+    return encode(ctx, exps, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, base + (int64_t)v.Hkv * 64, edims, estrides, ebox, CU_TENSOR_MAP_SWIZZLE_NONE, who);
 }
 
 template <Kind kKind, int kTiles>
 int launch(cp_ctx* ctx, const WideParams& w, const CacheView& view, cudaStream_t s, const char* who) {
     using W = Wide<kKind, kTiles>;
-    CUtensorMap k = {}, v = {};
-    if (kKind == kBf16) {
-        if (int rc = encode_kv(ctx, view, false, &k, who)) return rc;
-        if (int rc = encode_kv(ctx, view, true, &v, who)) return rc;
-    }
+    CUtensorMap k, v, ke = {}, ve = {};
+    if (int rc = encode_cache<kKind>(ctx, view, false, &k, &ke, who)) return rc;
+    if (int rc = encode_cache<kKind>(ctx, view, true, &v, &ve, who)) return rc;
     if (!ctx->tree_attr_set[kKind][kTiles - 1]) {
         if (int rc = check_cuda(cudaFuncSetAttribute(tree_wide_kernel<kKind, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize, W::kSmem),
                                 "cudaFuncSetAttribute(tree)")) return rc;
         ctx->tree_attr_set[kKind][kTiles - 1] = true;
     }
-    tree_wide_kernel<kKind, kTiles><<<(unsigned)(w.runs * w.classes), W::kThreads, W::kSmem, s>>>(k, v, w);
+    tree_wide_kernel<kKind, kTiles><<<(unsigned)(w.runs * w.classes), W::kThreads, W::kSmem, s>>>(k, v, ke, ve, w);
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
     const unsigned y = (unsigned)((w.class_rows + kWideJoinRows - 1) / kWideJoinRows);
     return launch_behind(tree_join_kernel<kKind>, dim3((unsigned)(w.runs * w.classes), y), 32 * kWideJoinRows, s, who, w);

@@ -14,8 +14,9 @@
 //   - Warps: two softmax warpgroups; a producer that fetches K/V tiles page by page; the issuers of S = Q K^T and of O += P V; a warp that gathers the
 //     unit's query rows.  S, P and O live in TMEM: S | P0 | P1 | O0 | O1.  S is one buffer that the tiles use in turn, read into registers at
 //     once, so the next product runs under the exponentials.
-//   - bf16 tiles come by TMA.  The rows of the other caches are copied by a fourth warpgroup with cp.async, which widens them into the tiles: E4M3 to
-//     fp16 (queries and weights are then fp16 as in the narrow form), 4-bit codes and exponents to bf16, both exactly.
+//   - K and V come by TMA, page by page.  E4M3 and 4-bit rows land in a ring of raw tiles, and a fourth warpgroup widens them into the tiles of the products:
+//     E4M3 to fp16 (queries and weights are then fp16 as in the narrow form), 4-bit codes and exponents to bf16, both exactly.  (Copied by the widening warps
+//     with cp.async, an E4M3 tile takes 3 us: with 64 registers a thread the copies wait for one another's addresses.)
 //   - Only the last tiles of a unit and those at a window's edge hide keys from rows.  Their masks are bits: of the tree's mask and of the window.  A hidden
 //     key's weight is zero, but zero times an infinity is not: the issuer of P V looks through the V of these tiles and clears what is no
 //     finite number; what some rows do see of it is added to their results when they are written.
@@ -32,7 +33,7 @@ constexpr int kWideCost = 3;                               // fixed cost of a un
 constexpr float kWideLag = 8.0f;                           // the running maximum may lag by a factor 2^8
 constexpr int kWideSplit = 3;                              // P is handed over in two pieces: three quarters of the keys, then the rest
 constexpr int kConvWarps = 4;
-constexpr int kMaxRing = 3;
+constexpr int kMaxRing = 3, kMaxRaw = 6;
 constexpr int kUnitBytes = 80;
 
 // kTiles: score tiles of a unit; with one, the warpgroups take the K/V tiles in turn.
@@ -46,14 +47,13 @@ struct Wide {
     // Rings of 32 KB tiles, one for K and one for V: a full barrier has one waiter, who has waited for each of its phases.  (With K and V in turn in one ring the
     // issuer of S can be at a slot whose V has not landed yet, when the tiles are taken in turn; its wait would take the phase before that for its own.)
     static constexpr int kStagesK = kRawTiles ? 2 : 3, kStagesV = 2, kStages = kStagesK + kStagesV;
-    static constexpr int kWarpKeys = kBlockN / kConvWarps;
-    static constexpr uint32_t kRawCodes = kWarpKeys * (kKind == kE4m3 ? 128u : 64u);
-    static constexpr uint32_t kRawBytes = kRawCodes + (kKind == kMx4 ? kWarpKeys * 4u : 0u);       // 4-bit: codes, then exponents
-    static constexpr int kRaw = kKind == kBf16 ? 0 : (kKind == kE4m3 ? (kTurns ? 3 : 2) : (kTurns ? 6 : 3));      // slots of a warp's ring
-    static constexpr int kQueryWarps = kRawTiles ? 2 : 1;
+    static constexpr uint32_t kRawCodes = kKind == kE4m3 ? 16384u : 8192u;                         // of the 128 keys of a tile
+    static constexpr uint32_t kRawBytes = kRawCodes + (kKind == kMx4 ? 2048u : 0u);                // 4-bit: then 16 bytes a key with the exponents of four heads
+    static constexpr int kRaw = kKind == kBf16 ? 0 : (kKind == kE4m3 ? (kTurns ? 3 : 2) : (kTurns ? 6 : 3));      // slots of the ring of raw tiles
+    static constexpr int kQueryWarps = 1;
     // shared memory: the query tiles, the ring, the raw tiles, what the warpgroups tell one another, barriers and small areas
     static constexpr uint32_t kQ = 0, kKV = kTiles * kTileBytes, kRawAt = kKV + kStages * kTileBytes;
-    static constexpr uint32_t kMl = kRawAt + kRaw * kConvWarps * kRawBytes;                        // [unit parity][warpgroup][row]: maximum and sum
+    static constexpr uint32_t kMl = kRawAt + kRaw * kRawBytes;                        // [unit parity][warpgroup][row]: maximum and sum
     static constexpr uint32_t kBar = kMl + (kTurns ? 2 * 2 * kBlockM * 8 : 0);
     static constexpr uint32_t kOdd = kBar + 48 * 8;        // [unit parity][2] keys whose V is no finite number (see odd_values)
     static constexpr uint32_t kScan = kOdd + 32;           // sums of the warps, then the run's start
@@ -76,7 +76,9 @@ enum WideBar : uint32_t {
     kWOFree = kWPvDone + 2,                  // + warpgroup: O has been read
     kWOdd = kWOFree + 2,                     // the unit's list of odd keys is complete
     kWMl = kWOdd + 1,                        // + warpgroup: its accumulator, maxima and sums of the unit are complete (tiles in turn)
-    kNumWideBars = kWMl + 2
+    kWRawFull = kWMl + 2,                    // + raw slot
+    kWRawEmpty = kWRawFull + kMaxRaw,        // + raw slot
+    kNumWideBars = kWRawEmpty + kMaxRaw
 };
 static_assert(kNumWideBars <= 48, "barrier area");
 
@@ -159,192 +161,167 @@ struct WideRing {
 };
 
 // ---------------------------------------------------------------------------------------------- producer
-// Load order = order of first use: K(j0), then K(j + 1) before V(j).  Lane i < pages of a tile holds a page id; those of the next K tile are
-// fetched while the current ones are used.  Pages that no row sees anything of are read as zeros.
-template <int kTiles>
-__device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx& c, WideUnits& units, const CUtensorMap* tmK, const CUtensorMap* tmV) {
-    using W = Wide<kBf16, kTiles>;
+struct WideMaps {
+    const CUtensorMap *k, *v, *k_exp, *v_exp;              // the last two: exponents of 4-bit rows
+};
+// Lane i < pages of a tile holds a page id; those of the next K tile are fetched while the current ones are used.  Pages that no row sees anything of are read as
+// zeros.  bf16: loads in order of first use, K(j0), then K(j + 1) before V(j), into the rings; the others K(j), V(j) into the raw ring.
+template <Kind kKind, int kTiles>
+__device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx& c, WideUnits& units, const WideMaps& maps) {
+    using W = Wide<kKind, kTiles>;
     const DecodeParams& p = w.d;
     const int lane = threadIdx.x & 31;
     const int page_tokens = 1 << p.page_shift, per_tile = kBlockN >> p.page_shift;
-    const uint32_t box_bytes = (uint32_t)page_tokens * 128u;
     const int outside = (int)p.num_pages;                  // a page coordinate behind the tensor: TMA fills zeros
     WideRing<W::kStagesK> kr = {0, 1};
     WideRing<W::kStagesV> vr = {0, 1};
+    WideRing<W::kRawTiles ? W::kRaw : 1> raw = {0, 1};
     for (; units.valid; units.next(p)) {
-        const Request r = units.cur.r;
+        const int len = units.cur.r.len, low = units.cur.r.low(p), head = units.cur.u;
         const int32_t* row = p.table + units.cur.b * p.table_stride;
         auto fetch = [&](int t) {
             const int key0 = units.key_of(t), key = key0 + lane * page_tokens;
             int id = outside;
-            if (lane < per_tile && key < r.len && (key + page_tokens > r.low(p) || key < p.sinks)) id = __ldg(row + (key >> p.page_shift));
+            if (lane < per_tile && key < len && (key + page_tokens > low || key < p.sinks)) id = __ldg(row + (key >> p.page_shift));
             return id;                                     // looked at when it is used: the load travels meanwhile
         };
         int ahead = fetch(units.t_begin), k_ids = 0, v_ids = 0;
         const int n_loads = 2 * (units.t_end - units.t_begin);
         int j = units.t_begin;                             // next K tile
         for (int ld = 0; ld < n_loads; ++ld) {
-            const bool is_v = ld == n_loads - 1 || (ld > 0 && (ld & 1) == 0);      // K(j0), then K(j + 1) before V(j)
+            const bool is_v = W::kRawTiles ? ld & 1 : ld == n_loads - 1 || (ld > 0 && (ld & 1) == 0);
             int ids;
             if (!is_v) {
                 v_ids = k_ids;
                 k_ids = ids = (uint32_t)ahead < (uint32_t)outside ? ahead : outside;
                 if (++j < units.t_end) ahead = fetch(j);
             } else {
-                ids = ld == n_loads - 1 ? k_ids : v_ids;
+                ids = W::kRawTiles || ld == n_loads - 1 ? k_ids : v_ids;
             }
-            const uint32_t slot = is_v ? W::kStagesK + vr.slot : kr.slot;
-            const uint32_t fbar = c.bars + (is_v ? kWVFull + vr.slot : kWKFull + kr.slot) * 8, dst = c.smem + W::kKV + slot * kTileBytes;
-            if (lane == 0) {
-                c.wait(is_v ? kWVEmpty + vr.slot : kWKEmpty + kr.slot, is_v ? vr.par : kr.par, ld);
-                mbar_expect_tx(fbar, kTileBytes);
-            }
-            __syncwarp();
-            if (lane < per_tile) {
+            if constexpr (W::kRawTiles) {
+                const uint32_t fbar = c.bars + (kWRawFull + raw.slot) * 8, dst = c.smem + W::kRawAt + raw.slot * W::kRawBytes;
+                if (lane == 0) {
+                    c.wait(kWRawEmpty + raw.slot, raw.par, ld);
+                    mbar_expect_tx(fbar, W::kRawBytes);
+                }
+                __syncwarp();
+                if (lane < per_tile) {
+                    const uint32_t row_bytes = kKind == kE4m3 ? 128u : 64u;
+                    tma_load_4d(dst + lane * page_tokens * row_bytes, is_v ? maps.v : maps.k, fbar, 0, head, 0, ids);
+                    if (kKind == kMx4)
+                        tma_load_3d(dst + W::kRawCodes + lane * page_tokens * 16, is_v ? maps.v_exp : maps.k_exp, fbar, head * 4 & ~15, 0, ids);
+                }
+                raw.advance();
+            } else {
+                const uint32_t slot = is_v ? W::kStagesK + vr.slot : kr.slot;
+                const uint32_t fbar = c.bars + (is_v ? kWVFull + vr.slot : kWKFull + kr.slot) * 8, dst = c.smem + W::kKV + slot * kTileBytes;
+                if (lane == 0) {
+                    c.wait(is_v ? kWVEmpty + vr.slot : kWKEmpty + kr.slot, is_v ? vr.par : kr.par, ld);
+                    mbar_expect_tx(fbar, kTileBytes);
+                }
+                __syncwarp();
+                if (lane < per_tile) {
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
-                    tma_load_4d(dst + half * kHalfBytes + lane * box_bytes, is_v ? tmV : tmK, fbar, half * 64, units.cur.u, 0, ids);
+                    for (int half = 0; half < 2; ++half)
+                        tma_load_4d(dst + half * kHalfBytes + lane * page_tokens * 128, is_v ? maps.v : maps.k, fbar, half * 64, head, 0, ids);
+                }
+                if (is_v) vr.advance();
+                else kr.advance();
             }
             __syncwarp();
-            if (is_v) vr.advance();
-            else kr.advance();
         }
     }
 }
 
-// ---------------------------------------------------------------------------------------------- raw tiles
-// E4M3 and 4-bit rows: a warp owns 32 keys of every tile.  It copies them (K, then V, tile by tile) into a ring of its own with cp.async, slots that no row sees as
-// zeros, and widens what has landed into the tiles that the tensor cores read: 16 E4M3 codes -> 16 fp16 values; a block of 32 4-bit codes -> 32 bf16
-// values, in whose groups of eight elements i and i + 4 stand side by side (the queries are laid out alike, and the columns of O are taken in that order).
-// 16-byte chunk x of key k sits at chunk x ^ (k & 7) of its row (4-bit rows of four chunks: x ^ (k / 2 & 3)), so that eight lanes with eight keys and the same
-// chunk meet no bank twice.
+// ---------------------------------------------------------------------------------------------- widening
+// A quarter of every raw tile each.  16 E4M3 codes -> 16 fp16 values; a block of 32 4-bit codes -> 32 bf16 values, in whose groups of eight elements i and
+// i + 4 stand side by side (the queries are laid out alike, and the columns of O are taken in that order).  The copies leave 16-byte chunk x of key k at
+// chunk x ^ (k & 7) of its row (4-bit rows of four chunks: x ^ (k / 2 & 3)), so that eight lanes with eight keys and the same chunk meet no bank twice.
 template <Kind kKind, int kTiles>
 __device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c, WideUnits& units, int cw) {
     using W = Wide<kKind, kTiles>;
-    const DecodeParams& p = w.d;
-    constexpr int kChunks = kKind == kE4m3 ? 8 : 4, kRowsPer = 32 / kChunks, kKeys = W::kWarpKeys, kCopies = kKeys / kRowsPer;
-    const int lane = threadIdx.x & 31, chunk = lane % kChunks, sub = lane / kChunks;
-    const int page_mask = (1 << p.page_shift) - 1;
-    const uint32_t mine = c.smem + W::kRawAt + cw * (W::kRaw * W::kRawBytes);
-    const int64_t row_step = kRowsPer * p.stride_tok;
-    // the copy to issue next: tile j of the unit, K or V; the pages of this warp's keys in it (with 16-token pages two) and in the next tile
-    int issued = 0, j = units.t_begin, in = 0, key0 = 0, id0 = -1, id1 = -1, ahead0 = -1, ahead1 = -1;
-    bool is_v = false, more = units.valid;
-    auto look_up = [&](int t) {
-        const int32_t* row = p.table + units.cur.b * p.table_stride;
-        const int key = units.key_of(t) + cw * kKeys, len = units.cur.r.len, low = units.cur.r.low(p);
-        auto page_of = [&](int k) {
-            const int first = k & ~page_mask;
-            int id = -1;
-            if (k < len && (first + page_mask + 1 > low || first < p.sinks)) id = __ldg(row + (k >> p.page_shift));
-            return id;                                     // looked at when it is used: the load travels meanwhile
-        };
-        ahead0 = page_of(key);
-        ahead1 = page_mask < kKeys - 1 ? page_of(key + 16) : ahead0;
-    };
-    auto copy = [&]() {
-        if (more) {
-            if (!is_v) {
-                key0 = units.key_of(j) + cw * kKeys;
-                id0 = (uint32_t)ahead0 < (uint32_t)p.num_pages ? ahead0 : -1;
-                id1 = (uint32_t)ahead1 < (uint32_t)p.num_pages ? ahead1 : -1;
-                if (j + 1 < units.t_end) look_up(j + 1);
-            }
-            const int len = units.cur.r.len, low = units.cur.r.low(p);
-            const uint32_t dst = mine + in * W::kRawBytes;
-            const uint8_t* cache = is_v ? p.v : p.k;
-            const bool all = id0 >= 0 && id1 >= 0 && key0 + kKeys <= len && (key0 >= low || key0 + kKeys <= p.sinks);
-            const int64_t off0 = id0 * p.stride_page + ((key0 & page_mask) + sub) * p.stride_tok;
-            const int64_t off1 = page_mask < kKeys - 1 ? id1 * p.stride_page + sub * p.stride_tok - (16 / kRowsPer) * row_step : off0;      // of the copy that would be the first
-            const uint8_t* base = cache + units.cur.u * p.stride_head + chunk * 16;
-#pragma unroll
-            for (int i = 0; i < kCopies; ++i) {
-                const int k = i * kRowsPer + sub, key = key0 + k;
-                const uint8_t* src = base + (i * kRowsPer < 16 ? off0 : off1) + i * row_step;
-                const uint32_t to = dst + k * (kChunks * 16) + ((chunk ^ (kKind == kE4m3 ? k & 7 : k >> 1 & 3)) << 4);
-                if (all) {
-                    cp_async16(to, src);
-                } else {
-                    const bool ok = (i * kRowsPer < 16 ? id0 : id1) >= 0 && key < len && (key >= low || key < p.sinks);
-                    cp_async16_or_zeros(to, ok ? src : p.k, ok);
-                }
-            }
-            if (kKind == kMx4) {
-                const int k = lane & (kKeys - 1), key = key0 + k, id = k < 16 ? id0 : id1;
-                const bool ok = id >= 0 && key < len && (key >= low || key < p.sinks) && lane < kKeys;
-                const uint8_t* src = ok ? cache + p.Hkv * 64 + units.cur.u * 4 + id * p.stride_page + (key & page_mask) * p.stride_tok : p.k;
-                if (lane < kKeys) cp_async4_or_zeros(dst + W::kRawCodes + k * 4, src, ok);
-            }
-            if (++in == W::kRaw) in = 0;
-            ++issued;
-            if (is_v && ++j == units.t_end) {
-                units.next(p);
-                j = units.t_begin;
-                more = units.valid;
-                if (more) look_up(j);
-            }
-            is_v = !is_v;
-        }
-        cp_commit();
-    };
-    if (more) look_up(j);
-    for (int i = 0; i < W::kRaw - 1; ++i) copy();
-    int out = 0;
-    bool v_now = false;
+    const int lane = threadIdx.x & 31;
+    WideRing<W::kRawTiles ? W::kRaw : 1> raw = {0, 0};
     WideRing<W::kStagesK> kr = {0, 1};
     WideRing<W::kStagesV> vr = {0, 1};
+    for (; units.valid; units.next(w.d)) {
+        const int n = 2 * (units.t_end - units.t_begin);
+        const int exp_byte = W::kRawCodes + (units.cur.u & 3) * 4;
 #pragma unroll 1
-    for (int ld = 0; ld < issued; ++ld) {
-        cp_wait<W::kRaw - 2>();
-        __syncwarp();                  // this slot has landed, and every lane has read the slot that is filled next
-        copy();
-        c.wait(v_now ? kWVEmpty + vr.slot : kWKEmpty + kr.slot, v_now ? vr.par : kr.par, ld);
-        __syncwarp();
-        const uint32_t src = mine + out * W::kRawBytes, tile = c.smem + W::kKV + (v_now ? W::kStagesK + vr.slot : kr.slot) * kTileBytes;
-        if (kKind == kE4m3) {
-#pragma unroll 4
-            for (int i = 0; i < kKeys / 4; ++i) {
-                const int item = i * 32 + lane, k = (item >> 6) * 8 + (item & 7), x = item >> 3 & 7, key = cw * kKeys + k;
-                const uint4 q = lds128(src + k * 128 + ((x ^ (k & 7)) << 4));
-                uint4 a, b;
-                widen4(q.x, a.x, a.y);
-                widen4(q.y, a.z, a.w);
-                widen4(q.z, b.x, b.y);
-                widen4(q.w, b.z, b.w);
-                const uint32_t row = tile + (x >> 2) * kHalfBytes + key * 128;
-                sts128(row + (((2 * x & 7) ^ (key & 7)) << 4), a);
-                sts128(row + (((2 * x + 1 & 7) ^ (key & 7)) << 4), b);
-            }
-        } else {
-#pragma unroll 2
-            for (int i = 0; i < kKeys / 8; ++i) {
-                const int item = i * 32 + lane, k = (item >> 5) * 8 + (item & 7), x = item >> 3 & 3, key = cw * kKeys + k;
-                const uint4 q = lds128(src + k * 64 + ((x ^ (k >> 1 & 3)) << 4));
-                const uint32_t e = lds32(src + W::kRawCodes + k * 4) >> (8 * x) & 255;
-                const uint32_t codes[4] = {q.x, q.y, q.z, q.w};
-                const uint32_t row = tile + (x >> 1) * kHalfBytes + key * 128;
-                // one factor of 2^(e - 127 + 126) while it is a bf16 number, else 2^126 and 2^(e - 127)
-                const bool near = __all_sync(0xffffffffu, e - 1 < 128u);
-                const uint32_t f = near ? (e + 126) * 0x00800080u : 0x7e807e80u;
-                const uint32_t f2 = e == 0 ? 0x00400040u : (e == 255 ? 0x7fc07fc0u : e * 0x00800080u);
+        for (int ld = 0; ld < n; ++ld) {
+            const bool is_v = ld & 1;
+            c.wait(kWRawFull + raw.slot, raw.par, ld);
+            c.wait(is_v ? kWVEmpty + vr.slot : kWKEmpty + kr.slot, is_v ? vr.par : kr.par, ld);
+            __syncwarp();
+            const uint32_t src = c.smem + W::kRawAt + raw.slot * W::kRawBytes;
+            const uint32_t tile = c.smem + W::kKV + (is_v ? W::kStagesK + vr.slot : kr.slot) * kTileBytes;
+            if (kKind == kE4m3) {
+                constexpr int kItems = 1024 / 32 / kConvWarps;
+                // item (16 codes): key (item / 64) * 8 + item % 8, chunk item / 8 % 8
+                const int k7 = lane & 7, x0 = lane >> 3;
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    uint4 o = make_uint4(mul_bf16x2(small_bf16<0>(codes[n]), f), mul_bf16x2(small_bf16<1>(codes[n]), f),
-                                         mul_bf16x2(small_bf16<2>(codes[n]), f), mul_bf16x2(small_bf16<3>(codes[n]), f));
-                    if (!near) o = make_uint4(mul_bf16x2(o.x, f2), mul_bf16x2(o.y, f2), mul_bf16x2(o.z, f2), mul_bf16x2(o.w, f2));
-                    sts128(row + (((4 * x + n & 7) ^ (key & 7)) << 4), o);
+                for (int i0 = 0; i0 < kItems; i0 += 4) {
+                    uint4 q[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int item = (i0 + i) * kConvWarps + cw, key = (item >> 1) * 8 + k7, x = (item & 1) * 4 + x0;
+                        q[i] = lds128(src + key * 128 + ((x ^ k7) << 4));
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int item = (i0 + i) * kConvWarps + cw, key = (item >> 1) * 8 + k7, x = (item & 1) * 4 + x0;
+                        uint4 a, b;
+                        widen4(q[i].x, a.x, a.y);
+                        widen4(q[i].y, a.z, a.w);
+                        widen4(q[i].z, b.x, b.y);
+                        widen4(q[i].w, b.z, b.w);
+                        const uint32_t row = tile + (x >> 2) * kHalfBytes + key * 128;
+                        sts128(row + (((2 * x & 7) ^ k7) << 4), a);
+                        sts128(row + (((2 * x + 1 & 7) ^ k7) << 4), b);
+                    }
+                }
+            } else {
+                constexpr int kItems = 512 / 32 / kConvWarps;
+                // item (a block): key item / 32 * 8 + item % 8, block item / 8 % 4
+                const int k7 = lane & 7, x = lane >> 3;
+                uint4 q[kItems];
+                uint32_t word[kItems];
+#pragma unroll
+                for (int i = 0; i < kItems; ++i) {
+                    const int key = (i * kConvWarps + cw) * 8 + k7;
+                    q[i] = lds128(src + key * 64 + ((x ^ (k7 >> 1)) << 4));
+                    word[i] = lds32(src + exp_byte + key * 16);
+                }
+#pragma unroll
+                for (int i = 0; i < kItems; ++i) {
+                    const int key = (i * kConvWarps + cw) * 8 + k7;
+                    const uint32_t e = word[i] >> (8 * x) & 255;
+                    const uint32_t codes[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+                    const uint32_t row = tile + (x >> 1) * kHalfBytes + key * 128;
+                    // one factor of 2^(e - 127 + 126) while it is a bf16 number, else 2^126 and 2^(e - 127)
+                    const bool near = __all_sync(0xffffffffu, e - 1 < 128u);
+                    const uint32_t f = near ? (e + 126) * 0x00800080u : 0x7e807e80u;
+                    const uint32_t f2 = e == 0 ? 0x00400040u : (e == 255 ? 0x7fc07fc0u : e * 0x00800080u);
+#pragma unroll
+                    for (int n4 = 0; n4 < 4; ++n4) {
+                        uint4 o = make_uint4(mul_bf16x2(small_bf16<0>(codes[n4]), f), mul_bf16x2(small_bf16<1>(codes[n4]), f),
+                                             mul_bf16x2(small_bf16<2>(codes[n4]), f), mul_bf16x2(small_bf16<3>(codes[n4]), f));
+                        if (!near) o = make_uint4(mul_bf16x2(o.x, f2), mul_bf16x2(o.y, f2), mul_bf16x2(o.z, f2), mul_bf16x2(o.w, f2));
+                        sts128(row + (((4 * x + n4 & 7) ^ k7) << 4), o);
+                    }
                 }
             }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // the tensor cores read what these lanes wrote
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(c.bars + (is_v ? kWVFull + vr.slot : kWKFull + kr.slot) * 8);
+                mbar_arrive(c.bars + (kWRawEmpty + raw.slot) * 8);
+            }
+            raw.advance();
+            if (is_v) vr.advance();
+            else kr.advance();
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");              // the tensor cores read what these lanes wrote
-        __syncwarp();
-        if (lane == 0) mbar_arrive(c.bars + (v_now ? kWVFull + vr.slot : kWKFull + kr.slot) * 8);
-        if (++out == W::kRaw) out = 0;
-        if (v_now) vr.advance();
-        else kr.advance();
-        v_now = !v_now;
     }
-    cp_wait<0>();
 }
 
 // ---------------------------------------------------------------------------------------------- queries
@@ -393,30 +370,36 @@ __device__ __forceinline__ void wide_queries(const WideParams& w, const WideCtx&
                 }
                 for (h += kStep; h >= p.G; h -= p.G) ++t;
             }
+            // E4M3: the largest magnitude of every row, as bits: the exponent is enough, and infinities and NaN stay the largest
+            uint32_t top[kBatch];
+            if (kKind == kE4m3) {
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    const uint32_t two = __vmaxu2(__vmaxu2(x[k].x & 0x7fff7fffu, x[k].y & 0x7fff7fffu), __vmaxu2(x[k].z & 0x7fff7fffu, x[k].w & 0x7fff7fffu));
+                    top[k] = max(two & 0xffffu, two >> 16);
+                }
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+                    for (int k = 0; k < kBatch; ++k) top[k] = max(top[k], __shfl_xor_sync(0xffffffffu, top[k], o));
+            }
 #pragma unroll
             for (int k = 0; k < (kKind == kBf16 ? 0 : kBatch); ++k) {
                 const int i = i0 + (lane >> 4) + k * kStep;
+                if (i >= rows) continue;
                 if (kKind == kMx4) {
-                    if (i < rows)
-                        sts128(place(i), make_uint4(__byte_perm(x[k].x, x[k].z, 0x5410), __byte_perm(x[k].x, x[k].z, 0x7632),
-                                                    __byte_perm(x[k].y, x[k].w, 0x5410), __byte_perm(x[k].y, x[k].w, 0x7632)));
+                    sts128(place(i), make_uint4(__byte_perm(x[k].x, x[k].z, 0x5410), __byte_perm(x[k].x, x[k].z, 0x7632),
+                                                __byte_perm(x[k].y, x[k].w, 0x5410), __byte_perm(x[k].y, x[k].w, 0x7632)));
                 } else {
-                    // largest magnitude of the row, as bits: exponents are enough, and infinities and NaN stay the largest
-                    uint32_t top = __vmaxu2(__vmaxu2(x[k].x & 0x7fff7fffu, x[k].y & 0x7fff7fffu), __vmaxu2(x[k].z & 0x7fff7fffu, x[k].w & 0x7fff7fffu));
-                    top = max(top & 0xffffu, top >> 16);
-#pragma unroll
-                    for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                    const int field = (int)(top >> 7);                    // of a zero or subnormal row 0
-                    const int e = top == 0 || field == 255 ? 0 : min(137 - max(field, 1), 126);
+                    const int field = (int)(top[k] >> 7);                 // of a zero or subnormal row 0
+                    const int e = top[k] == 0 || field == 255 ? 0 : min(137 - max(field, 1), 126);
                     const float up = copysignf(__uint_as_float((uint32_t)(127 + e) << 23), sign);
                     const uint32_t word[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
                     uint32_t o[4];
 #pragma unroll
                     for (int n = 0; n < 4; ++n) o[n] = pack_weights<true>(__uint_as_float(word[n] << 16) * up, __uint_as_float(word[n] & 0xffff0000u) * up);
-                    if (i < rows) {
-                        sts128(place(i), make_uint4(o[0], o[1], o[2], o[3]));
-                        if (chunk == 0) reinterpret_cast<int8_t*>(c.gen + W::kExp)[(round & 1) * kWideRows + i] = (int8_t)e;
-                    }
+                    sts128(place(i), make_uint4(o[0], o[1], o[2], o[3]));
+                    if (chunk == 0) reinterpret_cast<int8_t*>(c.gen + W::kExp)[(round & 1) * kWideRows + i] = (int8_t)e;
                 }
             }
         }
@@ -897,7 +880,8 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
 
 template <Kind kKind, int kTiles>
 __global__ void __launch_bounds__(Wide<kKind, kTiles>::kThreads, 1)
-tree_wide_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ WideParams w) {
+tree_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_ke,
+                 const __grid_constant__ CUtensorMap tm_ve, const __grid_constant__ WideParams w) {
     using W = Wide<kKind, kTiles>;
     constexpr int kThreadsHere = W::kThreads;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -918,6 +902,10 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
             mbar_init(c.bars + (kWKEmpty + s) * 8, 1);
             mbar_init(c.bars + (kWVFull + s) * 8, W::kRawTiles ? kConvWarps : 1);
             mbar_init(c.bars + (kWVEmpty + s) * 8, 1);
+        }
+        for (int s = 0; s < W::kRaw; ++s) {
+            mbar_init(c.bars + (kWRawFull + s) * 8, 1);
+            mbar_init(c.bars + (kWRawEmpty + s) * 8, kConvWarps);
         }
         mbar_init(c.bars + kWSFree * 8, 4);
         for (int h = 0; h < 2; ++h) {
@@ -1001,11 +989,11 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
                 wide_outputs<kKind, kTiles>(w, c, units);
             } else if (warp == 11) {
                 wide_queries<kKind, kTiles>(w, c, units, 0);
+            } else if (warp == 8) {
+                const WideMaps maps = {&tm_k, &tm_v, &tm_ke, &tm_ve};
+                wide_producer<kKind, kTiles>(w, c, units, maps);
             } else if constexpr (W::kRawTiles) {
-                if (warp == 8) wide_queries<kKind, kTiles>(w, c, units, 1);
-                else wide_widen<kKind, kTiles>(w, c, units, warp - 12);
-            } else {
-                wide_producer<kTiles>(w, c, units, &tmK, &tmV);
+                wide_widen<kKind, kTiles>(w, c, units, warp - 12);
             }
         }
     }

@@ -52,8 +52,12 @@ tree_plan_kernel(const int32_t* parent, const int32_t* tree_len, const int32_t* 
     token_slot[at] = t < m ? base + t : 0;
 }
 
-// Up to 32 rows per KV head take the narrow form, which reads the keys once for them.
-constexpr int kNarrowRows = 32;
+// Rows per KV head up to which the narrow form is taken.  It is faster up to 16 rows for every kind (37 requests of 4096 keys at 8 rows: bf16 95 us against 102, E4M3 65
+// against 112, 4-bit 75 against 145).  Its 32-row form costs a warp more than a tile's loads for 4-bit rows (24 rows 165 us against 148) and somewhat for bf16
+// (111 against 105, with 700 keys 39 against 32); E4M3 stays ahead with it (97 against 115).  Behind 32 rows it reads the keys again (48 rows: 209 / 183 / 265
+// us against 107 / 120 / 152).
+constexpr int kNarrowRows[3] = {16, 32, 16};
+constexpr int kLeastNarrowRows = 16;               // a workspace serves every kind
 
 template <typename Cache>
 int tree_attn(cp_ctx* ctx, const void* q, const Cache* cache, const int32_t* page_table, int64_t table_stride, const int32_t* kv_len,
@@ -73,7 +77,7 @@ int tree_attn(cp_ctx* ctx, const void* q, const Cache* cache, const int32_t* pag
     if (guard.rc()) return guard.rc();
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const CacheView view = view_of(cache);
-    if (p.rows > kNarrowRows) return launch_tree_wide(ctx, kind, &p, &view, workspace, stream, who);
+    if (p.rows > kNarrowRows[kind]) return launch_tree_wide(ctx, kind, &p, &view, workspace, stream, who);
     if (kind == kBf16) return launch_rows<1, kBf16, kTree>(ctx, p, s, who);
     if (kind == kE4m3) return p.Hkv % 2 == 0 ? launch_rows<2, kE4m3, kTree>(ctx, p, s, who) : launch_rows<1, kE4m3, kTree>(ctx, p, s, who);
     return p.Hkv % 4 == 0 ? launch_rows<4, kMx4, kTree>(ctx, p, s, who) : launch_rows<1, kMx4, kTree>(ctx, p, s, who);
@@ -100,7 +104,7 @@ extern "C" int cp_tree_plan(cp_ctx* ctx, const int32_t* parent, const int32_t* t
 
 extern "C" size_t cp_workspace_bytes_tree(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv) {
     const size_t narrow = cp_workspace_bytes_decode(B, n_q, Hq, Hkv);
-    return narrow == 0 || (int64_t)n_q * (Hq / Hkv) <= kNarrowRows ? narrow : std::max(narrow, tree_wide_workspace());
+    return narrow == 0 || (int64_t)n_q * (Hq / Hkv) <= kLeastNarrowRows ? narrow : std::max(narrow, tree_wide_workspace());
 }
 
 extern "C" int cp_tree_attn(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table, int64_t table_stride,

@@ -1,4 +1,4 @@
-// Attention of drafted trees (and of chains of tokens) with many query rows per KV head, n_q * Hq / Hkv of them, on the tcgen05 tensor cores, over paged caches
+// Attention of drafted trees with many query rows per KV head, n_q * Hq / Hkv of them, on the tcgen05 tensor cores, over paged caches
 // with lengths, masks and page tables on the device.
 //
 // With r rows a key costs 512 r flops and 512 bytes (bf16; E4M3 256, 4-bit 136): at 128 rows half of what the tensor cores can do while the keys
@@ -50,7 +50,6 @@ struct Wide {
     static constexpr uint32_t kRawCodes = kKind == kE4m3 ? 16384u : 8192u;                         // of the 128 keys of a tile
     static constexpr uint32_t kRawBytes = kRawCodes + (kKind == kMx4 ? 2048u : 0u);                // 4-bit: then 16 bytes a key with the exponents of four heads
     static constexpr int kRaw = kKind == kBf16 ? 0 : (kKind == kE4m3 ? (kTurns ? 3 : 2) : (kTurns ? 6 : 3));      // slots of the ring of raw tiles
-    static constexpr int kQueryWarps = 1;
     // shared memory: the query tiles, the ring, the raw tiles, what the warpgroups tell one another, barriers and small areas
     static constexpr uint32_t kQ = 0, kKV = kTiles * kTileBytes, kRawAt = kKV + kStages * kTileBytes;
     static constexpr uint32_t kMl = kRawAt + kRaw * kRawBytes;                        // [unit parity][warpgroup][row]: maximum and sum
@@ -76,7 +75,8 @@ enum WideBar : uint32_t {
     kWOFree = kWPvDone + 2,                  // + warpgroup: O has been read
     kWOdd = kWOFree + 2,                     // the unit's list of odd keys is complete
     kWMl = kWOdd + 1,                        // + warpgroup: its accumulator, maxima and sums of the unit are complete (tiles in turn)
-    kWRawFull = kWMl + 2,                    // + raw slot
+    kWQRaw = kWMl + 2,                       // the query rows are there, to be converted
+    kWRawFull = kWQRaw + 1,                  // + raw slot
     kWRawEmpty = kWRawFull + kMaxRaw,        // + raw slot
     kNumWideBars = kWRawEmpty + kMaxRaw
 };
@@ -136,10 +136,6 @@ struct WideUnits {
 };
 
 static_assert(sizeof(WideUnits) <= kUnitBytes, "room for the units");
-
-// The token of a row among the last m of its sequence, < 0 or >= m: none.  Chains are trees in which every token sees those before it; of a sequence shorter
-// than n_q the last rows are its tokens.
-__device__ __forceinline__ int wide_token(const DecodeParams& p, int t, int m) { return p.tree_mask ? t : t - (p.n_q - m); }
 
 struct WideCtx {
     uint32_t smem, bars, tmem;
@@ -233,7 +229,74 @@ __device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx
     }
 }
 
+// 16-byte chunk (of 16) of query row i: lines of 64 dims with the 128-byte swizzle, tiles of 128 rows
+__device__ __forceinline__ uint32_t wide_place(uint32_t q, int i, int chunk) {
+    const int in = i & (kBlockM - 1);
+    return q + (i / kBlockM) * kTileBytes + (chunk >> 3) * kHalfBytes + in * 128 + (((chunk & 7) ^ (in & 7)) << 4);
+}
+
 // ---------------------------------------------------------------------------------------------- widening
+// The query rows of a unit, in place, two a step of a warp.  E4M3: to fp16, scaled per row by a power of two that brings the largest element to [2^10, 2^11)
+// (what falls below 2^-24 of it is lost); the sign of the keys' scale joins here.  4-bit: elements i and i + 4 of every eight side by side.  Spread over the
+// widening warps, as the one that gathers the rows needs 9 us for 64 rows of E4M3.
+template <Kind kKind, int kTiles>
+__device__ __forceinline__ void wide_convert(const WideParams& w, const WideCtx& c, const WideUnits& units, int cw, int round) {
+    using W = Wide<kKind, kTiles>;
+    constexpr int kBatch = 4;                              // steps that go together
+    const DecodeParams& p = w.d;
+    const int lane = threadIdx.x & 31, chunk = lane & 15, sub = lane >> 4;
+    const int rows = min(w.class_rows, p.rows - (int)(blockIdx.x % w.classes) * w.class_rows);
+    const float sign = kKind == kE4m3 ? p.k_scale[units.cur.u] : 1.f;
+    c.wait(kWQRaw, round & 1, round);
+    __syncwarp();
+#pragma unroll 1
+    for (int i0 = 2 * cw; i0 < rows; i0 += 2 * kConvWarps * kBatch) {      // the same for all lanes
+        uint4 x[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int i = i0 + 2 * kConvWarps * k + sub;
+            x[k] = make_uint4(0, 0, 0, 0);
+            if (i < rows) x[k] = lds128(wide_place(c.smem + W::kQ, i, chunk));
+        }
+        // E4M3: the largest magnitude of every row, as bits: the exponent is enough, and infinities and NaN stay the largest
+        uint32_t top[kBatch];
+        if (kKind == kE4m3) {
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const uint32_t two = __vmaxu2(__vmaxu2(x[k].x & 0x7fff7fffu, x[k].y & 0x7fff7fffu), __vmaxu2(x[k].z & 0x7fff7fffu, x[k].w & 0x7fff7fffu));
+                top[k] = max(two & 0xffffu, two >> 16);
+            }
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) top[k] = max(top[k], __shfl_xor_sync(0xffffffffu, top[k], o));
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int i = i0 + 2 * kConvWarps * k + sub;
+            if (i >= rows) continue;
+            const uint32_t at = wide_place(c.smem + W::kQ, i, chunk);
+            if (kKind == kMx4) {
+                sts128(at, make_uint4(__byte_perm(x[k].x, x[k].z, 0x5410), __byte_perm(x[k].x, x[k].z, 0x7632),
+                                      __byte_perm(x[k].y, x[k].w, 0x5410), __byte_perm(x[k].y, x[k].w, 0x7632)));
+            } else {
+                const int field = (int)(top[k] >> 7);      // of a zero or subnormal row 0
+                const int e = top[k] == 0 || field == 255 ? 0 : min(137 - max(field, 1), 126);
+                const float up = copysignf(__uint_as_float((uint32_t)(127 + e) << 23), sign);
+                const uint32_t word[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+                uint32_t o[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) o[n] = pack_weights<true>(__uint_as_float(word[n] << 16) * up, __uint_as_float(word[n] & 0xffff0000u) * up);
+                sts128(at, make_uint4(o[0], o[1], o[2], o[3]));
+                if (chunk == 0) reinterpret_cast<int8_t*>(c.gen + W::kExp)[(round & 1) * kWideRows + i] = (int8_t)e;
+            }
+        }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) mbar_arrive(c.bars + kWQFull * 8);
+}
+
 // A quarter of every raw tile each.  16 E4M3 codes -> 16 fp16 values; a block of 32 4-bit codes -> 32 bf16 values, in whose groups of eight elements i and
 // i + 4 stand side by side (the queries are laid out alike, and the columns of O are taken in that order).  The copies leave 16-byte chunk x of key k at
 // chunk x ^ (k & 7) of its row (4-bit rows of four chunks: x ^ (k / 2 & 3)), so that eight lanes with eight keys and the same chunk meet no bank twice.
@@ -244,12 +307,13 @@ __device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c
     WideRing<W::kRawTiles ? W::kRaw : 1> raw = {0, 0};
     WideRing<W::kStagesK> kr = {0, 1};
     WideRing<W::kStagesV> vr = {0, 1};
-    for (; units.valid; units.next(w.d)) {
+    for (int round = 0; units.valid; units.next(w.d), ++round) {
         const int n = 2 * (units.t_end - units.t_begin);
         const int exp_byte = W::kRawCodes + (units.cur.u & 3) * 4;
 #pragma unroll 1
         for (int ld = 0; ld < n; ++ld) {
             const bool is_v = ld & 1;
+            if (ld == 1) wide_convert<kKind, kTiles>(w, c, units, cw, round);
             c.wait(kWRawFull + raw.slot, raw.par, ld);
             c.wait(is_v ? kWVEmpty + vr.slot : kWKEmpty + kr.slot, is_v ? vr.par : kr.par, ld);
             __syncwarp();
@@ -325,91 +389,40 @@ __device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c
 }
 
 // ---------------------------------------------------------------------------------------------- queries
-// Row i of the unit's class is token (r0 + i) / G, head (r0 + i) % G of the group; rows without a token are zeros.  128-byte swizzle lines, 64 dims a half.
-// E4M3: fp16, scaled per row by a power of two that brings the largest element to [2^10, 2^11) (what falls below 2^-24 of it is lost); the sign of the keys'
-// scale joins here.  4-bit: elements i and i + 4 of every eight side by side.
+// Row i of the unit's class is token (r0 + i) / G, head (r0 + i) % G of the group; rows without a token are zeros.  The widening warps convert them.
 template <Kind kKind, int kTiles>
-__device__ __forceinline__ void wide_queries(const WideParams& w, const WideCtx& c, WideUnits& units, int part) {
+__device__ __forceinline__ void wide_queries(const WideParams& w, const WideCtx& c, WideUnits& units) {
     using W = Wide<kKind, kTiles>;
-    constexpr int kStep = 2 * W::kQueryWarps, kBatch = 8;                 // rows of a step, steps whose loads are in flight together
     const DecodeParams& p = w.d;
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, chunk = lane & 15, sub = lane >> 4;
     const int r0 = (int)(blockIdx.x % w.classes) * w.class_rows, rows = min(w.class_rows, p.rows - r0);
-    const int chunk = lane & 15, first = 2 * part + (lane >> 4);
-    auto place = [&](int i) {
-        const int in = i & (kBlockM - 1);
-        return c.smem + W::kQ + (i / kBlockM) * kTileBytes + (chunk >> 3) * kHalfBytes + in * 128 + (((chunk & 7) ^ (in & 7)) << 4);
-    };
-    for (int i = first; i < kTiles * kBlockM; i += kStep)                 // rows behind the class's last stay zeros
-        if (i >= rows) {
-            sts128(place(i), make_uint4(0, 0, 0, 0));
-            if (kKind == kE4m3 && chunk == 0) {
-                reinterpret_cast<int8_t*>(c.gen + W::kExp)[i] = 0;
-                reinterpret_cast<int8_t*>(c.gen + W::kExp)[kWideRows + i] = 0;
-            }
-        }
+    auto place = [&](int i) { return wide_place(c.smem + W::kQ, i, chunk); };
+    for (int i = sub; i < kTiles * kBlockM; i += 2)        // rows behind the class's last stay zeros
+        if (i >= rows) sts128(place(i), make_uint4(0, 0, 0, 0));
+    if (kKind == kE4m3)
+        for (int i = lane; i < 2 * kWideRows; i += 32) reinterpret_cast<int8_t*>(c.gen + W::kExp)[i] = 0;
+    const int t0 = (r0 + sub) / p.G, h0 = r0 + sub - t0 * p.G;            // token and head of this lane's first row
+    const int64_t wrap = (int64_t)(p.Hq - p.G) * kDim;     // elements from the group's heads of a token to the next token's
     for (int round = 0; units.valid; units.next(p), ++round) {
         const int b = units.cur.b, m = units.cur.r.len - units.cur.r.base;
-        const __nv_bfloat16* q = p.q + ((int64_t)b * p.n_q * p.Hq + (int64_t)units.cur.u * p.G) * kDim + chunk * 8;
+        const int live = min(rows, m * p.G - r0);
+        const __nv_bfloat16* src = p.q + (((int64_t)b * p.n_q + t0) * p.Hq + (int64_t)units.cur.u * p.G + h0) * kDim + chunk * 8;
         c.wait(kWQEmpty, (round & 1) ^ 1, round);
         __syncwarp();
-        const float sign = kKind == kE4m3 ? p.k_scale[units.cur.u] : 1.f;
-        int t = (r0 + first) / p.G, h = r0 + first - t * p.G;             // token and head of the row
-        for (int i0 = 2 * part; i0 < rows; i0 += kStep * kBatch) {               // the same for all lanes
-            uint4 x[kBatch];
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                const int i = i0 + (lane >> 4) + k * kStep, live = wide_token(p, t, m);
-                const bool ok = i < rows && live >= 0 && live < m;
-                const __nv_bfloat16* src = ok ? q + ((int64_t)t * p.Hq + h) * kDim : p.q;
-                if (kKind == kBf16) {
-                    if (i < rows) cp_async16_or_zeros(place(i), src, ok);
-                } else {
-                    x[k] = make_uint4(0, 0, 0, 0);
-                    if (ok) x[k] = __ldg(reinterpret_cast<const uint4*>(src));
-                }
-                for (h += kStep; h >= p.G; h -= p.G) ++t;
-            }
-            // E4M3: the largest magnitude of every row, as bits: the exponent is enough, and infinities and NaN stay the largest
-            uint32_t top[kBatch];
-            if (kKind == kE4m3) {
-#pragma unroll
-                for (int k = 0; k < kBatch; ++k) {
-                    const uint32_t two = __vmaxu2(__vmaxu2(x[k].x & 0x7fff7fffu, x[k].y & 0x7fff7fffu), __vmaxu2(x[k].z & 0x7fff7fffu, x[k].w & 0x7fff7fffu));
-                    top[k] = max(two & 0xffffu, two >> 16);
-                }
-#pragma unroll
-                for (int o = 8; o > 0; o >>= 1)
-#pragma unroll
-                    for (int k = 0; k < kBatch; ++k) top[k] = max(top[k], __shfl_xor_sync(0xffffffffu, top[k], o));
-            }
-#pragma unroll
-            for (int k = 0; k < (kKind == kBf16 ? 0 : kBatch); ++k) {
-                const int i = i0 + (lane >> 4) + k * kStep;
-                if (i >= rows) continue;
-                if (kKind == kMx4) {
-                    sts128(place(i), make_uint4(__byte_perm(x[k].x, x[k].z, 0x5410), __byte_perm(x[k].x, x[k].z, 0x7632),
-                                                __byte_perm(x[k].y, x[k].w, 0x5410), __byte_perm(x[k].y, x[k].w, 0x7632)));
-                } else {
-                    const int field = (int)(top[k] >> 7);                 // of a zero or subnormal row 0
-                    const int e = top[k] == 0 || field == 255 ? 0 : min(137 - max(field, 1), 126);
-                    const float up = copysignf(__uint_as_float((uint32_t)(127 + e) << 23), sign);
-                    const uint32_t word[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
-                    uint32_t o[4];
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) o[n] = pack_weights<true>(__uint_as_float(word[n] << 16) * up, __uint_as_float(word[n] & 0xffff0000u) * up);
-                    sts128(place(i), make_uint4(o[0], o[1], o[2], o[3]));
-                    if (chunk == 0) reinterpret_cast<int8_t*>(c.gen + W::kExp)[(round & 1) * kWideRows + i] = (int8_t)e;
-                }
-            }
+        int h = h0;
+#pragma unroll 4
+        for (int i = sub; i < rows; i += 2) {
+            const bool ok = i < live;
+            cp_async16_or_zeros(place(i), ok ? src : p.q, ok);
+            src += 2 * kDim;
+            for (h += 2; h >= p.G; h -= p.G) src += wrap;
         }
-        if (kKind == kBf16) {
-            cp_commit();
-            cp_wait<0>();
-        }
+        cp_commit();
+        cp_wait<0>();
+        __syncwarp();
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the tensor cores read what these lanes wrote
         __syncwarp();
-        if (lane == 0) mbar_arrive(c.bars + kWQFull * 8);
+        if (lane == 0) mbar_arrive(c.bars + (W::kRawTiles ? kWQRaw : kWQFull) * 8);
     }
 }
 
@@ -700,7 +713,7 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
     for (int round = 0; units.valid; ++round) {
         const Request rq = units.cur.r;
         const int b = units.cur.b, u = units.cur.u, j0 = units.t_begin, n = units.t_end, m_tree = rq.len - rq.base;
-        const int tt = wide_token(p, t, m_tree);
+        const int tt = t;
         const bool live = in_class && tt >= 0 && tt < m_tree;             // rows without a token: zeros, -inf
         TreeRow tr;
         tr.mask = 0;
@@ -895,7 +908,8 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int run = (int)(blockIdx.x / w.classes);
     if (tid == 0) {
-        mbar_init(c.bars + kWQFull * 8, W::kQueryWarps);
+        mbar_init(c.bars + kWQFull * 8, W::kRawTiles ? kConvWarps : 1);
+        mbar_init(c.bars + kWQRaw * 8, 1);
         mbar_init(c.bars + kWQEmpty * 8, 1);
         for (int s = 0; s < kMaxRing; ++s) {
             mbar_init(c.bars + (kWKFull + s) * 8, W::kRawTiles ? kConvWarps : 1);
@@ -988,7 +1002,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             } else if (warp == 10) {
                 wide_outputs<kKind, kTiles>(w, c, units);
             } else if (warp == 11) {
-                wide_queries<kKind, kTiles>(w, c, units, 0);
+                wide_queries<kKind, kTiles>(w, c, units);
             } else if (warp == 8) {
                 const WideMaps maps = {&tm_k, &tm_v, &tm_ke, &tm_ve};
                 wide_producer<kKind, kTiles>(w, c, units, maps);

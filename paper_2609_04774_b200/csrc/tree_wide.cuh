@@ -69,8 +69,8 @@ enum WideBar : uint32_t {
     kWVFull = kWKEmpty + kMaxRing,           // + stage
     kWVEmpty = kWVFull + kMaxRing,           // + stage
     kWSReady = kWVEmpty + kMaxRing,          // + warpgroup: its scores are in the S buffer
-    kWSFree = kWSReady + 2,                  // the S buffer has been read
-    kWPReady = kWSFree + 1,                  // + 2 warpgroup + piece
+    kWSFree = kWSReady + 2,                  // + warpgroup: it has read the S buffer
+    kWPReady = kWSFree + 2,                  // + 2 warpgroup + piece
     kWPvDone = kWPReady + 4,                 // + warpgroup: P V of a step has finished
     kWOFree = kWPvDone + 2,                  // + warpgroup: O has been read
     kWOdd = kWOFree + 2,                     // the unit's list of odd keys is complete
@@ -143,7 +143,16 @@ struct WideCtx {
     volatile uint32_t* abort_flag;
     int32_t* status;
     __device__ __forceinline__ void wait(uint32_t id, uint32_t parity, int iter) const { mbar_wait(bars, id, parity, abort_flag, status, iter); }
+    // some wait has given up: whoever starts copies or products stops, so that little is in flight when the CTA ends (by the warp)
+    __device__ __forceinline__ bool given_up() const { return __any_sync(0xffffffffu, *abort_flag != 0); }
 };
+// Warps of a warpgroup that have rows of the CTA's class, one at least.  The others stay out (they would poll beside the widening warps:
+// 8192 4-bit keys of 37 requests, 64 rows 275 us, 255 like this).
+template <int kTiles>
+__device__ __forceinline__ int wide_warps(const WideParams& w, int wg) {
+    const int rows = min(w.class_rows, w.d.rows - (int)(blockIdx.x % w.classes) * w.class_rows) - (kTiles == 2 ? wg * kBlockM : 0);
+    return min(max((rows + 31) >> 5, 1), 4);
+}
 // A position in a ring: slot, and the parity of the phase that ends when it is filled (for the side that fills: when it was emptied).
 template <int kStages>
 struct WideRing {
@@ -185,6 +194,7 @@ __device__ __forceinline__ void wide_producer(const WideParams& w, const WideCtx
         const int n_loads = 2 * (units.t_end - units.t_begin);
         int j = units.t_begin;                             // next K tile
         for (int ld = 0; ld < n_loads; ++ld) {
+            if (c.given_up()) return;
             const bool is_v = W::kRawTiles ? ld & 1 : ld == n_loads - 1 || (ld > 0 && (ld & 1) == 0);
             int ids;
             if (!is_v) {
@@ -356,23 +366,33 @@ __device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c
                     q[i] = lds128(src + key * 64 + ((x ^ (k7 >> 1)) << 4));
                     word[i] = lds32(src + exp_byte + key * 16);
                 }
+                // one factor of 2^(e - 127 + 126) while it is a bf16 number, which is a branch for all items, so that their work is interleaved; else 2^126 and 2^(e - 127)
+                bool near = true;
 #pragma unroll
                 for (int i = 0; i < kItems; ++i) {
+                    word[i] = word[i] >> (8 * x) & 255;
+                    near &= word[i] - 1 < 128u;
+                }
+                auto store = [&](int i, bool far) {
                     const int key = (i * kConvWarps + cw) * 8 + k7;
-                    const uint32_t e = word[i] >> (8 * x) & 255;
-                    const uint32_t codes[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+                    const uint32_t e = word[i], codes[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
                     const uint32_t row = tile + (x >> 1) * kHalfBytes + key * 128;
-                    // one factor of 2^(e - 127 + 126) while it is a bf16 number, else 2^126 and 2^(e - 127)
-                    const bool near = __all_sync(0xffffffffu, e - 1 < 128u);
-                    const uint32_t f = near ? (e + 126) * 0x00800080u : 0x7e807e80u;
+                    const uint32_t f = far ? 0x7e807e80u : (e + 126) * 0x00800080u;
                     const uint32_t f2 = e == 0 ? 0x00400040u : (e == 255 ? 0x7fc07fc0u : e * 0x00800080u);
 #pragma unroll
                     for (int n4 = 0; n4 < 4; ++n4) {
                         uint4 o = make_uint4(mul_bf16x2(small_bf16<0>(codes[n4]), f), mul_bf16x2(small_bf16<1>(codes[n4]), f),
                                              mul_bf16x2(small_bf16<2>(codes[n4]), f), mul_bf16x2(small_bf16<3>(codes[n4]), f));
-                        if (!near) o = make_uint4(mul_bf16x2(o.x, f2), mul_bf16x2(o.y, f2), mul_bf16x2(o.z, f2), mul_bf16x2(o.w, f2));
+                        if (far) o = make_uint4(mul_bf16x2(o.x, f2), mul_bf16x2(o.y, f2), mul_bf16x2(o.z, f2), mul_bf16x2(o.w, f2));
                         sts128(row + (((4 * x + n4 & 7) ^ k7) << 4), o);
                     }
+                };
+                if (__all_sync(0xffffffffu, near)) {
+#pragma unroll
+                    for (int i = 0; i < kItems; ++i) store(i, false);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kItems; ++i) store(i, true);
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // the tensor cores read what these lanes wrote
@@ -403,7 +423,7 @@ __device__ __forceinline__ void wide_queries(const WideParams& w, const WideCtx&
         for (int i = lane; i < 2 * kWideRows; i += 32) reinterpret_cast<int8_t*>(c.gen + W::kExp)[i] = 0;
     const int t0 = (r0 + sub) / p.G, h0 = r0 + sub - t0 * p.G;            // token and head of this lane's first row
     const int64_t wrap = (int64_t)(p.Hq - p.G) * kDim;     // elements from the group's heads of a token to the next token's
-    for (int round = 0; units.valid; units.next(p), ++round) {
+    for (int round = 0; units.valid && !c.given_up(); units.next(p), ++round) {
         const int b = units.cur.b, m = units.cur.r.len - units.cur.r.base;
         const int live = min(rows, m * p.G - r0);
         const __nv_bfloat16* src = p.q + (((int64_t)b * p.n_q + t0) * p.Hq + (int64_t)units.cur.u * p.G + h0) * kDim + chunk * 8;
@@ -432,17 +452,23 @@ __device__ __forceinline__ void wide_scores(const WideParams& w, const WideCtx& 
     using W = Wide<kKind, kTiles>;
     constexpr uint32_t kIdesc = kKind == kE4m3 ? kIdescS & ~((1u << 7) | (1u << 10)) : kIdescS;      // fp16 or bf16 operands
     WideRing<W::kStagesK> pos = {0, 0};
-    uint32_t s_par = 1;                // parity of "the previous score tile was read"; 1: there is none yet
+    uint32_t f_par0 = 0, f_par1 = 0;   // parity of "the scores are read", per warpgroup
+    int prev = -1;                     // whose scores are in S
     const uint64_t q_desc = make_desc(c.smem + W::kQ, 16, 1024), k_desc = make_desc(c.smem + W::kKV, 16, 1024);
     for (int round = 0; units.valid; units.next(w.d), ++round) {
         const int j0 = units.t_begin, n = units.t_end;
         c.wait(kWQFull, round & 1, round);
 #pragma unroll 1
         for (int j = j0; j < n; ++j) {
+            if (c.given_up()) return;
             c.wait(kWKFull + pos.slot, pos.par, j);
             for (int q = 0; q < kTiles; ++q) {
-                c.wait(kWSFree, s_par, j);
-                s_par ^= 1u;
+                if (prev >= 0) {
+                    c.wait(kWSFree + prev, prev ? f_par1 : f_par0, j);
+                    if (prev) f_par1 ^= 1u;
+                    else f_par0 ^= 1u;
+                }
+                prev = kTiles == 2 ? q : (j - j0) & 1;
                 tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
@@ -450,7 +476,7 @@ __device__ __forceinline__ void wide_scores(const WideParams& w, const WideCtx& 
                         const uint32_t off = ((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4;
                         mma_ss(c.tmem + kWTmemS, q_desc + q * (kTileBytes >> 4) + off, k_desc + pos.slot * (kTileBytes >> 4) + off, kIdesc, ks > 0);
                     }
-                    tc_commit(c.bars + (kWSReady + (kTiles == 2 ? q : (j - j0) & 1)) * 8);
+                    tc_commit(c.bars + (kWSReady + prev) * 8);
                     if (q == kTiles - 1) {
                         tc_commit(c.bars + (kWKEmpty + pos.slot) * 8);
                         if (j == n - 1) tc_commit(c.bars + kWQEmpty * 8);
@@ -527,6 +553,7 @@ __device__ __forceinline__ void wide_outputs(const WideParams& w, const WideCtx&
         __syncwarp();
 #pragma unroll 1
         for (int j = j0; j < n; ++j) {
+            if (c.given_up()) return;
             c.wait(kWVFull + pos.slot, pos.par, j);
             const int key0 = units.key_of(j);
             if (!units.full(p, key0)) wide_clear<kKind == kE4m3>(p, units.cur.r, c.smem + W::kKV + (W::kStagesK + pos.slot) * kTileBytes, key0, odd);
@@ -657,7 +684,7 @@ __device__ __forceinline__ void wide_softmax_tile(const WideCtx& cx, float (&c0)
         tc_wait_st();                                                                   \
         tc_fence_before();                                                              \
         __syncwarp();                                                                   \
-        if ((threadIdx.x & 31) == 0) mbar_arrive(p_bar + ((q) == 3 ? 8 : 0));           \
+        if ((threadIdx.x & 31) == 0) mbar_arrive(p_bar + ((q) == 3 ? 8 : 0));    \
     }
     CP_WIDE_PIECE(c0, 0)
     CP_WIDE_PIECE(c1, 1)
@@ -683,7 +710,7 @@ __device__ __forceinline__ void wide_softmax_tile(const WideCtx& cx, float (&c0)
         tc_wait_ld();
         tc_fence_before();
         __syncwarp();
-        if ((threadIdx.x & 31) == 0) mbar_arrive(cx.bars + kWSFree * 8);
+        if ((threadIdx.x & 31) == 0) mbar_arrive(cx.bars + (kWSFree + wg) * 8);
         s_par ^= 1u;
     }
     const float2 st = __fadd2_rn(__fadd2_rn(sum0, sum1), __fadd2_rn(sum2, sum3));
@@ -708,17 +735,17 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
     const int r = cls * w.class_rows + row, t = r / p.G;                  // of the KV head; its token
     const bool in_class = row < w.class_rows && r < p.rows;
     constexpr int step = turns ? 2 : 1;
+    if (warp_in_wg >= wide_warps<kTiles>(w, wg)) return;
     float c = p.scale_log2;
     uint32_t s_par = 0, tile_cnt = 0;
     for (int round = 0; units.valid; ++round) {
         const Request rq = units.cur.r;
         const int b = units.cur.b, u = units.cur.u, j0 = units.t_begin, n = units.t_end, m_tree = rq.len - rq.base;
-        const int tt = t;
-        const bool live = in_class && tt >= 0 && tt < m_tree;             // rows without a token: zeros, -inf
+                const bool live = in_class && t < m_tree;                         // rows without a token: zeros, -inf
         TreeRow tr;
         tr.mask = 0;
         tr.lim = 0;
-        if (live) tr = tree_row(p, b, tt, rq.base, m_tree);
+        if (live) tr = tree_row(p, b, t, rq.base, m_tree);
         const int low = (live ? tr.lim : rq.len) - p.window;
         const int j1 = j0 + (turns ? wg : 0);                             // this warpgroup's first tile
         const bool some = j1 < n;
@@ -728,10 +755,11 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
             for (int j = j1; j < n; j += step) {
                 cx.wait(kWSReady + wg, s_par, j);
                 s_par ^= 1u;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(cx.bars + (kWSFree + wg) * 8);
                 if (j > j1) cx.wait(kWPvDone + wg, (tile_cnt - 1) & 1, j);
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(cx.bars + kWSFree * 8);
                     mbar_arrive(cx.bars + (kWPReady + 2 * wg) * 8);
                     mbar_arrive(cx.bars + (kWPReady + 2 * wg + 1) * 8);
                 }
@@ -751,7 +779,7 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
             tc_wait_ld();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(cx.bars + kWSFree * 8);
+            if (lane == 0) mbar_arrive(cx.bars + (kWSFree + wg) * 8);
             if (kF16) {
                 const int e = reinterpret_cast<const int8_t*>(cx.gen + W::kExp)[(round & 1) * kWideRows + row];
                 // c > 0: the sign of a scale is in the queries; with a scale of zero hidden keys must still be -inf
@@ -865,7 +893,7 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
                 mbar_arrive(cx.bars + (kWOFree + wg) * 8);
             }
         }
-        if (any_odd) wide_odd_row<kKind>(p, odd, b, rq.base, rq.len, u, tt, whole, at, cc0 * 32, cc1 * 32);
+        if (any_odd) wide_odd_row<kKind>(p, odd, b, rq.base, rq.len, u, t, whole, at, cc0 * 32, cc1 * 32);
         if (in_class && (!turns || wg == 0)) {
             if (whole) {
                 p.lse[(int64_t)head * ((int64_t)p.B * p.n_q) + (int64_t)b * p.n_q + t] =
@@ -921,13 +949,14 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             mbar_init(c.bars + (kWRawFull + s) * 8, 1);
             mbar_init(c.bars + (kWRawEmpty + s) * 8, kConvWarps);
         }
-        mbar_init(c.bars + kWSFree * 8, 4);
         for (int h = 0; h < 2; ++h) {
+            const int warps = wide_warps<kTiles>(w, h);    // one arrival per warp
             mbar_init(c.bars + (kWSReady + h) * 8, 1);
-            for (int q = 0; q < 2; ++q) mbar_init(c.bars + (kWPReady + 2 * h + q) * 8, 4);      // one arrival per warp
+            mbar_init(c.bars + (kWSFree + h) * 8, warps);
+            for (int q = 0; q < 2; ++q) mbar_init(c.bars + (kWPReady + 2 * h + q) * 8, warps);
             mbar_init(c.bars + (kWPvDone + h) * 8, 1);
-            mbar_init(c.bars + (kWOFree + h) * 8, W::kTurns ? 8 : 4);
-            mbar_init(c.bars + (kWMl + h) * 8, 4);
+            mbar_init(c.bars + (kWOFree + h) * 8, W::kTurns ? 2 * warps : warps);
+            mbar_init(c.bars + (kWMl + h) * 8, warps);
         }
         mbar_init(c.bars + kWOdd * 8, 1);
         *c.abort_flag = 0;

@@ -120,6 +120,9 @@ __device__ __forceinline__ void cp_async16_or_zeros(uint32_t dst, const void* sr
     const int n = valid ? 16 : 0;                          // 0: nothing is read, the 16 bytes become zeros
     asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_async4_or_zeros(uint32_t dst, const void* src, bool valid) {
     const int n = valid ? 4 : 0;
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
@@ -166,6 +169,11 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
     else
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// fp16, onto zero: no registers are to be cleared first
+__device__ __forceinline__ void mma16816_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -448,12 +456,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 const uint8_t* ks = p.k + off;
                 const uint8_t* vs = p.v + off;
                 const uint32_t dst = ring_s + slot_ld * kSlot;
-                if (kMx) {
-                    const int key = key0 + (lane & 15);
-                    const bool ok = in_pool && key < len && (key >= ld_low || key < p.sinks);
-                    const uint8_t* from = (lane < 16 ? p.k : p.v) + (ok ? next_page * p.stride_page + (key0 & page_mask) * p.stride_tok + ld_exp : 0);
-                    cp_async4_or_zeros(dst + 2 * kHalf + lane * 4, from, ok);
-                }
+                const uint8_t* es = (lane < 16 ? p.k : p.v) + (off - ld_head + ld_exp);          // 4-bit: this lane's exponents
                 if (in_pool && key0 + kSubKeys <= len && (key0 >= ld_low || key0 + kSubKeys <= p.sinks)) {
 #pragma unroll
                     for (int i = 0; i < kSteps; ++i) {
@@ -463,6 +466,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                         ks += step_bytes;
                         vs += step_bytes;
                     }
+                    if (kMx) cp_async4(dst + 2 * kHalf + lane * 4, es);
                 } else {                                   // some keys have no slot, or nobody sees them: zeros
 #pragma unroll
                     for (int i = 0; i < kSteps; ++i) {
@@ -471,6 +475,11 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                         const bool ok = in_pool && key < len && (key >= ld_low || key < p.sinks);
                         cp_async16_or_zeros(d, ok ? ks + i * step_bytes : p.k, ok);
                         cp_async16_or_zeros(d + kHalf, ok ? vs + i * step_bytes : p.v, ok);
+                    }
+                    if (kMx) {
+                        const int key = key0 + (lane & 15);
+                        const bool ok = in_pool && key < len && (key >= ld_low || key < p.sinks);
+                        cp_async4_or_zeros(dst + 2 * kHalf + lane * 4, ok ? es : p.k, ok);
                     }
                 }
             }
@@ -588,18 +597,22 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 qf[NT > 1 ? 1 : 0][ks][1] = r4[3];
             }
         }
-        // S^T += K Q^T of one step of 16 dims
-        auto score_step = [&](float (&sc)[NT][4], const uint32_t (&a)[4], int ks) {
+        // S^T += K Q^T of one step of 16 dims; first: S^T =
+        auto score_step = [&](float (&sc)[NT][4], const uint32_t (&a)[4], int ks, bool first = false) __attribute__((always_inline)) {
+            auto product = [&](float (&d)[4], uint32_t b0, uint32_t b1) {
+                if (first) mma16816_first(d, a, b0, b1);
+                else mma16816<kFp8 || kMx>(d, a, b0, b1);
+            };
             if (kQRegs) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma16816<kFp8 || kMx>(sc[nt], a, qf[kQRegs ? nt : 0][kQRegs ? ks : 0][0], qf[kQRegs ? nt : 0][kQRegs ? ks : 0][1]);
+                for (int nt = 0; nt < NT; ++nt) product(sc[nt], qf[kQRegs ? nt : 0][kQRegs ? ks : 0][0], qf[kQRegs ? nt : 0][kQRegs ? ks : 0][1]);
             } else {
 #pragma unroll
                 for (int nt = 0; nt < NT; nt += 2) {
                     uint32_t r4[4];
                     ldsm4(r4, (q_lane + nt * 8 * 256) ^ (ks << 5));
-                    mma16816<kFp8 || kMx>(sc[nt], a, r4[0], r4[1]);
-                    mma16816<kFp8 || kMx>(sc[nt + 1 < NT ? nt + 1 : nt], a, r4[2], r4[3]);
+                    product(sc[nt], r4[0], r4[1]);
+                    product(sc[nt + 1 < NT ? nt + 1 : nt], r4[2], r4[3]);
                 }
             }
         };
@@ -726,9 +739,12 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 else {
                     const uint32_t add = (uint32_t)v_up * 0x00800080u;
 #pragma unroll
-                    for (int blk = 0; blk < 4; ++blk) {
-                        v_mul[blk][0] = __byte_perm(__byte_perm(va.x, va.y, blk | (4 + blk) << 4), 0, 0x4140) * 128u + add;
-                        v_mul[blk][1] = __byte_perm(__byte_perm(vb.x, vb.y, blk | (4 + blk) << 4), 0, 0x4140) * 128u + add;
+                    for (int blk = 0; blk < 4; blk += 2) {
+                        const uint32_t a = __byte_perm(va.x, va.y, blk * 0x1111 + 0x5140), b = __byte_perm(vb.x, vb.y, blk * 0x1111 + 0x5140);
+                        v_mul[blk][0] = __byte_perm(a, 0, 0x4140) * 128u + add;
+                        v_mul[blk][1] = __byte_perm(b, 0, 0x4140) * 128u + add;
+                        v_mul[blk + 1][0] = __byte_perm(a, 0, 0x4342) * 128u + add;
+                        v_mul[blk + 1][1] = __byte_perm(b, 0, 0x4342) * 128u + add;
                     }
                 }
                 const uint32_t ea = lds32(et + g * 4), eb = lds32(et + 32 + g * 4);          // keys g, g + 8
@@ -743,11 +759,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                         widen8(r4[2 * half], a[0], a[2], b[0], b[2]);
                         widen8(r4[2 * half + 1], a[1], a[3], b[1], b[3]);
                         float part[NT][4];
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) part[nt][j] = 0.f;
-                        score_step(part, a, 2 * (blk + half));
+                        score_step(part, a, 2 * (blk + half), true);
                         score_step(part, b, 2 * (blk + half) + 1);
                         const float fa = __uint_as_float(__byte_perm(ua, 0, (blk + half) << 12 | 0x444) >> 1);
                         const float fb = __uint_as_float(__byte_perm(ub, 0, (blk + half) << 12 | 0x444) >> 1);

@@ -355,44 +355,35 @@ __device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c
                     }
                 }
             } else {
-                constexpr int kItems = 512 / 32 / kConvWarps;
-                // item (a block): key item / 32 * 8 + item % 8, block item / 8 % 4
+                // a step is 8 keys x 4 blocks
                 const int k7 = lane & 7, x = lane >> 3;
-                uint4 q[kItems];
-                uint32_t word[kItems];
-#pragma unroll
-                for (int i = 0; i < kItems; ++i) {
-                    const int key = (i * kConvWarps + cw) * 8 + k7;
-                    q[i] = lds128(src + key * 64 + ((x ^ (k7 >> 1)) << 4));
-                    word[i] = lds32(src + exp_byte + key * 16);
-                }
-                // one factor of 2^(e - 127 + 126) while it is a bf16 number, which is a branch for all items, so that their work is interleaved; else 2^126 and 2^(e - 127)
-                bool near = true;
-#pragma unroll
-                for (int i = 0; i < kItems; ++i) {
-                    word[i] = word[i] >> (8 * x) & 255;
-                    near &= word[i] - 1 < 128u;
-                }
-                auto store = [&](int i, bool far) {
-                    const int key = (i * kConvWarps + cw) * 8 + k7;
-                    const uint32_t e = word[i], codes[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
-                    const uint32_t row = tile + (x >> 1) * kHalfBytes + key * 128;
-                    const uint32_t f = far ? 0x7e807e80u : (e + 126) * 0x00800080u;
-                    const uint32_t f2 = e == 0 ? 0x00400040u : (e == 255 ? 0x7fc07fc0u : e * 0x00800080u);
-#pragma unroll
-                    for (int n4 = 0; n4 < 4; ++n4) {
-                        uint4 o = make_uint4(mul_bf16x2(small_bf16<0>(codes[n4]), f), mul_bf16x2(small_bf16<1>(codes[n4]), f),
-                                             mul_bf16x2(small_bf16<2>(codes[n4]), f), mul_bf16x2(small_bf16<3>(codes[n4]), f));
-                        if (far) o = make_uint4(mul_bf16x2(o.x, f2), mul_bf16x2(o.y, f2), mul_bf16x2(o.z, f2), mul_bf16x2(o.w, f2));
-                        sts128(row + (((4 * x + n4 & 7) ^ k7) << 4), o);
+                uint32_t from = src + (cw * 8 + k7) * 64 + ((x ^ (k7 >> 1)) << 4), e_from = src + exp_byte + (cw * 8 + k7) * 16;
+                uint32_t row = tile + (x >> 1) * kHalfBytes + (cw * 8 + k7) * 128;
+                uint4 q = lds128(from);
+                uint32_t word = lds32(e_from);
+#pragma unroll 1
+                for (int i = cw; i < 16; i += kConvWarps) {
+                    const uint32_t codes[4] = {q.x, q.y, q.z, q.w}, e = word >> (8 * x) & 255;
+                    if (i + kConvWarps < 16) {
+                        q = lds128(from += kConvWarps * 8 * 64);
+                        word = lds32(e_from += kConvWarps * 8 * 16);
                     }
-                };
-                if (__all_sync(0xffffffffu, near)) {
+                    // one factor of 2^(e - 127 + 126) while it is a bf16 number, else 2^126 and 2^(e - 127)
+                    const bool near = __all_sync(0xffffffffu, e - 1 < 128u);
+                    const uint32_t f = near ? (e + 126) * 0x00800080u : 0x7e807e80u;
+                    uint4 o[4];
 #pragma unroll
-                    for (int i = 0; i < kItems; ++i) store(i, false);
-                } else {
+                    for (int n4 = 0; n4 < 4; ++n4)
+                        o[n4] = make_uint4(mul_bf16x2(small_bf16<0>(codes[n4]), f), mul_bf16x2(small_bf16<1>(codes[n4]), f),
+                                           mul_bf16x2(small_bf16<2>(codes[n4]), f), mul_bf16x2(small_bf16<3>(codes[n4]), f));
+                    if (!near) {
+                        const uint32_t f2 = e == 0 ? 0x00400040u : (e == 255 ? 0x7fc07fc0u : e * 0x00800080u);
 #pragma unroll
-                    for (int i = 0; i < kItems; ++i) store(i, true);
+                        for (int n4 = 0; n4 < 4; ++n4) o[n4] = make_uint4(mul_bf16x2(o[n4].x, f2), mul_bf16x2(o[n4].y, f2), mul_bf16x2(o[n4].z, f2), mul_bf16x2(o[n4].w, f2));
+                    }
+#pragma unroll
+                    for (int n4 = 0; n4 < 4; ++n4) sts128(row + (((4 * x + n4 & 7) ^ k7) << 4), o[n4]);
+                    row += kConvWarps * 8 * 128;
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // the tensor cores read what these lanes wrote

@@ -330,29 +330,34 @@ __device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c
             const uint32_t src = c.smem + W::kRawAt + raw.slot * W::kRawBytes;
             const uint32_t tile = c.smem + W::kKV + (is_v ? W::kStagesK + vr.slot : kr.slot) * kTileBytes;
             if (kKind == kE4m3) {
-                constexpr int kItems = 1024 / 32 / kConvWarps;
-                // item (16 codes): key (item / 64) * 8 + item % 8, chunk item / 8 % 8
-                const int k7 = lane & 7, x0 = lane >> 3;
-#pragma unroll
-                for (int i0 = 0; i0 < kItems; i0 += 4) {
-                    uint4 q[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int item = (i0 + i) * kConvWarps + cw, key = (item >> 1) * 8 + k7, x = (item & 1) * 4 + x0;
-                        q[i] = lds128(src + key * 128 + ((x ^ k7) << 4));
+                // a step is 8 keys x all 8 chunks of 16 codes, two a lane
+                const int k7 = lane & 7, x = lane >> 3;
+                const uint32_t in0 = ((x ^ k7) << 4), in1 = (((x + 4) ^ k7) << 4), out0 = (((2 * x & 7) ^ k7) << 4), out1 = (((2 * x + 1 & 7) ^ k7) << 4);
+                uint32_t from = src + (cw * 8 + k7) * 128, row = tile + (cw * 8 + k7) * 128;
+                uint4 q0 = lds128(from + in0), q1 = lds128(from + in1);
+#pragma unroll 1
+                for (int i = cw; i < 16; i += kConvWarps) {
+                    const uint4 a = q0, b = q1;
+                    if (i + kConvWarps < 16) {
+                        from += kConvWarps * 8 * 128;
+                        q0 = lds128(from + in0);
+                        q1 = lds128(from + in1);
                     }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int item = (i0 + i) * kConvWarps + cw, key = (item >> 1) * 8 + k7, x = (item & 1) * 4 + x0;
-                        uint4 a, b;
-                        widen4(q[i].x, a.x, a.y);
-                        widen4(q[i].y, a.z, a.w);
-                        widen4(q[i].z, b.x, b.y);
-                        widen4(q[i].w, b.z, b.w);
-                        const uint32_t row = tile + (x >> 2) * kHalfBytes + key * 128;
-                        sts128(row + (((2 * x & 7) ^ k7) << 4), a);
-                        sts128(row + (((2 * x + 1 & 7) ^ k7) << 4), b);
-                    }
+                    // chunks 0 to 3 are the first 64 dims
+                    uint4 lo, hi;
+                    widen4(a.x, lo.x, lo.y);
+                    widen4(a.y, lo.z, lo.w);
+                    widen4(a.z, hi.x, hi.y);
+                    widen4(a.w, hi.z, hi.w);
+                    sts128(row + out0, lo);
+                    sts128(row + out1, hi);
+                    widen4(b.x, lo.x, lo.y);
+                    widen4(b.y, lo.z, lo.w);
+                    widen4(b.z, hi.x, hi.y);
+                    widen4(b.w, hi.z, hi.w);
+                    sts128(row + kHalfBytes + out0, lo);
+                    sts128(row + kHalfBytes + out1, hi);
+                    row += kConvWarps * 8 * 128;
                 }
             } else {
                 // a step is 8 keys x 4 blocks

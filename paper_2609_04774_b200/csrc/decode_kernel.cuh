@@ -1163,8 +1163,20 @@ template <int HP, Kind kKind, Mode kMode>
 int launch_rows(cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char* who) {
     const int blocks = row_blocks(p.rows);
     if (blocks == 1) return launch_decode<1, HP, kKind, kMode>(ctx, p, s, who);
-    if (blocks == 2) return launch_decode<2, HP, kKind, kMode>(ctx, p, s, who);
-    return launch_decode<4, HP, kKind, kMode>(ctx, p, s, who);
+    // bf16 and 4-bit trees of more than 16 rows take the tensor cores' form
+    if constexpr (kMode != kTree || kKind == kE4m3)
+        if (blocks == 4) return launch_decode<4, HP, kKind, kMode>(ctx, p, s, who);
+    return launch_decode<2, HP, kKind, kMode>(ctx, p, s, who);
+}
+// 4-bit rows are 64 bytes a head: four heads together read 256 contiguous bytes a token, two 128 (128 requests of 4000 keys: 202 us with four heads, 239 with two,
+// 342 with one).  But the more heads a unit has, the more pieces its key axis is cut into when there are few units, and all are joined: one request of
+// 4000 keys 20 us with four heads, 14 with two, 12 with one; 32000 keys 31, 25, 23; four of 4000 22, 17, 16, of 32000 62, 67, 78.  So with few keys,
+// as far as the page table's width tells, each head is by itself.
+template <Mode kMode>
+int launch_mx4(cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char* who) {
+    const bool few = (int64_t)p.B * p.Hkv * std::min(p.capacity, 1 << 15) <= 1 << 18;
+    if (few || p.Hkv % 2 != 0) return launch_rows<1, kMx4, kMode>(ctx, p, s, who);
+    return p.Hkv % 4 == 0 ? launch_rows<4, kMx4, kMode>(ctx, p, s, who) : launch_rows<2, kMx4, kMode>(ctx, p, s, who);
 }
 
 // A cache of any kind; strides in bytes.

@@ -4,8 +4,7 @@
 namespace {
 
 int decode_attn_mx4(cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char* who) {
-    if (p.Hkv % 4 == 0) return p.n_q > 1 ? launch_rows<4, kMx4, kChain>(ctx, p, s, who) : launch_rows<4, kMx4, kToken>(ctx, p, s, who);
-    return p.n_q > 1 ? launch_rows<1, kMx4, kChain>(ctx, p, s, who) : launch_rows<1, kMx4, kToken>(ctx, p, s, who);
+    return p.n_q > 1 ? launch_mx4<kChain>(ctx, p, s, who) : launch_mx4<kToken>(ctx, p, s, who);
 }
 
 // ---------------------------------------------------------------------------------------------- gather

@@ -80,7 +80,7 @@ int tree_attn(cp_ctx* ctx, const void* q, const Cache* cache, const int32_t* pag
     if (p.rows > kNarrowRows[kind]) return launch_tree_wide(ctx, kind, &p, &view, workspace, stream, who);
     if (kind == kBf16) return launch_rows<1, kBf16, kTree>(ctx, p, s, who);
     if (kind == kE4m3) return p.Hkv % 2 == 0 ? launch_rows<2, kE4m3, kTree>(ctx, p, s, who) : launch_rows<1, kE4m3, kTree>(ctx, p, s, who);
-    return p.Hkv % 4 == 0 ? launch_rows<4, kMx4, kTree>(ctx, p, s, who) : launch_rows<1, kMx4, kTree>(ctx, p, s, who);
+    return launch_mx4<kTree>(ctx, p, s, who);
 }
 
 }  // namespace

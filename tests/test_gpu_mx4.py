@@ -256,8 +256,16 @@ LENS = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 127, 128, 129, 300, 1000, 2049]
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
 @pytest.mark.parametrize("n_q", [1, 3])
 @pytest.mark.parametrize("Hq,Hkv", [(8, 4), (8, 2)])
-def test_decode_lengths(ctx, page, n_q, Hq, Hkv):
-    Decode(page + n_q, LENS, Hq, Hkv, page, n_q=n_q).check(ctx)
+@pytest.mark.parametrize("width", [None, 160])
+def test_decode_lengths(ctx, page, n_q, Hq, Hkv, width):
+    """Wide tables: units of several heads; narrow ones: of one."""
+    Decode(page + n_q, LENS, Hq, Hkv, page, n_q=n_q, width=width).check(ctx)
+
+
+@pytest.mark.parametrize("Hq,Hkv,n_q", [(8, 8, 1), (16, 8, 3), (40, 8, 3), (64, 8, 8), (12, 6, 2), (24, 2, 1), (24, 2, 3), (28, 4, 4)])
+@pytest.mark.parametrize("width", [None, 100])
+def test_decode_units_of_heads(ctx, Hq, Hkv, n_q, width):
+    Decode(Hq + n_q, [5, 700, 0, 1300, 64, 9], Hq, Hkv, 16, n_q=n_q, width=width).check(ctx)
 
 
 @pytest.mark.parametrize("Hq,Hkv,n_q", [(1, 1, 1), (8, 8, 1), (7, 1, 1), (9, 1, 1), (16, 1, 1), (17, 1, 1), (33, 1, 1), (64, 8, 4), (128, 4, 1), (128, 4, 2), (5, 5, 7), (12, 4, 5),
@@ -286,11 +294,11 @@ def test_decode_many(ctx):
 
 
 @pytest.mark.parametrize("n_q", [1, 3])
-@pytest.mark.parametrize("Hkv", [2, 4])
+@pytest.mark.parametrize("Hkv", [2, 4, 6])
 def test_decode_of_all_magnitudes(ctx, n_q, Hkv):
     """V with exponents from 0 to 253 and K with a few large and tiny blocks: the weights' common factor has to follow, in single tiles and over several."""
     for seed, lo, hi in ((0, 0, 20), (1, 100, 140), (2, 120, 200), (3, 200, 250), (4, 60, 180)):
-        s = Decode(seed, [500, 37, 3000], 8, Hkv, 32, n_q=n_q)
+        s = Decode(seed, [500, 37, 3000], 2 * Hkv if Hkv > 4 else 8, Hkv, 32, n_q=n_q)
         g = generator(seed + 50)
         e = s.kv.v[..., Hkv * 64:Hkv * 68]
         e.copy_(torch.where(e == 255, 255, torch.randint(lo, hi + 1, e.shape, generator=g, device="cuda")).to(torch.uint8))
@@ -307,10 +315,10 @@ def test_decode_of_all_magnitudes(ctx, n_q, Hkv):
 
 
 @pytest.mark.parametrize("n_q", [1, 4])
-@pytest.mark.parametrize("Hkv", [2, 4])
+@pytest.mark.parametrize("Hkv", [2, 4, 6, 8])
 def test_decode_of_nan_blocks(ctx, n_q, Hkv):
     """A NaN block of V reaches its 32 elements of the rows that see the key, one of K whole rows; also beside large exponents."""
-    s = Decode(7, [200, 500], 8, Hkv, 16, n_q=n_q)
+    s = Decode(7, [200, 500], 2 * Hkv if Hkv > 4 else 8, Hkv, 16, n_q=n_q)
     for b, t, which, byte in ((0, 199, "v", 2), (0, 198, "v", 7), (1, 40, "v", 1), (1, 499, "k", 5), (0, 150, "v", 4)):
         page, at = s.kv.where(b, torch.tensor(t, device="cuda"))
         getattr(s.kv, which)[page, at, Hkv * 64 + byte] = 255

@@ -40,6 +40,13 @@ def test_heads_and_rows(ctx, kind, Hq, Hkv, n_q):
     TreeStep(Hq + n_q, [5, 700, 131], trees(n_q, sizes), Hq, Hkv, 32, kind, n_q=n_q).check(ctx)
 
 
+@pytest.mark.parametrize("Hq,Hkv,n_q", [(8, 8, 1), (8, 8, 8), (8, 8, 16), (8, 4, 8), (12, 6, 5), (16, 2, 2), (16, 8, 5)])
+@pytest.mark.parametrize("width", [None, 100])
+def test_4_bit_units_of_heads(ctx, Hq, Hkv, n_q, width):
+    sizes = [n_q, max(1, n_q // 2), n_q, 1, n_q]
+    TreeStep(Hq + n_q, [5, 700, 131, 0, 1100], trees(n_q, sizes), Hq, Hkv, 16, "mx4", n_q=n_q, width=width).check(ctx, 300, 3)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("Hq", [4, 16])
 @pytest.mark.parametrize("window", [1, 2, 5, 16, 63, 64, 100, 128, 129, 500])

@@ -50,7 +50,8 @@ class Cache:
         g = generator(seed)
         self.lens, self.page, self.Hkv, self.kind = list(lens), page, Hkv, kind
         counts = [-(-n // page) for n in lens]
-        width = width or max(1, max(counts))
+        # 4-bit kernels take several heads a unit unless the table is narrow: with an even number of heads it is wide here, by default
+        width = width or max(1, max(counts), 65536 // page if kind == "mx4" and Hkv % 2 == 0 else 0)
         pool = sum(counts) + spare
         ids = torch.randperm(pool, generator=g, device="cuda").to(torch.int32)
         self.table = torch.full((len(lens), width), -1, dtype=torch.int32, device="cuda")

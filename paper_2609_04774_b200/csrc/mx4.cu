@@ -43,17 +43,20 @@ gather_mx4_kernel(const __grid_constant__ GatherParams p) {
     const uint8_t* cache = p.cache[which];
     uint4* rows = p.rows[which];
     const int64_t step = (int64_t)gridDim.x * kGatherThreads * kGatherItems;
-    const int per_token = p.Hkv * 16;
+    const uint32_t per_token = p.Hkv * 16;
     for (int64_t base = (int64_t)blockIdx.x * kGatherThreads * kGatherItems; base < p.items; base += step) {
         uint32_t codes[kGatherItems], e[kGatherItems];
         bool ok[kGatherItems];
+        const int64_t token0 = base / per_token;           // one division in 64 bits, then offsets
+        const uint32_t rest = (uint32_t)(base - token0 * per_token);
 #pragma unroll
         for (int i = 0; i < kGatherItems; ++i) {
             const int64_t at = base + i * kGatherThreads + threadIdx.x;
             ok[i] = at < p.items;
             if (!ok[i]) continue;
-            const int64_t token = at / per_token, t = p.t_begin + token;
-            const int vec = (int)(at - token * per_token);                // head * 16 + eighth of the codes' bytes
+            const uint32_t off = rest + i * kGatherThreads + threadIdx.x, tokens = off / per_token;
+            const int64_t t = p.t_begin + token0 + tokens;
+            const uint32_t vec = off - tokens * per_token;                // head * 16 + eighth of the codes' bytes
             const int64_t entry = t >> p.page_shift;
             const int32_t page = __ldg(p.table + entry);
             ok[i] = page >= 0 && page < p.num_pages;

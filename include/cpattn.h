@@ -479,10 +479,10 @@ int cp_decode_attn_fp8(cp_ctx* ctx, const void* q, const cp_kv_cache_fp8* cache,
  *   cp_rope_append_mx4  cp_rope_append into such a cache.  k (rotated) and v are quantised block by block: e = floor(log2(largest magnitude))
  *            - 2 + 127 (at least 0), codes to the nearest, ties to the even code, saturating at 6.  A block with an infinity or a NaN becomes
  *            NaN.  The codes are those of the exactly rotated values: where the fp32 rotation does not decide, it is redone in fp64.
- *   cp_kv_gather_mx4    the values of n logical tokens from t_begin as bf16 rows [n, Hkv, D] (exact up to e = 251; larger ones may overflow), what the
+ *   cp_kv_gather_mx4    the values of n logical tokens from t_begin as bf16 rows [n, Hkv, D] (exact up to e = 252, the largest that the append writes), what the
  *            prefill calls read: rows of whole pages are a cp_kv_cache with table 0, 1, 2, ..  Page ids as in cp_kv_gather.
  *   cp_decode_attn_mx4  cp_decode_attn over such a cache, same arguments, workspace and limits.  Weights are rounded to bf16, K and V are taken exactly
- *            (e up to 253), the queries lose what is below 2^-24 of a row's largest element.
+ *            (e up to 252), the queries lose what is below 2^-24 of a row's largest element.
  * Errors as in the calls they are forms of. */
 typedef struct {
     const void* k;          /* device */
@@ -517,12 +517,13 @@ int cp_decode_attn_mx4(cp_ctx* ctx, const void* q, const cp_kv_cache_mx4* cache,
  *            window or the sinks hold, by their positions.  The masks may be any bits (bits from tree_len on are
  *            ignored); the position of a token is base + (bits of its mask) - 1.  Rows behind the tree: zeros, lse = -inf.  A tree_len outside
  *            [0, min(n_q, kv_len[b])] is reported {code, b, block, tree_len} and counts as the nearest in it.  Workspace: cp_workspace_bytes_tree; limits,
- *            layouts and the rest as in cp_decode_attn[_fp8|_mx4].
+ *            layouts, roundings and the rest as in cp_decode_attn[_fp8|_mx4].  Beyond n_q * Hq / Hkv = 16 rows (E4M3: 32) magnitudes of V
+ *            reach 2^118 (a weight may be 2^8 for a while), and 4-bit caches take the queries exactly.
  *   cp_tree_commit   accepted [B]: the last drafted token that sequence b keeps (-1: none).  It and its ancestors n_0 < n_1 < .. become the sequence's next
  *            tokens: what slot base + n_i holds moves to slot base + i, K and V, in every layer of the pool; kv_len[b] = base + their number;
  *            path [B, n_q] receives n_0, n_1, .., then -1.  The table keeps its pages (as with a length that the caller lowers, see extend;
  *            the drafts must not lie in pages shared with a fork).  An accepted outside [-1, tree_len) is reported {code, b, block, accepted}
- *            and counts as -1; a token whose slot has no page of the pool is reported {code, table entry, block, id} and not moved.
+ *            and counts as -1; a token whose slot has no page of the pool is reported {code, table entry, block, id} and not moved.  B <= 65535.
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA. */
 int cp_tree_plan(cp_ctx* ctx, const int32_t* parent, const int32_t* tree_len, const int32_t* kv_len, int32_t B, int32_t n_q, int32_t n_axes,
                  uint64_t* mask, int32_t* positions, int32_t* token_seq, int32_t* token_slot, void* stream);
@@ -538,8 +539,8 @@ int cp_tree_attn_mx4(cp_ctx* ctx, const void* q, const cp_kv_cache_mx4* cache, c
                      int64_t sinks, float scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The care of the pages.  A pool is n_layers K and V caches of one geometry (layer l: k[l], v[l]; strides in BYTES, multiples of
- * 16; row_bytes = bytes of one head's row: 256 bf16, 128 E4M3; 4-bit rows are Hkv = 16-byte pieces of a token's row, row_bytes = 16, stride_head = 16) whose pages share one numbering, and refcount [num_pages] int32 on
- * the device: how many table entries name a page; 0 = free.  k and v are host arrays of device pointers, read before the call
+ * 16; row_bytes = bytes of one head's row: 256 bf16, 128 E4M3; 4-bit pools: row_bytes = 16, stride_head = 16 and Hkv = the 16-byte pieces of a
+ * token's row) whose pages share one numbering, and refcount [num_pages] int32 on the device: how many table entries name a page; 0 = free.  k and v are host arrays of device pointers, read before the call
  * returns; extend, evict and free look at num_pages and page_size only.  Pages are handed out lowest free id first, to the rows
  * in order.  cp_workspace_bytes_pages: workspace of the calls that take one, for n forks or copies (0 elsewhere); a workspace
  * belongs to one call at a time.  What cannot be done is skipped and reported as CP_ERR_BOUNDS by cp_ctx_poll_status.

@@ -10,8 +10,8 @@ from tests.serving_util import D, e4m3_codes, generator, normal
 
 FULL = binding.CP_NO_WINDOW
 MAGNITUDES = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64)
-# a softmax weight's rounding: bf16 for bf16 and 4-bit caches, fp16 for E4M3 ones (2^-16 more: weights below 2^-14 of the largest are subnormals); the wide
-# form has bf16 weights for all
+# a softmax weight's rounding: bf16 for bf16 and 4-bit caches, fp16 for E4M3 ones (2^-16 more: weights below 2^-14 of the largest are subnormals; with many
+# rows, where a weight's reference may be 2^8 off, the bound of bf16 is used)
 WEIGHT_EPS = {"bf16": 2.0 ** -8, "mx4": 2.0 ** -8, "fp8": 2.0 ** -11 + 2.0 ** -16}
 
 

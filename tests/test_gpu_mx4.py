@@ -198,10 +198,10 @@ def test_gather(ctx, Hkv, page, t_begin, n):
 
 
 def test_gather_of_every_code_and_exponent(ctx):
-    """All 16 codes with exponents 0..251 exactly (2^-128 .. 6 * 2^124), 255 as NaN; one of the pair alone; entries outside the pool."""
+    """All 16 codes with exponents 0..252 exactly (2^-128 .. 6 * 2^125), 255 as NaN; one of the pair alone; entries outside the pool."""
     rows = torch.zeros(16, 16, 80, dtype=torch.uint8, device="cuda")
     e = torch.arange(256, device="cuda", dtype=torch.uint8).view(16, 16)
-    e = torch.where(e > 251, 255, e.int()).to(torch.uint8)
+    e = torch.where(e > 252, 255, e.int()).to(torch.uint8)
     rows[..., :64] = (torch.arange(64, device="cuda") * 37 + 16 * (torch.arange(64, device="cuda") % 16)).to(torch.uint8)
     rows[..., 64:68] = e[..., None]
     cache = binding.make_cache_mx4(rows, rows, 1)
@@ -219,7 +219,7 @@ def test_gather_of_every_code_and_exponent(ctx):
         with pytest.raises(binding.CpError) as err:
             ctx.poll_status()
         assert err.value.code == binding.CP_ERR_BOUNDS
-        assert bool((k[48:64] == 7).all()) and torch.equal(k[64:252].double(), want[64:252]) and torch.equal(k[:48].double(), want[:48])
+        assert bool((k[48:64] == 7).all()) and torch.equal(k[64:253].double(), want[64:253]) and torch.equal(k[:48].double(), want[:48])
 
 
 # ---------------------------------------------------------------------------------------------------------------------- decode

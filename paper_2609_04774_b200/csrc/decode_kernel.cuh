@@ -243,6 +243,7 @@ __device__ __forceinline__ Request request_of(const DecodeParams& p, int b) {
     r.sink_tiles = p.sinks / kTile + (p.sinks % kTile != 0);
     r.skip = max(0, max(low, 0) / kTile - r.sink_tiles);   // tiles between sinks and window
     r.n = max(1, (r.len + kTile - 1) / kTile - r.skip);
+    if (kTree && r.base == r.len) r.n = 1;                 // no drafts: rows of zeros
     return r;
 }
 // A position in the list: request, unit (KV head major, then row group), tile.  On the axis that is cut into equal runs a unit

@@ -52,10 +52,10 @@ tree_plan_kernel(const int32_t* parent, const int32_t* tree_len, const int32_t* 
     token_slot[at] = t < m ? base + t : 0;
 }
 
-// Rows per KV head up to which the narrow form is taken.  It is faster up to 16 rows for every kind (37 requests of 4096 keys at 8 rows: bf16 95 us against 102, E4M3 65
-// against 112, 4-bit 75 against 145).  Its 32-row form costs a warp more than a tile's loads for 4-bit rows (24 rows 165 us against 148) and somewhat for bf16
-// (111 against 105, with 700 keys 39 against 32); E4M3 stays ahead with it (97 against 115).  Behind 32 rows it reads the keys again (48 rows: 209 / 183 / 265
-// us against 107 / 120 / 152).
+// Rows per KV head up to which the narrow form is taken.  It is faster up to 16 rows for every kind (37 requests of 4096 keys, 16 rows: bf16 99 us against 104,
+// E4M3 66 against 110, 4-bit 103 against 121; of 700 keys 27 / 31, 23 / 35, 30 / 37; one of 4096 13 / 17, 18 / 20, 15 / 20).  Its 32-row form costs more than the
+// loads of a tile for 4-bit rows (24 rows of 4096 keys 165 us against 121) and somewhat for bf16 (110 against 104); E4M3 stays ahead with it (97 against 110).
+// Behind 32 rows it reads the keys again (48 rows: 209 / 182 / 265 us against 106 / 111 / 121).
 constexpr int kNarrowRows[3] = {16, 32, 16};
 constexpr int kLeastNarrowRows = 16;               // a workspace serves every kind
 

@@ -257,3 +257,26 @@ def test_scales(ctx, Hq, scale):
     # |q k| scale adds up to at most about 130 * scale for normal inputs (128 products of mean magnitude 0.64, with margin), so 128 * 2^-23 of that
     err = 128 * 2.0 ** -23 * 130 * scale
     check_rows(s.out[0], s.lse, ref, scale, 2.0 ** -8 + 2 * err, lse_tol=2e-4 + 2 * err)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("Hq", [2, 8, 32])
+@pytest.mark.parametrize("power", [-70, -20, 40, 70])
+def test_queries_of_any_magnitude(ctx, kind, Hq, power):
+    """Queries times a power of two and a softmax scale divided by it; a zero row and one of a single element among them."""
+    s = TreeStep(6, [300, 20], trees(6, [13, 9]), Hq, 2, 64, kind, scale=D ** -0.5 * 2.0 ** -power)
+    s.q.mul_(2.0 ** power)
+    s.q[0, 3] = 0
+    s.q[0, 5, :, 1:] = 0
+    s.check(ctx)
+    s.check(ctx, 30, 2)
+
+
+@pytest.mark.parametrize("Hq", [4, 16, 64])
+def test_signs_and_zeros_of_head_scales(ctx, Hq):
+    """E4M3: scales of K that are negative or zero (all scores equal), scales of V that are negative or zero."""
+    s = TreeStep(11, [200, 0, 700], trees(3, [12, 12, 5]), Hq, 4, 16, "fp8")
+    s.kv.k_scale.copy_(torch.tensor([0.01, -0.013, 0.0, -0.0001], device="cuda"))
+    s.kv.v_scale.copy_(torch.tensor([-0.01, 0.02, 0.015, 0.0], device="cuda"))
+    s.check(ctx)
+    s.check(ctx, 50, 3)

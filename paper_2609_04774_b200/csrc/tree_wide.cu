@@ -41,10 +41,10 @@ int launch(cp_ctx* ctx, const WideParams& w, const CacheView& view, cudaStream_t
                                 "cudaFuncSetAttribute(tree)")) return rc;
         ctx->tree_attr_set[kKind][kTiles - 1] = true;
     }
-    tree_wide_kernel<kKind, kTiles><<<(unsigned)(w.runs * w.classes), W::kThreads, W::kSmem, s>>>(k, v, ke, ve, w);
+    tree_wide_kernel<kKind, kTiles><<<dim3((unsigned)w.classes, (unsigned)w.heads, (unsigned)w.runs), W::kThreads, W::kSmem, s>>>(k, v, ke, ve, w);
     if (int rc = check_cuda(cudaGetLastError(), who)) return rc;
     const unsigned y = (unsigned)((w.class_rows + kWideJoinRows - 1) / kWideJoinRows);
-    return launch_behind(tree_join_kernel<kKind>, dim3((unsigned)(w.runs * w.classes), y), 32 * kWideJoinRows, s, who, w);
+    return launch_behind(tree_join_kernel<kKind>, dim3((unsigned)(w.runs * w.classes * w.heads), y), 32 * kWideJoinRows, s, who, w);
 }
 
 }  // namespace
@@ -63,7 +63,8 @@ int launch_tree_wide(cp_ctx* ctx, int kind, const void* decode_params, const voi
     const int grid = std::min(ctx->num_sms, kMaxGrid);
     w.classes = (w.d.rows + kWideRows - 1) / kWideRows;
     w.class_rows = (w.d.rows + w.classes - 1) / w.classes;
-    w.runs = grid / w.classes;
+    w.heads = kind == kBf16 || w.classes > 1 ? 1 : (w.d.Hkv % 4 == 0 ? 4 : (w.d.Hkv % 2 == 0 ? 2 : 1));
+    w.runs = grid / (w.classes * w.heads);
     const size_t n = 2 * (size_t)kMaxGrid * kWideRows;
     w.d.part_o = static_cast<float*>(workspace);
     w.d.part_ml = w.d.part_o + n * kD;

@@ -7,8 +7,10 @@
 //   - Query row t * G + h of a KV head (token t, head h of the group) is a row of the M side.  Up to 256 rows are two 128-row score tiles that share the K/V
 //     tiles, one softmax warpgroup each.  Up to 128 rows are one, and the warpgroups take the K/V tiles in turn, each with an accumulator of its own; the
 //     two are added at the end of a unit (one warpgroup alone needs twice the time that the keys do to arrive).
-//   - More than 256 rows are several classes of equal height.  CTA c belongs to class c % classes and walks run c / classes of the key axis, so the
-//     classes read the same keys at the same time and all but one find them in L2.
+//   - More than 256 rows are several classes of equal height, whose CTAs walk the same runs of the key axis side by side: they
+//     read the same keys at the same time and all but one find them in L2.  So do the CTAs of up to four KV heads of E4M3 and 4-bit caches, whose rows of 128 and 64 bytes
+//     lie side by side (and share the exponents' 16 bytes): 64 requests with a window of 4096, 96 rows, E4M3 202 us with a head by itself, 186 with two or four;
+//     28 rows, 4-bit 217 / 209 / 208; bf16 no change.
 //   - The key axis is all (request, KV head) units one after the other, 128 keys a step, cut into equal runs, one per CTA of a class, whatever
 //     the lengths are (the scheme of the narrow form: Cursor); pieces of cut units are joined by a second launch.
 //   - Warps: two softmax warpgroups; a producer that fetches K/V tiles page by page; the issuers of S = Q K^T and of O += P V; a warp that gathers the
@@ -91,7 +93,13 @@ struct WideParams {
     DecodeParams d;
     int32_t classes;           // row classes of a KV head
     int32_t class_rows;        // rows of a class (the last may have fewer)
-    int32_t runs;              // CTAs of a class
+    int32_t heads;             // KV heads whose units are walked side by side
+    int32_t runs;              // CTAs of a class and head
+    // CTA (x, y, z): row class, head of the group, run; x counts fastest, so what reads the same tokens starts together
+    __device__ __forceinline__ int cls() const { return (int)blockIdx.x; }
+    __device__ __forceinline__ int head() const { return (int)blockIdx.y; }
+    __device__ __forceinline__ int run() const { return (int)blockIdx.z; }
+    __device__ __forceinline__ int64_t place() const { return (int64_t)(head() * classes + cls()) * runs + run(); }       // in the workspace: runs side by side
 };
 
 // The units of this CTA, one after the other: request b, KV head u, tiles [t_begin, t_end).  Every warp has a copy in shared memory that it steps by itself, which
@@ -99,12 +107,14 @@ struct WideParams {
 struct WideUnits {
     Cursor<kBlockN, true> cur;
     int64_t x1;
-    int t_begin, t_end;
+    int t_begin, t_end, heads;
     bool whole, valid;
     // by one lane
-    __device__ __forceinline__ void begin(const DecodeParams& p, const int32_t* start, int64_t x0, int64_t end) {
+    __device__ __forceinline__ void begin(const WideParams& w, const int32_t* start, int64_t x0, int64_t end) {
+        const DecodeParams& p = w.d;
+        heads = w.heads;
         cur.b = start[0];
-        cur.u = start[1];
+        cur.u = start[1] * heads + w.head();
         cur.t = max(0, start[2] - kWideCost);
         cur.x = x0 - start[2];
         cur.r = request_of<kBlockN, true>(p, cur.b);
@@ -123,8 +133,9 @@ struct WideUnits {
         if ((threadIdx.x & 31) == 0) {
             cur.t = 0;
             cur.x += kWideCost + cur.r.n;
-            if (++cur.u == p.Hkv) {
-                cur.u = 0;
+            cur.u += heads;
+            if (cur.u >= p.Hkv) {
+                cur.u -= p.Hkv;
                 if (++cur.b < p.B) cur.r = request_of<kBlockN, true>(p, cur.b);
             }
             span();
@@ -153,7 +164,7 @@ struct WideCtx {
 // 8192 4-bit keys of 37 requests, 64 rows 275 us, 255 like this).
 template <int kTiles>
 __device__ __forceinline__ int wide_warps(const WideParams& w, int wg) {
-    const int rows = min(w.class_rows, w.d.rows - (int)(blockIdx.x % w.classes) * w.class_rows) - (kTiles == 2 ? wg * kBlockM : 0);
+    const int rows = min(w.class_rows, w.d.rows - w.cls() * w.class_rows) - (kTiles == 2 ? wg * kBlockM : 0);
     return min(max((rows + 31) >> 5, 1), 4);
 }
 // A position in a ring: slot, and the parity of the phase that ends when it is filled (for the side that fills: when it was emptied).
@@ -258,7 +269,7 @@ __device__ __forceinline__ void wide_convert(const WideParams& w, const WideCtx&
     constexpr int kBatch = 4;                              // steps that go together
     const DecodeParams& p = w.d;
     const int lane = threadIdx.x & 31, chunk = lane & 15, sub = lane >> 4;
-    const int rows = min(w.class_rows, p.rows - (int)(blockIdx.x % w.classes) * w.class_rows);
+    const int rows = min(w.class_rows, p.rows - w.cls() * w.class_rows);
     const float sign = kKind == kE4m3 ? p.k_scale[units.cur.u] : 1.f;
     c.wait(kWQRaw, round & 1, round);
     __syncwarp();
@@ -414,7 +425,7 @@ __device__ __forceinline__ void wide_queries(const WideParams& w, const WideCtx&
     using W = Wide<kKind, kTiles>;
     const DecodeParams& p = w.d;
     const int lane = threadIdx.x & 31, chunk = lane & 15, sub = lane >> 4;
-    const int r0 = (int)(blockIdx.x % w.classes) * w.class_rows, rows = min(w.class_rows, p.rows - r0);
+    const int r0 = w.cls() * w.class_rows, rows = min(w.class_rows, p.rows - r0);
     auto place = [&](int i) { return wide_place(c.smem + W::kQ, i, chunk); };
     for (int i = sub; i < kTiles * kBlockM; i += 2)        // rows behind the class's last stay zeros
         if (i >= rows) sts128(place(i), make_uint4(0, 0, 0, 0));
@@ -728,7 +739,7 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
     const int lane = threadIdx.x & 31, warp_in_wg = threadIdx.x >> 5 & 3;
     const uint32_t lane_addr = (uint32_t)(warp_in_wg * 32) << 16;
     const uint32_t s_tmem = cx.tmem + lane_addr + kWTmemS, p_tmem = cx.tmem + lane_addr + kWTmemP + wg * 64, o_tmem = cx.tmem + lane_addr + kWTmemO + wg * 128;
-    const int cls = (int)(blockIdx.x % w.classes), run = (int)(blockIdx.x / w.classes);
+    const int cls = w.cls(), run = w.run();
     constexpr bool turns = W::kTurns;
     const int tile_row = warp_in_wg * 32 + lane, row = (turns ? 0 : wg * kBlockM) + tile_row;      // of the class
     const int r = cls * w.class_rows + row, t = r / p.G;                  // of the KV head; its token
@@ -828,7 +839,7 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
         const float inv = !whole ? 1.f : (l == 0.f ? 0.f : (kF16 ? p.v_scale[u] : 1.f) / l);
         f0 *= inv;
         f1 *= inv;
-        const int64_t slot = 2 * ((int64_t)cls * w.runs + run) + (j0 > 0 ? 0 : 1);
+        const int64_t slot = 2 * w.place() + (j0 > 0 ? 0 : 1);
         const int head = u * p.G + r - t * p.G;
         // offset of this row in the destination, -1: none
         const int64_t at = !in_class ? -1 : (whole ? (((int64_t)b * p.n_q + t) * p.Hq + head) * kD : (slot * kWideRows + row) * kD);
@@ -907,7 +918,7 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
             int64_t last = min((x_end * ctas - 1) / total, (int64_t)ctas - 1);
             while (run_begin(total, last, ctas) >= x_end) --last;
             while (run_begin(total, last + 1, ctas) < x_end) ++last;
-            int32_t* meta = p.meta + ((int64_t)cls * w.runs + run) * 4;
+            int32_t* meta = p.meta + w.place() * 4;
             meta[0] = b;
             meta[1] = u;
             meta[2] = (int32_t)(last - run + 1);
@@ -933,7 +944,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     c.abort_flag = reinterpret_cast<volatile uint32_t*>(c.gen + W::kAbort);
     c.status = p.status;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int run = (int)(blockIdx.x / w.classes);
+    const int run = w.run();
     if (tid == 0) {
         mbar_init(c.bars + kWQFull * 8, W::kRawTiles ? kConvWarps : 1);
         mbar_init(c.bars + kWQRaw * 8, 1);
@@ -974,7 +985,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         const int b = tid * per + i;
         if (b >= p.B) break;
         mine += request_of<kBlockN, true>(p, b).n + kWideCost;
-        if (blockIdx.x == 0) {
+        if ((blockIdx.x | blockIdx.y | blockIdx.z) == 0) {
             const int len = p.kv_len[b];
             if (len > p.capacity || len < 0) report_status(p.status, CP_ERR_BOUNDS, b, len);
             if (p.tree_len && (p.tree_len[b] < 0 || p.tree_len[b] > min(p.n_q, len))) report_status(p.status, CP_ERR_BOUNDS, b, p.tree_len[b]);
@@ -987,7 +998,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         if (lane >= o) inc += y;
     }
     if (lane == 31) scan[warp] = inc;
-    if (tid == 0) p.meta[((int64_t)(blockIdx.x % w.classes) * w.runs + run) * 4 + 3] = 0;
+    if (tid == 0) p.meta[w.place() * 4 + 3] = 0;
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -997,15 +1008,16 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         if (i < warp) before += scan[i];
         total += scan[i];
     }
-    total *= p.Hkv;
-    before *= p.Hkv;
+    const int groups = p.Hkv / w.heads;
+    total *= groups;
+    before *= groups;
     const int ctas = (int)min((int64_t)w.runs, total);
     const int64_t x0 = run < ctas ? run_begin(total, run, ctas) : total, x1 = run < ctas ? run_begin(total, run + 1, ctas) : total;
-    if (x0 >= before && x0 < before + mine * p.Hkv) {
+    if (x0 >= before && x0 < before + mine * groups) {
         int b = tid * per;
         int64_t at = before;
         while (true) {
-            const int64_t n = (int64_t)(request_of<kBlockN, true>(p, b).n + kWideCost) * p.Hkv;
+            const int64_t n = (int64_t)(request_of<kBlockN, true>(p, b).n + kWideCost) * groups;
             if (x0 < at + n) break;
             at += n;
             ++b;
@@ -1018,7 +1030,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     __syncthreads();
     if (x0 < x1) {
         WideUnits& units = *reinterpret_cast<WideUnits*>(c.gen + W::kUnits + warp * kUnitBytes);
-        if (lane == 0) units.begin(p, start, x0, x1);
+        if (lane == 0) units.begin(w, start, x0, x1);
         __syncwarp();
         if (warp < 8) {
             asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(W::kRegsSoftmax));
@@ -1061,7 +1073,7 @@ tree_join_kernel(const __grid_constant__ WideParams w) {
     wait_for_launch_before();
     const int v = blockIdx.x, row = blockIdx.y * kWideJoinRows + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int4 me = *reinterpret_cast<const int4*>(p.meta + 4 * v);
-    const int r = v / w.runs * w.class_rows + row;
+    const int r = v / w.runs % w.classes * w.class_rows + row;
     if (me.w == 0 || row >= w.class_rows || r >= p.rows) return;
     auto slot_of = [&](int k) { return (int64_t)(k == 0 ? 2 * v + 1 : 2 * (v + k)) * kWideRows + row; };
     float mx = kNoKey;

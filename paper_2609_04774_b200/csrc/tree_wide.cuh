@@ -44,7 +44,7 @@ constexpr int kUnitBytes = 80;
 // kTiles: score tiles of a unit; with one, the warpgroups take the K/V tiles in turn.
 template <Kind kKind, int kTiles>
 struct Wide {
-    static constexpr bool kRawTiles = kKind != kBf16, kTurns = kTiles == 1;
+    static constexpr bool kRawTiles = kKind != kBf16, kTurns = kTiles == 1, kHelp = kKind == kMx4 && kTurns;
     static constexpr int kThreads = kRawTiles ? 512 : 384;
     // register budgets after the roles split; they stay below the register file by one step at least
     static constexpr int kRegsSoftmax = kRawTiles ? 184 : 200, kRegsOther = kRawTiles ? 64 : 104;
@@ -160,12 +160,17 @@ struct WideCtx {
     // some wait has given up: whoever starts copies or products stops, so that little is in flight when the CTA ends (by the warp)
     __device__ __forceinline__ bool given_up() const { return __any_sync(0xffffffffu, *abort_flag != 0); }
 };
-// Warps of a warpgroup that have rows of the CTA's class, one at least.  The others stay out (they would poll beside the widening warps:
-// 8192 4-bit keys of 37 requests, 64 rows 275 us, 255 like this).
+// Warps of a warpgroup that have rows of the CTA's class, one at least.  The others stay out (they would poll beside the widening warps: 8192 4-bit keys of 37 requests,
+// 64 rows 275 us, 255 like this), or help to widen 4-bit tiles.
 template <int kTiles>
 __device__ __forceinline__ int wide_warps(const WideParams& w, int wg) {
     const int rows = min(w.class_rows, w.d.rows - w.cls() * w.class_rows) - (kTiles == 2 ? wg * kBlockM : 0);
     return min(max((rows + 31) >> 5, 1), 4);
+}
+// Warps that widen: a warpgroup, and of 4-bit tiles of up to 128 rows the softmax warps without rows (28 rows 205 -> 175 us, 64 rows 225 -> 196 us).
+template <Kind kKind, int kTiles>
+__device__ __forceinline__ int wide_widening(const WideParams& w) {
+    return kConvWarps + (Wide<kKind, kTiles>::kHelp ? 8 - wide_warps<kTiles>(w, 0) - wide_warps<kTiles>(w, 1) : 0);
 }
 // A position in a ring: slot, and the parity of the phase that ends when it is filled (for the side that fills: when it was emptied).
 template <int kStages>
@@ -264,7 +269,7 @@ __device__ __forceinline__ uint32_t wide_place(uint32_t q, int i, int chunk) {
 // (what falls below 2^-24 of it is lost); the sign of the keys' scale joins here.  4-bit: elements i and i + 4 of every eight side by side.  Spread over the
 // widening warps, as the one that gathers the rows needs 9 us for 64 rows of E4M3.
 template <Kind kKind, int kTiles>
-__device__ __forceinline__ void wide_convert(const WideParams& w, const WideCtx& c, const WideUnits& units, int cw, int round) {
+__device__ __forceinline__ void wide_convert(const WideParams& w, const WideCtx& c, const WideUnits& units, int cw, int warps, int round) {
     using W = Wide<kKind, kTiles>;
     constexpr int kBatch = 4;                              // steps that go together
     const DecodeParams& p = w.d;
@@ -274,11 +279,11 @@ __device__ __forceinline__ void wide_convert(const WideParams& w, const WideCtx&
     c.wait(kWQRaw, round & 1, round);
     __syncwarp();
 #pragma unroll 1
-    for (int i0 = 2 * cw; i0 < rows; i0 += 2 * kConvWarps * kBatch) {      // the same for all lanes
+    for (int i0 = 2 * cw; i0 < rows; i0 += 2 * warps * kBatch) {      // the same for all lanes
         uint4 x[kBatch];
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            const int i = i0 + 2 * kConvWarps * k + sub;
+            const int i = i0 + 2 * warps * k + sub;
             x[k] = make_uint4(0, 0, 0, 0);
             if (i < rows) x[k] = lds128(wide_place(c.smem + W::kQ, i, chunk));
         }
@@ -297,7 +302,7 @@ __device__ __forceinline__ void wide_convert(const WideParams& w, const WideCtx&
         }
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            const int i = i0 + 2 * kConvWarps * k + sub;
+            const int i = i0 + 2 * warps * k + sub;
             if (i >= rows) continue;
             const uint32_t at = wide_place(c.smem + W::kQ, i, chunk);
             if (kKind == kMx4) {
@@ -321,13 +326,13 @@ __device__ __forceinline__ void wide_convert(const WideParams& w, const WideCtx&
     if (lane == 0) mbar_arrive(c.bars + kWQFull * 8);
 }
 
-// A quarter of every raw tile each.  16 E4M3 codes -> 16 fp16 values; a block of 32 4-bit codes -> 32 bf16 values, in whose groups of eight elements i and
+// A share of every raw tile each.  16 E4M3 codes -> 16 fp16 values; a block of 32 4-bit codes -> 32 bf16 values, in whose groups of eight elements i and
 // i + 4 stand side by side (the queries are laid out alike, and the columns of O are taken in that order).  The copies leave 16-byte chunk x of key k at
 // chunk x ^ (k & 7) of its row (4-bit rows of four chunks: x ^ (k / 2 & 3)), so that eight lanes with eight keys and the same chunk meet no bank twice.
 template <Kind kKind, int kTiles>
 __device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c, WideUnits& units, int cw) {
     using W = Wide<kKind, kTiles>;
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, warps = W::kHelp ? wide_widening<kKind, kTiles>(w) : kConvWarps;
     WideRing<W::kRawTiles ? W::kRaw : 1> raw = {0, 0};
     WideRing<W::kStagesK> kr = {0, 1};
     WideRing<W::kStagesV> vr = {0, 1};
@@ -337,7 +342,7 @@ __device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c
 #pragma unroll 1
         for (int ld = 0; ld < n; ++ld) {
             const bool is_v = ld & 1;
-            if (ld == 1) wide_convert<kKind, kTiles>(w, c, units, cw, round);
+            if (ld == 1) wide_convert<kKind, kTiles>(w, c, units, cw, warps, round);
             c.wait(kWRawFull + raw.slot, raw.par, ld);
             c.wait(is_v ? kWVEmpty + vr.slot : kWKEmpty + kr.slot, is_v ? vr.par : kr.par, ld);
             __syncwarp();
@@ -350,10 +355,10 @@ __device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c
                 uint32_t from = src + (cw * 8 + k7) * 128, row = tile + (cw * 8 + k7) * 128;
                 uint4 q0 = lds128(from + in0), q1 = lds128(from + in1);
 #pragma unroll 1
-                for (int i = cw; i < 16; i += kConvWarps) {
+                for (int i = cw; i < 16; i += warps) {
                     const uint4 a = q0, b = q1;
-                    if (i + kConvWarps < 16) {
-                        from += kConvWarps * 8 * 128;
+                    if (i + warps < 16) {
+                        from += warps * 8 * 128;
                         q0 = lds128(from + in0);
                         q1 = lds128(from + in1);
                     }
@@ -371,7 +376,7 @@ __device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c
                     widen4(b.w, hi.z, hi.w);
                     sts128(row + kHalfBytes + out0, lo);
                     sts128(row + kHalfBytes + out1, hi);
-                    row += kConvWarps * 8 * 128;
+                    row += warps * 8 * 128;
                 }
             } else {
                 // a step is 8 keys x 4 blocks
@@ -381,11 +386,11 @@ __device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c
                 uint4 q = lds128(from);
                 uint32_t word = lds32(e_from);
 #pragma unroll 1
-                for (int i = cw; i < 16; i += kConvWarps) {
+                for (int i = cw; i < 16; i += warps) {
                     const uint32_t codes[4] = {q.x, q.y, q.z, q.w}, e = word >> (8 * x) & 255;
-                    if (i + kConvWarps < 16) {
-                        q = lds128(from += kConvWarps * 8 * 64);
-                        word = lds32(e_from += kConvWarps * 8 * 16);
+                    if (i + warps < 16) {
+                        q = lds128(from += warps * 8 * 64);
+                        word = lds32(e_from += warps * 8 * 16);
                     }
                     // one factor of 2^(e - 127 + 126) while it is a bf16 number, else 2^126 and 2^(e - 127)
                     const bool near = __all_sync(0xffffffffu, e - 1 < 128u);
@@ -402,7 +407,7 @@ __device__ __forceinline__ void wide_widen(const WideParams& w, const WideCtx& c
                     }
 #pragma unroll
                     for (int n4 = 0; n4 < 4; ++n4) sts128(row + (((4 * x + n4 & 7) ^ k7) << 4), o[n4]);
-                    row += kConvWarps * 8 * 128;
+                    row += warps * 8 * 128;
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // the tensor cores read what these lanes wrote
@@ -745,7 +750,7 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
     const int r = cls * w.class_rows + row, t = r / p.G;                  // of the KV head; its token
     const bool in_class = row < w.class_rows && r < p.rows;
     constexpr int step = turns ? 2 : 1;
-    if (warp_in_wg >= wide_warps<kTiles>(w, wg)) return;
+    if (!W::kHelp && warp_in_wg >= wide_warps<kTiles>(w, wg)) return;
     float c = p.scale_log2;
     uint32_t s_par = 0, tile_cnt = 0;
     for (int round = 0; units.valid; ++round) {
@@ -946,18 +951,19 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int run = w.run();
     if (tid == 0) {
-        mbar_init(c.bars + kWQFull * 8, W::kRawTiles ? kConvWarps : 1);
+        const int widening = W::kRawTiles ? wide_widening<kKind, kTiles>(w) : 1;
+        mbar_init(c.bars + kWQFull * 8, widening);
         mbar_init(c.bars + kWQRaw * 8, 1);
         mbar_init(c.bars + kWQEmpty * 8, 1);
         for (int s = 0; s < kMaxRing; ++s) {
-            mbar_init(c.bars + (kWKFull + s) * 8, W::kRawTiles ? kConvWarps : 1);
+            mbar_init(c.bars + (kWKFull + s) * 8, widening);
             mbar_init(c.bars + (kWKEmpty + s) * 8, 1);
-            mbar_init(c.bars + (kWVFull + s) * 8, W::kRawTiles ? kConvWarps : 1);
+            mbar_init(c.bars + (kWVFull + s) * 8, widening);
             mbar_init(c.bars + (kWVEmpty + s) * 8, 1);
         }
         for (int s = 0; s < W::kRaw; ++s) {
             mbar_init(c.bars + (kWRawFull + s) * 8, 1);
-            mbar_init(c.bars + (kWRawEmpty + s) * 8, kConvWarps);
+            mbar_init(c.bars + (kWRawEmpty + s) * 8, widening);
         }
         for (int h = 0; h < 2; ++h) {
             const int warps = wide_warps<kTiles>(w, h);    // one arrival per warp
@@ -1032,9 +1038,14 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         WideUnits& units = *reinterpret_cast<WideUnits*>(c.gen + W::kUnits + warp * kUnitBytes);
         if (lane == 0) units.begin(w, start, x0, x1);
         __syncwarp();
+        int widener = warp >= 12 ? warp - 12 : -1;
+        if (W::kHelp && warp < 8) {
+            const int wg = warp >> 2, spare = (warp & 3) - wide_warps<kTiles>(w, wg);
+            if (spare >= 0) widener = kConvWarps + spare + (wg ? 4 - wide_warps<kTiles>(w, 0) : 0);
+        }
         if (warp < 8) {
             asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(W::kRegsSoftmax));
-            wide_softmax<kKind, kTiles>(w, c, units, warp >> 2, total, ctas);
+            if (!W::kHelp || widener < 0) wide_softmax<kKind, kTiles>(w, c, units, warp >> 2, total, ctas);
         } else {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(W::kRegsOther));
             if (warp == 9) {
@@ -1046,9 +1057,12 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             } else if (warp == 8) {
                 const WideMaps maps = {&tm_k, &tm_v, &tm_ke, &tm_ve};
                 wide_producer<kKind, kTiles>(w, c, units, maps);
-            } else if constexpr (W::kRawTiles) {
+            } else if constexpr (W::kRawTiles && !W::kHelp) {
                 wide_widen<kKind, kTiles>(w, c, units, warp - 12);
             }
+        }
+        if constexpr (W::kHelp) {
+            if (widener >= 0) wide_widen<kKind, kTiles>(w, c, units, widener);     // one place, so one copy of the code
         }
     }
     let_next_launch_begin();           // not earlier: nothing is to be set up beside a block whose warps pass registers on

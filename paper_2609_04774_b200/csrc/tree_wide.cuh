@@ -16,7 +16,7 @@
 //   - Warps: two softmax warpgroups; a producer that fetches K/V tiles page by page; the issuers of S = Q K^T and of O += P V; a warp that gathers the
 //     unit's query rows with cp.async.  S, P and O live in TMEM: S | P0 | P1 | O0 | O1.  S is one buffer that the tiles use in turn, read
 //     into registers at once, so the next product runs under the exponentials.
-//   - K and V come by TMA, page by page.  E4M3 and 4-bit rows land in a ring of raw tiles, and a fourth warpgroup widens them into the tiles of the products:
+//   - K and V come by TMA, page by page.  E4M3 and 4-bit rows land in a ring of raw tiles, and a fourth warpgroup (with the softmax warps that have no rows, for 4-bit rows) widens them into the tiles of the products:
 //     E4M3 to fp16 (queries and weights are then fp16 as in the narrow form), 4-bit codes and exponents to bf16, both exactly.  (Copied by the widening warps
 //     with cp.async, an E4M3 tile takes 3 us: with 64 registers a thread the copies wait for one another's addresses.)
 //   - Only the last tiles of a unit and those at a window's edge hide keys from rows.  Their masks are bits: of the tree's mask and of the window.  A hidden
@@ -24,8 +24,7 @@
 //     finite number; what some rows do see of it is added to their results when they are written.
 // Every wait is bounded, as in the prefill kernel.
 // Measured, 37 requests of 8192 keys, 32 / 8 heads, pages of 64 (the copy rate needs 193 / 96 / 51 us): bf16 194, 202 and 283 us with 64, 128 and 256 rows (6.4 TB/s up to
-// 128 rows, then the tensor and MUFU pipes: 1120 TFLOP/s of visible pairs); E4M3 192, 194, 302 and 4-bit 225, 233, 328 us, bound by the widening (0.6 and 0.8 us a
-// tile).  A unit costs 9 to 22 us beside its tiles: 4 until its queries are there, 2 of epilogue, 1 to 3 where the warpgroups wait for one another.
+// 128 rows, then the tensor and MUFU pipes: 1120 TFLOP/s of visible pairs); E4M3 182, 191, 299 and 4-bit 196, 233, 328 us, bound by the chain from a raw tile to the second product.  A unit costs 9 to 22 us beside its tiles: 4 until its queries are there, 2 of epilogue, 1 to 3 where the warpgroups wait for one another.
 #pragma once
 
 #include "decode_kernel.cuh"

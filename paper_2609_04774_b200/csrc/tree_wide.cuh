@@ -784,21 +784,21 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
             tc_fence_after();
         } else if (some) {
             float s0[32], s1[32], s2[32], s3[32];
+            int e = 0;
             cx.wait(kWSReady + wg, s_par, j1);
             __syncwarp();
             s_par ^= 1u;
             tc_fence_after();
             CP_LOAD_S3(s0, s1, s2)
             TMEM_LD32(s_tmem + 96, s3, 0);
+            // before this warp says that S is free: the next unit's scores may then be computed, and the queries of the one behind it overwrite the exponent
+            if (kF16) e = reinterpret_cast<const volatile int8_t*>(cx.gen + W::kExp)[(round & 1) * kWideRows + row];
             tc_wait_ld();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(cx.bars + (kWSFree + wg) * 8);
-            if (kF16) {
-                const int e = reinterpret_cast<const int8_t*>(cx.gen + W::kExp)[(round & 1) * kWideRows + row];
-                // c > 0: the sign of a scale is in the queries; with a scale of zero hidden keys must still be -inf
-                c = fmaxf(fabsf(p.k_scale[u]) * p.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23), 1e-35f);
-            }
+            // c > 0: the sign of a scale is in the queries; with a scale of zero hidden keys must still be -inf
+            if (kF16) c = fmaxf(fabsf(p.k_scale[u]) * p.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23), 1e-35f);
 #pragma unroll 1
             for (int j = j1; j < n; j += step) {
                 const int key0 = units.key_of(j);

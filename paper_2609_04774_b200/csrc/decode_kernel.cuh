@@ -297,7 +297,8 @@ __device__ __forceinline__ TreeRow tree_row(const DecodeParams& p, int b, int t,
 // The infinities and NaN of V, at one dim, among the listed keys (late: those that only some rows see, from base on; early: from the
 // lowest window's first key on) that token t of request b sees.  Only those are nonzero: 0 + inf, whatever the weight.
 template <Kind kKind, bool kTree>
-__device__ __forceinline__ float odd_values(const DecodeParams& p, const unsigned long long* keys, int b, int base, int len, int h, int t, int dim) {
+__device__ __forceinline__ float odd_values(const DecodeParams& p, unsigned long long late_keys, unsigned long long early_keys, int b, int base, int len, int h, int t,
+                                            int dim) {
     TreeRow row;
     if (kTree) row = tree_row(p, b, t, base, len - base);
     const int lim = kTree ? row.lim : base + t;
@@ -305,7 +306,7 @@ __device__ __forceinline__ float odd_values(const DecodeParams& p, const unsigne
 #pragma unroll 1
     for (int early = 0; early < 2; ++early) {
 #pragma unroll 1
-        for (unsigned long long todo = keys[early]; todo != 0; todo &= todo - 1) {
+        for (unsigned long long todo = early ? early_keys : late_keys; todo != 0; todo &= todo - 1) {
             const int bit = __ffsll(todo) - 1, key = base - (early ? p.window : 0) + bit;
             if (kTree && !early) {
                 if (!(row.mask >> bit & 1)) continue;
@@ -1052,7 +1053,7 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
             for (int i = tid; i < HP * kRows * kDim; i += kThreads) {
                 const int at = i / kDim, dim = i % kDim, hs = at / kRows, r = r0 + at % kRows, t = r / p.G;
                 if (r >= p.rows || (kTreed && t >= rq.len - rq.base)) continue;
-                const float x = odd_values<kKind, kTreed>(p, odd_keys + (q_cur * HP + hs) * 2, b, rq.base, rq.len, h0 + hs, t, dim);
+                const float x = odd_values<kKind, kTreed>(p, odd_keys[(q_cur * HP + hs) * 2], odd_keys[(q_cur * HP + hs) * 2 + 1], b, rq.base, rq.len, h0 + hs, t, dim);
                 if (x == 0.f) continue;
                 if (whole) {
                     __nv_bfloat16* o = p.out + (((int64_t)b * p.n_q + t) * p.Hq + (h0 + hs) * p.G + r - t * p.G) * kDim + dim;

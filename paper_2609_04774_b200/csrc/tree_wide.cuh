@@ -563,7 +563,9 @@ __device__ __forceinline__ void wide_outputs(const WideParams& w, const WideCtx&
     for (int round = 0; units.valid; units.next(p), ++round) {
         const int j0 = units.t_begin, n = units.t_end;
         unsigned long long* odd = reinterpret_cast<unsigned long long*>(c.gen + W::kOdd) + 2 * (round & 1);
-        if (lane < 2) odd[lane] = 0;   // its readers, of the unit before the last, are done: the last unit's P came behind them
+        // Its readers, of the unit before the last, took their copies before they arrived at kWOFree, which the first tiles of the last unit waited for: with
+        // two score tiles one barrier for each of the warpgroups, with one the first tile's for both.
+        if (lane < 2) odd[lane] = 0;
         __syncwarp();
 #pragma unroll 1
         for (int j = j0; j < n; ++j) {
@@ -618,11 +620,11 @@ __device__ __forceinline__ void wide_hide(float (&s)[32], uint32_t seen) {
 
 // What wide_clear took out of the V that a row sees joins the elements [d0, d1) of the row just written.
 template <Kind kKind>
-__device__ __forceinline__ void wide_odd_row(const DecodeParams& p, const unsigned long long* odd, int b, int base, int len, int u, int t, bool whole, int64_t at,
-                                             int d0, int d1) {
+__device__ __forceinline__ void wide_odd_row(const DecodeParams& p, unsigned long long late, unsigned long long early, int b, int base, int len, int u, int t, bool whole,
+                                             int64_t at, int d0, int d1) {
 #pragma unroll 1
     for (int dim = d0; dim < d1; ++dim) {
-        const float x = odd_values<kKind, true>(p, odd, b, base, len, u, t, dim);
+        const float x = odd_values<kKind, true>(p, late, early, b, base, len, u, t, dim);
         if (x == 0.f) continue;
         if (whole) p.out[at + dim] = __float2bfloat16_rn(__bfloat162float(p.out[at + dim]) + x);
         else p.part_o[at + dim] += x;
@@ -838,8 +840,10 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
         }
         cx.wait(kWOdd, round & 1, n);
         __syncwarp();
-        const unsigned long long* odd = reinterpret_cast<const unsigned long long*>(cx.gen + W::kOdd) + 2 * (round & 1);
-        const bool any_odd = live && (odd[0] | odd[1]) != 0;
+        // a copy of the list, before this warp arrives at kWOFree: from then on it may be cleared for the unit after the next
+        const volatile unsigned long long* odd = reinterpret_cast<const volatile unsigned long long*>(cx.gen + W::kOdd) + 2 * (round & 1);
+        const unsigned long long odd_late = odd[0], odd_early = odd[1];
+        const bool any_odd = live && (odd_late | odd_early) != 0;
         const float inv = !whole ? 1.f : (l == 0.f ? 0.f : (kF16 ? p.v_scale[u] : 1.f) / l);
         f0 *= inv;
         f1 *= inv;
@@ -907,7 +911,7 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
                 mbar_arrive(cx.bars + (kWOFree + wg) * 8);
             }
         }
-        if (any_odd) wide_odd_row<kKind>(p, odd, b, rq.base, rq.len, u, t, whole, at, cc0 * 32, cc1 * 32);
+        if (any_odd) wide_odd_row<kKind>(p, odd_late, odd_early, b, rq.base, rq.len, u, t, whole, at, cc0 * 32, cc1 * 32);
         if (in_class && (!turns || wg == 0)) {
             if (whole) {
                 p.lse[(int64_t)head * ((int64_t)p.B * p.n_q) + (int64_t)b * p.n_q + t] =

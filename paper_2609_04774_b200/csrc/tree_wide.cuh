@@ -823,6 +823,9 @@ __device__ __forceinline__ void wide_softmax(const WideParams& w, const WideCtx&
         const bool both = turns && n - j0 > 1;
         if (turns) {
             // the warpgroups tell one another their maxima and sums; then each reads half of the columns of both accumulators, which lie in the same lanes
+            // Without a tile of this unit nothing has kept this warp behind the others: one of them may still be in the last unit, and this one's arrival would be taken
+            // for the other's there.  (With a tile, the first product onto the accumulator has waited for the same barrier.)
+            if (!some && round > 0) cx.wait(kWOFree + wg, (round - 1) & 1, n);
             float2* ml = reinterpret_cast<float2*>(cx.gen + W::kMl) + (round & 1) * 2 * kBlockM;
             ml[wg * kBlockM + tile_row] = make_float2(m, l);
             tc_fence_before();

@@ -44,9 +44,10 @@ def test_queries_of_another_magnitude_in_every_request(ctx, Hq, n_q):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "fp8", "mx4"])
-@pytest.mark.parametrize("Hq,n_q", [(32, 16), (64, 12)])
+@pytest.mark.parametrize("Hq,n_q", [(2, 30), (2, 40), (8, 16), (16, 16), (32, 16), (64, 12)])
 def test_upper_dims_of_drafts_that_are_no_numbers(ctx, kind, Hq, n_q):
-    """The upper half of one draft's V row is infinite (bf16) or NaN in every second request and one of its heads: exactly the rows that see it become that."""
+    """The upper half of one draft's V row is infinite (bf16) or NaN in every second request and one of its heads: exactly the rows that see it become that.
+    Up to 128 rows the warpgroups take the tiles in turn: the one without a tile has to wait for the warps that put such values into their rows."""
     s = short_requests(Hq + n_q, kind, Hq, n_q)
     G = Hq // 2
     want = torch.zeros(len(s.bases), n_q, Hq, 128, dtype=torch.bool, device="cuda")

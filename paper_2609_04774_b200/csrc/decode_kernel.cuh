@@ -285,7 +285,7 @@ __device__ __forceinline__ TreeRow tree_row(const DecodeParams& p, int b, int t,
     const int pos = base + __popcll(r.mask) - 1;
     r.lim = pos + 1;
     r.pad = 0;
-    if (p.window < 64) {                                   // positions of drafted tokens differ by 64 at most
+    if (p.window <= 64) {                                  // positions of drafted tokens differ by 64 at most: all drafts seen, and none
         for (unsigned long long todo = r.mask; todo != 0; todo &= todo - 1) {
             const int u = __ffsll(todo) - 1, at = base + (chain ? u : __popcll(masks[u] & inside) - 1);
             if (pos - at >= p.window && at >= p.sinks) r.mask &= ~(1ull << u);

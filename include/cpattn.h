@@ -504,19 +504,19 @@ int cp_decode_attn_mx4(cp_ctx* ctx, const void* q, const cp_kv_cache_mx4* cache,
                        const int32_t* kv_len, int32_t B, int32_t n_q, int32_t Hq, int64_t window, int64_t sinks, float scale, void* out,
                        float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Trees of drafted tokens.  Sequence b has kv_len[b] tokens in its table row, of which the last tree_len[b] (0..n_q; tree_len NULL: n_q each)
- * are a tree of drafts: with base = kv_len[b] - tree_len[b], drafted token t sits in slot base + t, and at position base + depth(t), the
+/* Trees of drafted tokens.  Sequence b has kv_len[b] tokens in its table row, of which the last tree_len[b] (0..n_q; tree_len NULL: n_q each,
+ * or all of a shorter sequence) are a tree of drafts: with base = kv_len[b] - tree_len[b], drafted token t sits in slot base + t, and at position base + depth(t), the
  * depth of a token without a parent among the drafts being 0.  parent  device [B, n_q] int32: parent[b][t] < t, or -1: the sequence itself.
  * A step: cp_pages_extend, cp_tree_plan, then layer by layer cp_rope_append and cp_tree_attn, the choice of the accepted
- * tokens, cp_tree_commit.  Entries behind a sequence's tree_len are padding.  n_q <= 64.
+ * tokens, cp_tree_commit.  Entries behind a sequence's tree_len are padding.  n_q <= 64.  A tree_len outside [0, min(n_q, kv_len[b])] counts as the
+ * nearest in it, and cp_tree_plan and cp_tree_attn report it {code, b, block, tree_len}.
  *   cp_tree_plan   mask [B, n_q]: bits of the drafted tokens that a token sees, its ancestors and itself (0 behind the tree); positions [n_axes,
  *            B * n_q] (the same on every axis), token_seq (b; -1 behind the tree: padding) and token_slot [B * n_q] as cp_rope_append takes
  *            them (0 behind the tree).  A parent outside [-1, t) is reported as CP_ERR_BOUNDS {code, b * n_q + t, block, parent} and
  *            counts as -1.
  *   cp_tree_attn   cp_decode_attn where row t sees the keys before base as a token at its position does, and of the drafts those of its mask that its
  *            window or the sinks hold, by their positions.  The masks may be any bits (bits from tree_len on are
- *            ignored); the position of a token is base + (bits of its mask) - 1.  Rows behind the tree: zeros, lse = -inf.  A tree_len outside
- *            [0, min(n_q, kv_len[b])] is reported {code, b, block, tree_len} and counts as the nearest in it.  Workspace: cp_workspace_bytes_tree; limits,
+ *            ignored); the position of a token is base + (bits of its mask) - 1.  Rows behind the tree: zeros, lse = -inf.  Workspace: cp_workspace_bytes_tree; limits,
  *            layouts, roundings and the rest as in cp_decode_attn[_fp8|_mx4].  Beyond n_q * Hq / Hkv = 16 rows (E4M3: 32) magnitudes of V
  *            reach 2^118 (a weight may be 2^8 for a while), and 4-bit caches take the queries exactly.
  *   cp_tree_commit   accepted [B]: the last drafted token that sequence b keeps (-1: none).  It and its ancestors n_0 < n_1 < .. become the sequence's next

@@ -16,7 +16,7 @@ tree_plan_kernel(const int32_t* parent, const int32_t* tree_len, const int32_t* 
     const int b = blockIdx.x, t = threadIdx.x;
     const int len = max(kv_len[b], 0), asked = tree_len ? tree_len[b] : n_q;
     const int m = min(max(asked, 0), min(n_q, len));
-    if (t == 0 && m != asked) report_status(status, CP_ERR_BOUNDS, b, asked);
+    if (t == 0 && tree_len && m != asked) report_status(status, CP_ERR_BOUNDS, b, asked);
     int to = -1;
     if (t < m) {
         to = parent[(int64_t)b * n_q + t];

@@ -135,7 +135,8 @@ __device__ __forceinline__ uint32_t block_exponents(uint32_t ea, int ca, uint32_
 __device__ __forceinline__ uint32_t scale_byte(uint32_t f) { return f == 255 ? 255u : (f > 2 ? f - 2 : 0u); }
 // 2^(127 - byte), exact; byte <= 252 (255: any)
 __device__ __forceinline__ float scale_up(uint32_t byte) { return __uint_as_float((byte > 253 ? 1u : 254u - byte) << 23); }
-// x as fp32 so that every border of a shorter format is on the right side: inexact values get an odd last bit.
+// x as fp32 so that every border of a shorter format is on the right side: inexact values get an odd last bit.  Finite values beyond the range become the largest
+// fp32 number: exponent byte 252, code 6.
 __device__ __forceinline__ float to_odd(double x) {
     const float f = __double2float_rz(x);
     return (double)f == x || !(fabsf(f) < INFINITY) ? f : __uint_as_float(__float_as_uint(f) | 1u);
@@ -334,8 +335,9 @@ rope_append_kernel(const __grid_constant__ RopeParams p) {
                     err_b = turn_b ? kTurnError * (kPairs ? 2.f * mb : ma + mb) : 0.f;
                 }
                 uint32_t f = block_exponents(exponent8(xa, -err_a), ca, exponent8(xb, -err_b), cb, lanes);
+                // a field of 255: an infinity or NaN of the input, or a rotation that left the fp32 range, which only the way through fp64 tells apart
                 bool unsure = false;
-                if (kind == 1) unsure = f != block_exponents(exponent8(xa, err_a), ca, exponent8(xb, err_b), cb, lanes);
+                if (kind == 1) unsure = f != block_exponents(exponent8(xa, err_a), ca, exponent8(xb, err_b), cb, lanes) || __vcmpeq4(f, 0xffffffffu) != 0;
                 uint32_t codes_a, codes_b;
                 auto code8 = [&](const float (&x)[8], int chunk, float err, bool& differ) {
                     const float up = scale_up(scale_byte(f >> (8 * (chunk >> 2)) & 255));

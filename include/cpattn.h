@@ -478,7 +478,7 @@ int cp_decode_attn_fp8(cp_ctx* ctx, const void* q, const cp_kv_cache_fp8* cache,
  * page_size) * stride_tok; both strides in bytes, multiples of 16, stride_tok >= 68 * Hkv; k and v 16-byte aligned.
  *   cp_rope_append_mx4  cp_rope_append into such a cache.  k (rotated) and v are quantised block by block: e = floor(log2(largest magnitude))
  *            - 2 + 127 (at least 0), codes to the nearest, ties to the even code, saturating at 6.  A block with an infinity or a NaN becomes
- *            NaN; a finite k that the rotation takes out of the fp32 range counts as the largest fp32 number (e = 252, code 6).  The codes are those of the exactly rotated values: where the fp32 rotation does not decide, it is redone in fp64.
+ *            NaN; a finite k that the rotation takes out of the fp32 range counts as the largest fp32 number (e = 252, code 6).  The codes are those of the exactly rotated values (a zero has either sign): where the fp32 rotation does not decide, it is redone in fp64.
  *   cp_kv_gather_mx4    the values of n logical tokens from t_begin as bf16 rows [n, Hkv, D] (exact up to e = 252, the largest that the append writes), what the
  *            prefill calls read: rows of whole pages are a cp_kv_cache with table 0, 1, 2, ..  Page ids as in cp_kv_gather.
  *   cp_decode_attn_mx4  cp_decode_attn over such a cache, same arguments, workspace and limits.  Weights are rounded to bf16, K and V are taken exactly

@@ -1,4 +1,6 @@
-"""cp_rope_append_mx4 at the ends of the range: rotated keys beyond the fp32 numbers."""
+"""cp_rope_append_mx4 at the ends of the range: rotated keys beyond the fp32 numbers, keys that are mostly zeros."""
+import math
+
 import pytest
 import torch
 
@@ -46,3 +48,60 @@ def test_finite_keys_that_leave_the_range_saturate(ctx, interleaved, Hkv):
     want = mx4_quantise(x.clamp(-top, top))
     assert torch.equal(got[:, Hkv * 64:], want[:, Hkv * 64:]) and int(got[:, Hkv * 64:].max()) == 252
     assert torch.equal(mx4_values(got, Hkv), mx4_values(want, Hkv))
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("sections", [[64], [24]])
+def test_keys_that_are_mostly_zeros(ctx, interleaved, sections):
+    """Zeros of either sign, alone and in pairs, among other elements."""
+    g = generator(4)
+    n, Hkv = 300, 4
+    zero = torch.copysign(torch.zeros(n, Hkv, D, device="cuda"), torch.randn(n, Hkv, D, generator=g, device="cuda")).bfloat16()
+    r = None
+    for share in (0.5, 0.97):
+        k = torch.where(torch.rand(n, Hkv, D, generator=g, device="cuda") < share, zero, normal(g, n, Hkv, D))
+        r = Rows(2, n, 4, Hkv, 16, sections, interleaved, x=(k, normal(g, n, Hkv, D)))
+        r.check(ctx)
+    r = Rows(2, n, 4, Hkv, 16, sections, interleaved, x=(zero, zero))
+    got, _ = written(ctx, r)
+    assert bool((got[:, :Hkv * 64] & 0x77 == 0).all()) and bool((got[:, Hkv * 64:] == 0).all())
+
+
+@pytest.mark.parametrize("freq", [2e-7, 1e-6, 4e-6, 2e-5])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_blocks_of_what_a_small_turn_brings_over(ctx, interleaved, freq):
+    """The first element of every pair is zero and the angle a few millionths: its rotated value is not much larger than the rotation's error in fp32."""
+    g = generator(6)
+    n, Hkv = 600, 4
+    k = normal(g, n, Hkv, D)
+    k[..., 0::2 if interleaved else 1][..., :D // 2] = 0
+    r = Rows(2, n, 4, Hkv, 16, [64], interleaved, x=(k, normal(g, n, Hkv, D)))
+    r.rope.freq[:] = [freq * (1 + i / 64) for i in range(64)]
+    r.positions.copy_(torch.randint(-3, 4, r.positions.shape, generator=g, device="cuda"))
+    r.check(ctx)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_zeros_cost_nothing(ctx, interleaved):
+    """A cache of zeros in half of the pairs is written about as fast as one without (every head that goes through the rotation in 64 bits costs many times a
+    head's time, and a chunk without an undecided value is the rule)."""
+    g = generator(5)
+    n, Hkv = 16384, 8
+    dense, v = normal(g, n, Hkv, D), normal(g, n, Hkv, D)
+    gone = torch.rand(n, Hkv, D // 2, generator=g, device="cuda") < 0.5
+    gone = torch.stack([gone, gone], -1).flatten(-2) if interleaved else torch.cat([gone, gone], -1)
+
+    def time(k):
+        r = Rows(2, n, 4, Hkv, 64, [64], interleaved, x=(k, v))
+        best = math.inf
+        for _ in range(12):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            binding.cp_rope_append_mx4(ctx, r.rope, None, r.k_rows, r.v_rows, r.positions, r.seq, r.slot, r.cache, r.table, None)
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b))
+        return best
+
+    full, sparse = time(dense), time(dense.masked_fill(gone, 0))
+    assert sparse <= 1.3 * full, (full, sparse)

@@ -103,9 +103,9 @@ __device__ __forceinline__ uint2 quantize8(const float (&x)[8], float sc, float 
 // ---- 4-bit blocks.  A head is owned by eight lanes, two chunks of eight elements each, which may lie in any of its four blocks.
 // A code depends on where a value lies between the format's few borders and an exponent on which side of a power of two the block's largest
 // is, so the fp32 rotation (off by less than kTurnError times the pair's magnitudes: 2^-23 from the angle, 2^-23 from the sine and cosine, three
-// roundings of 2^-24) is only trusted where values that much smaller and larger give the same codes and exponents; otherwise the head is
+// roundings of 2^-24; among the subnormals the roundings are half a step each of 2^-149, a product's and the sum's, hence kTurnStep) is only trusted where values that much smaller and larger give the same codes and exponents; otherwise the head is
 // rotated again in fp64 (about one head in ten thousand).  16384 tokens: see the figures above.
-constexpr float kTurnError = 5e-7f;
+constexpr float kTurnError = 5e-7f, kTurnStep = 0x1p-149f;
 
 // E2M1 codes of two values, the first in the low half: nearest, ties to even, saturating at 6.
 __device__ __forceinline__ uint32_t e2m1x2(float a, float b) {
@@ -331,8 +331,8 @@ rope_append_kernel(const __grid_constant__ RopeParams p) {
                         ma = fmaxf(ma, fabsf(in_a[j]));
                         mb = fmaxf(mb, fabsf(in_b[j]));
                     }
-                    err_a = turn_a ? kTurnError * (kPairs ? 2.f * ma : ma + mb) : 0.f;
-                    err_b = turn_b ? kTurnError * (kPairs ? 2.f * mb : ma + mb) : 0.f;
+                    err_a = turn_a ? fmaf(kTurnError, kPairs ? 2.f * ma : ma + mb, kTurnStep) : 0.f;
+                    err_b = turn_b ? fmaf(kTurnError, kPairs ? 2.f * mb : ma + mb, kTurnStep) : 0.f;
                 }
                 uint32_t f = block_exponents(exponent8(xa, -err_a), ca, exponent8(xb, -err_b), cb, lanes);
                 // a field of 255: an infinity or NaN of the input, or a rotation that left the fp32 range, which only the way through fp64 tells apart

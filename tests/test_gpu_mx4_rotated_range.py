@@ -1,4 +1,4 @@
-"""cp_rope_append_mx4 at the ends of the range: rotated keys beyond the fp32 numbers, keys that are mostly zeros."""
+"""cp_rope_append_mx4 at the ends of the range: rotated keys beyond the fp32 numbers, keys among the smallest ones, keys that are mostly zeros."""
 import math
 
 import pytest
@@ -47,6 +47,20 @@ def test_finite_keys_that_leave_the_range_saturate(ctx, interleaved, Hkv):
     assert bool((x.abs() > top).any())
     want = mx4_quantise(x.clamp(-top, top))
     assert torch.equal(got[:, Hkv * 64:], want[:, Hkv * 64:]) and int(got[:, Hkv * 64:].max()) == 252
+    assert torch.equal(mx4_values(got, Hkv), mx4_values(want, Hkv))
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_the_smallest_keys(ctx, interleaved):
+    """Magnitudes of 2^-133 to 2^-120, where fp32 has fewer bits: the rotation's error is then a step of the smallest numbers, not a share of the value."""
+    g = generator(9)
+    n, Hkv = 2000, 8
+    power = torch.randint(-133, -119, (n, Hkv, 1), generator=g, device="cuda").double()
+    k = (normal(g, n, Hkv, D).double().clamp(-1.5, 1.5) * torch.exp2(power)).bfloat16()
+    r = Rows(2, n, 4, Hkv, 16, [64], interleaved, x=(k, normal(g, n, Hkv, D)))
+    got, x = written(ctx, r)
+    want = mx4_quantise(x)
+    assert torch.equal(got[:, Hkv * 64:], want[:, Hkv * 64:])
     assert torch.equal(mx4_values(got, Hkv), mx4_values(want, Hkv))
 
 

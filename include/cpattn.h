@@ -482,7 +482,8 @@ int cp_decode_attn_fp8(cp_ctx* ctx, const void* q, const cp_kv_cache_fp8* cache,
  *   cp_kv_gather_mx4    the values of n logical tokens from t_begin as bf16 rows [n, Hkv, D] (exact up to e = 252, the largest that the append writes), what the
  *            prefill calls read: rows of whole pages are a cp_kv_cache with table 0, 1, 2, ..  Page ids as in cp_kv_gather.
  *   cp_decode_attn_mx4  cp_decode_attn over such a cache, same arguments, workspace and limits.  Weights are rounded to bf16, K and V are taken exactly
- *            (e up to 252), the queries lose what is below 2^-24 of a row's largest element.
+ *            (e up to 252; of K up to 233, 6 * 2^106, beyond which the sums of the products may leave the fp32 range), the queries lose what is below 2^-24 of a row's largest
+ *            element.
  * Errors as in the calls they are forms of. */
 typedef struct {
     const void* k;          /* device */

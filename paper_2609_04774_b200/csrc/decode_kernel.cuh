@@ -568,13 +568,15 @@ decode_kernel(const __grid_constant__ DecodeParams p) {
                 if (lane == 0) ml[row] = down;             // the merge area is free between units
             }
             __syncthreads();
-            // c > 0: the sign of a scale is in the queries; with a scale of zero (all scores 0) hidden keys must still be -inf * c = -inf
+            // c > 0: the sign of a scale is in the queries; with a scale of zero (all scores 0) hidden keys must still be -inf * c = -inf.  Products of E4M3 codes stay
+            // below 2^27, so 1e-35 is nothing to them; of 4-bit rows they reach 2^126, and c is exact down to the smallest numbers
             // 4-bit: the keys' exponents join with one too many (see take)
+            constexpr float kLeast = kMx ? 0x1p-149f : 1e-35f;
             const float ks = (kFp8 ? fabsf(p.k_scale[h0 + sub]) : 0.5f) * p.scale_log2;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                c_row[nt][0] = fmaxf(ks * ml[sub * kRows + nt * 8 + 2 * qd], 1e-35f);
-                c_row[nt][1] = fmaxf(ks * ml[sub * kRows + nt * 8 + 2 * qd + 1], 1e-35f);
+                c_row[nt][0] = fmaxf(ks * ml[sub * kRows + nt * 8 + 2 * qd], kLeast);
+                c_row[nt][1] = fmaxf(ks * ml[sub * kRows + nt * 8 + 2 * qd + 1], kLeast);
             }
             __syncthreads();
         }

@@ -24,7 +24,7 @@ extern "C" size_t cp_workspace_bytes_decode(int32_t B, int32_t n_q, int32_t Hq, 
     if (B < 0 || n_q < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0) return 0;
     const int64_t rows = (int64_t)n_q * (Hq / Hkv);
     if (B > kMaxDecodeBatch || n_q > kMaxDecodeTokens || rows > kMaxDecodeRows) return 0;
-    return decode_workspace((int)rows);
+    return decode_workspace((int)rows, Hkv % 4 == 0);      // of every kind of cache
 }
 
 extern "C" int cp_decode_attn(cp_ctx* ctx, const void* q, const cp_kv_cache* cache, const int32_t* page_table, int64_t table_stride,

@@ -1142,19 +1142,20 @@ decode_join_kernel(const __grid_constant__ DecodeParams p, int heads, int rows_p
 }
 
 constexpr int kMaxDecodeGrid = 2 * kMaxGrid;
-constexpr int kMaxHeads = 4;                               // largest HP
 constexpr int kMaxDecodeTokens = 64, kMaxDecodeRows = 1024, kMaxDecodeBatch = 65536;      // limits of a call: n_q, rows per KV head, B
 inline int row_blocks(int rows) { return rows <= 8 ? 1 : (rows <= 16 ? 2 : 4); }
 
-// Workspace: partial rows and their (maximum, sum) of two pieces per CTA, and four words per CTA.
-size_t decode_workspace(int rows) {
-    const size_t n = 2 * (size_t)kMaxDecodeGrid * kMaxHeads * row_blocks(rows) * 8;
-    return (n * (kDim + 2) * sizeof(float) + kMaxDecodeGrid * 16 + 255) / 256 * 256;
+// Workspace: partial rows and their (maximum, sum) of two pieces per CTA, and four words per CTA.  With nt blocks of 8 rows, two heads of two CTAs an SM or four of one; four heads
+// of two CTAs are 4-bit units of one block (four_heads: the KV heads are a multiple of four).
+constexpr size_t partial_rows(int nt, bool four_heads) { return 2 * (size_t)kMaxDecodeGrid * (four_heads && nt == 1 ? 4 : 2) * nt * 8; }
+inline size_t decode_workspace(int rows, bool four_heads) {
+    return (partial_rows(row_blocks(rows), four_heads) * (kDim + 2) * sizeof(float) + kMaxDecodeGrid * 16 + 255) / 256 * 256;
 }
 
 template <int NT, int HP, Kind kKind, Mode kMode>
 int launch_decode(cp_ctx* ctx, const DecodeParams& p, cudaStream_t s, const char* who) {
     using Sh = Shape<NT, HP, kKind>;
+    static_assert(2 * kMaxGrid * Sh::kCtas * HP * Sh::kRows <= partial_rows(NT, kKind == kMx4 && HP == 4), "the workspace holds the pieces of every CTA");
     const int grid = std::min(ctx->num_sms, kMaxGrid) * Sh::kCtas;
     const uint32_t variant = 1u << (9 * (NT / 2) + 3 * (HP / 2) + (int)kMode);      // NT and HP are 1, 2 or 4
     if (!(ctx->decode_attr_set[kKind] & variant)) {
@@ -1193,15 +1194,16 @@ struct CacheView {
     const float *k_scale, *v_scale;
     int64_t num_pages, stride_page, stride_tok, stride_head;
     int32_t page_size, Hkv;
+    Kind kind;
 };
 inline CacheView view_of(const cp_kv_cache* c) {
-    return {c->k, c->v, nullptr, nullptr, c->num_pages, c->stride_page * 2, c->stride_tok * 2, c->stride_head * 2, c->page_size, c->Hkv};
+    return {c->k, c->v, nullptr, nullptr, c->num_pages, c->stride_page * 2, c->stride_tok * 2, c->stride_head * 2, c->page_size, c->Hkv, kBf16};
 }
 inline CacheView view_of(const cp_kv_cache_fp8* c) {
-    return {c->k, c->v, c->k_scale, c->v_scale, c->num_pages, c->stride_page, c->stride_tok, c->stride_head, c->page_size, c->Hkv};
+    return {c->k, c->v, c->k_scale, c->v_scale, c->num_pages, c->stride_page, c->stride_tok, c->stride_head, c->page_size, c->Hkv, kE4m3};
 }
 inline CacheView view_of(const cp_kv_cache_mx4* c) {
-    return {c->k, c->v, nullptr, nullptr, c->num_pages, c->stride_page, c->stride_tok, 64, c->page_size, c->Hkv};
+    return {c->k, c->v, nullptr, nullptr, c->num_pages, c->stride_page, c->stride_tok, 64, c->page_size, c->Hkv, kMx4};
 }
 
 // The checks and parameters that the decode and the tree calls share.  On CP_OK with B == 0 there is nothing to launch.
@@ -1226,7 +1228,8 @@ inline int decode_params(cp_ctx* ctx, const void* q, const CacheView& c, const i
     if (B > kMaxDecodeBatch || table_stride > (0x7fffff00ll >> shift) || num_pages > 0x7fffffffll)
         return set_error(CP_ERR_UNSUPPORTED, "%s: B=%d (at most 65536), a table row of %lld entries or %lld pages", who, B,
                          (long long)table_stride, (long long)num_pages);
-    const size_t need = decode_workspace((int)rows);
+    const bool four_heads = c.kind == kMx4 && Hkv % 4 == 0;
+    const size_t need = decode_workspace((int)rows, four_heads);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)
         return set_error(CP_ERR_WORKSPACE, "%s: workspace %p of %zu bytes; need %zu bytes, 256-byte aligned", who, workspace, workspace_bytes, need);
     if (!ctx) return set_error(CP_ERR_INVALID_ARG, "%s: ctx is NULL", who);
@@ -1260,7 +1263,7 @@ inline int decode_params(cp_ctx* ctx, const void* q, const CacheView& c, const i
     p.out = static_cast<__nv_bfloat16*>(out);
     p.lse = lse;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    const size_t n = 2 * (size_t)kMaxDecodeGrid * kMaxHeads * nt * 8;
+    const size_t n = partial_rows(nt, four_heads);
     p.part_o = reinterpret_cast<float*>(ws);
     p.part_ml = p.part_o + n * kDim;
     p.meta = reinterpret_cast<int32_t*>(p.part_ml + n * 2);

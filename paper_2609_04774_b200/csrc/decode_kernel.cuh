@@ -279,15 +279,14 @@ struct TreeRow {
 __device__ __forceinline__ TreeRow tree_row(const DecodeParams& p, int b, int t, int base, int m) {
     const unsigned long long inside = m >= 64 ? ~0ull : (1ull << m) - 1;
     const unsigned long long* masks = p.tree_mask + (int64_t)b * p.n_q;
-    const bool chain = p.tree_mask == nullptr;             // every token sees those before it
     TreeRow r;
-    r.mask = t < m ? (chain ? (2ull << t) - 1 : masks[t]) & inside : 0;
+    r.mask = t < m ? masks[t] & inside : 0;
     const int pos = base + __popcll(r.mask) - 1;
     r.lim = pos + 1;
     r.pad = 0;
     if (p.window <= 64) {                                  // positions of drafted tokens differ by 64 at most: all drafts seen, and none
         for (unsigned long long todo = r.mask; todo != 0; todo &= todo - 1) {
-            const int u = __ffsll(todo) - 1, at = base + (chain ? u : __popcll(masks[u] & inside) - 1);
+            const int u = __ffsll(todo) - 1, at = base + __popcll(masks[u] & inside) - 1;
             if (pos - at >= p.window && at >= p.sinks) r.mask &= ~(1ull << u);
         }
     }

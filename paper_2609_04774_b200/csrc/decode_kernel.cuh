@@ -31,7 +31,7 @@
 // (from L2 where it can): four contexts of 64K keys, four draft tokens, 64 / 4 heads: 170 us against 93 for 32 / 4, E4M3 160 against 99.
 // 4-bit caches: K's codes become fp16 by the hardware's conversion and its exponents join the scores of each block; V's codes become bf16 by shifts (small_bf16) and its
 // exponents join the weights, which is exact but takes three operations a pair of codes.  128 requests of 257..16384 keys, 32 / 8 heads: 174 us, 2.7 TB/s: ALU
-// pipe 61 %, issue 64 % busy (545 instructions for 16 keys of a head); 96 requests with a window of 8192 and two tokens, 64 / 8 heads: 333 us; one request
+// pipe 57 %, issue 58 % of the elapsed cycles (545 instructions for 16 keys of a head); 96 requests with a window of 8192 and two tokens, 64 / 8 heads: 333 us; one request
 // of 4097 keys: 12.6 us.
 #pragma once
 
@@ -81,7 +81,7 @@ struct Shape {
     static constexpr int kTreeAt = (kInvAt + HP * kRows * 4 + 15) / 16 * 16;
     static constexpr int kTreeBufs = kKind == kBf16 ? 2 : 1;
     static constexpr int kTail = kTreeAt + kTreeBufs * kRows * 16;
-    static constexpr int kStages = (228 * 1024 / kCtas - 1024 - kMl - kQ - kTail) / (kGroups * kSlot);     // bf16 3, E4M3 3 or 6, 4-bit 5, 9 or 11
+    static constexpr int kStages = (228 * 1024 / kCtas - 1024 - kMl - kQ - kTail) / (kGroups * kSlot);     // bf16 3, E4M3 3 or 6, 4-bit 5 to 12
     static constexpr int kRing = kStages * kGroups * kSlot;
     static constexpr int kSmem = kRing + kMl + kQ + kTail;
     static constexpr int kPassTiles = std::min(8, 2 * kHalf / (NT * 4 * 32 * 4));      // 16-dim blocks of O that fit a slot

@@ -52,10 +52,13 @@ tree_plan_kernel(const int32_t* parent, const int32_t* tree_len, const int32_t* 
     token_slot[at] = t < m ? base + t : 0;
 }
 
-// Rows per KV head up to which the narrow form is taken.  It is faster up to 16 rows for every kind (37 requests of 4096 keys, 16 rows: bf16 99 us against 104,
-// E4M3 66 against 110, 4-bit 103 against 121; of 700 keys 27 / 31, 23 / 35, 30 / 37; one of 4096 13 / 17, 18 / 20, 15 / 20).  Its 32-row form costs more than the
-// loads of a tile for 4-bit rows (24 rows of 4096 keys 165 us against 121) and somewhat for bf16 (110 against 104); E4M3 stays ahead with it (97 against 110).
-// Behind 32 rows it reads the keys again (48 rows: 209 / 182 / 265 us against 106 / 111 / 121).
+// Rows per KV head up to which the narrow form is taken (us narrow / wide; B requests x keys, 32 / 8 heads).
+//          16 rows: 37 x 4096  37 x 700   1 x 4096     24 rows: 37 x 4096  37 x 700   1 x 4096     32 rows: 37 x 4096  37 x 700   1 x 4096
+//   bf16            98 / 103    27 / 31    13 / 17             108 / 104    39 / 31    17 / 18             109 / 106    39 / 31    18 / 18
+//   E4M3            66 / 101    22 / 34    18 / 19              97 / 101    34 / 34    25 / 19              99 / 101    35 / 35    26 / 20
+//   4-bit          103 / 105    29 / 35    15 / 19             165 / 105    45 / 35    20 / 19             174 / 105    46 / 36    20 / 20
+// Up to 16 rows the narrow form is faster for every kind.  Its 32-row form costs more than the loads of a tile for 4-bit rows and somewhat for bf16; with E4M3 it is 2 to 4 % ahead on long
+// batches, level on short ones and behind on a single request.  Behind 32 rows it reads the keys again (48 rows, 37 x 4096: 208 / 107, 183 / 102, 261 / 108).
 constexpr int kNarrowRows[3] = {16, 32, 16};
 constexpr int kLeastNarrowRows = 16;               // a workspace serves every kind
 

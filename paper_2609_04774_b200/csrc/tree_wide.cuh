@@ -23,8 +23,9 @@
 //     key's weight is zero, but zero times an infinity is not: the issuer of P V looks through the V of these tiles and clears what is no
 //     finite number; what some rows do see of it is added to their results when they are written.
 // Every wait is bounded, as in the prefill kernel.
-// Measured, 37 requests of 8192 keys, 32 / 8 heads, pages of 64 (the copy rate needs 193 / 96 / 51 us): bf16 194, 202 and 283 us with 64, 128 and 256 rows (6.4 TB/s up to
-// 128 rows, then the tensor and MUFU pipes: 1120 TFLOP/s of visible pairs); E4M3 182, 191, 299 and 4-bit 196, 233, 328 us, bound by the chain from a raw tile to the second product.  A unit costs 9 to 22 us beside its tiles: 4 until its queries are there, 2 of epilogue, 1 to 3 where the warpgroups wait for one another.
+// Measured, 37 requests of 8192 keys, 32 / 8 heads, pages of 64 (the copy rate needs 193 / 96 / 51 us): bf16 199, 208 and 294 us with 64, 128 and 256 rows (6.2 TB/s up to
+// 128 rows, then the tensor and MUFU pipes: 1080 TFLOP/s of visible pairs); E4M3 190, 192, 298 and 4-bit 202, 235, 315 us, bound by the chain from a raw tile to the second product,
+// in which shared memory's data pipe is the busiest (57 %: 33 by the warps that widen, 24 by the tensor cores).  A unit costs 9 to 22 us beside its tiles: 4 until its queries are there, 2 of epilogue, 1 to 3 where the warpgroups wait for one another.
 #pragma once
 
 #include "decode_kernel.cuh"
